@@ -49,7 +49,8 @@ typedef enum {
   CKV_ERR_UNSUPPORTED = 2, /* valid but not implemented: head_dim != 128, window > 64, Hkv > 64, ... */
   CKV_ERR_WORKSPACE = 3,   /* ws is null, misaligned or shorter than ckv_workspace_bytes() */
   CKV_ERR_CUDA = 4,        /* a CUDA runtime call or launch failed */
-  CKV_ERR_TIMEOUT = 5      /* a bounded device-side wait expired (see ckv_device_status) */
+  CKV_ERR_TIMEOUT = 5,     /* a bounded device-side wait expired (see ckv_device_status) */
+  CKV_ERR_PAGE = 6         /* device-side: a page or row index outside its buffer was met (see ckv_device_status) */
 } ckv_status;
 
 typedef enum { CKV_BF16 = 0, CKV_F32 = 1 } ckv_dtype;
@@ -310,8 +311,98 @@ ckv_status ckv_score_noalloc(const ckv_shape* shape, const ckv_params* params, c
                              const void* k, const float* head_w, float* scores, float* colmass,
                              void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * The decoder's side: what makes the rotated queries and keys that the pass reads, and a paged cache that takes the rows
+ * it kept, grows by the new tokens, and is attended over.  Not part of the retention pass.
+ *
+ * Tokens are packed: unit u (a sequence in one layer) owns the rows token_starts[u] .. token_starts[u+1]-1 of the token
+ * arrays (token_starts [Nu+1] int32, ascending; a unit may own none).  Rows outside token_starts[0] .. token_starts[Nu]-1
+ * are padding: not read, and nothing is written for them.
+ * The cache is two pools k_pages, v_pages [n_pages, page_size, d]; row j of KV head g of unit u is row j % page_size of
+ * page page_table[u, g, j / page_size] (page_table [Nu, Hkv, max_pages] int32), and lengths [Nu, Hkv] int32 counts
+ * the rows each head holds: the heads of a unit keep different numbers of rows, so table and lengths are per head.  Only
+ * the table entries of pages that hold rows are read; a page may be shared by several readers.
+ * A page number outside the pool, or a row past the table's last page, is never followed: the row is left out, and
+ * ckv_device_status(ws) reports CKV_ERR_PAGE.  Cache rows behind a head's length may hold anything, NaN included.
+ * The calls use only the current device's memory and are capturable; a work space serves one call at a time.
+ */
+typedef struct {
+  int32_t n_units;     /* Nu >= 1; Nu * Hkv <= 65536 */
+  int32_t n_q_heads;   /* H, a multiple of n_kv_heads */
+  int32_t n_kv_heads;  /* Hkv <= 64 */
+  int32_t head_dim;    /* d; must be 128 */
+  int32_t dtype;       /* ckv_dtype of tokens, pages and outputs */
+  int32_t n_tokens;    /* T >= 0: rows of the token arrays, padding included; T <= 2^20 */
+  int32_t max_new;     /* most tokens any unit has in a call, as far as known; 0: not known (T).  It only picks kernels:
+                          the results are right whatever it says */
+  int32_t causal;      /* ckv_paged_attend: 1: a unit's tokens are its heads' last rows and see no later ones;
+                          0: they see every row */
+  int32_t page_size;   /* 16, 32, 64, 128 or 256 rows */
+  int32_t n_pages;     /* >= 1 */
+  int32_t max_pages;   /* >= 1; max_pages * page_size <= 2^24 */
+  float scale;         /* factor of the logits; 0: 1 / sqrt(d) */
+  int64_t q_stride_tok, q_stride_head;     /* elements; q [T, H, d], last dimension contiguous */
+  int64_t kv_stride_tok, kv_stride_head;   /* elements; k and v [T, Hkv, d] */
+  int64_t page_stride, page_stride_row;    /* elements; shared by k_pages and v_pages */
+} ckv_paged;
+
+typedef struct {
+  const double* inv_freq;  /* DEVICE [rot_dim / 2]: radians per position of each pair (NULL when rot_dim is 0) */
+  const float* q_norm_w;   /* DEVICE [d], or NULL: queries are not normed */
+  const float* k_norm_w;   /* DEVICE [d], or NULL: keys are not normed */
+  int32_t rot_dim;         /* rotated leading dimensions: a multiple of 16, 0..128; the others pass through */
+  int32_t interleaved;     /* pair i is dimensions (2i, 2i+1) if 1, (i, i + rot_dim/2) if 0 */
+  float rot_scale;         /* factor of cosine and sine (1, or a context extension's attention factor) */
+  float norm_eps;          /* >= 0 */
+} ckv_rotary;
+
+/*
+ * Norms of queries and keys for each head and their position rotation in one pass:
+ *   y = x * w / sqrt(mean(x^2) + norm_eps)   (where there is a weight),
+ *   (y_a, y_b) -> rot_scale * (y_a cos - y_b sin, y_b cos + y_a sin),  angle = position * inv_freq[pair] in 64 bits.
+ * positions [T] int32.  q_out [T,H,d], k_out [T,Hkv,d]: dense, or q_out == q / k_out == k (in place, the inputs'
+ * strides).  Either pair may be NULL.  Of `paged` only the token fields are read (the page fields may be 0).
+ */
+ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const void* q, const void* k,
+                      const int32_t* positions, const int32_t* token_starts, void* q_out, void* k_out, void* stream);
+
+/* Bytes of work space ckv_append, ckv_gather_pages and ckv_paged_attend need (0 on invalid arguments). */
+size_t ckv_paged_workspace_bytes(const ckv_paged* paged);
+
+/*
+ * Appends the units' new tokens to the cache: token i of unit u becomes row lengths[u,g] + i of every head g, its key
+ * normed and rotated as in ckv_rotate, its value as it is.  rotary NULL: keys are stored as they are.  q_or_null is
+ * normed and rotated into q_out in the same launch (as in ckv_rotate).  new_lengths_or_null [Nu,Hkv] receives
+ * lengths + the unit's tokens and must not overlap lengths.  Pages that two heads share must not be written.
+ */
+ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const void* q_or_null, const void* k,
+                      const void* v, const int32_t* positions, const int32_t* token_starts, const int32_t* lengths,
+                      const int32_t* page_table, void* q_out, void* k_pages, void* v_pages,
+                      int32_t* new_lengths_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ckv_gather into pages: the rows the pass kept (indices, budgets, offsets as it left them) become rows 0 .. budgets-1 of
+ * every head of the cache, bit copies, and lengths [Nu,Hkv] = budgets.  `shape` and `paged` agree in units, KV heads and
+ * dtype.
+ */
+ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, const ckv_paged* paged, const void* k,
+                            const void* v, const int32_t* indices, const int32_t* budgets, const int32_t* offsets,
+                            const int32_t* page_table, void* k_pages, void* v_pages, int32_t* lengths, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/*
+ * Attention of the units' tokens over the cache; with `causal`, lengths count the tokens' own rows (append first).  With n
+ * tokens in unit u, its token i sees rows j <= lengths[u,g] - n + i of head g (causal), or every row j < lengths[u,g].
+ *   out [T,H,d] = softmax(scale q k^T) v in the dtype of `paged`;  lse_or_null [T,H] fp32 = ln sum_j exp(scale q . k_j).
+ * A token that sees no row gets zeros and -infinity.  Each sum is 32-bit and taken in an order that the shapes,
+ * lengths and token counts alone decide.
+ */
+ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k_pages, const void* v_pages,
+                            const int32_t* page_table, const int32_t* lengths, const int32_t* token_starts, void* out,
+                            float* lse_or_null, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronises `stream` and returns what device code recorded in the status word of `ws` since the last
- * such call (CKV_OK or CKV_ERR_TIMEOUT), or CKV_ERR_CUDA if the stream is in error.  A recorded code survives
+ * such call (CKV_OK, CKV_ERR_TIMEOUT or CKV_ERR_PAGE), or CKV_ERR_CUDA if the stream is in error.  A recorded code survives
  * later calls on the work space until this function reports it, which also clears it.  ws == NULL reads the
  * fixed scratch of ckv_score_noalloc on the current device.  Work space that no call has used yet reads CKV_OK. */
 ckv_status ckv_device_status(const void* ws, void* stream);

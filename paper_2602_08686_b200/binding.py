@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libckv.so")
 
 BF16, F32 = 0, 1
 POOL_NONE, POOL_MAX, POOL_AVG = 0, 1, 2
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_PAGE = range(7)
 
 
 class CkvError(RuntimeError):
@@ -60,6 +60,19 @@ class ckv_params(C.Structure):
                 ("reserved2_", C.c_int32), ("gate_coords", C.c_void_p), ("tuning", C.POINTER(ckv_tuning))]
 
 
+class ckv_paged(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_units", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "n_tokens", "max_new",
+                                         "causal", "page_size", "n_pages", "max_pages")] + \
+               [("scale", C.c_float)] + \
+               [(n, C.c_int64) for n in ("q_stride_tok", "q_stride_head", "kv_stride_tok", "kv_stride_head",
+                                         "page_stride", "page_stride_row")]
+
+
+class ckv_rotary(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("q_norm_w", C.c_void_p), ("k_norm_w", C.c_void_p), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("rot_scale", C.c_float), ("norm_eps", C.c_float)]
+
+
 _lib = None
 
 
@@ -92,6 +105,13 @@ def lib() -> C.CDLL:
         L.ckv_gather.argtypes = [shp, prm, vp, vp, i32p, i32p, vp, vp, vp]
         L.ckv_compress.argtypes = [shp, prm, vp, vp, vp, fp, fp, vp, vp, i32p, i32p, i32p, fp, i32p, fp, vp, sz, vp]
         L.ckv_compress_host.argtypes = [shp, prm, vp, vp, vp, fp, fp, vp, vp, i32p, i32p, i32p, vp, sz, vp, sz, vp]
+        pgd, rty = C.POINTER(ckv_paged), C.POINTER(ckv_rotary)
+        L.ckv_paged_workspace_bytes.restype = sz
+        L.ckv_paged_workspace_bytes.argtypes = [pgd]
+        L.ckv_rotate.argtypes = [pgd, rty] + [vp] * 7
+        L.ckv_append.argtypes = [pgd, rty] + [vp] * 12 + [sz, vp]
+        L.ckv_gather_pages.argtypes = [shp, prm, pgd] + [vp] * 10 + [sz, vp]
+        L.ckv_paged_attend.argtypes = [pgd] + [vp] * 9 + [sz, vp]
         L.ckv_device_status.argtypes = [vp, vp]
         L.ckv_gate_depth_map_host.argtypes = [fp, C.c_int, C.c_int, C.c_int64, fp]
         L.ckv_set_scan_events.argtypes = [vp, vp]
@@ -103,6 +123,7 @@ def lib() -> C.CDLL:
         L.ckv_status_string.argtypes = [C.c_int]
         L.ckv_allocate_rows_host.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int64, vp, vp]
         for name in ("ckv_score", "ckv_score_noalloc", "ckv_budget", "ckv_select", "ckv_vnorm", "ckv_unit_max", "ckv_kept_mass", "ckv_attend", "ckv_prompt_mass", "ckv_global_scores", "ckv_gather", "ckv_compress", "ckv_compress_host",
+                     "ckv_rotate", "ckv_append", "ckv_gather_pages", "ckv_paged_attend",
                      "ckv_device_status", "ckv_version", "ckv_allocate_rows_host"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -379,6 +400,196 @@ def ckv_allocate_rows_host(n: int, f: int, P: int, demands) -> list[int]:
     if rc:
         raise ValueError(f"ckv_allocate_rows_host failed with {rc}")
     return list(out)
+
+
+# ------------------------------------------------------------------------------------ the paged cache
+# The structs of the paged calls are made once and used for many calls.  They carry the layout (shape, strides, dtype, device)
+# their tensors had, and every call compares what it is given with it: a tensor laid out differently, or one of
+# another device, would be read wrongly.  A call runs on its tensors' device, on that device's current stream unless told otherwise.
+def _layout(t: torch.Tensor | None):
+    return None if t is None else (tuple(t.shape), t.stride(), t.dtype, t.device)
+
+
+def _same(t: torch.Tensor, layout, name: str) -> int:
+    """The tensor's address, once its layout is the struct's (strides of extents of one do not matter)."""
+    if layout is None:
+        raise ValueError(f"{name}: the struct was made without it")
+    shape, stride, dtype, device = layout
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {shape} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.stride() != stride and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), stride)):
+        raise ValueError(f"{name} has strides {t.stride()}; the struct was made for {stride}")
+    return t.data_ptr()
+
+
+def _dense(t: torch.Tensor, shape, dtype, device, name: str) -> int:
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense {tuple(shape)} {dtype} on {device}")
+    return t.data_ptr()
+
+
+def _paged_call(fn, what: str, device, stream, *args) -> None:
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _paged_call(fn, what, device, stream, *args)
+    s = torch.cuda.current_stream() if stream is None else stream
+    status = fn(*args, s.cuda_stream)
+    if status != OK:
+        raise CkvError(status, what)
+
+
+def make_packed(q: torch.Tensor | None, k: torch.Tensor | None, n_units: int, max_new: int = 0) -> ckv_paged:
+    """Struct of packed tokens alone, for ckv_rotate: q [T, H, d] and / or k [T, Hkv, d], last dimension contiguous."""
+    t = q if q is not None else k
+    if t is None or t.dim() != 3 or (q is not None and k is not None and (q.shape[0] != k.shape[0] or q.dtype != k.dtype)):
+        raise ValueError("q and k must be [T, heads, d] of one dtype")
+    for x in (q, k):
+        if x is not None and (x.dim() != 3 or (x.stride(2) != 1 and x.shape[2] > 1)):
+            raise ValueError("q and k must be 3-D with a contiguous last dimension")
+    H = q.shape[1] if q is not None else k.shape[1]
+    Hkv = k.shape[1] if k is not None else H
+    pg = ckv_paged(int(n_units), H, Hkv, t.shape[2], _dtype_code(t), t.shape[0], int(max_new), 1, 0, 0, 0, 0.0)
+    if q is not None:
+        pg.q_stride_tok, pg.q_stride_head = q.stride(0), q.stride(1)
+    if k is not None:
+        pg.kv_stride_tok, pg.kv_stride_head = k.stride(0), k.stride(1)
+    pg._q, pg._k, pg._pages, pg._device, pg._dtype = _layout(q), _layout(k), None, t.device, t.dtype
+    pg._starts = (pg.n_units + 1,)
+    return pg
+
+
+def make_paged(k_pages: torch.Tensor, page_table: torch.Tensor, q: torch.Tensor | None = None,
+               k_new: torch.Tensor | None = None, n_q_heads: int = 0, max_new: int = 0, causal: bool = True,
+               scale: float = 0.0) -> ckv_paged:
+    """Struct of a paged cache: k_pages [n_pages, page_size, d] (v_pages laid out alike), page_table [Nu, Hkv, max_pages]
+    int32, and the packed tokens q [T, H, d], k_new [T, Hkv, d] (v_new laid out alike) of the calls that have any."""
+    if k_pages.dim() != 3 or k_pages.stride(2) != 1 or page_table.dim() != 3:
+        raise ValueError("k_pages must be [n_pages, page_size, d] with a contiguous last dimension, page_table [Nu, Hkv, max_pages]")
+    if page_table.dtype != torch.int32 or not page_table.is_contiguous():
+        raise ValueError("page_table must be a dense int32 tensor")
+    Nu, Hkv, max_pages = page_table.shape
+    if q is None and k_new is None:
+        pg = ckv_paged(Nu, int(n_q_heads) or Hkv, Hkv, k_pages.shape[2], _dtype_code(k_pages), 0, int(max_new), 1, 0, 0, 0, 0.0)
+        pg._q = pg._k = None
+    else:
+        pg = make_packed(q, k_new, Nu, max_new)
+        if q is None:
+            pg.n_q_heads = int(n_q_heads) or Hkv
+        if (q is not None and q.dtype != k_pages.dtype) or (k_new is not None and (k_new.dtype != k_pages.dtype or k_new.shape[1] != Hkv)):
+            raise ValueError("tokens and pages must agree in dtype and KV heads")
+    pg.n_kv_heads, pg.causal, pg.scale = Hkv, int(bool(causal)), float(scale)
+    pg.n_pages, pg.page_size, pg.max_pages = k_pages.shape[0], k_pages.shape[1], max_pages
+    pg.page_stride, pg.page_stride_row = k_pages.stride(0), k_pages.stride(1)
+    pg._pages, pg._device, pg._dtype = _layout(k_pages), k_pages.device, k_pages.dtype
+    pg._table, pg._heads, pg._starts = tuple(page_table.shape), (Nu, Hkv), (Nu + 1,)
+    pg._ws_bytes = ckv_paged_workspace_bytes(pg)
+    return pg
+
+
+def make_rotary(inv_freq: torch.Tensor | None, interleaved: bool = False, q_norm_w: torch.Tensor | None = None,
+                k_norm_w: torch.Tensor | None = None, rot_scale: float = 1.0, norm_eps: float = 1e-6) -> ckv_rotary:
+    """Rotation and norms: inv_freq [rot_dim / 2] float64 (None: no rotation), norm weights [d] float32 (None: no norm);
+    the struct keeps references to the tensors."""
+    for t, dt, name in ((inv_freq, torch.float64, "inv_freq"), (q_norm_w, torch.float32, "q_norm_w"),
+                        (k_norm_w, torch.float32, "k_norm_w")):
+        if t is not None and (t.dtype != dt or not t.is_contiguous() or t.dim() != 1):
+            raise ValueError(f"{name} must be a dense 1-D {dt} tensor")
+    for t in (q_norm_w, k_norm_w):
+        if t is not None and t.numel() != 128:
+            raise ValueError("a norm weight has head_dim elements")
+    kept = [t for t in (inv_freq, q_norm_w, k_norm_w) if t is not None]
+    if any(t.device != kept[0].device for t in kept):
+        raise ValueError("inv_freq and the norm weights must be on one device")
+    ptr = [None if t is None else t.data_ptr() for t in (inv_freq, q_norm_w, k_norm_w)]
+    r = ckv_rotary(*ptr, 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), float(rot_scale), float(norm_eps))
+    r._keep, r._device = kept, kept[0].device if kept else None
+    return r
+
+
+def ckv_paged_workspace_bytes(paged: ckv_paged) -> int:
+    return int(lib().ckv_paged_workspace_bytes(C.byref(paged)))
+
+
+def alloc_paged_workspace(paged: ckv_paged, device=None) -> torch.Tensor:
+    nbytes = ckv_paged_workspace_bytes(paged)
+    if nbytes == 0:
+        raise CkvError(ERR_INVALID_ARG, "ckv_paged_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=paged._device if device is None else device)
+
+
+def _rotary_of(pg: ckv_paged, rotary: ckv_rotary | None):
+    if rotary is None:
+        return None
+    if rotary._device is not None and rotary._device != pg._device:
+        raise ValueError(f"the rotary tables are on {rotary._device}, the tokens on {pg._device}")
+    return C.byref(rotary)
+
+
+def _tokens_out(pg, out, t, layout, name):
+    """A token output: the input itself (in place) or a dense tensor of its shape."""
+    if t is None:
+        return None
+    if out.data_ptr() == t.data_ptr():
+        return _same(out, layout, name)
+    return _dense(out, layout[0], pg._dtype, pg._device, name)
+
+
+def _ws_of(pg, ws):
+    if ws.device != pg._device or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws must be a dense uint8 tensor on the device of the pages")
+    return ws.data_ptr()
+
+
+def ckv_rotate(paged, rotary, q, k, positions, token_starts, q_out, k_out, stream=None):
+    """Norms and rotation of q [T, H, d] and k [T, Hkv, d] (either may be None) into q_out, k_out (dense, or in place)."""
+    T = paged.n_tokens
+    dev = paged._device
+    _paged_call(lib().ckv_rotate, "ckv_rotate", dev, stream, C.byref(paged), _rotary_of(paged, rotary),
+                None if q is None else _same(q, paged._q, "q"), None if k is None else _same(k, paged._k, "k"),
+                _dense(positions, (T,), torch.int32, dev, "positions"),
+                _dense(token_starts, paged._starts, torch.int32, dev, "token_starts"),
+                _tokens_out(paged, q_out, q, paged._q, "q_out"), _tokens_out(paged, k_out, k, paged._k, "k_out"))
+
+
+def ckv_append(paged, rotary, k, v, positions, token_starts, lengths, page_table, k_pages, v_pages, ws, q=None, q_out=None,
+               new_lengths=None, stream=None):
+    """Appends the tokens' keys (normed, rotated; as they are when rotary is None) and values to the cache; q goes normed and
+    rotated into q_out; new_lengths receives the heads' lengths with the tokens."""
+    dev, i32 = paged._device, torch.int32
+    _paged_call(lib().ckv_append, "ckv_append", dev, stream, C.byref(paged), _rotary_of(paged, rotary),
+                None if q is None else _same(q, paged._q, "q"), _same(k, paged._k, "k"), _same(v, paged._k, "v"),
+                None if positions is None else _dense(positions, (paged.n_tokens,), i32, dev, "positions"),
+                _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(lengths, paged._heads, i32, dev, "lengths"),
+                _dense(page_table, paged._table, i32, dev, "page_table"), _tokens_out(paged, q_out, q, paged._q, "q_out"),
+                _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
+                None if new_lengths is None else _dense(new_lengths, paged._heads, i32, dev, "new_lengths"),
+                _ws_of(paged, ws), ws.numel())
+
+
+def ckv_gather_pages(shape, params, paged, k, v, indices, budgets, offsets, page_table, k_pages, v_pages, lengths, ws, stream=None):
+    """The rows the retention pass kept of k, v, into the pages of a cache; lengths receives the heads' budgets."""
+    dev, i32 = paged._device, torch.int32
+    _check_kv(shape, k, "k"), _check_kv(shape, v, "v")
+    if k.device != dev or v.device != dev:
+        raise ValueError(f"k and v must be on {dev}")
+    Nu, Hkv = paged._heads
+    _paged_call(lib().ckv_gather_pages, "ckv_gather_pages", dev, stream, C.byref(shape), C.byref(params), C.byref(paged),
+                k.data_ptr(), v.data_ptr(), _dense(indices, (Nu, rows_per_unit(shape, params)), i32, dev, "indices"),
+                _dense(budgets, paged._heads, i32, dev, "budgets"), _dense(offsets, (Nu, Hkv + 1), i32, dev, "offsets"),
+                _dense(page_table, paged._table, i32, dev, "page_table"), _same(k_pages, paged._pages, "k_pages"),
+                _same(v_pages, paged._pages, "v_pages"), _dense(lengths, paged._heads, i32, dev, "lengths"), _ws_of(paged, ws),
+                ws.numel())
+
+
+def ckv_paged_attend(paged, q, k_pages, v_pages, page_table, lengths, token_starts, out, ws, lse=None, stream=None):
+    """Attention of the packed tokens q [T, H, d] over the cache (lengths count the tokens' own rows when causal)."""
+    dev, i32 = paged._device, torch.int32
+    qs = paged._q
+    _paged_call(lib().ckv_paged_attend, "ckv_paged_attend", dev, stream, C.byref(paged), _same(q, qs, "q"),
+                _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
+                _dense(page_table, paged._table, i32, dev, "page_table"), _dense(lengths, paged._heads, i32, dev, "lengths"),
+                _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(out, qs[0], paged._dtype, dev, "out"),
+                None if lse is None else _dense(lse, qs[0][:2], torch.float32, dev, "lse"), _ws_of(paged, ws), ws.numel())
 
 
 # ------------------------------------------------------------------------------------ convenience

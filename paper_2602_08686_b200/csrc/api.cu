@@ -5,7 +5,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "ckv_common.cuh"
+#include "paged.cuh"
 
 namespace ckv {
 
@@ -182,8 +182,6 @@ static bool all_aligned4(std::initializer_list<const void*> ps) {
 // Word kStatusMagicWord of the status section says that words 0..7 (the status code and the waits that were in
 // progress when it was set) are meaningful; a work space seen for the first time has them cleared.  The words
 // behind them (counters, the scan's flags and queues) are cleared on every call.
-constexpr int kStatusMagicWord = 63;
-constexpr int kStatusMagic = 0x434b5631;
 __global__ void ws_reset_kernel(int* status, size_t n_flag_words) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, step = (size_t)gridDim.x * blockDim.x;
   if (i == 0 && status[kStatusMagicWord] != kStatusMagic) {
@@ -551,7 +549,7 @@ ckv_status ckv_device_status(const void* ws, void* stream) {
   // a recorded code is reported once: clear it (and the words that name the waits) for the calls that follow
   if (cudaMemsetAsync(const_cast<char*>(base), 0, 8 * sizeof(int32_t), st) != cudaSuccess) return CKV_ERR_CUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return CKV_ERR_CUDA;
-  return CKV_ERR_TIMEOUT;
+  return words[0] == kStatusPage ? CKV_ERR_PAGE : CKV_ERR_TIMEOUT;
 }
 
 int ckv_set_score_path(int path) {
@@ -602,6 +600,7 @@ const char* ckv_status_string(ckv_status status) {
     case CKV_ERR_WORKSPACE: return "work space missing, misaligned or too small";
     case CKV_ERR_CUDA: return "CUDA error";
     case CKV_ERR_TIMEOUT: return "device-side wait timed out";
+    case CKV_ERR_PAGE: return "page or row index outside its buffer";
   }
   return "unknown status";
 }

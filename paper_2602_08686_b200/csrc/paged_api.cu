@@ -1,0 +1,204 @@
+// Host side of the paged-cache entry points: argument validation and work space.
+#include <initializer_list>
+
+#include "paged.cuh"
+
+using namespace ckv;
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+bool good(std::initializer_list<const void*> ps, size_t a) {
+  for (const void* p : ps)
+    if (!p || !aligned(p, a)) return false;
+  return true;
+}
+int64_t esize(const ckv_paged& pg) { return pg.dtype == CKV_BF16 ? 2 : 4; }
+
+// What a token array [T, heads, d] with these strides covers, in bytes.
+struct Range {
+  uintptr_t lo, hi;
+};
+Range range_of(const void* p, int64_t T, int64_t heads, int64_t tok, int64_t head, int64_t esz) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  return {lo, lo + (uintptr_t)(((T - 1) * tok + (heads - 1) * head + kHeadDim) * esz)};
+}
+bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+
+ckv_status check_tokens(const ckv_paged* pg) {
+  if (!pg) return CKV_ERR_INVALID_ARG;
+  if (pg->n_units < 1 || pg->n_q_heads < 1 || pg->n_kv_heads < 1 || pg->n_tokens < 0 || pg->max_new < 0)
+    return CKV_ERR_INVALID_ARG;
+  if (pg->n_q_heads % pg->n_kv_heads) return CKV_ERR_INVALID_ARG;
+  if (pg->dtype != CKV_BF16 && pg->dtype != CKV_F32) return CKV_ERR_INVALID_ARG;
+  if (pg->head_dim != kHeadDim || pg->n_kv_heads > kMaxKvHeads || pg->n_tokens > (1 << 20) || pg->n_q_heads > 65535)
+    return CKV_ERR_UNSUPPORTED;
+  if ((int64_t)pg->n_units * pg->n_kv_heads > 65536) return CKV_ERR_UNSUPPORTED;
+  return CKV_OK;
+}
+// Strides of a token array: rows on 16-byte boundaries that do not overlap one another.
+bool token_strides(const ckv_paged& pg, int64_t tok, int64_t head, int heads) {
+  const int64_t e = esize(pg);
+  if (tok < 0 || head < 0 || (tok * e) % 16 || (head * e) % 16) return false;
+  if ((heads > 1 && head < kHeadDim) || (pg.n_tokens > 1 && tok < kHeadDim)) return false;
+  return tok < ((int64_t)1 << 40) && head < ((int64_t)1 << 40);
+}
+ckv_status check_pages(const ckv_paged* pg) {
+  if (pg->page_size < 1 || pg->n_pages < 1 || pg->max_pages < 1) return CKV_ERR_INVALID_ARG;
+  if (pg->causal != 0 && pg->causal != 1) return CKV_ERR_INVALID_ARG;
+  if (!(pg->scale > -3.0e38f && pg->scale < 3.0e38f)) return CKV_ERR_INVALID_ARG;
+  const int P = pg->page_size;
+  if (P != 16 && P != 32 && P != 64 && P != 128 && P != 256) return CKV_ERR_UNSUPPORTED;
+  if ((int64_t)pg->max_pages * P > (1 << 24)) return CKV_ERR_UNSUPPORTED;
+  const int64_t e = esize(*pg);
+  if ((pg->page_stride * e) % 16 || (pg->page_stride_row * e) % 16) return CKV_ERR_INVALID_ARG;
+  if (pg->page_stride_row < kHeadDim) return CKV_ERR_INVALID_ARG;
+  if (pg->n_pages > 1 && pg->page_stride < (P - 1) * pg->page_stride_row + kHeadDim) return CKV_ERR_INVALID_ARG;
+  if (pg->page_stride_row >= ((int64_t)1 << 32) || pg->page_stride < 0 || pg->page_stride >= ((int64_t)1 << 38))
+    return CKV_ERR_UNSUPPORTED;
+  return CKV_OK;
+}
+ckv_status check_rotary(const ckv_rotary* r) {
+  if (r->rot_dim < 0 || r->rot_dim > kHeadDim) return CKV_ERR_INVALID_ARG;
+  if (r->rot_dim % 16) return CKV_ERR_UNSUPPORTED;
+  if (r->interleaved != 0 && r->interleaved != 1) return CKV_ERR_INVALID_ARG;
+  if (r->rot_dim && !good({r->inv_freq}, 8)) return CKV_ERR_INVALID_ARG;
+  if ((r->q_norm_w && !aligned(r->q_norm_w, 4)) || (r->k_norm_w && !aligned(r->k_norm_w, 4))) return CKV_ERR_INVALID_ARG;
+  if (!(r->norm_eps >= 0.f && r->norm_eps < 3.0e38f) || !(r->rot_scale > -3.0e38f && r->rot_scale < 3.0e38f))
+    return CKV_ERR_INVALID_ARG;
+  return CKV_OK;
+}
+ckv_status check_paged_ws(const ckv_paged& pg, const void* ws, size_t ws_bytes) {
+  if (!ws || !aligned(ws, 256) || ws_bytes < paged_ws(pg).total) return CKV_ERR_WORKSPACE;
+  return CKV_OK;
+}
+// An output is either its own input (in place) or dense and apart from everything that is read.
+bool out_ok(const ckv_paged& pg, const void* out, const void* in, int heads, std::initializer_list<Range> read) {
+  if (!good({out}, 16)) return false;
+  if (out == in) return true;
+  const Range o = range_of(out, pg.n_tokens, heads, (int64_t)heads * kHeadDim, kHeadDim, esize(pg));
+  for (const Range& r : read)
+    if (overlap(o, r)) return false;
+  return true;
+}
+
+#define CKV_TRY(expr)                  \
+  do {                                 \
+    ckv_status st__ = (expr);          \
+    if (st__ != CKV_OK) return st__;   \
+  } while (0)
+#define CKV_CUDA(expr)                               \
+  do {                                               \
+    if ((expr) != cudaSuccess) return CKV_ERR_CUDA;  \
+  } while (0)
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+size_t ckv_paged_workspace_bytes(const ckv_paged* paged) {
+  if (check_tokens(paged) != CKV_OK || check_pages(paged) != CKV_OK) return 0;
+  return paged_ws(*paged).total;
+}
+
+ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const void* q, const void* k,
+                      const int32_t* positions, const int32_t* token_starts, void* q_out, void* k_out, void* stream) {
+  CKV_TRY(check_tokens(paged));
+  if (!rotary) return CKV_ERR_INVALID_ARG;
+  CKV_TRY(check_rotary(rotary));
+  if (paged->n_tokens == 0) return CKV_OK;
+  if (!q && !k) return CKV_ERR_INVALID_ARG;
+  if (!good({positions, token_starts}, 4)) return CKV_ERR_INVALID_ARG;
+  const int H = paged->n_q_heads, Hkv = paged->n_kv_heads;
+  if (q && (!aligned(q, 16) || !token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, H))) return CKV_ERR_INVALID_ARG;
+  if (k && (!aligned(k, 16) || !token_strides(*paged, paged->kv_stride_tok, paged->kv_stride_head, Hkv)))
+    return CKV_ERR_INVALID_ARG;
+  const int64_t T = paged->n_tokens, e = esize(*paged);
+  const Range qr = q ? range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e) : Range{0, 0};
+  const Range kr = k ? range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e) : Range{0, 0};
+  if (q && !out_ok(*paged, q_out, q, H, {qr, kr})) return CKV_ERR_INVALID_ARG;
+  if (k && !out_ok(*paged, k_out, k, Hkv, {qr, kr})) return CKV_ERR_INVALID_ARG;
+  if (q && k && q_out != q && k_out != k &&
+      overlap(range_of(q_out, T, H, (int64_t)H * kHeadDim, kHeadDim, e), range_of(k_out, T, Hkv, (int64_t)Hkv * kHeadDim, kHeadDim, e)))
+    return CKV_ERR_INVALID_ARG;
+  CKV_CUDA(launch_rotate(*paged, rotary, q, k, nullptr, positions, token_starts, q_out, k_out, nullptr, nullptr, nullptr,
+                         nullptr, nullptr, nullptr, (cudaStream_t)stream));
+  return CKV_OK;
+}
+
+ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const void* q_or_null, const void* k,
+                      const void* v, const int32_t* positions, const int32_t* token_starts, const int32_t* lengths,
+                      const int32_t* page_table, void* q_out, void* k_pages, void* v_pages,
+                      int32_t* new_lengths_or_null, void* ws, size_t ws_bytes, void* stream) {
+  CKV_TRY(check_tokens(paged));
+  CKV_TRY(check_pages(paged));
+  if (rotary) CKV_TRY(check_rotary(rotary));
+  if (!good({token_starts, lengths, page_table}, 4)) return CKV_ERR_INVALID_ARG;
+  if (new_lengths_or_null) {
+    const uintptr_t n = (uintptr_t)paged->n_units * paged->n_kv_heads * sizeof(int32_t);
+    const uintptr_t a = reinterpret_cast<uintptr_t>(lengths), b = reinterpret_cast<uintptr_t>(new_lengths_or_null);
+    if (b % 4 || (a < b + n && b < a + n)) return CKV_ERR_INVALID_ARG;
+  }
+  CKV_TRY(check_paged_ws(*paged, ws, ws_bytes));
+  if (paged->n_tokens == 0 && !new_lengths_or_null) return CKV_OK;
+  const bool any = paged->n_tokens > 0;
+  if (any) {
+    const int H = paged->n_q_heads, Hkv = paged->n_kv_heads;
+    if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
+    if ((rotary && rotary->rot_dim) && !good({positions}, 4)) return CKV_ERR_INVALID_ARG;
+    if (!token_strides(*paged, paged->kv_stride_tok, paged->kv_stride_head, Hkv)) return CKV_ERR_INVALID_ARG;
+    if (q_or_null) {
+      if (!aligned(q_or_null, 16) || !token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, H))
+        return CKV_ERR_INVALID_ARG;
+      const int64_t T = paged->n_tokens, e = esize(*paged);
+      const Range kr = range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
+      const Range vr = range_of(v, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
+      if (!out_ok(*paged, q_out, q_or_null, H, {range_of(q_or_null, T, H, paged->q_stride_tok, paged->q_stride_head, e), kr, vr}))
+        return CKV_ERR_INVALID_ARG;
+    }
+  }
+  CKV_CUDA(launch_rotate(*paged, rotary, any ? q_or_null : nullptr, any ? k : nullptr, any ? v : nullptr, positions,
+                         token_starts, q_out, nullptr, lengths, page_table, k_pages, v_pages, new_lengths_or_null,
+                         reinterpret_cast<int*>(static_cast<char*>(ws) + paged_ws(*paged).status), (cudaStream_t)stream));
+  return CKV_OK;
+}
+
+ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, const ckv_paged* paged, const void* k,
+                            const void* v, const int32_t* indices, const int32_t* budgets, const int32_t* offsets,
+                            const int32_t* page_table, void* k_pages, void* v_pages, int32_t* lengths, void* ws,
+                            size_t ws_bytes, void* stream) {
+  if (ckv_workspace_bytes(shape, params) == 0) return CKV_ERR_INVALID_ARG;   // shape and params as everywhere else
+  CKV_TRY(check_tokens(paged));
+  CKV_TRY(check_pages(paged));
+  if (shape->n_units != paged->n_units || shape->n_kv_heads != paged->n_kv_heads || shape->dtype != paged->dtype)
+    return CKV_ERR_INVALID_ARG;
+  if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
+  if (!good({indices, budgets, offsets, page_table, lengths}, 4) || lengths == budgets) return CKV_ERR_INVALID_ARG;
+  CKV_TRY(check_paged_ws(*paged, ws, ws_bytes));
+  CKV_CUDA(launch_gather_pages(*shape, *params, *paged, k, v, indices, budgets, offsets, page_table, k_pages, v_pages, lengths,
+                               reinterpret_cast<int*>(static_cast<char*>(ws) + paged_ws(*paged).status),
+                               (cudaStream_t)stream));
+  return CKV_OK;
+}
+
+ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k_pages, const void* v_pages,
+                            const int32_t* page_table, const int32_t* lengths, const int32_t* token_starts, void* out,
+                            float* lse_or_null, void* ws, size_t ws_bytes, void* stream) {
+  CKV_TRY(check_tokens(paged));
+  CKV_TRY(check_pages(paged));
+  CKV_TRY(check_paged_ws(*paged, ws, ws_bytes));
+  if (paged->n_tokens == 0) return CKV_OK;
+  if (!good({q, k_pages, v_pages, out}, 16) || !good({page_table, lengths, token_starts}, 4)) return CKV_ERR_INVALID_ARG;
+  if (lse_or_null && !aligned(lse_or_null, 4)) return CKV_ERR_INVALID_ARG;
+  if (!token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, paged->n_q_heads)) return CKV_ERR_INVALID_ARG;
+  const int64_t T = paged->n_tokens, H = paged->n_q_heads, e = esize(*paged);
+  if (overlap(range_of(out, T, H, H * kHeadDim, kHeadDim, e), range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e)))
+    return CKV_ERR_INVALID_ARG;
+  CKV_CUDA(launch_paged_attend(*paged, q, k_pages, v_pages, page_table, lengths, token_starts, out, lse_or_null,
+                               static_cast<char*>(ws), (cudaStream_t)stream));
+  return CKV_OK;
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

@@ -1,0 +1,288 @@
+// Attention of new tokens over a paged cache: o = softmax(scale q k^T) v, causal inside the chunk, one pass over the
+// keys with a running maximum m and sum l per query row,
+//   m' = max(m, x),  l' = l 2^(m - m') + 2^(x - m'),  o' = o 2^(m - m') + 2^(x - m') v,   x = scale log2(e) q.k,
+// which can be cut anywhere along the keys: partial (m, l, o) of any two ranges join by the same rule.
+//
+// This file has the kernel for fp32 inputs, the join of split items and the choice of kernels.
+//
+// attend_rows_kernel: fp32 arithmetic on the CUDA cores, blocks of four query rows.  A warp takes eight keys at a
+// time, eight lanes per key with 16 dimensions each: queries, keys, values and the output all stay in registers, nothing
+// is staged, and each of the four groups of eight lanes keeps its own running (m, l, o); they join when the item ends.
+#include <cuda_bf16.h>
+
+#include "paged_work.cuh"
+
+namespace ckv {
+namespace {
+
+constexpr int kRowsM = 4;            // query rows of a block
+constexpr int kRowsThreads = 256;
+constexpr int kRowsWarps = kRowsThreads / 32;
+constexpr int kRowsTile = kRowsWarps * 8;   // keys a CTA takes per step
+constexpr int kWorkers = 148;        // one CTA per SM
+
+template <bool BF16>
+__device__ __forceinline__ void load16(const char* row, int l8, float (&x)[16]) {
+  // the 16 dimensions of lane l8 of 8: 16-byte pieces l8, l8 + 8, ... of the row (coalesced over the eight lanes)
+  if (BF16) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint4 r = *reinterpret_cast<const uint4*>(row + (c * 8 + l8) * 16);
+      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[c * 8 + 2 * i] = __uint_as_float(w[i] << 16);
+        x[c * 8 + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float4 r = *reinterpret_cast<const float4*>(row + (c * 8 + l8) * 16);
+      x[c * 4] = r.x, x[c * 4 + 1] = r.y, x[c * 4 + 2] = r.z, x[c * 4 + 3] = r.w;
+    }
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ int dim16(int l8, int i) {   // which dimension load16 put into x[i]
+  return BF16 ? ((i >> 3) * 8 + l8) * 8 + (i & 7) : ((i >> 2) * 8 + l8) * 4 + (i & 3);
+}
+
+struct RowsSmem {
+  Plan plan;
+  float2 ml[kRowsWarps][kRowsM];
+  float o[kRowsWarps][kRowsM][kHeadDim];
+};
+
+template <bool BF16>
+__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a, ckv_paged pg, float x_scale,
+                                                                      const char* __restrict__ q,
+                                                                      const char* __restrict__ kp,
+                                                                      const char* __restrict__ vp, void* __restrict__ out,
+                                                                      float* __restrict__ lse) {
+  constexpr int E = BF16 ? 2 : 4;
+  __shared__ RowsSmem sm;
+  pdl_wait();
+  make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
+  pdl_launch_dependents();
+  long long left = sm.plan.left;
+  if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
+  if (left == 0) return;
+  int pair = sm.plan.pair, block = sm.plan.block, t0 = sm.plan.t0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
+  for (;;) {
+    const Item it = make_item(a, pair, block, t0, left);
+    const int rows = block_rows(a, it);
+    float qr[kRowsM][16], acc[kRowsM][16], m[kRowsM], l[kRowsM];
+    int limit[kRowsM];
+#pragma unroll
+    for (int r = 0; r < kRowsM; ++r) {
+      m[r] = -INFINITY, l[r] = 0.f, limit[r] = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[r][i] = 0.f, qr[r][i] = 0.f;
+      if (r < rows) {
+        const int row = it.block * a.M + r, token = row / a.G, h = it.g * a.G + (row - token * a.G);
+        load16<BF16>(q + ((it.first + token) * pg.q_stride_tok + h * pg.q_stride_head) * E, l8, qr[r]);
+        limit[r] = row_limit(a, it, r);
+      }
+    }
+    const int end = min(it.t1 * a.tile, it.visible);
+    for (int j0 = it.t0 * a.tile; j0 < end; j0 += a.tile) {
+      float x[2][kRowsM], kv[2][16], vv[2][16];
+      int key[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        key[s] = j0 + warp * 8 + s * 4 + grp;
+        int page = -1;
+        if (key[s] < end) page = page_of(a, it, key[s] >> a.log_p);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) kv[s][i] = 0.f, vv[s][i] = 0.f;
+        if (page >= 0) {
+          const int64_t at = (page * pg.page_stride + (key[s] & (a.P - 1)) * pg.page_stride_row) * E;
+          load16<BF16>(kp + at, l8, kv[s]);
+          load16<BF16>(vp + at, l8, vv[s]);
+        } else {
+          key[s] = 0x7fffffff;   // hidden from every row
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int r = 0; r < kRowsM; ++r) {
+          float d = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) d = fmaf(qr[r][i], kv[s][i], d);
+#pragma unroll
+          for (int b = 1; b < 8; b <<= 1) d += __shfl_xor_sync(0xffffffffu, d, b);
+          x[s][r] = key[s] < limit[r] ? d * x_scale : -INFINITY;
+        }
+#pragma unroll
+      for (int r = 0; r < kRowsM; ++r) {
+        const float top = fmaxf(m[r], fmaxf(x[0][r], x[1][r]));
+        const float ref = top == -INFINITY ? 0.f : top;
+        const float c = exp2f(m[r] - ref), p0 = exp2f(x[0][r] - ref), p1 = exp2f(x[1][r] - ref);
+        m[r] = top;
+        l[r] = fmaf(l[r], c, p0 + p1);
+        // a hidden key's value may be anything: its row is skipped, not multiplied by zero
+        const bool s0 = key[0] < limit[r], s1 = key[1] < limit[r];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float o = acc[r][i] * c;
+          if (s0) o = fmaf(p0, vv[0][i], o);
+          if (s1) o = fmaf(p1, vv[1][i], o);
+          acc[r][i] = o;
+        }
+      }
+    }
+    // join the four groups of the warp, then the warps
+#pragma unroll
+    for (int r = 0; r < kRowsM; ++r) {
+      float top = m[r];
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+      const float c = top == -INFINITY ? 0.f : exp2f(m[r] - top);
+      float sum = l[r] * c;
+      sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+      if (lane == 0) sm.ml[warp][r] = make_float2(top, sum);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float o = acc[r][i] * c;
+        o += __shfl_xor_sync(0xffffffffu, o, 8);
+        o += __shfl_xor_sync(0xffffffffu, o, 16);
+        if (grp == 0) sm.o[warp][r][dim16<BF16>(l8, i)] = o;
+      }
+    }
+    __syncthreads();
+    const bool whole = it.t0 == 0 && it.t1 == it.tiles;
+    const int which = it.t0 > 0 ? 0 : 1;
+    const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.slot_rows;
+    for (int e = threadIdx.x; e < rows * kHeadDim; e += kRowsThreads) {
+      const int r = e / kHeadDim, d = e - r * kHeadDim;
+      float top = -INFINITY;
+      for (int w = 0; w < kRowsWarps; ++w) top = fmaxf(top, sm.ml[w][r].x);
+      float sum = 0.f, o = 0.f;
+      for (int w = 0; w < kRowsWarps; ++w) {
+        const float c = top == -INFINITY ? 0.f : exp2f(sm.ml[w][r].x - top);
+        sum = fmaf(sm.ml[w][r].y, c, sum);
+        o = fmaf(sm.o[w][r][d], c, o);
+      }
+      if (whole) {
+        const int64_t at = out_row(a, it, r);
+        o = top == -INFINITY ? 0.f : o / sum;
+        if (BF16) static_cast<__nv_bfloat16*>(out)[at * kHeadDim + d] = __float2bfloat16(o);
+        else static_cast<float*>(out)[at * kHeadDim + d] = o;
+        if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      } else {
+        a.o[(slot + r) * kHeadDim + d] = o;
+        if (d == 0) a.ml[slot + r] = make_float2(top, sum);
+      }
+    }
+    if (!whole && threadIdx.x == 0) {
+      int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
+      sp[2 * which] = pair, sp[2 * which + 1] = block;
+    }
+    left -= it.t1 - it.t0;
+    if (left <= 0 || !next_item(a, pair, block, it.n)) return;
+    t0 = 0;
+    __syncthreads();
+  }
+}
+
+// Worker w's slot 1 holds the beginning of an item that the workers after it went on with (their slots 0): the parts are
+// added up in worker order.  One CTA per (worker, eight rows), 32 threads per row.
+constexpr int kJoinRows = 8;
+template <bool BF16>
+__global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int workers, void* __restrict__ out,
+                                                              float* __restrict__ lse) {
+  pdl_wait();
+  const int w = blockIdx.x;
+  const int4 mine = a.split[w];
+  if (mine.z < 0) return;
+  const Item it = make_item(a, mine.z, mine.w, 0, 1ll << 40);
+  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), d = (threadIdx.x & 31) * 4;
+  if (r >= block_rows(a, it)) return;
+  int last = w + 1;
+  while (last < workers && a.split[last].x == mine.z && a.split[last].y == mine.w) ++last;
+  float2 ml = a.ml[((int64_t)w * 2 + 1) * a.slot_rows + r];
+  float4 o = *reinterpret_cast<const float4*>(a.o + (((int64_t)w * 2 + 1) * a.slot_rows + r) * kHeadDim + d);
+  for (int p = w + 1; p < last; ++p) {
+    const int64_t slot = (int64_t)p * 2 * a.slot_rows + r;
+    const float2 x = a.ml[slot];
+    const float4 y = *reinterpret_cast<const float4*>(a.o + slot * kHeadDim + d);
+    const float top = fmaxf(ml.x, x.x), ref = top == -INFINITY ? 0.f : top;
+    const float ca = exp2f(ml.x - ref), cb = exp2f(x.x - ref);
+    ml = make_float2(top, ml.y * ca + x.y * cb);
+    o.x = o.x * ca + y.x * cb, o.y = o.y * ca + y.y * cb, o.z = o.z * ca + y.z * cb, o.w = o.w * ca + y.w * cb;
+  }
+  const bool none = ml.x == -INFINITY;
+  const float inv = none ? 0.f : 1.0f / ml.y;
+  const int64_t at = out_row(a, it, r);
+  if (BF16) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+    const uint2 v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + at * kHeadDim + d) = v;
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + at * kHeadDim + d) =
+        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  }
+  if (lse && d == 0) lse[at] = none ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
+}
+
+int log2_of(int p) {
+  int l = 0;
+  while ((1 << l) < p) ++l;
+  return l;
+}
+
+}  // namespace
+
+template <bool BF16>
+cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(workers, (a.slot_rows + kJoinRows - 1) / kJoinRows), cfg.blockDim = dim3(32 * kJoinRows), cfg.stream = st;
+  cudaLaunchAttribute attr = pdl_attribute();
+  cfg.attrs = &attr, cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel<BF16>, a, workers, out, lse);
+  count_launch();
+  return e;
+}
+
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+PagedWs paged_ws(const ckv_paged& pg) {
+  PagedWs w{};
+  (void)pg;
+  size_t o = 0;
+  w.status = o, o += 256;
+  w.split = o, o = up256(o + kWorkers * sizeof(int4));
+  w.ml = o, o = up256(o + (size_t)kWorkers * 2 * kRowsM * sizeof(float2));
+  w.o = o, o = up256(o + (size_t)kWorkers * 2 * kRowsM * kHeadDim * sizeof(float));
+  w.total = o;
+  return w;
+}
+
+cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
+                                const int32_t* table, const int32_t* lengths, const int32_t* starts, void* out, float* lse,
+                                char* ws, cudaStream_t st) {
+  const PagedWs w = paged_ws(pg);
+  WorkArgs a{};
+  a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = pg.causal;
+  a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4, a.min_rows = 0, a.max_rows = 0x7fffffff;
+  a.P = pg.page_size, a.log_p = log2_of(pg.page_size), a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
+  a.starts = starts, a.lengths = lengths, a.table = table, a.status = reinterpret_cast<int*>(ws + w.status);
+  a.split = reinterpret_cast<int4*>(ws + w.split), a.ml = reinterpret_cast<float2*>(ws + w.ml);
+  a.o = reinterpret_cast<float*>(ws + w.o), a.slot_rows = kRowsM;
+  const float x_scale = (pg.scale != 0.f ? pg.scale : 0.08838834764831845f) * kLog2e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
+  cudaLaunchAttribute attr = pdl_attribute();
+  cfg.attrs = &attr, cfg.numAttrs = 1;
+  const bool bf16 = pg.dtype == CKV_BF16;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, bf16 ? attend_rows_kernel<true> : attend_rows_kernel<false>, a, pg, x_scale,
+                                     (const char*)q, (const char*)k_pages, (const char*)v_pages, out, lse);
+  count_launch();
+  if (e == cudaSuccess) e = bf16 ? launch_join<true>(a, kWorkers, out, lse, st) : launch_join<false>(a, kWorkers, out, lse, st);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace ckv

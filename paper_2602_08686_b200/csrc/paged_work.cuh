@@ -1,0 +1,188 @@
+// Work schedule of the attention over pages, and the join of split results.
+//
+// An item is one block of query rows of one (unit, KV head): the rows r = token * G + head of the unit's tokens and the
+// group's G query heads, `M` of them.  Its cost is the number of key tiles its last token sees (at least one, so that rows
+// that see nothing are written too).  Lengths and token counts live on the device, so the split is made there:
+// every worker (CTA) adds up the costs, takes an equal share of the total sequence of tiles and works through the items
+// in it.  The first of them may have been begun by the worker before, the last may be finished by the next: those two
+// leave unnormalised partial results in the worker's two slots, and join_kernel adds up what belongs together in worker
+// order (the result does not depend on timing).
+#pragma once
+#include "paged.cuh"
+
+namespace ckv {
+
+struct WorkArgs {
+  int Nu, H, Hkv, G, T, causal;
+  int M;            // query rows of a block
+  int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
+  int tile;         // keys per tile
+  int granule;      // least tiles per worker
+  int min_rows;     // only units with more query rows per head than this ...
+  int max_rows;     // ... and at most this many
+  int P, log_p, n_pages, max_pages;
+  const int32_t *starts, *lengths, *table;
+  int* status;
+  int4* split;      // [workers]: (pair, block) in slot 0 (begun by an earlier worker) and slot 1 (not finished), or -1
+  float2* ml;       // [workers][2][slot_rows]
+  float* o;         // [workers][2][slot_rows][128]
+  int slot_rows;
+};
+
+struct Item {
+  int u, g, block;       // block of rows
+  int first, n, len;     // the unit's first token and token count; rows the head holds
+  int rows;              // query rows of the unit (n * G)
+  int visible;           // rows the block's last token sees
+  int tiles;             // tiles of the whole item
+  int t0, t1;            // this worker's part
+};
+
+__device__ __forceinline__ int unit_blocks(const WorkArgs& a, int n) {
+  const int64_t rows = (int64_t)n * a.G;
+  if (rows <= a.min_rows || rows > a.max_rows) return 0;
+  return a.tokens ? (n + a.tokens - 1) / a.tokens : (int)((rows + a.M - 1) / a.M);
+}
+__device__ __forceinline__ int head_length(const WorkArgs& a, int pair) {
+  return min(max(a.lengths[pair], 0), a.max_pages << a.log_p);
+}
+// rows that the last token of a block sees
+__device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, int block) {
+  if (!a.causal) return len;
+  const int64_t end = a.tokens ? (int64_t)(block + 1) * a.tokens : ((int64_t)(block + 1) * a.M + a.G - 1) / a.G;
+  const int last = (int)(end < n ? end : n) - 1;
+  return min(max(len - n + last + 1, 0), len);
+}
+__device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) / a.tile, 1); }
+
+struct Plan {           // in shared memory
+  long long warp_sum[32];
+  long long total;
+  long long left;       // tiles this worker still has to do
+  int pair, block, t0;  // where it starts
+  int workers;          // workers that have something to do
+};
+
+// All threads of the CTA.  Returns with the worker's share in `plan`.
+template <int NT>
+__device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& plan) {
+  const int pairs = a.Nu * a.Hkv;
+  const int per = (pairs + NT - 1) / NT;
+  const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto cost_of = [&](int p) {
+    int first, n;
+    unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
+    const int nb = unit_blocks(a, n);
+    if (nb == 0) return 0ll;
+    const int len = head_length(a, p);
+    long long c = 0;
+    for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b));
+    return c;
+  };
+  long long mine = 0;
+  for (int p = p0; p < p1; ++p) mine += cost_of(p);
+  long long incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 31) plan.warp_sum[warp] = incl;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    long long s = 0;
+    for (int w = 0; w < NT / 32; ++w) {
+      const long long x = plan.warp_sum[w];
+      plan.warp_sum[w] = s;
+      s += x;
+    }
+    plan.total = s;
+  }
+  __syncthreads();
+  const long long total = plan.total;
+  const long long most = (total + a.granule - 1) / a.granule;
+  const int workers = (int)(most < n_workers ? most : n_workers);
+  const long long begin = worker < workers ? total * worker / workers : total;
+  const long long end = worker < workers ? total * (worker + 1) / workers : total;
+  if (threadIdx.x == 0) plan.left = end - begin, plan.workers = workers;
+  const long long before = plan.warp_sum[warp] + incl - mine;
+  if (end > begin && begin >= before && begin < before + mine) {
+    long long at = begin - before;
+    for (int p = p0; p < p1; ++p) {
+      const long long c = cost_of(p);
+      if (at >= c) {
+        at -= c;
+        continue;
+      }
+      int first, n, b = 0;
+      unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
+      const int len = head_length(a, p);
+      for (;; ++b) {
+        const int t = tiles_of(a, block_visible(a, n, len, b));
+        if (at < t) break;
+        at -= t;
+      }
+      plan.pair = p, plan.block = b, plan.t0 = (int)at;
+      break;
+    }
+  }
+  __syncthreads();
+}
+
+// The item at (pair, block), from tile t0, at most `left` tiles of it.
+__device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block, int t0, long long left) {
+  Item it;
+  it.u = pair / a.Hkv, it.g = pair - it.u * a.Hkv, it.block = block;
+  unit_tokens(a.starts, it.u, a.T, it.first, it.n);
+  it.len = head_length(a, pair);
+  if (it.len != a.lengths[pair] && threadIdx.x == 0) report_status(a.status, kStatusPage);
+  it.rows = it.n * a.G;
+  it.visible = block_visible(a, it.n, it.len, block);
+  it.tiles = tiles_of(a, it.visible);
+  it.t0 = t0;
+  it.t1 = (int)(left < it.tiles - t0 ? t0 + left : it.tiles);
+  return it;
+}
+// Moves to the next item that has rows; false behind the last one.
+__device__ __forceinline__ bool next_item(const WorkArgs& a, int& pair, int& block, int n) {
+  if (block + 1 < unit_blocks(a, n)) {
+    ++block;
+    return true;
+  }
+  block = 0;
+  while (++pair < a.Nu * a.Hkv) {
+    int first, m;
+    unit_tokens(a.starts, pair / a.Hkv, a.T, first, m);
+    if (unit_blocks(a, m) > 0) return true;
+    pair = (pair / a.Hkv) * a.Hkv + a.Hkv - 1;   // the unit's other heads have none either
+  }
+  return false;
+}
+// Rows of the block, and where query row r of it (token, head) lives.
+__device__ __forceinline__ int block_rows(const WorkArgs& a, const Item& it) {
+  return min(a.M, it.rows - it.block * a.M);
+}
+__device__ __forceinline__ int64_t out_row(const WorkArgs& a, const Item& it, int r) {
+  const int row = it.block * a.M + r;
+  const int token = row / a.G;
+  return (int64_t)(it.first + token) * a.H + it.g * a.G + (row - token * a.G);
+}
+// Rows of the cache that query row r of the block sees.
+__device__ __forceinline__ int row_limit(const WorkArgs& a, const Item& it, int r) {
+  if (!a.causal) return it.len;
+  const int token = (it.block * a.M + r) / a.G;
+  return min(max(it.len - it.n + token + 1, 0), it.len);
+}
+// Pool row (page * page_size + row within) is not formed: the pool's strides are free.  A bad page gives -1.
+__device__ __forceinline__ int page_of(const WorkArgs& a, const Item& it, int slot) {
+  const int p = a.table[((int64_t)it.u * a.Hkv + it.g) * a.max_pages + slot];
+  if ((unsigned)p < (unsigned)a.n_pages) return p;
+  report_status(a.status, kStatusPage);
+  return -1;
+}
+
+template <bool BF16>
+cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, cudaStream_t st);
+
+}  // namespace ckv

@@ -1,0 +1,464 @@
+"""GPU tests of the paged-cache operators against plain 64-bit statements of them (tests/paged_reference.py).
+
+Tolerances count roundings.  An output in bf16 is off by at most half a step of its value, 2^-8 relative (`finfo.eps / 2`); fp32
+arithmetic contributes multiples of 2^-24.
+  rotate: fp32 angle of a fraction of a turn (2^-25 turns: 1.9e-7 rad) and its sine and cosine, three products and a sum, and
+    with norms a 128-term sum of squares (relative 2^-24 * 8, a shuffle tree), a root and a division: at most 40 * 2^-24 of
+    |a| + |b| of the pair.
+  attend: a logit is a dot product of 128 terms in fp32: off by dx <= 132 * 2^-24 * |q| |k| * scale (Cauchy-Schwarz on the
+    absolute products); the exponential of it moves by a factor 1 + dx + 2^-22 (exp2f and its argument, |x| <= 64); sums of
+    non-negative terms over at most `depth` sequential additions add depth * 2^-24.  With r = dx + 2^-20 + depth * 2^-24:
+    lse is off by at most r + 2^-23 |lse|; the output by 2 r max|v| (numerator and denominator) + 2^-24 |out|.
+    In bf16 the probabilities are rounded for the product with v, 2^-8 relative each, so at most 2^-8 max|v| in the worst
+    case, and the output once more, 2^-8 |out|.  Those roundings are independent: over all outputs the 2-norm of the error is
+    bounded by 2 * 2^-8 of the outputs' 2-norm wherever no single key carries the row, and never by more than the first bound.
+"""
+import math
+
+import pytest
+import torch
+
+import paged_reference as R
+from paper_2602_08686_b200 import inputs as gen
+
+pytestmark = pytest.mark.gpu
+D = 128
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2602_08686_b200 import binding
+    binding.lib()
+    assert torch.cuda.is_available()
+    return binding
+
+
+def starts_of(counts, lead=0):
+    s = [lead]
+    for c in counts:
+        s.append(s[-1] + c)
+    return s
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------------------------------------------------------ rotate
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,Hkv,T,rot,interleaved,norm,in_place", [
+    (32, 8, 1, 128, False, False, False), (28, 4, 3, 128, True, True, False), (8, 1, 17, 64, False, True, True),
+    (5, 5, 33, 96, True, False, True), (16, 2, 2500, 128, False, True, False), (1, 1, 2371, 16, False, False, False),
+    (7, 7, 9, 0, False, True, False), (64, 64, 5, 32, True, True, True), (3, 1, 4, 112, False, False, False)])
+def test_rotate(B, dtype, H, Hkv, T, rot, interleaved, norm, in_place):
+    g = torch.Generator(device="cuda").manual_seed(T + rot)
+    lead, pad = (1, 2) if T > 4 else (0, 0)       # padding rows before the first and behind the last unit
+    qkv = torch.randn(T, H + 2 * Hkv, D, generator=g, device="cuda").to(dtype)
+    before = qkv.clone()
+    q, k = qkv[:, :H], qkv[:, H:H + Hkv]
+    pos = torch.randint(-5, 1 << 20, (T,), generator=g, device="cuda", dtype=torch.int32)
+    inv = 10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64, device="cuda") / max(rot, 1)) if rot else None
+    w = [1 + 0.2 * torch.randn(D, generator=g, device="cuda") if norm else None for _ in range(2)]
+    starts = starts_of([T - lead - pad], lead)
+    rotary = B.make_rotary(inv, interleaved=interleaved, q_norm_w=w[0], k_norm_w=w[1], rot_scale=1.25, norm_eps=1e-5)
+    outs = (q, k) if in_place else (torch.full((T, H, D), 7.0, device="cuda").to(dtype), torch.full((T, Hkv, D), 7.0, device="cuda").to(dtype))
+    B.ckv_rotate(B.make_packed(q, k, 1), rotary, q, k, pos, i32(starts), *outs)
+    for x, wt, out in ((before[:, :H], w[0], outs[0]), (before[:, H:H + Hkv], w[1], outs[1])):
+        live = slice(lead, T - pad)
+        want = R.turn(x, pos, inv, wt, 1e-5, interleaved, 1.25)
+        size = want.abs() + R.turn(x, pos, inv, wt, 1e-5, interleaved, 1.25).roll(1, -1).abs().amax(-1, keepdim=True)
+        tol = 40 * EPS * size + (2.0 ** -8 if dtype == torch.bfloat16 else 2 * EPS) * want.abs()
+        assert ((out.double() - want).abs() <= tol)[live].all(), ((out.double() - want).abs() / tol)[live].max()
+        for rows in (slice(0, lead), slice(T - pad, T)):
+            assert torch.equal(out[rows], x[rows] if in_place else torch.full_like(out[rows], 7.0))
+    if in_place:
+        assert torch.equal(qkv[:, H + Hkv:], before[:, H + Hkv:])     # the values between are untouched
+
+
+def test_rotate_one_side_only_and_plain_copies(B):
+    x = torch.randn(6, 4, D, device="cuda")
+    inv = 10000.0 ** (-torch.arange(0, 128, 2, dtype=torch.float64, device="cuda") / 128)
+    pos, st = torch.arange(6, dtype=torch.int32, device="cuda"), i32([0, 6])
+    out = torch.zeros_like(x)
+    B.ckv_rotate(B.make_packed(x, None, 1), B.make_rotary(inv), x, None, pos, st, out, None)
+    ref = R.turn(x, pos, inv)
+    assert (out.double() - ref).abs().max() <= 40 * EPS * 2 * x.abs().max()
+    out2 = torch.zeros_like(x)
+    B.ckv_rotate(B.make_packed(None, x, 1), B.make_rotary(inv), None, x, pos, st, None, out2)
+    assert torch.equal(out, out2)
+    B.ckv_rotate(B.make_packed(x, None, 1), B.make_rotary(None), x, None, pos, st, out, None)
+    assert torch.equal(out, x)                              # no norm, no rotation: the same bits
+
+
+# ------------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,Hkv,page,counts,lens,rot,norm", [
+    (32, 8, 64, [1], [[0]], 128, False), (8, 2, 16, [1, 0, 5], [[15, 16], [3, 4], [31, 0]], 128, True),
+    (28, 4, 32, [40, 1, 2], [[0, 1, 31, 32], [33, 63, 64, 65], [5, 6, 7, 8]], 64, True),
+    (4, 4, 256, [300, 2], [[255, 256, 257, 0], [511, 1, 2, 3]], 0, False), (2, 1, 128, [2000], [[77]], 128, False)])
+def test_append(B, dtype, H, Hkv, page, counts, lens, rot, norm):
+    lens = [row if len(row) == Hkv else row * Hkv for row in lens]
+    g = torch.Generator(device="cuda").manual_seed(sum(counts) + page)
+    pad = 3
+    c = R.Cache(lens, page, max_extra=max(counts), dtype=dtype, device="cuda", poison=3.0, row_pad=8 if page == 32 else 0)
+    starts = starts_of(counts)
+    T = starts[-1] + pad
+    qkv = torch.randn(T, H + 2 * Hkv, D, generator=g, device="cuda").to(dtype)
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    pos = torch.randint(0, 1 << 18, (T,), generator=g, device="cuda", dtype=torch.int32)
+    inv = 10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64, device="cuda") / max(rot, 1)) if rot else None
+    w = [1 + 0.2 * torch.randn(D, generator=g, device="cuda") if norm else None for _ in range(2)]
+    rotary = B.make_rotary(inv, q_norm_w=w[0], k_norm_w=w[1]) if rot or norm else None
+    pg = B.make_paged(c.k_pages, c.table, q=q, k_new=k, max_new=max(counts))
+    ws = B.alloc_paged_workspace(pg)
+    q_out = torch.full((T, H, D), 5.0, device="cuda").to(dtype)
+    new = torch.full((len(counts), Hkv), -1, dtype=torch.int32, device="cuda")
+    want_k, want_v = (p.double().clone() for p in c.pools)
+    size_k = want_k.abs()
+    tk = R.turn(k, pos, inv, w[1])
+    for u in range(len(counts)):
+        for gg in range(Hkv):
+            for i in range(counts[u]):
+                j = lens[u][gg] + i
+                at = int(c.table[u, gg, j // page]), j % page
+                want_k[at][:D], want_v[at][:D] = tk[starts[u] + i, gg], v[starts[u] + i, gg].double()
+                size_k[at][:D] = 2 * tk[starts[u] + i, gg].abs().max()
+    B.ckv_append(pg, rotary, k, v, pos, i32(starts), c.lengths, c.table, c.k_pages, c.v_pages, ws, q=q, q_out=q_out, new_lengths=new)
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 2 * EPS
+    assert torch.equal(c.pools[1].double(), want_v)
+    assert ((c.pools[0].double() - want_k).abs() <= 40 * EPS * size_k + half * want_k.abs()).all()
+    untouched = want_k == 3.0
+    assert torch.equal(c.pools[0].double()[untouched], want_k[untouched])
+    tq = R.turn(q, pos, inv, w[0])
+    live = slice(0, starts[-1])
+    assert ((q_out.double() - tq).abs() <= 80 * EPS * tq.abs().amax(-1, keepdim=True) + half * tq.abs())[live].all()
+    assert (q_out[starts[-1]:] == 5.0).all()
+    assert torch.equal(new, c.lengths + i32(counts)[:, None])
+    assert B.ckv_device_status(ws) == B.OK
+    # without queries and new lengths: the same pages
+    again = [p.clone() for p in c.pools]
+    B.ckv_append(pg, rotary, k, v, pos, i32(starts), c.lengths, c.table, c.k_pages, c.v_pages, ws)
+    assert torch.equal(again[0], c.pools[0]) and torch.equal(again[1], c.pools[1])
+
+
+def test_append_leaves_out_rows_that_have_no_page_and_says_so(B):
+    c = R.Cache([[20, 3]], 16, max_extra=4, dtype=torch.float32, device="cuda", poison=3.0)
+    k = torch.randn(4, 2, D, device="cuda")
+    pg = B.make_paged(c.k_pages, c.table, k_new=k)
+    ws = torch.randint(0, 255, (B.ckv_paged_workspace_bytes(pg),), dtype=torch.uint8, device="cuda")   # nobody cleared it
+    args = lambda table, lengths: (pg, None, k, k, None, i32([0, 4]), lengths, table, c.k_pages, c.v_pages, ws)
+    before = c.pools[0].clone()
+    for bad in (torch.full_like(c.table, -1), torch.full_like(c.table, 1 << 30)):
+        B.ckv_append(*args(bad, c.lengths))
+        assert B.ckv_device_status(ws) == B.ERR_PAGE and B.ckv_device_status(ws) == B.OK
+    for lengths in (i32([[-4, -9]]), i32([[2147483647, 1 << 30]])):
+        B.ckv_append(*args(c.table, lengths))
+        assert B.ckv_device_status(ws) == B.ERR_PAGE
+    assert torch.equal(before, c.pools[0])
+    B.ckv_append(*args(c.table, c.lengths))
+    assert B.ckv_device_status(ws) == B.OK
+    assert torch.equal(c.k_pages[c.table[0, 1, 0].long(), 3:7], k[:, 1])
+
+
+# ---------------------------------------------------------------------------------------- gather into pages
+@pytest.mark.parametrize("cfg_name,page,L", [("c1", 16, 2048), ("c2", 64, 4096), ("c5", 256, 1111)])
+def test_gather_pages(B, cfg_name, page, L):
+    from test_gpu_parity import params_of, problem_of
+    cfg = gen.shrink(gen.CONFIGS[cfg_name], n_layers=2, batch=1, seq_len=L, budget_per_head=128, n_needles=4)
+    b = gen.make_batch(cfg, "cuda")
+    P = params_of(B, problem_of(cfg, 2))
+    out = B.compress(b["q"], b["k"], b["v"], b["head_w"], b["sens"], P)
+    shape, params = B.make_shape(b["q"], b["k"]), B.make_params(P, b["head_w"], b["sens"])
+    bud = out["budgets"].tolist()
+    c = R.Cache(bud, page, dtype=b["k"].dtype, device="cuda", poison=9.0)
+    for p in c.pools:
+        p.fill_(9.0)
+    pg = B.make_paged(c.k_pages, c.table, n_q_heads=cfg.n_q_heads)
+    ws = B.alloc_paged_workspace(pg)
+    lengths = torch.full_like(out["budgets"], -1)
+    B.ckv_gather_pages(shape, params, pg, b["k"], b["v"], out["indices"], out["budgets"], out["offsets"], c.table, c.k_pages,
+                       c.v_pages, lengths, ws)
+    assert torch.equal(lengths, out["budgets"]) and B.ckv_device_status(ws) == B.OK
+    off = out["offsets"].tolist()
+    for pool, src in zip((c.k_pages, c.v_pages), ("k_out", "v_out")):
+        want = torch.full_like(pool, 9.0)
+        for u in range(2):
+            for g in range(cfg.n_kv_heads):
+                for j in range(bud[u][g]):
+                    want[int(c.table[u, g, j // page]), j % page] = out[src][u, off[u][g] + j]
+        assert torch.equal(pool, want)
+    short = torch.full_like(c.table, -1)
+    B.ckv_gather_pages(shape, params, pg, b["k"], b["v"], out["indices"], out["budgets"], out["offsets"], short, c.k_pages,
+                       c.v_pages, lengths, ws)
+    assert B.ckv_device_status(ws) == B.ERR_PAGE
+
+
+# ------------------------------------------------------------------------------------------------ attend
+def run_attend(B, c, q, starts, causal=True, scale=0.0, max_new=0, lse=True):
+    pg = B.make_paged(c.k_pages, c.table, q=q, causal=causal, scale=scale, max_new=max_new)
+    n = B.ckv_paged_workspace_bytes(pg)
+    ws = torch.full((n + 512,), 0xAB, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, 11.0, device="cuda").to(q.dtype)
+    l = torch.full(q.shape[:2], 11.0, device="cuda") if lse else None
+    B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, c.lengths, i32(starts), out, ws[256:256 + n], lse=l)
+    assert B.ckv_device_status(ws[256:256 + n]) == B.OK
+    assert (ws[:256] == 0xAB).all() and (ws[256 + n:] == 0xAB).all()
+    return out, l
+
+
+def check_attend(c, q, starts, out, lse, causal=True, scale=None, spread=True):
+    want, want_lse = R.attend(q, starts, c.rows, causal, scale)
+    live = torch.zeros(q.shape[0], dtype=torch.bool, device="cuda")
+    live[starts[0]:starts[-1]] = True
+    s = 1 / math.sqrt(D) if scale is None else abs(scale)
+    kmax = max([float(k.double().norm(dim=-1).max()) for row in c.rows for k, _ in row if k.shape[0]] + [0.0])
+    vmax = max([float(v.double().abs().max()) for row in c.rows for _, v in row if v.shape[0]] + [0.0])
+    depth = max(max(r) for r in c.lens) / 8 + 256
+    r = 132 * EPS * float(q[live].double().norm(dim=-1).max()) * kmax * s + 2.0 ** -20 + depth * EPS
+    tol = 2 * r * vmax + (2.0 ** -8 * (vmax + want.abs()) if q.dtype == torch.bfloat16 else EPS * want.abs())
+    err = (out.double() - want).abs()
+    assert (err <= tol)[live].all(), float((err / tol)[live].max())
+    if q.dtype == torch.bfloat16 and spread and bool(live.any()):
+        assert err[live].norm() <= 2 * 2.0 ** -8 * want[live].norm() + 2 * r * vmax * math.sqrt(err[live].numel())
+    if lse is not None:
+        none = torch.isinf(want_lse)
+        assert torch.equal((lse == -math.inf)[live], none[live])
+        seen = live[:, None] & ~none
+        assert ((lse.double() - want_lse).abs() <= r + 2 * EPS * want_lse.abs())[seen].all()
+        assert (lse[~live] == 11.0).all()
+    assert (out[~live] == 11.0).all()
+
+
+CASES = [
+    # H, Hkv, page, tokens per unit, rows per (unit, head) after the tokens
+    (8, 2, 16, [1], [[1, 1]]),
+    (8, 2, 16, [1], [[0, 5]]),
+    (32, 8, 64, [1], [[512, 400, 1, 63, 64, 65, 127, 129]]),
+    (28, 4, 16, [1, 1, 1], [[100, 0, 17, 256], [1, 2, 3, 4], [700, 701, 699, 15]]),
+    (28, 4, 32, [5, 3, 0, 1], [[300, 5, 31, 33], [64, 65, 3, 3], [9, 9, 9, 9], [128, 127, 129, 1]]),
+    (16, 16, 128, [2, 7], [[130] * 16, [200] * 16]),
+    (24, 2, 64, [3], [[1000, 37]]),
+    (40, 1, 64, [4, 1], [[333], [90]]),
+    (8, 1, 256, [16], [[5000]]),
+    (4, 4, 16, [33, 1, 70], [[33, 40, 1000, 64], [9, 8, 7, 6], [70, 71, 300, 128]]),
+    (32, 8, 64, [130], [[130, 131, 200, 256, 257, 640, 1000, 2000]]),
+    (28, 4, 16, [19, 200], [[19, 20, 500, 128], [200, 255, 256, 1100]]),
+    (6, 2, 128, [257, 1, 64], [[300, 1500], [1500, 1], [64, 65]]),
+    (8, 8, 32, [128, 129], [[128, 129, 130, 500, 140, 150, 160, 170], [129, 300, 301, 302, 303, 304, 305, 306]]),
+    (128, 1, 64, [5], [[77]]),
+    (130, 1, 64, [3], [[77]]),
+    (8, 2, 64, [7], [[3, 6]]),                       # more tokens than rows: the first ones see nothing
+    (8, 2, 64, [300], [[100, 290]]),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,Hkv,page,counts,lens", CASES)
+def test_attend(B, dtype, causal, H, Hkv, page, counts, lens):
+    """Rows behind the lengths, pages of nobody and padding tokens are NaN; table entries of no row point far outside."""
+    c = R.Cache(lens, page, dtype=dtype, device="cuda", seed=H + page, row_pad=8 if page == 32 else 0)
+    starts = starts_of(counts, 2)
+    g = torch.Generator(device="cuda").manual_seed(len(counts))
+    qkv = torch.randn(starts[-1] + 3, H + 4, D, generator=g, device="cuda").to(dtype)
+    qkv[:2] = float("nan")
+    qkv[starts[-1]:] = float("nan")
+    q = qkv[:, 1:1 + H]
+    for max_new in (0, max(counts)):
+        out, lse = run_attend(B, c, q, starts, causal, max_new=max_new)
+        check_attend(c, q, starts, out, lse, causal)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("counts,length", [([1], 40000), ([1, 1], 9000), ([6], 20000), ([100], 9000), ([700], 3000)])
+def test_attend_long(B, dtype, counts, length):
+    """Items split over many CTAs."""
+    lens = [[length - 7 * u, length // 3] for u in range(len(counts))]
+    c = R.Cache(lens, 64, dtype=dtype, device="cuda", seed=length)
+    q = torch.randn(sum(counts), 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(dtype)
+    st = starts_of(counts)
+    out, lse = run_attend(B, c, q, st, max_new=max(counts))
+    check_attend(c, q, st, out, lse)
+    out2, lse2 = run_attend(B, c, q, st, max_new=max(counts), lse=False)
+    assert torch.equal(out, out2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("counts", [[1], [40], [200]])
+def test_attend_large_logits_and_scales(B, dtype, counts):
+    """One key far above the others, negative and tiny scales, and logits of hundreds that grow along the cache (the running
+    maximum moves at every tile)."""
+    n = counts[0]
+    c = R.Cache([[n + 900, n + 130]], 32, dtype=dtype, device="cuda", seed=3)
+    for g in range(2):
+        k, v = c.rows[0][g]
+        ramp = torch.linspace(0.0, 6.0, k.shape[0]).double()[:, None]
+        k2 = (k.double() * ramp).to(dtype)
+        c.rows[0][g] = (k2, v)
+        for j in range(k.shape[0]):
+            c.k_pages[int(c.table[0, g, j // 32]), j % 32] = k2[j].cuda()
+    q = torch.randn(n, 8, D, device="cuda").to(dtype)
+    for scale in (0.0, 1.0, -0.7, 1e-3):
+        out, lse = run_attend(B, c, q, [0, n], scale=scale)
+        check_attend(c, q, [0, n], out, lse, scale=scale or None, spread=False)
+
+
+@pytest.mark.parametrize("counts", [[1], [5], [150]])
+def test_attend_masked_infinities(B, counts):
+    """Infinite and NaN keys and values behind what a token sees do not reach it."""
+    n = counts[0]
+    for poison in (float("inf"), float("-inf"), float("nan"), torch.finfo(torch.bfloat16).min):
+        c = R.Cache([[n + 50, n + 64]], 64, dtype=torch.bfloat16, device="cuda", poison=poison)
+        # the chunk's last token is poison too: only its own query may see it
+        q = torch.randn(n, 8, D, device="cuda").bfloat16()
+        if n > 1:
+            for g in range(2):
+                j = c.lens[0][g] - 1
+                c.k_pages[int(c.table[0, g, j // 64]), j % 64] = poison
+                c.v_pages[int(c.table[0, g, j // 64]), j % 64] = poison
+        out, lse = run_attend(B, c, q, [0, n])
+        seen = n - 1 if n > 1 else 1
+        rows = [[(k, v) for k, v in c.rows[0]]]
+        want, want_lse = R.attend(q, [0, n], rows)
+        assert (out.double() - want).abs()[:seen].max() <= 0.03
+        assert (lse.double() - want_lse).abs()[:seen].max() <= 1e-3
+
+
+@pytest.mark.parametrize("dtype,counts", [(torch.float32, [2]), (torch.bfloat16, [2]), (torch.bfloat16, [90])])
+def test_attend_leaves_out_bad_pages_and_says_so(B, dtype, counts):
+    n = counts[0]
+    c = R.Cache([[n + 200, n + 77]], 16, dtype=dtype, device="cuda")
+    q = torch.randn(n, 4, D, device="cuda").to(dtype)
+    pg = B.make_paged(c.k_pages, c.table, q=q, causal=False)
+    ws = B.alloc_paged_workspace(pg)
+    out, lse = torch.zeros_like(q), torch.zeros(n, 4, device="cuda")
+    table = c.table.clone()
+    table[0, 0, 2] = -1
+    table[0, 1, 0] = c.k_pages.shape[0]
+    B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, table, c.lengths, i32([0, n]), out, ws, lse=lse)
+    assert B.ckv_device_status(ws) == B.ERR_PAGE and B.ckv_device_status(ws) == B.OK
+    keep = [torch.cat((k[:32], k[48:])) for k in c.rows[0][0]], [k[16:] for k in c.rows[0][1]]
+    want, want_lse = R.attend(q, [0, n], [[tuple(keep[0]), tuple(keep[1])]], causal=False)
+    assert (out.double() - want).abs().max() <= 0.03 and (lse.double() - want_lse).abs().max() <= 1e-3
+    # a length past the table's pages ends at its last page
+    B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, i32([[1 << 30, -5]]), i32([0, n]), out, ws, lse=lse)
+    assert B.ckv_device_status(ws) == B.ERR_PAGE
+    assert (out[:, 2:] == 0).all() and (lse[:, 2:] == -math.inf).all()
+    # token starts that run off the tokens or backwards are never followed
+    B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, c.lengths, i32([-7, 1 << 30]), out, ws, lse=lse)
+    B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, c.lengths, i32([n, 0]), out, ws, lse=lse)
+    assert B.ckv_device_status(ws) == B.OK
+
+
+def test_attend_same_bits_again_and_on_two_streams(B):
+    for counts in ([1, 1], [60, 3]):
+        c = R.Cache([[3000, 100], [777, 2500]], 64, dtype=torch.bfloat16, device="cuda")
+        q = torch.randn(sum(counts), 16, D, device="cuda").bfloat16()
+        st = i32(starts_of(counts))
+        pg = B.make_paged(c.k_pages, c.table, q=q, max_new=max(counts))
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        ws = [B.alloc_paged_workspace(pg) for _ in range(2)]
+        outs = [torch.zeros_like(q) for _ in range(2)]
+        torch.cuda.synchronize()
+        first = None
+        for _ in range(5):
+            for s, w, o in zip(streams, ws, outs):
+                B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, c.lengths, st, o, w, stream=s)
+            torch.cuda.synchronize()
+            first = outs[0].clone() if first is None else first
+            assert torch.equal(outs[0], first) and torch.equal(outs[1], first)
+
+
+def test_offsets_past_32_bits(B):
+    """A pool of more than 2^32 bytes and 2^31 elements: appended to and read at its far end."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    P, n_pages = 256, 70000            # 2.29e9 elements, 4.6 GB a pool
+    kp, vp = (torch.empty(n_pages, P, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.tensor([[[n_pages - 1, 3, n_pages - 2]]], dtype=torch.int32, device="cuda")
+    x = torch.randn(600, 1, D, device="cuda").bfloat16()
+    v = torch.randn(600, 1, D, device="cuda").bfloat16()
+    for n in (600, 1):
+        q = torch.randn(n, 4, D, device="cuda").bfloat16()
+        pg = B.make_paged(kp, table, q=q)
+        pk = B.make_paged(kp, table, k_new=x)
+        ws = B.alloc_paged_workspace(pg)
+        new = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+        B.ckv_append(pk, None, x, v, None, i32([0, 600]), i32([[0]]), table, kp, vp, ws, new_lengths=new)
+        assert torch.equal(kp[n_pages - 1], x[:P, 0]) and torch.equal(vp[n_pages - 2, :88], v[512:, 0])
+        out, lse = torch.zeros_like(q), torch.zeros(n, 4, device="cuda")
+        B.ckv_paged_attend(pg, q, kp, vp, table, new, i32([0, n]), out, ws, lse=lse)
+        want, want_lse = R.attend(q, [0, n], [[(x[:, 0], v[:, 0])]])
+        assert (out.double() - want).abs().max() <= 0.05 and (lse.double() - want_lse).abs().max() <= 1e-3
+
+
+# ------------------------------------------------------------------------------------- as they are used together
+@pytest.mark.parametrize("cfg_name,chunk", [("c2", 1), ("c2", 80), ("c5", 3), ("c1", 2)])
+def test_prompt_to_decode(B, cfg_name, chunk):
+    """rotate -> the retention pass -> gather_pages -> (append -> attend) over several steps, the steps as one captured graph
+    replayed with new tokens; against the 64-bit statement on the rows the pass kept."""
+    from test_gpu_parity import params_of, problem_of
+    Nu, L = 2, 1500
+    cfg = gen.shrink(gen.CONFIGS[cfg_name], n_layers=Nu, batch=1, seq_len=L, budget_per_head=160, n_needles=4)
+    H, Hkv, W = cfg.n_q_heads, cfg.n_kv_heads, cfg.window
+    dt = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
+    b = gen.make_batch(cfg, "cuda")
+    qkv = torch.randn(Nu * L, H + 2 * Hkv, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(4)).to(dt)
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    pos = torch.arange(L, dtype=torch.int32, device="cuda").repeat(Nu)
+    inv = 500000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+    rotary = B.make_rotary(inv, q_norm_w=torch.ones(D, device="cuda"), k_norm_w=torch.ones(D, device="cuda"))
+    B.ckv_rotate(B.make_packed(q, k, Nu), rotary, q, k, pos, i32([0, L, 2 * L]), q, k)
+    kd, vd = k.unflatten(0, (Nu, L)).transpose(1, 2), v.unflatten(0, (Nu, L)).transpose(1, 2)
+    qw = q.unflatten(0, (Nu, L))[:, L - W:].transpose(1, 2)
+    P = params_of(B, problem_of(cfg, Nu))
+    kept = B.compress(qw, kd, vd, b["head_w"], b["sens"], P)
+    shape, params = B.make_shape(qw, kd), B.make_params(P, b["head_w"], b["sens"])
+    bud = kept["budgets"].tolist()
+    steps = 3
+    c = R.Cache(bud, 32, max_extra=steps * chunk, dtype=dt, device="cuda")
+    T = Nu * chunk
+    new = torch.zeros(T, H + 2 * Hkv, D, device="cuda", dtype=dt)
+    nq, nk, nv = new[:, :H], new[:, H:H + Hkv], new[:, H + Hkv:]
+    pg = B.make_paged(c.k_pages, c.table, q=nq, k_new=nk, max_new=chunk)
+    po = B.make_paged(c.k_pages, c.table, q=torch.empty(T, H, D, device="cuda", dtype=dt), max_new=chunk)
+    ws = B.alloc_paged_workspace(pg)
+    lengths, grown = torch.zeros(Nu, Hkv, dtype=torch.int32, device="cuda"), torch.zeros(Nu, Hkv, dtype=torch.int32, device="cuda")
+    npos, st = torch.zeros(T, dtype=torch.int32, device="cuda"), i32(starts_of([chunk] * Nu))
+    q_out, out = torch.zeros(T, H, D, device="cuda", dtype=dt), torch.zeros(T, H, D, device="cuda", dtype=dt)
+    lse = torch.zeros(T, H, device="cuda")
+
+    def step():
+        B.ckv_append(pg, rotary, nk, nv, npos, st, lengths, c.table, c.k_pages, c.v_pages, ws, q=nq, q_out=q_out, new_lengths=grown)
+        B.ckv_paged_attend(po, q_out, c.k_pages, c.v_pages, c.table, grown, st, out, ws, lse=lse)
+        lengths.copy_(grown)
+
+    off = kept["offsets"].tolist()
+    rows = [[[kept[x][u, off[u][g]:off[u][g] + bud[u][g]].double() for x in ("k_out", "v_out")] for g in range(Hkv)] for u in range(Nu)]
+    graph = torch.cuda.CUDAGraph()
+    step()                                          # warm-up on an empty cache; its rows are overwritten below
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    B.ckv_gather_pages(shape, params, pg, kd, vd, kept["indices"], kept["budgets"], kept["offsets"], c.table, c.k_pages, c.v_pages,
+                       lengths, ws)
+    for s in range(steps):
+        new.copy_(torch.randn(new.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(50 + s)))
+        npos.copy_((L + s * chunk + torch.arange(chunk, device="cuda", dtype=torch.int32)).repeat(Nu))
+        graph.replay()
+        rk = R.turn(nk, npos, inv, torch.ones(D, device="cuda")).to(dt)
+        rq = R.turn(nq, npos, inv, torch.ones(D, device="cuda"))
+        for u in range(Nu):
+            for g in range(Hkv):
+                kk, vv = rows[u][g]
+                rows[u][g] = [torch.cat((kk, rk[u * chunk:(u + 1) * chunk, g].double())),
+                              torch.cat((vv, nv[u * chunk:(u + 1) * chunk, g].double()))]
+        want, want_lse = R.attend(rq.to(dt), [0, chunk, 2 * chunk], rows)
+        # a key or query that rounds the other way moves a logit by 2 * 2^-8 * |q| |k| / sqrt(d) / sqrt(d) in the mean: 0.05 in bf16
+        bf = dt == torch.bfloat16
+        assert (out.double() - want).abs().max() <= (0.1 if bf else 1e-4)
+        assert (out.double() - want).norm() <= (3 * 2.0 ** -8 if bf else 1e-5) * want.norm()
+        assert (lse.double() - want_lse).abs().max() <= (0.02 if bf else 1e-4)
+    assert grown.tolist() == [[x + steps * chunk for x in r] for r in bud]
+    assert B.ckv_device_status(ws) == B.OK

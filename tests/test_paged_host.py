@@ -1,0 +1,183 @@
+"""The paged-cache entry points on the host: argument errors are reported before anything is launched, the binding
+compares every tensor with the layout its struct was made for.  No GPU needed: no call below passes validation."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2602_08686_b200 import binding as B
+from paper_2602_08686_b200 import build as ckv_build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    ckv_build.build_lib()
+
+
+FAKE = 256 * 1024          # never dereferenced
+BIG = 1 << 40
+
+
+def paged(**kw):
+    base = dict(n_units=2, n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=B.BF16, n_tokens=10, max_new=5, causal=1,
+                page_size=64, n_pages=100, max_pages=9, scale=0.0, q_stride_tok=48 * 128, q_stride_head=128,
+                kv_stride_tok=48 * 128, kv_stride_head=128, page_stride=64 * 128, page_stride_row=128)
+    base.update(kw)
+    pg = B.ckv_paged()
+    for k, v in base.items():
+        setattr(pg, k, v)
+    return pg
+
+
+def rotary(**kw):
+    base = dict(inv_freq=FAKE, q_norm_w=FAKE, k_norm_w=FAKE, rot_dim=128, interleaved=0, rot_scale=1.0, norm_eps=1e-6)
+    base.update(kw)
+    return B.ckv_rotary(*[base[k] for k, _ in B.ckv_rotary._fields_])
+
+
+BAD_TOKENS = [(dict(n_units=0), B.ERR_INVALID_ARG), (dict(n_q_heads=30), B.ERR_INVALID_ARG), (dict(n_tokens=-1), B.ERR_INVALID_ARG),
+              (dict(dtype=2), B.ERR_INVALID_ARG), (dict(head_dim=64), B.ERR_UNSUPPORTED), (dict(max_new=-1), B.ERR_INVALID_ARG),
+              (dict(n_kv_heads=128, n_q_heads=128), B.ERR_UNSUPPORTED), (dict(n_tokens=(1 << 20) + 1), B.ERR_UNSUPPORTED),
+              (dict(n_units=8193), B.ERR_UNSUPPORTED)]
+BAD_PAGES = [(dict(page_size=0), B.ERR_INVALID_ARG), (dict(page_size=48), B.ERR_UNSUPPORTED), (dict(page_size=8), B.ERR_UNSUPPORTED),
+             (dict(page_size=512), B.ERR_UNSUPPORTED), (dict(n_pages=0), B.ERR_INVALID_ARG), (dict(max_pages=0), B.ERR_INVALID_ARG),
+             (dict(max_pages=1 << 20), B.ERR_UNSUPPORTED), (dict(page_stride=64 * 128 - 8), B.ERR_INVALID_ARG),
+             (dict(page_stride_row=120), B.ERR_INVALID_ARG), (dict(page_stride_row=130), B.ERR_INVALID_ARG),
+             (dict(causal=2), B.ERR_INVALID_ARG), (dict(scale=float("nan")), B.ERR_INVALID_ARG),
+             (dict(scale=float("inf")), B.ERR_INVALID_ARG)]
+BAD_Q = [(dict(q_stride_tok=4), B.ERR_INVALID_ARG), (dict(q_stride_head=0), B.ERR_INVALID_ARG), (dict(q_stride_tok=0), B.ERR_INVALID_ARG),
+         (dict(q_stride_tok=-128), B.ERR_INVALID_ARG)]
+
+
+def call(name, pg, rot=None, **over):
+    L = B.lib()
+    far = lambda i: FAKE + i * (1 << 30)
+    a = dict(q=far(1), k=far(2), v=far(3), positions=far(4), starts=far(5), lengths=far(6), table=far(7), q_out=far(8),
+             k_out=far(9), k_pages=far(10), v_pages=far(11), new_lengths=far(12), out=far(13), lse=far(14), ws=far(15), ws_bytes=BIG)
+    a.update(over)
+    p = C.byref(pg)
+    r = None if rot is None else C.byref(rot)
+    if name == "rotate":
+        return L.ckv_rotate(p, r, a["q"], a["k"], a["positions"], a["starts"], a["q_out"], a["k_out"], None)
+    if name == "append":
+        return L.ckv_append(p, r, a["q"], a["k"], a["v"], a["positions"], a["starts"], a["lengths"], a["table"], a["q_out"],
+                            a["k_pages"], a["v_pages"], a["new_lengths"], a["ws"], a["ws_bytes"], None)
+    return L.ckv_paged_attend(p, a["q"], a["k_pages"], a["v_pages"], a["table"], a["lengths"], a["starts"], a["out"], a["lse"],
+                              a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("change,want", BAD_TOKENS + BAD_PAGES)
+def test_bad_shapes(change, want):
+    pg = paged(**change)
+    assert B.ckv_paged_workspace_bytes(pg) == 0
+    assert call("append", pg, rotary()) == want
+    assert call("attend", pg) == want
+    if "page" not in str(change) and "causal" not in change and "scale" not in change:
+        assert call("rotate", pg, rotary()) == want
+
+
+@pytest.mark.parametrize("change,want", BAD_Q)
+def test_bad_strides(change, want):
+    for name in ("rotate", "append", "attend"):
+        assert call(name, paged(**change), rotary()) == want, name
+    kv = {k.replace("q_", "kv_"): v for k, v in change.items()}
+    for name in ("rotate", "append"):
+        assert call(name, paged(**kv), rotary()) == want, name
+
+
+@pytest.mark.parametrize("change,want", [(dict(rot_dim=-16), B.ERR_INVALID_ARG), (dict(rot_dim=144), B.ERR_INVALID_ARG),
+                                         (dict(rot_dim=24), B.ERR_UNSUPPORTED), (dict(interleaved=2), B.ERR_INVALID_ARG),
+                                         (dict(inv_freq=None), B.ERR_INVALID_ARG), (dict(inv_freq=FAKE + 4), B.ERR_INVALID_ARG),
+                                         (dict(norm_eps=-1.0), B.ERR_INVALID_ARG), (dict(norm_eps=float("nan")), B.ERR_INVALID_ARG),
+                                         (dict(rot_scale=float("inf")), B.ERR_INVALID_ARG), (dict(q_norm_w=FAKE + 2), B.ERR_INVALID_ARG)])
+def test_bad_rotary(change, want):
+    assert call("rotate", paged(), rotary(**change)) == want
+    assert call("append", paged(), rotary(**change)) == want
+
+
+def test_bad_pointers_and_work_space():
+    pg, rot = paged(), rotary()
+    assert B.ckv_paged_workspace_bytes(pg) > 256
+    assert call("rotate", pg, None) == B.ERR_INVALID_ARG
+    for name, ptrs in (("rotate", "positions starts q_out k_out"), ("append", "k v positions starts lengths table q_out k_pages v_pages"),
+                       ("attend", "q k_pages v_pages table lengths starts out")):
+        for x in ptrs.split():
+            assert call(name, pg, rot, **{x: None}) == B.ERR_INVALID_ARG, (name, x)
+            assert call(name, pg, rot, **{x: FAKE + (1 << 34) + 2}) == B.ERR_INVALID_ARG, (name, x)
+    assert call("rotate", pg, rot, q=None, k=None) == B.ERR_INVALID_ARG
+    for name in ("append", "attend"):
+        assert call(name, pg, rot, ws=None) == B.ERR_WORKSPACE
+        assert call(name, pg, rot, ws=FAKE + (1 << 34) + 16) == B.ERR_WORKSPACE
+        assert call(name, pg, rot, ws_bytes=B.ckv_paged_workspace_bytes(pg) - 1) == B.ERR_WORKSPACE
+    assert call("append", pg, rot, k_pages=FAKE, v_pages=FAKE) == B.ERR_INVALID_ARG
+    # outputs on top of inputs
+    assert call("append", pg, rot, new_lengths=FAKE + 6 * (1 << 30)) == B.ERR_INVALID_ARG
+    assert call("append", pg, rot, new_lengths=FAKE + 6 * (1 << 30) + 60) == B.ERR_INVALID_ARG
+    assert call("attend", pg, out=FAKE + 1 * (1 << 30)) == B.ERR_INVALID_ARG
+    assert call("rotate", pg, rot, q_out=FAKE + 1 * (1 << 30) + 16) == B.ERR_INVALID_ARG
+    assert call("rotate", pg, rot, q_out=FAKE + 2 * (1 << 30)) == B.ERR_INVALID_ARG      # the keys' input
+    assert call("rotate", pg, rot, q_out=FAKE + 9 * (1 << 30) + 256) == B.ERR_INVALID_ARG  # the keys' output
+
+
+def test_calls_without_tokens_are_empty():
+    pg = paged(n_tokens=0)
+    assert call("rotate", pg, rotary(), q=None, k=None, positions=None) == B.OK
+    assert call("attend", pg, q=None, out=None) == B.OK
+    assert call("append", pg, rotary(), q=None, k=None, v=None, positions=None, new_lengths=None) == B.OK
+
+
+def test_gather_pages_refusals():
+    s = B.ckv_shape(2, 32, 8, 128, 4096, 32, B.BF16, 0, 32 * 32 * 128, 32 * 128, 128, 8 * 4096 * 128, 4096 * 128, 128)
+    p = B.make_params(B.Params(), None, None)
+    far = [FAKE + i * (1 << 30) for i in range(20)]
+
+    def go(pg, k=far[1], k_pages=far[6], lengths=far[8], ws_bytes=BIG, shape=s):
+        return B.lib().ckv_gather_pages(C.byref(shape), C.byref(p), C.byref(pg), k, far[2], far[3], far[4], far[5], far[9], k_pages,
+                                        far[7], lengths, far[10], ws_bytes, None)
+
+    for change in (dict(n_units=3), dict(n_kv_heads=4), dict(dtype=B.F32)):
+        assert go(paged(**change)) == B.ERR_INVALID_ARG, change
+    assert go(paged(page_size=48)) == B.ERR_UNSUPPORTED
+    assert go(paged(), k=None) == B.ERR_INVALID_ARG
+    assert go(paged(), k_pages=far[6] + 8) == B.ERR_INVALID_ARG
+    assert go(paged(), lengths=far[4]) == B.ERR_INVALID_ARG
+    assert go(paged(), ws_bytes=16) == B.ERR_WORKSPACE
+    bad = B.ckv_shape(2, 32, 8, 64, 4096, 32, B.BF16, 0, 32 * 32 * 128, 32 * 128, 128, 8 * 4096 * 128, 4096 * 128, 128)
+    assert go(paged(), shape=bad) == B.ERR_INVALID_ARG
+
+
+def test_the_binding_compares_layouts():
+    kp = torch.zeros(6, 16, 128, dtype=torch.bfloat16)
+    table = torch.zeros(1, 2, 3, dtype=torch.int32)
+    qkv = torch.zeros(4, 12, 128, dtype=torch.bfloat16)
+    q, k = qkv[:, :8], qkv[:, 8:10]
+    pg = B.make_paged(kp, table, q=q, k_new=k, max_new=4)
+    assert (pg.n_units, pg.n_q_heads, pg.n_kv_heads, pg.n_tokens, pg.max_pages, pg.page_size) == (1, 8, 2, 4, 3, 16)
+    assert pg.q_stride_tok == 12 * 128 and pg.page_stride == 16 * 128
+    starts, lengths = torch.zeros(2, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32)
+    out, ws = torch.zeros(4, 8, 128, dtype=torch.bfloat16), torch.zeros(1 << 20, dtype=torch.uint8)
+
+    def attend(**kw):
+        a = dict(q=q, k_pages=kp, v_pages=kp.clone(), page_table=table, lengths=lengths, token_starts=starts, out=out, ws=ws)
+        a.update(kw)
+        B.ckv_paged_attend(pg, **a)
+
+    for kw in (dict(q=q.contiguous()), dict(q=q.float()), dict(q=q[:3]), dict(v_pages=kp.transpose(0, 1)), dict(v_pages=kp.float()),
+               dict(page_table=table.long()), dict(page_table=table[:, :1]), dict(lengths=lengths[0]),
+               dict(token_starts=starts.long()), dict(token_starts=torch.zeros(3, dtype=torch.int32)), dict(out=out[:3]),
+               dict(out=out.float()), dict(out=torch.zeros(4, 128, 8, dtype=torch.bfloat16).transpose(1, 2)),
+               dict(lse=torch.zeros(4, 8, 1)), dict(ws=ws[::2]), dict(ws=ws.to(torch.int8))):
+        with pytest.raises(ValueError):
+            attend(**kw)
+    with pytest.raises(ValueError):
+        B.make_paged(kp, table.long(), q=q)
+    with pytest.raises(ValueError):
+        B.make_paged(kp.transpose(1, 2), table, q=q)
+    with pytest.raises(ValueError):
+        B.make_paged(kp, table, q=q.float())
+    with pytest.raises(ValueError):
+        B.make_rotary(torch.zeros(64))
+    with pytest.raises(ValueError):
+        B.make_rotary(torch.zeros(64, dtype=torch.float64), q_norm_w=torch.zeros(64))
+    with pytest.raises(TypeError):
+        B.make_packed(q.half(), k.half(), 1)
