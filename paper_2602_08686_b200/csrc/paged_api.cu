@@ -68,10 +68,10 @@ ckv_status check_rotary(const ckv_rotary* r) {
     return CKV_ERR_INVALID_ARG;
   return CKV_OK;
 }
-ckv_status check_paged_ws(const ckv_paged& pg, const void* ws, size_t ws_bytes) {
-  if (!ws || !aligned(ws, 256) || ws_bytes < paged_ws(pg).total) return CKV_ERR_WORKSPACE;
-  return CKV_OK;
+ckv_status check_paged_ws(size_t need, const void* ws, size_t ws_bytes) {
+  return ws && aligned(ws, 256) && ws_bytes >= need ? CKV_OK : CKV_ERR_WORKSPACE;
 }
+constexpr size_t kStatusBytes = 256;   // all that the calls without partial results use
 // An output is either its own input (in place) or dense and apart from everything that is read.
 bool out_ok(const ckv_paged& pg, const void* out, const void* in, int heads, std::initializer_list<Range> read) {
   if (!good({out}, 16)) return false;
@@ -140,7 +140,7 @@ ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const vo
     const uintptr_t a = reinterpret_cast<uintptr_t>(lengths), b = reinterpret_cast<uintptr_t>(new_lengths_or_null);
     if (b % 4 || (a < b + n && b < a + n)) return CKV_ERR_INVALID_ARG;
   }
-  CKV_TRY(check_paged_ws(*paged, ws, ws_bytes));
+  CKV_TRY(check_paged_ws(kStatusBytes, ws, ws_bytes));
   if (paged->n_tokens == 0 && !new_lengths_or_null) return CKV_OK;
   const bool any = paged->n_tokens > 0;
   if (any) {
@@ -175,7 +175,7 @@ ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, co
     return CKV_ERR_INVALID_ARG;
   if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
   if (!good({indices, budgets, offsets, page_table, lengths}, 4) || lengths == budgets) return CKV_ERR_INVALID_ARG;
-  CKV_TRY(check_paged_ws(*paged, ws, ws_bytes));
+  CKV_TRY(check_paged_ws(kStatusBytes, ws, ws_bytes));
   CKV_CUDA(launch_gather_pages(*shape, *params, *paged, k, v, indices, budgets, offsets, page_table, k_pages, v_pages, lengths,
                                reinterpret_cast<int*>(static_cast<char*>(ws) + paged_ws(*paged).status),
                                (cudaStream_t)stream));
@@ -187,7 +187,7 @@ ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k
                             float* lse_or_null, void* ws, size_t ws_bytes, void* stream) {
   CKV_TRY(check_tokens(paged));
   CKV_TRY(check_pages(paged));
-  CKV_TRY(check_paged_ws(*paged, ws, ws_bytes));
+  CKV_TRY(check_paged_ws(paged_ws(*paged).total, ws, ws_bytes));
   if (paged->n_tokens == 0) return CKV_OK;
   if (!good({q, k_pages, v_pages, out}, 16) || !good({page_table, lengths, token_starts}, 4)) return CKV_ERR_INVALID_ARG;
   if (lse_or_null && !aligned(lse_or_null, 4)) return CKV_ERR_INVALID_ARG;

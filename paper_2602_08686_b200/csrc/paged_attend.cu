@@ -248,15 +248,27 @@ cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, c
   return e;
 }
 
+template cudaError_t launch_join<true>(const WorkArgs&, int, void*, float*, cudaStream_t);
+template cudaError_t launch_join<false>(const WorkArgs&, int, void*, float*, cudaStream_t);
+
+// Units with up to this many query rows per KV head go to the kernel for few rows, the others to the tensor cores.
+constexpr int kFewRows = 32;
+static bool wants_tc(const ckv_paged& pg) {
+  const int64_t G = pg.n_q_heads / pg.n_kv_heads, most = pg.max_new > 0 ? pg.max_new : pg.n_tokens;
+  return pg.dtype == CKV_BF16 && G <= 128 && most * G > kFewRows;
+}
+
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 PagedWs paged_ws(const ckv_paged& pg) {
   PagedWs w{};
-  (void)pg;
   size_t o = 0;
   w.status = o, o += 256;
-  w.split = o, o = up256(o + kWorkers * sizeof(int4));
-  w.ml = o, o = up256(o + (size_t)kWorkers * 2 * kRowsM * sizeof(float2));
-  w.o = o, o = up256(o + (size_t)kWorkers * 2 * kRowsM * kHeadDim * sizeof(float));
+  const size_t workers[2] = {(size_t)kWorkers, (size_t)(wants_tc(pg) ? kTcWorkers : 0)}, rows[2] = {kRowsM, kTcRows};
+  for (int i = 0; i < 2; ++i) {
+    w.split[i] = o, o = up256(o + workers[i] * sizeof(int4));
+    w.ml[i] = o, o = up256(o + workers[i] * 2 * rows[i] * sizeof(float2));
+    w.o[i] = o, o = up256(o + workers[i] * 2 * rows[i] * kHeadDim * sizeof(float));
+  }
   w.total = o;
   return w;
 }
@@ -265,20 +277,29 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
                                 const int32_t* table, const int32_t* lengths, const int32_t* starts, void* out, float* lse,
                                 char* ws, cudaStream_t st) {
   const PagedWs w = paged_ws(pg);
+  const bool bf16 = pg.dtype == CKV_BF16, tc = wants_tc(pg);
+  const float scale = pg.scale != 0.f ? pg.scale : 0.08838834764831845f;
   WorkArgs a{};
   a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = pg.causal;
-  a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4, a.min_rows = 0, a.max_rows = 0x7fffffff;
   a.P = pg.page_size, a.log_p = log2_of(pg.page_size), a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
   a.starts = starts, a.lengths = lengths, a.table = table, a.status = reinterpret_cast<int*>(ws + w.status);
-  a.split = reinterpret_cast<int4*>(ws + w.split), a.ml = reinterpret_cast<float2*>(ws + w.ml);
-  a.o = reinterpret_cast<float*>(ws + w.o), a.slot_rows = kRowsM;
-  const float x_scale = (pg.scale != 0.f ? pg.scale : 0.08838834764831845f) * kLog2e;
+  auto slots = [&](int i, int rows) {
+    a.split = reinterpret_cast<int4*>(ws + w.split[i]), a.ml = reinterpret_cast<float2*>(ws + w.ml[i]);
+    a.o = reinterpret_cast<float*>(ws + w.o[i]), a.slot_rows = rows;
+  };
+  if (tc) {
+    slots(1, kTcRows);
+    a.min_rows = kFewRows, a.max_rows = 0x7fffffff;
+    const cudaError_t e = launch_attend_tc(pg, a, scale, q, k_pages, v_pages, out, lse, st);
+    if (e != cudaSuccess) return e;
+  }
+  slots(0, kRowsM);
+  a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4, a.min_rows = 0, a.max_rows = tc ? kFewRows : 0x7fffffff;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
-  const bool bf16 = pg.dtype == CKV_BF16;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, bf16 ? attend_rows_kernel<true> : attend_rows_kernel<false>, a, pg, x_scale,
+  cudaError_t e = cudaLaunchKernelEx(&cfg, bf16 ? attend_rows_kernel<true> : attend_rows_kernel<false>, a, pg, scale * kLog2e,
                                      (const char*)q, (const char*)k_pages, (const char*)v_pages, out, lse);
   count_launch();
   if (e == cudaSuccess) e = bf16 ? launch_join<true>(a, kWorkers, out, lse, st) : launch_join<false>(a, kWorkers, out, lse, st);

@@ -182,6 +182,12 @@ __device__ __forceinline__ int page_of(const WorkArgs& a, const Item& it, int sl
   return -1;
 }
 
+constexpr int kTcWorkers = 148;      // CTAs of the tensor-core kernel, one per SM
+constexpr int kTcRows = 256;         // query rows of its blocks
+
+// `base`: everything but the block and tile sizes; scale not 0.
+cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float scale, const void* q, const void* k_pages,
+                             const void* v_pages, void* out, float* lse, cudaStream_t st);
 template <bool BF16>
 cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, cudaStream_t st);
 
