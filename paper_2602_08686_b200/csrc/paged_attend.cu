@@ -21,32 +21,15 @@ constexpr int kRowsWarps = kRowsThreads / 32;
 constexpr int kRowsTile = kRowsWarps * 8;   // keys a CTA takes per step
 constexpr int kWorkers = 148;        // one CTA per SM
 
-template <bool BF16>
+// the 16 dimensions of lane l8 of 8: 16-byte pieces l8, l8 + 8, ... of the row (coalesced over the eight lanes)
 __device__ __forceinline__ void load16(const char* row, int l8, float (&x)[16]) {
-  // the 16 dimensions of lane l8 of 8: 16-byte pieces l8, l8 + 8, ... of the row (coalesced over the eight lanes)
-  if (BF16) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const uint4 r = *reinterpret_cast<const uint4*>(row + (c * 8 + l8) * 16);
-      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[c * 8 + 2 * i] = __uint_as_float(w[i] << 16);
-        x[c * 8 + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const float4 r = *reinterpret_cast<const float4*>(row + (c * 8 + l8) * 16);
-      x[c * 4] = r.x, x[c * 4 + 1] = r.y, x[c * 4 + 2] = r.z, x[c * 4 + 3] = r.w;
-    }
+  for (int c = 0; c < 4; ++c) {
+    const float4 r = *reinterpret_cast<const float4*>(row + (c * 8 + l8) * 16);
+    x[c * 4] = r.x, x[c * 4 + 1] = r.y, x[c * 4 + 2] = r.z, x[c * 4 + 3] = r.w;
   }
 }
-template <bool BF16>
-__device__ __forceinline__ int dim16(int l8, int i) {   // which dimension load16 put into x[i]
-  return BF16 ? ((i >> 3) * 8 + l8) * 8 + (i & 7) : ((i >> 2) * 8 + l8) * 4 + (i & 3);
-}
+__device__ __forceinline__ int dim16(int l8, int i) { return ((i >> 2) * 8 + l8) * 4 + (i & 3); }   // dimension in x[i]
 
 struct RowsSmem {
   Plan plan;
@@ -54,13 +37,12 @@ struct RowsSmem {
   float o[kRowsWarps][kRowsM][kHeadDim];
 };
 
-template <bool BF16>
 __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a, ckv_paged pg, float x_scale,
                                                                       const char* __restrict__ q,
                                                                       const char* __restrict__ kp,
-                                                                      const char* __restrict__ vp, void* __restrict__ out,
+                                                                      const char* __restrict__ vp, float* __restrict__ out,
                                                                       float* __restrict__ lse) {
-  constexpr int E = BF16 ? 2 : 4;
+  constexpr int E = 4;
   __shared__ RowsSmem sm;
   pdl_wait();
   make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
@@ -82,7 +64,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       for (int i = 0; i < 16; ++i) acc[r][i] = 0.f, qr[r][i] = 0.f;
       if (r < rows) {
         const int row = it.block * a.M + r, token = row / a.G, h = it.g * a.G + (row - token * a.G);
-        load16<BF16>(q + ((it.first + token) * pg.q_stride_tok + h * pg.q_stride_head) * E, l8, qr[r]);
+        load16(q + ((it.first + token) * pg.q_stride_tok + h * pg.q_stride_head) * E, l8, qr[r]);
         limit[r] = row_limit(a, it, r);
       }
     }
@@ -99,8 +81,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         for (int i = 0; i < 16; ++i) kv[s][i] = 0.f, vv[s][i] = 0.f;
         if (page >= 0) {
           const int64_t at = (page * pg.page_stride + (key[s] & (a.P - 1)) * pg.page_stride_row) * E;
-          load16<BF16>(kp + at, l8, kv[s]);
-          load16<BF16>(vp + at, l8, vv[s]);
+          load16(kp + at, l8, kv[s]);
+          load16(vp + at, l8, vv[s]);
         } else {
           key[s] = 0x7fffffff;   // hidden from every row
         }
@@ -150,7 +132,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         float o = acc[r][i] * c;
         o += __shfl_xor_sync(0xffffffffu, o, 8);
         o += __shfl_xor_sync(0xffffffffu, o, 16);
-        if (grp == 0) sm.o[warp][r][dim16<BF16>(l8, i)] = o;
+        if (grp == 0) sm.o[warp][r][dim16(l8, i)] = o;
       }
     }
     __syncthreads();
@@ -170,8 +152,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       if (whole) {
         const int64_t at = out_row(a, it, r);
         o = top == -INFINITY ? 0.f : o / sum;
-        if (BF16) static_cast<__nv_bfloat16*>(out)[at * kHeadDim + d] = __float2bfloat16(o);
-        else static_cast<float*>(out)[at * kHeadDim + d] = o;
+        out[at * kHeadDim + d] = o;
         if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
       } else {
         a.o[(slot + r) * kHeadDim + d] = o;
@@ -263,7 +244,8 @@ PagedWs paged_ws(const ckv_paged& pg) {
   PagedWs w{};
   size_t o = 0;
   w.status = o, o += 256;
-  const size_t workers[2] = {(size_t)kWorkers, (size_t)(wants_tc(pg) ? kTcWorkers : 0)}, rows[2] = {kRowsM, kTcRows};
+  const size_t few = pg.dtype == CKV_BF16 ? kMmaRows : kRowsM;
+  const size_t workers[2] = {kWorkers, wants_tc(pg) ? (size_t)kTcWorkers : 0}, rows[2] = {few, kTcRows};
   for (int i = 0; i < 2; ++i) {
     w.split[i] = o, o = up256(o + workers[i] * sizeof(int4));
     w.ml[i] = o, o = up256(o + workers[i] * 2 * rows[i] * sizeof(float2));
@@ -293,16 +275,22 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
     const cudaError_t e = launch_attend_tc(pg, a, scale, q, k_pages, v_pages, out, lse, st);
     if (e != cudaSuccess) return e;
   }
+  a.min_rows = 0, a.max_rows = tc ? kFewRows : 0x7fffffff;
+  if (bf16) {
+    slots(0, kMmaRows);
+    const int64_t most = (int64_t)(pg.max_new > 0 ? pg.max_new : pg.n_tokens) * a.G;
+    return launch_attend_mma(pg, a, (int)(most < kMmaRows ? most : kMmaRows), scale, q, k_pages, v_pages, out, lse, st);
+  }
   slots(0, kRowsM);
-  a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4, a.min_rows = 0, a.max_rows = tc ? kFewRows : 0x7fffffff;
+  a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, bf16 ? attend_rows_kernel<true> : attend_rows_kernel<false>, a, pg, scale * kLog2e,
-                                     (const char*)q, (const char*)k_pages, (const char*)v_pages, out, lse);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, attend_rows_kernel, a, pg, scale * kLog2e, (const char*)q, (const char*)k_pages,
+                                     (const char*)v_pages, (float*)out, lse);
   count_launch();
-  if (e == cudaSuccess) e = bf16 ? launch_join<true>(a, kWorkers, out, lse, st) : launch_join<false>(a, kWorkers, out, lse, st);
+  if (e == cudaSuccess) e = launch_join<false>(a, kWorkers, out, lse, st);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -188,6 +188,12 @@ constexpr int kTcRows = 256;         // query rows of its blocks
 // `base`: everything but the block and tile sizes; scale not 0.
 cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float scale, const void* q, const void* k_pages,
                              const void* v_pages, void* out, float* lse, cudaStream_t st);
+constexpr int kMmaWorkers = 148;     // CTAs of the bf16 kernel for few rows
+constexpr int kMmaRows = 32;         // most query rows of its blocks
+constexpr int kMmaTile = 64;         // keys per tile of its schedule
+// rows: the most query rows per KV head that any unit it is to take has.
+cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
+                              const void* v_pages, void* out, float* lse, cudaStream_t st);
 template <bool BF16>
 cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, cudaStream_t st);
 
