@@ -11,10 +11,9 @@ constexpr int kStatusPage = 4096;           // status code: a page or row index 
 // Work space of the paged calls (byte offsets from the 256-byte aligned base).
 struct PagedWs {
   size_t status;   // 64 x int32 as in WsLayout
-  // partial results of split items, of the kernel for few query rows and of the tensor-core kernel:
-  size_t split[2]; // int32 [workers][4]                    what each worker left in its two partial slots
-  size_t ml[2];    // float2 [workers][2][rows]             running maximum (base 2) and sum
-  size_t o[2];     // float [workers][2][rows][128]         unnormalised output
+  size_t split;    // int32 [workers][4]                    what each worker left in its two slots for partial results
+  size_t ml;       // float2 [workers][2][rows]             running maximum (base 2) and sum of a partial result
+  size_t o;        // float [workers][2][rows][128]         its unnormalised output
   size_t total;
 };
 PagedWs paged_ws(const ckv_paged& pg);

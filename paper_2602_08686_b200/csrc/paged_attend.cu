@@ -19,7 +19,6 @@ constexpr int kRowsM = 4;            // query rows of a block
 constexpr int kRowsThreads = 256;
 constexpr int kRowsWarps = kRowsThreads / 32;
 constexpr int kRowsTile = kRowsWarps * 8;   // keys a CTA takes per step
-constexpr int kWorkers = 148;        // one CTA per SM
 
 // the 16 dimensions of lane l8 of 8: 16-byte pieces l8, l8 + 8, ... of the row (coalesced over the eight lanes)
 __device__ __forceinline__ void load16(const char* row, int l8, float (&x)[16]) {
@@ -47,13 +46,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
   pdl_wait();
   make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
   pdl_launch_dependents();
-  long long left = sm.plan.left;
   if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
-  if (left == 0) return;
-  int pair = sm.plan.pair, block = sm.plan.block, t0 = sm.plan.t0;
+  Walk walk;
+  walk.start(a, sm.plan);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
-  for (;;) {
-    const Item it = make_item(a, pair, block, t0, left);
+  for (; walk.live; walk.next(a)) {
+    const Item& it = walk.it;
     const int rows = block_rows(a, it);
     float qr[kRowsM][16], acc[kRowsM][16], m[kRowsM], l[kRowsM];
     int limit[kRowsM];
@@ -161,11 +159,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
     }
     if (!whole && threadIdx.x == 0) {
       int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
-      sp[2 * which] = pair, sp[2 * which + 1] = block;
+      sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
     }
-    left -= it.t1 - it.t0;
-    if (left <= 0 || !next_item(a, pair, block, it.n)) return;
-    t0 = 0;
     __syncthreads();
   }
 }
@@ -232,7 +227,7 @@ cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, c
 template cudaError_t launch_join<true>(const WorkArgs&, int, void*, float*, cudaStream_t);
 template cudaError_t launch_join<false>(const WorkArgs&, int, void*, float*, cudaStream_t);
 
-// Units with up to this many query rows per KV head go to the kernel for few rows, the others to the tensor cores.
+// Up to this many query rows per KV head in every unit, the call goes to the kernel for few rows, else to the tensor cores.
 constexpr int kFewRows = 32;
 static bool wants_tc(const ckv_paged& pg) {
   const int64_t G = pg.n_q_heads / pg.n_kv_heads, most = pg.max_new > 0 ? pg.max_new : pg.n_tokens;
@@ -244,13 +239,10 @@ PagedWs paged_ws(const ckv_paged& pg) {
   PagedWs w{};
   size_t o = 0;
   w.status = o, o += 256;
-  const size_t few = pg.dtype == CKV_BF16 ? kMmaRows : kRowsM;
-  const size_t workers[2] = {kWorkers, wants_tc(pg) ? (size_t)kTcWorkers : 0}, rows[2] = {few, kTcRows};
-  for (int i = 0; i < 2; ++i) {
-    w.split[i] = o, o = up256(o + workers[i] * sizeof(int4));
-    w.ml[i] = o, o = up256(o + workers[i] * 2 * rows[i] * sizeof(float2));
-    w.o[i] = o, o = up256(o + workers[i] * 2 * rows[i] * kHeadDim * sizeof(float));
-  }
+  const size_t rows = wants_tc(pg) ? kTcRows : (pg.dtype == CKV_BF16 ? kMmaRows : kRowsM);
+  w.split = o, o = up256(o + kWorkers * sizeof(int4));
+  w.ml = o, o = up256(o + kWorkers * 2 * rows * sizeof(float2));
+  w.o = o, o = up256(o + kWorkers * 2 * rows * kHeadDim * sizeof(float));
   w.total = o;
   return w;
 }
@@ -265,23 +257,17 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = pg.causal;
   a.P = pg.page_size, a.log_p = log2_of(pg.page_size), a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
   a.starts = starts, a.lengths = lengths, a.table = table, a.status = reinterpret_cast<int*>(ws + w.status);
-  auto slots = [&](int i, int rows) {
-    a.split = reinterpret_cast<int4*>(ws + w.split[i]), a.ml = reinterpret_cast<float2*>(ws + w.ml[i]);
-    a.o = reinterpret_cast<float*>(ws + w.o[i]), a.slot_rows = rows;
-  };
+  a.split = reinterpret_cast<int4*>(ws + w.split), a.ml = reinterpret_cast<float2*>(ws + w.ml), a.o = reinterpret_cast<float*>(ws + w.o);
   if (tc) {
-    slots(1, kTcRows);
-    a.min_rows = kFewRows, a.max_rows = 0x7fffffff;
-    const cudaError_t e = launch_attend_tc(pg, a, scale, q, k_pages, v_pages, out, lse, st);
-    if (e != cudaSuccess) return e;
+    a.slot_rows = kTcRows;
+    return launch_attend_tc(pg, a, scale, q, k_pages, v_pages, out, lse, st);
   }
-  a.min_rows = 0, a.max_rows = tc ? kFewRows : 0x7fffffff;
   if (bf16) {
-    slots(0, kMmaRows);
+    a.slot_rows = kMmaRows;
     const int64_t most = (int64_t)(pg.max_new > 0 ? pg.max_new : pg.n_tokens) * a.G;
     return launch_attend_mma(pg, a, (int)(most < kMmaRows ? most : kMmaRows), scale, q, k_pages, v_pages, out, lse, st);
   }
-  slots(0, kRowsM);
+  a.slot_rows = kRowsM;
   a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;

@@ -62,14 +62,13 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
   pdl_wait();
   make_plan<kThreads>(a, blockIdx.x, gridDim.x, sm.plan);
   pdl_launch_dependents();
-  long long left = sm.plan.left;
   if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
-  if (left == 0) return;
-  int pair = sm.plan.pair, block = sm.plan.block, t0 = sm.plan.t0;
+  Walk walk;
+  walk.start(a, sm.plan);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, p = lane >> 2, c = lane & 3;
   const int64_t row_bytes = pg.page_stride_row * 2, page_bytes = pg.page_stride * 2;
-  for (;;) {
-    const Item it = make_item(a, pair, block, t0, left);
+  for (; walk.live; walk.next(a)) {
+    const Item& it = walk.it;
     const int rows = block_rows(a, it);
     const int end = min(it.t1 * a.tile, it.visible), begin = it.t0 * a.tile + warp * kGroup;
     // The page of the group at key j: its first row's address offset, or -1 for none.
@@ -284,11 +283,8 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
     }
     if (!whole && threadIdx.x == 0) {
       int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
-      sp[2 * which] = pair, sp[2 * which + 1] = block;
+      sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
     }
-    left -= it.t1 - it.t0;
-    if (left <= 0 || !next_item(a, pair, block, it.n)) return;
-    t0 = 0;
     __syncthreads();
   }
 }
@@ -300,7 +296,7 @@ cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, float x_scale, const 
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<MT, NW>));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(kMmaWorkers), cfg.blockDim = dim3(NW * 32), cfg.dynamicSmemBytes = sizeof(Smem<MT, NW>), cfg.stream = st;
+  cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(NW * 32), cfg.dynamicSmemBytes = sizeof(Smem<MT, NW>), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, kernel, a, pg, x_scale, (const char*)q, (const char*)kp, (const char*)vp, (__nv_bfloat16*)out, lse);
@@ -318,7 +314,7 @@ cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int row
   const float x_scale = scale * kLog2e;
   const cudaError_t e = rows <= 16 ? launch<1, kMmaWarps>(pg, a, x_scale, q, k_pages, v_pages, out, lse, st)
                                    : launch<2, 8>(pg, a, x_scale, q, k_pages, v_pages, out, lse, st);
-  return e != cudaSuccess ? e : launch_join<true>(a, kMmaWorkers, out, lse, st);
+  return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, out, lse, st);
 }
 
 }  // namespace ckv

@@ -59,6 +59,8 @@ struct __align__(1024) Smem {
   uint64_t full[kStages], empty[kStages];
   uint64_t q_full, q_empty;
   uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t join_full, join_done;                // stream 1's result is there; stream 0 has read it
+  float2 other[kTile];                          // stream 1's maximum and sum per row
   uint32_t bad[kInfo];                          // which pages of a key tile are missing (bit per page)
   uint32_t odd[kInfo][4];                       // which rows of a value tile were not finite and have been zeroed
   Plan plan;
@@ -78,25 +80,9 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
   return __all_sync(0xffffffffu, bar_wait(bar, parity, w, code));
 }
 
-// Walks the worker's items; every role keeps its own copy.
-struct Walk {
-  int pair, block, t0;
-  long long left;
-  Item it;
-  __device__ void start(const Plan& p) { pair = p.pair, block = p.block, t0 = p.t0, left = p.left; }
-  __device__ void load(const WorkArgs& a) { it = make_item(a, pair, block, t0, left); }
-  __device__ bool next(const WorkArgs& a) {
-    left -= it.t1 - it.t0;
-    if (left <= 0 || !next_item(a, pair, block, it.n)) return false;
-    t0 = 0;
-    load(a);
-    return true;
-  }
-};
-// query tiles of the item that have tokens (1 or 2)
-__device__ __forceinline__ int streams_of(const TcArgs& a, const Item& it) {
-  return it.n - it.block * a.w.tokens > a.TQ ? 2 : 1;
-}
+// How an item is cut up.  Two query tiles: each stream has one, and takes every key tile.  One query tile (the tokens
+// fill no more than half of the block): both streams work on it, on every other key tile, and join at the end.
+__device__ __forceinline__ bool paired(const Item& it) { return it.weight == 2; }
 
 // First row of the item's j-th key tile that the block's first token does not see (128: it sees them all).  Where every
 // token sees every row there is none.
@@ -109,15 +95,14 @@ __device__ __forceinline__ int late_row(const TcArgs& a, const Item& it, int j) 
 __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUtensorMap* qm, const CUtensorMap* km,
                                           const CUtensorMap* vm, const Waiter& w, int lane) {
   Walk k;
-  k.start(sm.plan);
-  k.load(a.w);
+  k.start(a.w, sm.plan);
   uint32_t n_loads = 0, n_items = 0, n_tiles = 0;
   const int slot_of_lane = lane >> 1, half = lane & 1;
   const bool copies = slot_of_lane < a.pages_per_tile;
   const int tiles_per_page = a.w.P > kTile ? a.w.P / kTile : 1;
-  do {
+  for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
-    const int ns = streams_of(a, it);
+    const int ns = it.weight;
     if (!wait_warp(smem_u32(&sm.q_empty), (n_items & 1) ^ 1, w, 1)) return;
     if (lane == 0) bar_arrive_tx(smem_u32(&sm.q_full), ns * a.q_bytes);
     __syncwarp();
@@ -155,29 +140,66 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
       }
     }
     ++n_items;
-  } while (k.next(a.w));
+  }
+}
+
+// 0 * NaN is not 0: value rows that no query sees are zeroed, and so are rows with an infinity or a NaN that some of the
+// block's tokens do not see yet (the softmax threads add those to the tokens that do).
+__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Item& it, int j, uint32_t nv, uint32_t n_tiles, int lane) {
+  const int valid = it.visible - (it.t0 + j) * kTile, late = late_row(a, it, j);
+  const uint32_t bad = *(volatile uint32_t*)&sm.bad[n_tiles % kInfo];
+  if (valid < kTile || bad || late < kTile) {
+    uint4* v = reinterpret_cast<uint4*>(sm.kv[nv % kStages]);
+    if (lane < 4) sm.odd[n_tiles % kInfo][lane] = 0u;
+    __syncwarp();
+    const int piece = (lane & 8) * (kTile) + (lane & 7);      // 16-byte piece lane & 15 of a row: its half, its place
+#pragma unroll 4
+    for (int r0 = late; r0 < min(valid, kTile); r0 += 2) {
+      const int row = min(r0 + (lane >> 4), kTile - 1);
+      const uint4 x = v[piece + row * 8];
+      const uint32_t e = 0x7f807f80u;
+      const uint32_t hit = __vcmpeq2(x.x & e, e) | __vcmpeq2(x.y & e, e) | __vcmpeq2(x.z & e, e) | __vcmpeq2(x.w & e, e);
+      const uint32_t any = __ballot_sync(0xffffffffu, hit != 0u && row < valid);
+      if (any) {
+        if ((any >> (lane & 16)) & 0xffffu) v[piece + row * 8] = make_uint4(0u, 0u, 0u, 0u);
+        if ((lane & 15) == 0 && ((any >> lane) & 0xffffu)) atomicOr(&sm.odd[n_tiles % kInfo][row >> 5], 1u << (row & 31));
+      }
+    }
+    if (valid < kTile || bad)
+      for (int e = lane; e < 2 * kTile * 8; e += 32) {
+        const int row = (e >> 3) & (kTile - 1);
+        if (row >= valid || (bad >> (row >> a.w.log_p) & 1)) v[e] = make_uint4(0u, 0u, 0u, 0u);
+      }
+    fence_async_smem();
+    __syncwarp();
+  }
 }
 
 __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int lane) {
   Walk k;
-  k.start(sm.plan);
-  k.load(a.w);
+  k.start(a.w, sm.plan);
   uint32_t n_use = 0, n_items = 0, n_tiles = 0, n_p[2] = {0, 0};
   const uint32_t q_lo[2] = {desc_lo(smem_u32(sm.q[0]), 16), desc_lo(smem_u32(sm.q[1]), 16)};
   const uint32_t kv0 = smem_u32(sm.kv[0]);
   auto full = [&](uint32_t n) { return wait_warp(smem_u32(&sm.full[n % kStages]), (n / kStages) & 1, w, 3); };
-  auto qk = [&](int s, uint32_t n) {
+  auto release = [&](uint32_t n) {
+    if (lane == 0) tc_commit(smem_u32(&sm.empty[n % kStages]));
+  };
+  auto qk = [&](int s, int q_tile, uint32_t n) {   // S_s = Q K^T
     if (lane == 0) {
       const uint32_t b = desc_lo(kv0 + (n % kStages) * kTileBytes, 16);
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) {   // 16 dimensions = 32 bytes of a 128-byte swizzled row; the second half is 16 KB on
         const uint32_t off = (kk & 3) * 2 + (kk >> 2) * (kHalf >> 4);
-        mma_ss(tmem + kColS + s * 128, desc_of(q_lo[s] + off), desc_of(b + off), a.idesc_qk, kk > 0);
+        mma_ss(tmem + kColS + s * 128, desc_of(q_lo[q_tile] + off), desc_of(b + off), a.idesc_qk, kk > 0);
       }
       tc_commit(smem_u32(&sm.s_full[s]));
     }
   };
-  auto pv = [&](int s, uint32_t n, bool accumulate) {
+  auto pv = [&](int s, uint32_t n, bool accumulate) {   // O_s += P_s V, once P_s is there
+    if (!wait_warp(smem_u32(&sm.p_full[s]), n_p[s] & 1, w, 5)) return false;
+    ++n_p[s];
+    tc_fence_after();
     if (lane == 0) {
       const uint32_t b = desc_lo(kv0 + (n % kStages) * kTileBytes, kHalf);   // 64-dimension halves 16 KB apart
 #pragma unroll
@@ -186,71 +208,51 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
                accumulate || kk > 0);
       tc_commit(smem_u32(&sm.pv_done[s]));
     }
+    return true;
   };
-  do {
+  // The products of one stream are issued in the order S(j), O(j), S(j + 1): the tensor pipe runs them in that order, so S(j + 1)
+  // may take the columns that O(j) reads P from without waiting for it.
+  for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
-    const int ns = streams_of(a, it), n = it.t1 - it.t0;
-    if (!wait_warp(smem_u32(&sm.q_full), n_items & 1, w, 4) || !full(n_use)) return;
-    tc_fence_after();
-    for (int s = 0; s < ns; ++s) qk(s, n_use);
-    if (lane == 0) {
-      tc_commit(smem_u32(&sm.empty[n_use % kStages]));
-      if (n == 1) tc_commit(smem_u32(&sm.q_empty));
+    const int n = it.t1 - it.t0;
+    const bool pair = paired(it);
+    const int ahead = pair ? 1 : 2;      // a stream's next key tile
+    if (!wait_warp(smem_u32(&sm.q_full), n_items & 1, w, 4)) return;
+    for (int j = 0; j < min(ahead, n); ++j) {
+      if (!full(n_use + 2 * j)) return;
+      tc_fence_after();
+      qk(j, 0, n_use + 2 * j);
+      if (pair) qk(1, 1, n_use + 2 * j);
+      release(n_use + 2 * j);
+      if (j == n - 1 && lane == 0) tc_commit(smem_u32(&sm.q_empty));
     }
     for (int j = 0; j < n; ++j, ++n_tiles) {
-      const uint32_t nv = n_use + 2 * j + 1, nk = nv + 1;
+      const uint32_t nv = n_use + 2 * j + 1, nk = n_use + 2 * (j + ahead);
+      const bool more = j + ahead < n;
       if (!full(nv)) return;
-      // 0 * NaN is not 0: value rows that no query sees are zeroed, and so are rows with an infinity or a NaN that some
-      // of the block's tokens do not see yet (the softmax threads add those to the tokens that do)
-      const int valid = it.visible - (it.t0 + j) * kTile, late = late_row(a, it, j);
-      const uint32_t bad = *(volatile uint32_t*)&sm.bad[n_tiles % kInfo];
-      if (valid < kTile || bad || late < kTile) {
-        uint4* v = reinterpret_cast<uint4*>(sm.kv[nv % kStages]);
-        if (lane < 4) sm.odd[n_tiles % kInfo][lane] = 0u;
-        __syncwarp();
-        const int piece = (lane & 8) * (kTile) + (lane & 7);      // 16-byte piece lane & 15 of a row: its half, its place
-#pragma unroll 4
-        for (int r0 = late; r0 < min(valid, kTile); r0 += 2) {
-          const int row = min(r0 + (lane >> 4), kTile - 1);
-          const uint4 x = v[piece + row * 8];
-          const uint32_t e = 0x7f807f80u;
-          const uint32_t hit = __vcmpeq2(x.x & e, e) | __vcmpeq2(x.y & e, e) | __vcmpeq2(x.z & e, e) | __vcmpeq2(x.w & e, e);
-          const uint32_t any = __ballot_sync(0xffffffffu, hit != 0u && row < valid);
-          if (any) {
-            if ((any >> (lane & 16)) & 0xffffu) v[piece + row * 8] = make_uint4(0u, 0u, 0u, 0u);
-            if ((lane & 15) == 0 && ((any >> lane) & 0xffffu)) atomicOr(&sm.odd[n_tiles % kInfo][row >> 5], 1u << (row & 31));
-          }
-        }
-        if (valid < kTile || bad)
-          for (int e = lane; e < 2 * kTile * 8; e += 32) {
-            const int row = (e >> 3) & (kTile - 1);
-            if (row >= valid || (bad >> (row >> a.w.log_p) & 1)) v[e] = make_uint4(0u, 0u, 0u, 0u);
-          }
-        fence_async_smem();
-        __syncwarp();
-      }
-      for (int s = 0; s < ns; ++s) {
-        if (!wait_warp(smem_u32(&sm.p_full[s]), n_p[s] & 1, w, 5)) return;
-        ++n_p[s];
+      clean_values(a, sm, it, j, nv, n_tiles, lane);
+      const int s = pair ? 0 : j & 1;
+      if (!pv(s, nv, j >= ahead)) return;
+      if (!pair) release(nv);
+      if (more) {
+        if (!full(nk)) return;
         tc_fence_after();
-        pv(s, nv, j > 0);
-        if (s == ns - 1 && lane == 0) tc_commit(smem_u32(&sm.empty[nv % kStages]));
-        if (j + 1 < n) {   // in issue order behind the product that reads P_s, whose columns it overwrites
-          if (s == 0) {
-            if (!full(nk)) return;
-            tc_fence_after();
-          }
-          qk(s, nk);
-          if (s == ns - 1 && lane == 0) {
-            tc_commit(smem_u32(&sm.empty[nk % kStages]));
-            if (j + 2 == n) tc_commit(smem_u32(&sm.q_empty));
-          }
+        qk(s, 0, nk);
+        if (!pair) release(nk);
+      }
+      if (pair) {
+        if (!pv(1, nv, j > 0)) return;
+        release(nv);
+        if (more) {
+          qk(1, 1, nk);
+          release(nk);
         }
       }
+      if (more && j + ahead == n - 1 && lane == 0) tc_commit(smem_u32(&sm.q_empty));
     }
     n_use += 2 * n;
     ++n_items;
-  } while (k.next(a.w));
+  }
 }
 
 // The exponentials of one tile of one row, to TMEM as bf16; returns their sum.
@@ -303,27 +305,24 @@ __device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o
 __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int stream, int quarter,
                                              int lane) {
   Walk k;
-  k.start(sm.plan);
-  k.load(a.w);
-  uint32_t n_s = 0, n_all = 0;     // tiles of this stream so far; key tiles of the CTA so far
+  k.start(a.w, sm.plan);
+  uint32_t n_s = 0, n_all = 0, n_join = 0;   // tiles of this stream so far; key tiles of the CTA; joins of the streams
   const int r = quarter * 32 + lane;                        // row of the query tile
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const uint32_t s_addr = tmem + lanes + kColS + stream * 128, o_addr = tmem + lanes + kColO + stream * 128;
   const uint32_t bar_s = smem_u32(&sm.s_full[stream]), bar_p = smem_u32(&sm.p_full[stream]), bar_o = smem_u32(&sm.pv_done[stream]);
-  do {
+  for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
-    if (stream >= streams_of(a, it)) {
-      n_all += n;
-      continue;
-    }
-    const int tok0 = it.block * a.w.tokens + stream * a.TQ;   // first token of the tile
+    const bool pair = paired(it);
+    const int j0 = pair ? 0 : stream, step = pair ? 1 : 2, q_tile = pair ? stream : 0;
+    const int tok0 = it.block * a.w.tokens + q_tile * a.TQ;   // first token of the tile
     const int token = tok0 + r / a.w.G;
     const bool live = r < a.TQ * a.w.G && token < it.n;
     auto limit_of = [&](int tk) { return a.w.causal ? min(max(it.len - it.n + tk + 1, 0), it.len) : it.len; };
     const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
     float m = -INFINITY, l = 0.f;
-    for (int j = 0; j < n; ++j, ++n_s, ++n_all) {
+    for (int j = j0; j < n; j += step, ++n_s) {
       const int key0 = (it.t0 + j) * kTile;
       if (!wait_warp(bar_s, n_s & 1, w, 6)) return;
       tc_fence_after();
@@ -332,7 +331,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       float s[kTile];
 #pragma unroll
       for (int i = 0; i < kTile; ++i) s[i] = __uint_as_float(raw[i]);
-      const uint32_t bad = *(volatile uint32_t*)&sm.bad[n_all % kInfo];
+      const uint32_t bad = *(volatile uint32_t*)&sm.bad[(n_all + j) % kInfo];
       if (key0 + kTile > least || bad) {
 #pragma unroll
         for (int i = 0; i < kTile; ++i)
@@ -350,7 +349,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
         const float f = raise ? ex2(m - top) : 1.0f;
         if (raise) m = top;
         l *= f;
-        if (j > 0) {
+        if (j > j0) {
           if (!wait_warp(bar_o, (n_s - 1) & 1, w, 7)) return;
           tc_fence_after();
 #pragma unroll
@@ -370,18 +369,46 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       if (lane == 0) bar_arrive(bar_p);
     }
     // the item's output: normalised, or a partial result for the join
-    if (!wait_warp(bar_o, (n_s - 1) & 1, w, 7)) return;
-    tc_fence_after();
+    if (j0 < n) {
+      if (!wait_warp(bar_o, (n_s - 1) & 1, w, 7)) return;
+      tc_fence_after();
+    }
     // value rows that were left out because they are not finite, for the tokens that see them
     for (int j = n - 1; j >= 0 && late_row(a, it, j) < kTile; --j) {
+      if (!pair && (j & 1) != stream) continue;
       for (int x = 0; x < 4; ++x) {
-        uint32_t odd = *(volatile uint32_t*)&sm.odd[(n_all - n + j) % kInfo][x];
+        uint32_t odd = *(volatile uint32_t*)&sm.odd[(n_all + j) % kInfo][x];
         for (; odd; odd &= odd - 1) add_row(a, it, o_addr, (it.t0 + j) * kTile + x * 32 + __ffs(odd) - 1, limit, token, r % a.w.G, m);
       }
     }
+    n_all += n;
+    // one query tile: stream 1 leaves its maximum and sum, stream 0 takes its output from TMEM (the same lanes, other columns)
+    float f0 = 1.0f, f1 = 0.f;
+    if (!pair && n > 1) {
+      if (stream == 1) {
+        sm.other[r] = make_float2(m, l);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_u32(&sm.join_full));
+        if (!wait_warp(smem_u32(&sm.join_done), n_join & 1, w, 8)) return;
+        tc_fence_after();
+        ++n_join;
+        continue;
+      }
+      if (!wait_warp(smem_u32(&sm.join_full), n_join & 1, w, 8)) return;
+      tc_fence_after();
+      ++n_join;
+      const float2 x = sm.other[r];
+      const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
+      f0 = ex2(m - ref), f1 = ex2(x.x - ref);
+      l = l * f0 + x.y * f1, m = top;
+    } else if (!pair && stream == 1) {
+      continue;
+    }
+    const bool joined = !pair && n > 1;
     const bool whole = it.t0 == 0 && it.t1 == it.tiles;
     const int which = it.t0 > 0 ? 0 : 1;
-    const int br = stream * a.TQ * a.w.G + r;                // row of the block
+    const int br = q_tile * a.TQ * a.w.G + r;                // row of the block
     const bool none = m == -INFINITY;
     const float inv = none ? 0.f : 1.0f / l;
     const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.w.slot_rows + br;
@@ -390,6 +417,12 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     for (int c = 0; c < 4; ++c) {
       uint32_t o[32];
       tmem_ld32(o_addr + c * 32, o);
+      if (joined) {
+        uint32_t o1[32];
+        tmem_ld32(o_addr + 128 + c * 32, o1);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+      }
       if (!live) continue;
       if (whole) {
         uint4* dst = reinterpret_cast<uint4*>(a.out + at * kHeadDim + c * 32);
@@ -411,12 +444,16 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       if (!whole) a.w.ml[slot] = make_float2(m, l);
       else if (a.lse) a.lse[at] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     }
-    tc_fence_before();   // O is read before this stream's next P is announced
+    tc_fence_before();   // O is read before the streams' next P is announced
+    if (joined) {
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_u32(&sm.join_done));
+    }
     if (!whole && r == 0 && stream == 0) {
       int* sp = reinterpret_cast<int*>(a.w.split + blockIdx.x);
       sp[2 * which] = k.pair, sp[2 * which + 1] = k.block;
     }
-  } while (k.next(a.w));
+  }
 }
 
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ CUtensorMap qm,
@@ -436,6 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     bar_init(smem_u32(&sm.q_full), 1), bar_init(smem_u32(&sm.q_empty), 1);
     for (int s = 0; s < 2; ++s)
       bar_init(smem_u32(&sm.s_full[s]), 1), bar_init(smem_u32(&sm.p_full[s]), 4), bar_init(smem_u32(&sm.pv_done[s]), 1);
+    bar_init(smem_u32(&sm.join_full), 4), bar_init(smem_u32(&sm.join_done), 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
     sm.abort_flag = 0;
@@ -449,14 +487,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   if (threadIdx.x == 0) a.w.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
   __syncthreads();
   const Waiter w{&sm.abort_flag, a.w.status, a.wait_ns};
-  const bool work = sm.plan.left > 0;
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    if (work) softmax_role(a, sm, tmem, w, warp >> 2, warp & 3, lane);
+    softmax_role(a, sm, tmem, w, warp >> 2, warp & 3, lane);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (work && warp == 8) mma_role(a, sm, tmem, w, lane);
-    if (work && warp == 9) load_role(a, sm, &qm, &km, &vm, w, lane);
+    if (warp == 8) mma_role(a, sm, tmem, w, lane);
+    if (warp == 9) load_role(a, sm, &qm, &km, &vm, w, lane);
   }
   tc_fence_before();
   __syncthreads();
@@ -509,7 +546,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   TcArgs a{};
   a.w = base;
   a.TQ = kTile / base.G;
-  a.w.tokens = 2 * a.TQ, a.w.M = a.w.tokens * base.G, a.w.tile = kTile, a.w.granule = 1;
+  a.w.tokens = 2 * a.TQ, a.w.M = a.w.tokens * base.G, a.w.tile = kTile, a.w.granule = 2;
   a.x_scale = (scale < 0.f ? -scale : scale) * kLog2e;
   a.idesc_qk = kIdescQK | (scale < 0.f ? kNegateA : 0u);
   a.q_bytes = 2u * (uint32_t)(a.TQ * base.G) * 128u;
@@ -534,12 +571,12 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   if (e != cudaSuccess) return e;
   if (attrs.numRegs * kThreads < kSoftmaxRegs * 256 + kOtherRegs * 128) return cudaErrorLaunchOutOfResources;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(kTcWorkers), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = sizeof(Smem), cfg.stream = st;
+  cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = sizeof(Smem), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, attend_tc_kernel, qm, km, vm, a);
   count_launch();
-  return e != cudaSuccess ? e : launch_join<true>(a.w, kTcWorkers, out, lse, st);
+  return e != cudaSuccess ? e : launch_join<true>(a.w, kWorkers, out, lse, st);
 }
 
 }  // namespace ckv

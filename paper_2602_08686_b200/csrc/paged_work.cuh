@@ -2,9 +2,10 @@
 //
 // An item is one block of query rows of one (unit, KV head): the rows r = token * G + head of the unit's tokens and the
 // group's G query heads, `M` of them.  Its cost is the number of key tiles its last token sees (at least one, so that rows
-// that see nothing are written too).  Lengths and token counts live on the device, so the split is made there:
-// every worker (CTA) adds up the costs, takes an equal share of the total sequence of tiles and works through the items
-// in it.  The first of them may have been begun by the worker before, the last may be finished by the next: those two
+// that see nothing are written too), times two where the block fills more than half of its rows.  Lengths and token counts
+// live on the device, so the split is made there: every worker (CTA) adds up the costs, takes an equal share of the total
+// and works through the items in it; a tile belongs to the share its cost begins in.  The first item may have been begun by the
+// worker before, the last may be finished by the next: those two
 // leave unnormalised partial results in the worker's two slots, and join_kernel adds up what belongs together in worker
 // order (the result does not depend on timing).
 #pragma once
@@ -17,9 +18,7 @@ struct WorkArgs {
   int M;            // query rows of a block
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
   int tile;         // keys per tile
-  int granule;      // least tiles per worker
-  int min_rows;     // only units with more query rows per head than this ...
-  int max_rows;     // ... and at most this many
+  int granule;      // least cost per worker, at least 2
   int P, log_p, n_pages, max_pages;
   const int32_t *starts, *lengths, *table;
   int* status;
@@ -35,13 +34,12 @@ struct Item {
   int rows;              // query rows of the unit (n * G)
   int visible;           // rows the block's last token sees
   int tiles;             // tiles of the whole item
+  int weight;            // cost of each
   int t0, t1;            // this worker's part
 };
 
 __device__ __forceinline__ int unit_blocks(const WorkArgs& a, int n) {
-  const int64_t rows = (int64_t)n * a.G;
-  if (rows <= a.min_rows || rows > a.max_rows) return 0;
-  return a.tokens ? (n + a.tokens - 1) / a.tokens : (int)((rows + a.M - 1) / a.M);
+  return a.tokens ? (n + a.tokens - 1) / a.tokens : (int)(((int64_t)n * a.G + a.M - 1) / a.M);
 }
 __device__ __forceinline__ int head_length(const WorkArgs& a, int pair) {
   return min(max(a.lengths[pair], 0), a.max_pages << a.log_p);
@@ -55,12 +53,16 @@ __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, 
 }
 __device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) / a.tile, 1); }
 
+// 2: the block fills both of the query tiles of whole tokens that make it up
+__device__ __forceinline__ int weight_of(const WorkArgs& a, int n, int block) {
+  return a.tokens && 2 * (n - block * a.tokens) > a.tokens ? 2 : 1;
+}
+
 struct Plan {           // in shared memory
   long long warp_sum[32];
   long long total;
-  long long left;       // tiles this worker still has to do
-  int pair, block, t0;  // where it starts
-  int workers;          // workers that have something to do
+  long long begin, end; // the worker's share, relative to the cost before the item it starts in
+  int pair, block;      // that item
 };
 
 // All threads of the CTA.  Returns with the worker's share in `plan`.
@@ -77,7 +79,7 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
     if (nb == 0) return 0ll;
     const int len = head_length(a, p);
     long long c = 0;
-    for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b));
+    for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
     return c;
   };
   long long mine = 0;
@@ -101,11 +103,13 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
   }
   __syncthreads();
   const long long total = plan.total;
-  const long long most = (total + a.granule - 1) / a.granule;
+  // rounded down: every share is at least `granule` >= 2 wide, so that a tile begins in each (the join follows an item from one
+  // worker to the next and stops at the first that has no part in it)
+  const long long most = max(total / a.granule, 1ll);
   const int workers = (int)(most < n_workers ? most : n_workers);
   const long long begin = worker < workers ? total * worker / workers : total;
   const long long end = worker < workers ? total * (worker + 1) / workers : total;
-  if (threadIdx.x == 0) plan.left = end - begin, plan.workers = workers;
+  if (threadIdx.x == 0 && begin >= end) plan.begin = plan.end = 0;
   const long long before = plan.warp_sum[warp] + incl - mine;
   if (end > begin && begin >= before && begin < before + mine) {
     long long at = begin - before;
@@ -119,19 +123,19 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
       unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
       const int len = head_length(a, p);
       for (;; ++b) {
-        const int t = tiles_of(a, block_visible(a, n, len, b));
+        const int t = tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
         if (at < t) break;
         at -= t;
       }
-      plan.pair = p, plan.block = b, plan.t0 = (int)at;
+      plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + (end - begin);
       break;
     }
   }
   __syncthreads();
 }
 
-// The item at (pair, block), from tile t0, at most `left` tiles of it.
-__device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block, int t0, long long left) {
+// The item at (pair, block): its tiles whose cost begins in [begin, end), relative to the cost before the item.
+__device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block, long long begin, long long end) {
   Item it;
   it.u = pair / a.Hkv, it.g = pair - it.u * a.Hkv, it.block = block;
   unit_tokens(a.starts, it.u, a.T, it.first, it.n);
@@ -140,8 +144,10 @@ __device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block
   it.rows = it.n * a.G;
   it.visible = block_visible(a, it.n, it.len, block);
   it.tiles = tiles_of(a, it.visible);
-  it.t0 = t0;
-  it.t1 = (int)(left < it.tiles - t0 ? t0 + left : it.tiles);
+  it.weight = weight_of(a, it.n, block);
+  const long long cost = (long long)it.tiles * it.weight;
+  const int from = (int)(begin < cost ? begin : cost), to = (int)(end < cost ? end : cost);
+  it.t0 = (from + it.weight - 1) / it.weight, it.t1 = (to + it.weight - 1) / it.weight;
   return it;
 }
 // Moves to the next item that has rows; false behind the last one.
@@ -159,6 +165,33 @@ __device__ __forceinline__ bool next_item(const WorkArgs& a, int& pair, int& blo
   }
   return false;
 }
+// Walks a worker's items: for (Walk k(...); k.more(); k.next()) ... k.it
+struct Walk {
+  int pair, block;
+  long long begin, end;
+  bool live;
+  Item it;
+  __device__ __forceinline__ void settle(const WorkArgs& a) {   // to the first item with tiles for this worker
+    while (live) {
+      it = make_item(a, pair, block, begin, end);
+      if (it.t1 > it.t0) return;
+      step(a);
+    }
+  }
+  __device__ __forceinline__ void step(const WorkArgs& a) {
+    end -= (long long)it.tiles * it.weight, begin = 0;
+    live = end > 0 && next_item(a, pair, block, it.n);
+  }
+  __device__ __forceinline__ void start(const WorkArgs& a, const Plan& p) {
+    pair = p.pair, block = p.block, begin = p.begin, end = p.end, live = end > begin;
+    settle(a);
+  }
+  __device__ __forceinline__ bool next(const WorkArgs& a) {
+    step(a);
+    settle(a);
+    return live;
+  }
+};
 // Rows of the block, and where query row r of it (token, head) lives.
 __device__ __forceinline__ int block_rows(const WorkArgs& a, const Item& it) {
   return min(a.M, it.rows - it.block * a.M);
@@ -182,16 +215,15 @@ __device__ __forceinline__ int page_of(const WorkArgs& a, const Item& it, int sl
   return -1;
 }
 
-constexpr int kTcWorkers = 148;      // CTAs of the tensor-core kernel, one per SM
-constexpr int kTcRows = 256;         // query rows of its blocks
+constexpr int kWorkers = 148;        // CTAs of every attention kernel, one per SM
+constexpr int kTcRows = 256;         // query rows of a block of the tensor-core kernel
 
 // `base`: everything but the block and tile sizes; scale not 0.
 cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float scale, const void* q, const void* k_pages,
                              const void* v_pages, void* out, float* lse, cudaStream_t st);
-constexpr int kMmaWorkers = 148;     // CTAs of the bf16 kernel for few rows
-constexpr int kMmaRows = 32;         // most query rows of its blocks
+constexpr int kMmaRows = 32;         // most query rows of a block of the bf16 kernel for few rows
 constexpr int kMmaTile = 64;         // keys per tile of its schedule
-// rows: the most query rows per KV head that any unit it is to take has.
+// rows: the most query rows per KV head that a unit is expected to have.
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
 template <bool BF16>
