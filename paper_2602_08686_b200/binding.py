@@ -407,7 +407,7 @@ def ckv_allocate_rows_host(n: int, f: int, P: int, demands) -> list[int]:
 # their tensors had, and every call compares what it is given with it: a tensor laid out differently, or one of
 # another device, would be read wrongly.  A call runs on its tensors' device, on that device's current stream unless told otherwise.
 def _layout(t: torch.Tensor | None):
-    return None if t is None else (tuple(t.shape), t.stride(), t.dtype, t.device)
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
 def _same(t: torch.Tensor, layout, name: str) -> int:
@@ -415,25 +415,26 @@ def _same(t: torch.Tensor, layout, name: str) -> int:
     if layout is None:
         raise ValueError(f"{name}: the struct was made without it")
     shape, stride, dtype, device = layout
-    if t.shape != shape or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {shape} {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{name} must be {tuple(shape)} {dtype} on device {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     if t.stride() != stride and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), stride)):
         raise ValueError(f"{name} has strides {t.stride()}; the struct was made for {stride}")
     return t.data_ptr()
 
 
-def _dense(t: torch.Tensor, shape, dtype, device, name: str) -> int:
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a dense {tuple(shape)} {dtype} on {device}")
+def _dense(t: torch.Tensor, shape, dtype, device: int, name: str) -> int:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense {tuple(shape)} {dtype} on device {device}")
     return t.data_ptr()
 
 
-def _paged_call(fn, what: str, device, stream, *args) -> None:
-    if device.index != torch.cuda.current_device():
+def _paged_call(fn, what: str, device: int, stream, *args) -> None:
+    if device < 0:
+        raise ValueError("the paged calls take CUDA tensors")
+    if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return _paged_call(fn, what, device, stream, *args)
-    s = torch.cuda.current_stream() if stream is None else stream
-    status = fn(*args, s.cuda_stream)
+    status = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
     if status != OK:
         raise CkvError(status, what)
 
@@ -453,8 +454,8 @@ def make_packed(q: torch.Tensor | None, k: torch.Tensor | None, n_units: int, ma
         pg.q_stride_tok, pg.q_stride_head = q.stride(0), q.stride(1)
     if k is not None:
         pg.kv_stride_tok, pg.kv_stride_head = k.stride(0), k.stride(1)
-    pg._q, pg._k, pg._pages, pg._device, pg._dtype = _layout(q), _layout(k), None, t.device, t.dtype
-    pg._starts = (pg.n_units + 1,)
+    pg._q, pg._k, pg._pages, pg._device, pg._dtype = _layout(q), _layout(k), None, t.get_device(), t.dtype
+    pg._starts, pg._ref = (pg.n_units + 1,), C.byref(pg)
     return pg
 
 
@@ -480,9 +481,8 @@ def make_paged(k_pages: torch.Tensor, page_table: torch.Tensor, q: torch.Tensor 
     pg.n_kv_heads, pg.causal, pg.scale = Hkv, int(bool(causal)), float(scale)
     pg.n_pages, pg.page_size, pg.max_pages = k_pages.shape[0], k_pages.shape[1], max_pages
     pg.page_stride, pg.page_stride_row = k_pages.stride(0), k_pages.stride(1)
-    pg._pages, pg._device, pg._dtype = _layout(k_pages), k_pages.device, k_pages.dtype
-    pg._table, pg._heads, pg._starts = tuple(page_table.shape), (Nu, Hkv), (Nu + 1,)
-    pg._ws_bytes = ckv_paged_workspace_bytes(pg)
+    pg._pages, pg._device, pg._dtype = _layout(k_pages), k_pages.get_device(), k_pages.dtype
+    pg._table, pg._heads, pg._starts, pg._ref = tuple(page_table.shape), (Nu, Hkv), (Nu + 1,), C.byref(pg)
     return pg
 
 
@@ -502,7 +502,7 @@ def make_rotary(inv_freq: torch.Tensor | None, interleaved: bool = False, q_norm
         raise ValueError("inv_freq and the norm weights must be on one device")
     ptr = [None if t is None else t.data_ptr() for t in (inv_freq, q_norm_w, k_norm_w)]
     r = ckv_rotary(*ptr, 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), float(rot_scale), float(norm_eps))
-    r._keep, r._device = kept, kept[0].device if kept else None
+    r._keep, r._device, r._ref = kept, kept[0].get_device() if kept else None, C.byref(r)
     return r
 
 
@@ -514,15 +514,15 @@ def alloc_paged_workspace(paged: ckv_paged, device=None) -> torch.Tensor:
     nbytes = ckv_paged_workspace_bytes(paged)
     if nbytes == 0:
         raise CkvError(ERR_INVALID_ARG, "ckv_paged_workspace_bytes")
-    return torch.empty(nbytes, dtype=torch.uint8, device=paged._device if device is None else device)
+    return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", paged._device) if device is None else device)
 
 
 def _rotary_of(pg: ckv_paged, rotary: ckv_rotary | None):
     if rotary is None:
         return None
     if rotary._device is not None and rotary._device != pg._device:
-        raise ValueError(f"the rotary tables are on {rotary._device}, the tokens on {pg._device}")
-    return C.byref(rotary)
+        raise ValueError(f"the rotary tables are on device {rotary._device}, the tokens on {pg._device}")
+    return rotary._ref
 
 
 def _tokens_out(pg, out, t, layout, name):
@@ -535,7 +535,7 @@ def _tokens_out(pg, out, t, layout, name):
 
 
 def _ws_of(pg, ws):
-    if ws.device != pg._device or ws.dtype != torch.uint8 or not ws.is_contiguous():
+    if ws.get_device() != pg._device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise ValueError("ws must be a dense uint8 tensor on the device of the pages")
     return ws.data_ptr()
 
@@ -544,7 +544,7 @@ def ckv_rotate(paged, rotary, q, k, positions, token_starts, q_out, k_out, strea
     """Norms and rotation of q [T, H, d] and k [T, Hkv, d] (either may be None) into q_out, k_out (dense, or in place)."""
     T = paged.n_tokens
     dev = paged._device
-    _paged_call(lib().ckv_rotate, "ckv_rotate", dev, stream, C.byref(paged), _rotary_of(paged, rotary),
+    _paged_call(lib().ckv_rotate, "ckv_rotate", dev, stream, paged._ref, _rotary_of(paged, rotary),
                 None if q is None else _same(q, paged._q, "q"), None if k is None else _same(k, paged._k, "k"),
                 _dense(positions, (T,), torch.int32, dev, "positions"),
                 _dense(token_starts, paged._starts, torch.int32, dev, "token_starts"),
@@ -556,7 +556,7 @@ def ckv_append(paged, rotary, k, v, positions, token_starts, lengths, page_table
     """Appends the tokens' keys (normed, rotated; as they are when rotary is None) and values to the cache; q goes normed and
     rotated into q_out; new_lengths receives the heads' lengths with the tokens."""
     dev, i32 = paged._device, torch.int32
-    _paged_call(lib().ckv_append, "ckv_append", dev, stream, C.byref(paged), _rotary_of(paged, rotary),
+    _paged_call(lib().ckv_append, "ckv_append", dev, stream, paged._ref, _rotary_of(paged, rotary),
                 None if q is None else _same(q, paged._q, "q"), _same(k, paged._k, "k"), _same(v, paged._k, "v"),
                 None if positions is None else _dense(positions, (paged.n_tokens,), i32, dev, "positions"),
                 _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(lengths, paged._heads, i32, dev, "lengths"),
@@ -570,10 +570,10 @@ def ckv_gather_pages(shape, params, paged, k, v, indices, budgets, offsets, page
     """The rows the retention pass kept of k, v, into the pages of a cache; lengths receives the heads' budgets."""
     dev, i32 = paged._device, torch.int32
     _check_kv(shape, k, "k"), _check_kv(shape, v, "v")
-    if k.device != dev or v.device != dev:
-        raise ValueError(f"k and v must be on {dev}")
+    if k.get_device() != dev or v.get_device() != dev:
+        raise ValueError(f"k and v must be on device {dev}")
     Nu, Hkv = paged._heads
-    _paged_call(lib().ckv_gather_pages, "ckv_gather_pages", dev, stream, C.byref(shape), C.byref(params), C.byref(paged),
+    _paged_call(lib().ckv_gather_pages, "ckv_gather_pages", dev, stream, C.byref(shape), C.byref(params), paged._ref,
                 k.data_ptr(), v.data_ptr(), _dense(indices, (Nu, rows_per_unit(shape, params)), i32, dev, "indices"),
                 _dense(budgets, paged._heads, i32, dev, "budgets"), _dense(offsets, (Nu, Hkv + 1), i32, dev, "offsets"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _same(k_pages, paged._pages, "k_pages"),
@@ -585,7 +585,7 @@ def ckv_paged_attend(paged, q, k_pages, v_pages, page_table, lengths, token_star
     """Attention of the packed tokens q [T, H, d] over the cache (lengths count the tokens' own rows when causal)."""
     dev, i32 = paged._device, torch.int32
     qs = paged._q
-    _paged_call(lib().ckv_paged_attend, "ckv_paged_attend", dev, stream, C.byref(paged), _same(q, qs, "q"),
+    _paged_call(lib().ckv_paged_attend, "ckv_paged_attend", dev, stream, paged._ref, _same(q, qs, "q"),
                 _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _dense(lengths, paged._heads, i32, dev, "lengths"),
                 _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(out, qs[0], paged._dtype, dev, "out"),

@@ -1,5 +1,7 @@
 // What the kernels around the paged cache share: row addressing, error reports and the work schedule of the attention.
 #pragma once
+#include <atomic>
+
 #include "ckv_common.cuh"
 
 namespace ckv {
@@ -37,6 +39,21 @@ __device__ __forceinline__ void unit_tokens(const int32_t* starts, int u, int T,
   first = min(max(starts[u], 0), T);
   count = max(min(starts[u + 1], T) - first, 0);
 }
+
+// A kernel's attributes are set once on each device.
+struct PerDevice {
+  std::atomic<bool> done[kMaxDevices] = {};
+  template <class F>
+  cudaError_t once(F&& f) {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < kMaxDevices && done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+    const cudaError_t r = f();
+    if (r == cudaSuccess && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
+    return r;
+  }
+};
 
 // Launchers (each returns cudaGetLastError() after queuing its kernels).
 cudaError_t launch_rotate(const ckv_paged& pg, const ckv_rotary* rot, const void* q, const void* k, const void* v,

@@ -176,20 +176,38 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int wo
   const int4 mine = a.split[w];
   if (mine.z < 0) return;
   const Item it = make_item(a, mine.z, mine.w, 0, 1ll << 40);
-  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), d = (threadIdx.x & 31) * 4;
+  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), d = (threadIdx.x & 31) * 4;   // a warp per row
   if (r >= block_rows(a, it)) return;
-  int last = w + 1;
-  while (last < workers && a.split[last].x == mine.z && a.split[last].y == mine.w) ++last;
+  // the workers after w that have a part: the lanes look at 32 of them at once
+  const int lane = threadIdx.x & 31;
+  int parts = 0;
+  for (int w0 = w + 1;; w0 += 32) {
+    const int x = w0 + lane;
+    const int4 s = x < workers ? a.split[x] : make_int4(-1, -1, -1, -1);
+    const unsigned no = ~__ballot_sync(0xffffffffu, s.x == mine.z && s.y == mine.w);
+    parts += no ? __ffs(no) - 1 : 32;
+    if (no) break;
+  }
   float2 ml = a.ml[((int64_t)w * 2 + 1) * a.slot_rows + r];
   float4 o = *reinterpret_cast<const float4*>(a.o + (((int64_t)w * 2 + 1) * a.slot_rows + r) * kHeadDim + d);
-  for (int p = w + 1; p < last; ++p) {
-    const int64_t slot = (int64_t)p * 2 * a.slot_rows + r;
-    const float2 x = a.ml[slot];
-    const float4 y = *reinterpret_cast<const float4*>(a.o + slot * kHeadDim + d);
-    const float top = fmaxf(ml.x, x.x), ref = top == -INFINITY ? 0.f : top;
-    const float ca = exp2f(ml.x - ref), cb = exp2f(x.x - ref);
-    ml = make_float2(top, ml.y * ca + x.y * cb);
-    o.x = o.x * ca + y.x * cb, o.y = o.y * ca + y.y * cb, o.z = o.z * ca + y.z * cb, o.w = o.w * ca + y.w * cb;
+  constexpr int kBatch = 4;                       // parts in flight
+  for (int p0 = 1; p0 <= parts; p0 += kBatch) {
+    float2 x[kBatch];
+    float4 y[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int64_t slot = (int64_t)(w + min(p0 + b, parts)) * 2 * a.slot_rows + r;
+      x[b] = a.ml[slot];
+      y[b] = *reinterpret_cast<const float4*>(a.o + slot * kHeadDim + d);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (p0 + b > parts) break;
+      const float top = fmaxf(ml.x, x[b].x), ref = top == -INFINITY ? 0.f : top;
+      const float ca = exp2f(ml.x - ref), cb = exp2f(x[b].x - ref);
+      ml = make_float2(top, ml.y * ca + x[b].y * cb);
+      o.x = o.x * ca + y[b].x * cb, o.y = o.y * ca + y[b].y * cb, o.z = o.z * ca + y[b].z * cb, o.w = o.w * ca + y[b].w * cb;
+    }
   }
   const bool none = ml.x == -INFINITY;
   const float inv = none ? 0.f : 1.0f / ml.y;

@@ -19,6 +19,7 @@ namespace ckv {
 namespace {
 
 constexpr int kMmaWarps = 8;        // warps of the 16-row form
+constexpr int kWholeRows = 1024;    // caches of up to this many rows per head are not split
 constexpr int kGroup = 16;          // keys per warp and step
 constexpr float kRaise = 8.0f;      // powers of two a row may exceed its reference before the output is rescaled
 
@@ -293,7 +294,10 @@ template <int MT, int NW>
 cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, float x_scale, const void* q, const void* kp, const void* vp, void* out,
                    float* lse, cudaStream_t st) {
   auto kernel = attend_mma_kernel<MT, NW>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<MT, NW>));
+  static PerDevice ready;
+  cudaError_t e = ready.once([&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<MT, NW>));
+  });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(NW * 32), cfg.dynamicSmemBytes = sizeof(Smem<MT, NW>), cfg.stream = st;
@@ -311,10 +315,12 @@ cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int row
   WorkArgs a = base;
   a.tokens = 0, a.tile = kMmaTile, a.granule = 2;
   a.M = rows <= 16 ? 16 : 32;
+  // A short cache is not split: joining parts takes another launch, and a CTA reads kWholeRows rows in about the time of one.
+  a.whole = (int64_t)a.max_pages * a.P <= kWholeRows;
   const float x_scale = scale * kLog2e;
   const cudaError_t e = rows <= 16 ? launch<1, kMmaWarps>(pg, a, x_scale, q, k_pages, v_pages, out, lse, st)
                                    : launch<2, 8>(pg, a, x_scale, q, k_pages, v_pages, out, lse, st);
-  return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, out, lse, st);
+  return e != cudaSuccess || a.whole ? e : launch_join<true>(a, kWorkers, out, lse, st);
 }
 
 }  // namespace ckv

@@ -563,13 +563,16 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
       !make_map(&km, k_pages, pg.page_size, pg.page_stride_row, pg.n_pages, pg.page_stride, true, rows, 1) ||
       !make_map(&vm, v_pages, pg.page_size, pg.page_stride_row, pg.n_pages, pg.page_stride, true, rows, 1))
     return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+  static PerDevice ready;
+  cudaError_t e = ready.once([] {
+    cudaError_t r = cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+    // setmaxnreg hands out what the launch holds: a build with fewer registers would wait for ever
+    cudaFuncAttributes attrs;
+    if (r == cudaSuccess) r = cudaFuncGetAttributes(&attrs, attend_tc_kernel);
+    if (r == cudaSuccess && attrs.numRegs * kThreads < kSoftmaxRegs * 256 + kOtherRegs * 128) r = cudaErrorLaunchOutOfResources;
+    return r;
+  });
   if (e != cudaSuccess) return e;
-  // setmaxnreg hands out what the launch holds: a build with fewer registers would wait for ever
-  cudaFuncAttributes attrs;
-  e = cudaFuncGetAttributes(&attrs, attend_tc_kernel);
-  if (e != cudaSuccess) return e;
-  if (attrs.numRegs * kThreads < kSoftmaxRegs * 256 + kOtherRegs * 128) return cudaErrorLaunchOutOfResources;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = sizeof(Smem), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();

@@ -19,6 +19,7 @@ struct WorkArgs {
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
   int tile;         // keys per tile
   int granule;      // least cost per worker, at least 2
+  int whole;        // items are not split: each goes to the share its cost begins in
   int P, log_p, n_pages, max_pages;
   const int32_t *starts, *lengths, *table;
   int* status;
@@ -107,8 +108,15 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
   // worker to the next and stops at the first that has no part in it)
   const long long most = max(total / a.granule, 1ll);
   const int workers = (int)(most < n_workers ? most : n_workers);
-  const long long begin = worker < workers ? total * worker / workers : total;
-  const long long end = worker < workers ? total * (worker + 1) / workers : total;
+  long long begin = total, end = total;
+  if (worker < workers) {
+    if (total < (1 << 24)) {   // 32-bit divisions where they do: the plan is all latency
+      begin = (unsigned)total * (unsigned)worker / (unsigned)workers;
+      end = (unsigned)total * (unsigned)(worker + 1) / (unsigned)workers;
+    } else {
+      begin = total * worker / workers, end = total * (worker + 1) / workers;
+    }
+  }
   if (threadIdx.x == 0 && begin >= end) plan.begin = plan.end = 0;
   const long long before = plan.warp_sum[warp] + incl - mine;
   if (end > begin && begin >= before && begin < before + mine) {
@@ -146,6 +154,10 @@ __device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block
   it.tiles = tiles_of(a, it.visible);
   it.weight = weight_of(a, it.n, block);
   const long long cost = (long long)it.tiles * it.weight;
+  if (a.whole) {
+    it.t0 = begin > 0 ? it.tiles : 0, it.t1 = it.tiles;
+    return it;
+  }
   const int from = (int)(begin < cost ? begin : cost), to = (int)(end < cost ? end : cost);
   it.t0 = (from + it.weight - 1) / it.weight, it.t1 = (to + it.weight - 1) / it.weight;
   return it;
