@@ -18,9 +18,10 @@
 namespace ckv {
 namespace {
 
-constexpr int kMmaWarps = 8;        // warps of the 16-row form
-constexpr int kWholeRows = 1024;    // caches of up to this many rows per head are not split
+constexpr int kMmaWarps = 8;
+constexpr int kClusterRows = 1024;  // rows of a cache per CTA up to which clusters take it
 constexpr int kGroup = 16;          // keys per warp and step
+constexpr int kCtaKeys = kMmaWarps * kGroup;
 constexpr float kRaise = 8.0f;      // powers of two a row may exceed its reference before the output is rescaled
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -50,29 +51,65 @@ struct Smem {
   uint4 q[MT][2][4][32];                       // query fragments: [tile][rows +0 / +8][piece][lane]
   float2 ml[NW][16 * MT];
   float o[NW][16 * MT][kHeadDim + 4];
+  float2 cta_ml[16 * MT];                      // the CTA's result, for the others of its cluster
+  float cta_o[16 * MT][kHeadDim];
 };
 
-template <int MT, int NW>
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float2 ld_peer(const void* mine, int rank) {   // the same place in another CTA's shared memory
+  uint32_t at;
+  float2 x;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
+  return x;
+}
+
+// kCluster: every item is one cluster's (of n_cta CTAs), whose warps share its keys and whose results join through distributed
+// shared memory; no schedule, no second kernel.  Otherwise the items are split evenly over the grid.
+template <int MT, int NW, bool kCluster>
 __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_paged pg, float x_scale,
                                                                 const char* __restrict__ q, const char* __restrict__ kp,
                                                                 const char* __restrict__ vp, __nv_bfloat16* __restrict__ out,
-                                                                float* __restrict__ lse) {
+                                                                float* __restrict__ lse, int n_cta) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Smem<MT, NW>& sm = *reinterpret_cast<Smem<MT, NW>*>(smem_raw);
   constexpr int kThreads = NW * 32;
-  pdl_wait();
-  make_plan<kThreads>(a, blockIdx.x, gridDim.x, sm.plan);
-  pdl_launch_dependents();
-  if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
-  Walk walk;
-  walk.start(a, sm.plan);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, p = lane >> 2, c = lane & 3;
   const int64_t row_bytes = pg.page_stride_row * 2, page_bytes = pg.page_stride * 2;
-  for (; walk.live; walk.next(a)) {
+  pdl_wait();
+  Walk walk;
+  const int rank = kCluster ? (int)blockIdx.x % n_cta : 0;
+  const int stride = (kCluster ? n_cta : 1) * NW * kGroup;     // keys all warps take per step
+  int early_page = 0;                                          // table entry of the warp's first group, asked for ahead of the lengths
+  auto cluster_item = [&](int pair, int block) {               // the next item of this cluster that has rows
+    walk.live = false;
+    for (; pair < a.Nu * a.Hkv; pair += gridDim.x / n_cta, block = 0) {
+      const int slot = (rank * NW + warp) * kGroup >> a.log_p;
+      if (slot < a.max_pages) early_page = a.table[(int64_t)pair * a.max_pages + slot];
+      walk.it = make_item(a, pair, block, 0, 1ll << 40);
+      if (block < unit_blocks(a, walk.it.n)) {
+        walk.pair = pair, walk.block = block, walk.live = true;
+        return;
+      }
+    }
+  };
+  if (kCluster) {
+    cluster_item(blockIdx.x / n_cta, 0);
+  } else {
+    make_plan<kThreads>(a, blockIdx.x, gridDim.x, sm.plan);
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
+    walk.start(a, sm.plan);
+  }
+  while (walk.live) {
     const Item& it = walk.it;
     const int rows = block_rows(a, it);
-    const int end = min(it.t1 * a.tile, it.visible), begin = it.t0 * a.tile + warp * kGroup;
-    // The page of the group at key j: its first row's address offset, or -1 for none.
+    const int end = min(it.t1 * a.tile, it.visible), begin = it.t0 * a.tile + (rank * NW + warp) * kGroup;
+    // The page of the group at key j, or -1 for none.
     auto page_at = [&](int j) { return j < end ? page_of(a, it, j >> a.log_p) : -1; };
     uint4 kr[2][4], vr[4][2];
     auto load_k = [&](int j, int page) {
@@ -94,7 +131,8 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         for (int h = 0; h < 2; ++h) vr[e][h] = have ? ldg16(at + h * 128) : make_uint4(0u, 0u, 0u, 0u);
       }
     };
-    int page = page_at(begin), next_page = page_at(begin + NW * kGroup);
+    int page = kCluster && (unsigned)early_page < (unsigned)a.n_pages && begin < end ? early_page : page_at(begin);
+    int next_page = page_at(begin + stride);
     load_k(begin, page);
     load_v(begin, page);
     // query fragments: the same for every warp
@@ -124,7 +162,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
       for (int i = 0; i < 16; ++i) o[mt][i][0] = o[mt][i][1] = o[mt][i][2] = o[mt][i][3] = 0.f;
     }
     __syncthreads();
-    for (int j = begin; j < end; j += NW * kGroup) {
+    for (int j = begin; j < end; j += stride) {
       float s[MT][2][4];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
@@ -141,8 +179,8 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         }
       }
       const int now_page = page;
-      page = next_page, next_page = page_at(j + 2 * NW * kGroup);
-      load_k(j + NW * kGroup, page);
+      page = next_page, next_page = page_at(j + 2 * stride);
+      load_k(j + stride, page);
       uint32_t pr[MT][4];
       const bool mask = j + kGroup > least || now_page < 0;
 #pragma unroll
@@ -215,7 +253,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) mma16816(o[mt][h * 8 + i], pr[mt][0], pr[mt][1], pr[mt][2], pr[mt][3], b0, b1);
         }
-      load_v(j + NW * kGroup, page);
+      load_v(j + stride, page);
       for (; odd; odd &= odd - 1) {
         const int key = __ffs(odd) - 1;
         const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(vp + now_page * page_bytes + ((j & (a.P - 1)) + key) * row_bytes);
@@ -256,6 +294,12 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
     const bool whole = it.t0 == 0 && it.t1 == it.tiles;
     const int which = it.t0 > 0 ? 0 : 1;
     const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.slot_rows;
+    auto finish = [&](int r, int d, float top, float sum, float2 x) {
+      const int64_t at = out_row(a, it, r);
+      const float inv = top == -INFINITY ? 0.f : 1.0f / sum;
+      *reinterpret_cast<uint32_t*>(out + at * kHeadDim + d) = bf16x2(x.x * inv, x.y * inv);
+      if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    };
     for (int e = threadIdx.x; e < rows * (kHeadDim / 2); e += kThreads) {
       const int r = e / (kHeadDim / 2), d = (e - r * (kHeadDim / 2)) * 2;
       float top = -INFINITY;
@@ -272,38 +316,68 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         sum = fmaf(ml.y, f, sum);
         x.x = fmaf(y.x, f, x.x), x.y = fmaf(y.y, f, x.y);
       }
-      if (whole) {
-        const int64_t at = out_row(a, it, r);
-        const float inv = top == -INFINITY ? 0.f : 1.0f / sum;
-        *reinterpret_cast<uint32_t*>(out + at * kHeadDim + d) = bf16x2(x.x * inv, x.y * inv);
-        if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      if (kCluster && n_cta > 1) {
+        *reinterpret_cast<float2*>(&sm.cta_o[r][d]) = x;
+        if (d == 0) sm.cta_ml[r] = make_float2(top, sum);
+      } else if (kCluster || whole) {
+        finish(r, d, top, sum, x);
       } else {
         *reinterpret_cast<float2*>(a.o + (slot + r) * kHeadDim + d) = x;
         if (d == 0) a.ml[slot + r] = make_float2(top, sum);
       }
     }
-    if (!whole && threadIdx.x == 0) {
-      int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
-      sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
+    if (kCluster) {
+      if (n_cta > 1) {
+        cluster_sync();
+        // the CTAs share the rows' outputs; parts are added in the order of their ranks
+        for (int e = rank * kThreads + threadIdx.x; e < rows * (kHeadDim / 2); e += n_cta * kThreads) {
+          const int r = e / (kHeadDim / 2), d = (e - r * (kHeadDim / 2)) * 2;
+          float2 ml[8], y[8], x = make_float2(0.f, 0.f);
+          float top = -INFINITY, sum = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k < n_cta) ml[k] = ld_peer(&sm.cta_ml[r], k), y[k] = ld_peer(&sm.cta_o[r][d], k), top = fmaxf(top, ml[k].x);
+          const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k < n_cta) {
+              const float f = ex2(ml[k].x - ref);
+              sum = fmaf(ml[k].y, f, sum);
+              x.x = fmaf(y[k].x, f, x.x), x.y = fmaf(y[k].y, f, x.y);
+            }
+          finish(r, d, top, sum, x);
+        }
+        cluster_sync();   // nobody's memory is written again or given back while it is read
+      }
+      cluster_item(walk.pair, walk.block + 1);
+    } else {
+      if (!whole && threadIdx.x == 0) {
+        int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
+        sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
+      }
+      walk.next(a);
     }
     __syncthreads();
   }
 }
 
-template <int MT, int NW>
-cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, float x_scale, const void* q, const void* kp, const void* vp, void* out,
-                   float* lse, cudaStream_t st) {
-  auto kernel = attend_mma_kernel<MT, NW>;
+template <int MT, int NW, bool kCluster>
+cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, int grid, int n_cta, float x_scale, const void* q, const void* kp,
+                   const void* vp, void* out, float* lse, cudaStream_t st) {
+  auto kernel = attend_mma_kernel<MT, NW, kCluster>;
   static PerDevice ready;
   cudaError_t e = ready.once([&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<MT, NW>));
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(NW * 32), cfg.dynamicSmemBytes = sizeof(Smem<MT, NW>), cfg.stream = st;
-  cudaLaunchAttribute attr = pdl_attribute();
-  cfg.attrs = &attr, cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kernel, a, pg, x_scale, (const char*)q, (const char*)kp, (const char*)vp, (__nv_bfloat16*)out, lse);
+  cfg.gridDim = dim3(grid), cfg.blockDim = dim3(NW * 32), cfg.dynamicSmemBytes = sizeof(Smem<MT, NW>), cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0] = pdl_attribute();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = n_cta, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = n_cta > 1 ? 2 : 1;
+  e = cudaLaunchKernelEx(&cfg, kernel, a, pg, x_scale, (const char*)q, (const char*)kp, (const char*)vp, (__nv_bfloat16*)out, lse, n_cta);
   count_launch();
   return e;
 }
@@ -315,12 +389,23 @@ cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int row
   WorkArgs a = base;
   a.tokens = 0, a.tile = kMmaTile, a.granule = 2;
   a.M = rows <= 16 ? 16 : 32;
-  // A short cache is not split: joining parts takes another launch, and a CTA reads kWholeRows rows in about the time of one.
-  a.whole = (int64_t)a.max_pages * a.P <= kWholeRows;
   const float x_scale = scale * kLog2e;
-  const cudaError_t e = rows <= 16 ? launch<1, kMmaWarps>(pg, a, x_scale, q, k_pages, v_pages, out, lse, st)
-                                   : launch<2, 8>(pg, a, x_scale, q, k_pages, v_pages, out, lse, st);
-  return e != cudaSuccess || a.whole ? e : launch_join<true>(a, kWorkers, out, lse, st);
+  // Short caches go to clusters: as many CTAs per head as the heads leave room for, as long as each has rows to read and none has
+  // more than kClusterRows.
+  const int64_t pairs = (int64_t)a.Nu * a.Hkv, capacity = (int64_t)a.max_pages * a.P;
+  int n_cta = 1;
+  while (n_cta < 8 && pairs * n_cta * 2 <= kWorkers && n_cta * kCtaKeys < capacity) n_cta *= 2;
+  cudaError_t e;
+  if (capacity <= (int64_t)n_cta * kClusterRows) {
+    int64_t clusters = 2 * kWorkers / n_cta;
+    if (pairs < clusters) clusters = pairs;
+    const int grid = (int)clusters * n_cta;
+    return rows <= 16 ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
+                      : launch<2, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st);
+  }
+  e = rows <= 16 ? launch<1, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
+                 : launch<2, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st);
+  return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, out, lse, st);
 }
 
 }  // namespace ckv

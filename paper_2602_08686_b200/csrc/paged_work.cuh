@@ -19,7 +19,6 @@ struct WorkArgs {
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
   int tile;         // keys per tile
   int granule;      // least cost per worker, at least 2
-  int whole;        // items are not split: each goes to the share its cost begins in
   int P, log_p, n_pages, max_pages;
   const int32_t *starts, *lengths, *table;
   int* status;
@@ -154,10 +153,6 @@ __device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block
   it.tiles = tiles_of(a, it.visible);
   it.weight = weight_of(a, it.n, block);
   const long long cost = (long long)it.tiles * it.weight;
-  if (a.whole) {
-    it.t0 = begin > 0 ? it.tiles : 0, it.t1 = it.tiles;
-    return it;
-  }
   const int from = (int)(begin < cost ? begin : cost), to = (int)(end < cost ? end : cost);
   it.t0 = (from + it.weight - 1) / it.weight, it.t1 = (to + it.weight - 1) / it.weight;
   return it;
