@@ -183,10 +183,10 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
   const uint32_t kv0 = smem_u32(sm.kv[0]);
   auto full = [&](uint32_t n) { return wait_warp(smem_u32(&sm.full[n % kStages]), (n / kStages) & 1, w, 3); };
   auto release = [&](uint32_t n) {
-    if (lane == 0) tc_commit(smem_u32(&sm.empty[n % kStages]));
+    if (elect()) tc_commit(smem_u32(&sm.empty[n % kStages]));
   };
   auto qk = [&](int s, int q_tile, uint32_t n) {   // S_s = Q K^T
-    if (lane == 0) {
+    if (elect()) {
       const uint32_t b = desc_lo(kv0 + (n % kStages) * kTileBytes, 16);
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) {   // 16 dimensions = 32 bytes of a 128-byte swizzled row; the second half is 16 KB on
@@ -200,7 +200,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
     if (!wait_warp(smem_u32(&sm.p_full[s]), n_p[s] & 1, w, 5)) return false;
     ++n_p[s];
     tc_fence_after();
-    if (lane == 0) {
+    if (elect()) {
       const uint32_t b = desc_lo(kv0 + (n % kStages) * kTileBytes, kHalf);   // 64-dimension halves 16 KB apart
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)     // 16 keys = 16 rows of 128 bytes
@@ -224,7 +224,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
       qk(j, 0, n_use + 2 * j);
       if (pair) qk(1, 1, n_use + 2 * j);
       release(n_use + 2 * j);
-      if (j == n - 1 && lane == 0) tc_commit(smem_u32(&sm.q_empty));
+      if (j == n - 1 && elect()) tc_commit(smem_u32(&sm.q_empty));
     }
     for (int j = 0; j < n; ++j, ++n_tiles) {
       const uint32_t nv = n_use + 2 * j + 1, nk = n_use + 2 * (j + ahead);
@@ -248,7 +248,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
           release(nk);
         }
       }
-      if (more && j + ahead == n - 1 && lane == 0) tc_commit(smem_u32(&sm.q_empty));
+      if (more && j + ahead == n - 1 && elect()) tc_commit(smem_u32(&sm.q_empty));
     }
     n_use += 2 * n;
     ++n_items;
