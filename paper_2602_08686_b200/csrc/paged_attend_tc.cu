@@ -2,18 +2,21 @@
 //
 // An item is up to two tiles of 128 query rows of one (unit, KV head): a tile holds whole tokens, row = token * G + head, so one TMA
 // box {G heads, 128 / G tokens} of q is a K-major operand.  Keys and values come in tiles of 128 rows, one TMA box per page and
-// 64-dimension half, into a ring of five 32 KB stages (K0 V0 K1 V1 ...).  Per tile of keys and query tile s ("stream"):
-//   S_s = Q_s K^T     M = N = K = 128, into 128 TMEM columns
-//   P_s = 2^(x - m)   one thread per row: a row's 128 logits are one thread's registers, so maximum and sum need no shuffles;
-//                     P goes back as bf16 over the columns S came from (the rounding tensor cores want; the sum l is of the
-//                     unrounded values)
-//   O_s += P_s V      A = P from TMEM, V as it lies in memory ([keys][dims], MN-major B), into 128 TMEM columns
-// The two streams take turns: while the tensor cores run one stream's products the other's softmax runs on the CUDA cores.
-// Both sides need about 1024 clocks per tile (4.2 MFMA at 4096 per clock; 16384 exponentials at 16 per clock).
-// The running maximum is only raised when a row exceeds it by more than 2^8 (P <= 256 then loses nothing in bf16 and
-// the fp32 sums): O is rescaled in TMEM a few times per item instead of at every tile, by the softmax threads themselves.
-// Warps 0-3 and 4-7: softmax of stream 0 and 1; warp 8: MMA issue; warp 9: TMA; warps 10, 11 only make the launch a multiple of
-// a warpgroup.  Registers are split 208 / 88 by setmaxnreg (256 * 208 + 128 * 88 = 384 * 168, the launch's total).
+// 64-dimension half, into a ring of five 32 KB stages (K0 V0 K1 V1 ...), and are worked on in steps of 64.  Per step and query
+// tile s ("stream"):
+//   S = Q_s K^T       M = 128, N = 64, K = 128, into one of the stream's two buffers of 64 TMEM columns
+//   P = 2^(x - m)     one thread per row: a row's 64 logits are one thread's registers, so nothing is shuffled; P goes back as
+//                     bf16 over the columns S came from (the rounding tensor cores want; the sum l is of the unrounded values)
+//   O_s += P V        A = P from TMEM, V as it lies in memory ([keys][dims], MN-major B), into 128 TMEM columns
+// With two buffers a stream's logits are a step ahead of its softmax, so that the softmax threads do not wait for the tensor
+// cores (512 TMEM columns hold two streams' outputs and four 64-column buffers, or two of 128: with those the two took turns
+// and a pair of 128-key tiles took 3500 clocks).  N = 64 costs the first product half as much again (48 clocks for 32 of
+// arithmetic: A and B are read from shared memory at 128 bytes a clock), 2600 clocks per pair of 128-key tiles in all.
+// No maximum is taken per step.  Any reference m gives the same softmax, up to overflow: P, l and O are floating-point, and a
+// common factor costs none of their bits.  So a row keeps the reference of its first visible step, and the sums tell
+// whether an exponential left the range (2^64: then, and only then, the maximum is taken, O is rescaled in TMEM and
+// the step is done again).
+// Warps 0-3 and 4-7: softmax of stream 0 and 1; warps 8, 9: their MMAs; warp 10: TMA.
 // Every wait is bounded and reports CKV_ERR_TIMEOUT through the status word.
 #include "paged_work.cuh"
 #include "tc_ptx.cuh"
@@ -23,18 +26,18 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 384;
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+constexpr int kThreads = 352;
 constexpr int kStages = 5;
-constexpr int kTile = 128;
+constexpr int kTile = 128, kStep = 64;         // keys of a tile, and of a step
 constexpr uint32_t kHalf = 128 * 128;          // 128 rows x 64 bf16
 constexpr uint32_t kTileBytes = 2 * kHalf;
 constexpr int kInfo = 8;                       // ring of per-tile notes from the loader
-constexpr float kRaise = 8.0f;                 // how far (in powers of two) a row may exceed its reference before O is rescaled
-constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
-constexpr uint32_t kIdescPV = kIdescQK | (1u << 16);   // B (the values) is MN-major
+constexpr float kOverflow = 1.8446744e19f;     // 2^64: a step's sum above it is done again with a new reference
+constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);   // fp32 += bf16 * bf16, M = 128
+constexpr uint32_t kIdescQK = kIdesc | ((64u >> 3) << 17);
+constexpr uint32_t kIdescPV = kIdesc | ((128u >> 3) << 17) | (1u << 16);                // B (the values) is MN-major
 constexpr uint32_t kNegateA = 1u << 13;
-constexpr uint32_t kColS = 0, kColO = 256;     // TMEM columns: S_0, S_1, O_0, O_1
+constexpr uint32_t kColS = 0, kColO = 256;     // TMEM columns: two buffers of stream 0, of stream 1, O_0, O_1
 
 struct TcArgs {
   WorkArgs w;
@@ -58,7 +61,8 @@ struct __align__(1024) Smem {
   uint8_t q[2][kTileBytes];
   uint64_t full[kStages], empty[kStages];
   uint64_t q_full, q_empty;
-  uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t clean;                               // a value tile of a pair of streams has been looked at
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2];   // [stream][buffer]
   uint64_t join_full, join_done;                // stream 1's result is there; stream 0 has read it
   float2 other[kTile];                          // stream 1's maximum and sum per row
   uint32_t bad[kInfo];                          // which pages of a key tile are missing (bit per page)
@@ -145,11 +149,12 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
 
 // 0 * NaN is not 0: value rows that no query sees are zeroed, and so are rows with an infinity or a NaN that some of the
 // block's tokens do not see yet (the softmax threads add those to the tokens that do).
-__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Item& it, int j, uint32_t nv, uint32_t n_tiles, int lane) {
+__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Item& it, int j, uint32_t slot, uint32_t n_tiles,
+                                             int lane) {
   const int valid = it.visible - (it.t0 + j) * kTile, late = late_row(a, it, j);
   const uint32_t bad = *(volatile uint32_t*)&sm.bad[n_tiles % kInfo];
   if (valid < kTile || bad || late < kTile) {
-    uint4* v = reinterpret_cast<uint4*>(sm.kv[nv % kStages]);
+    uint4* v = reinterpret_cast<uint4*>(sm.kv[slot]);
     if (lane < 4) sm.odd[n_tiles % kInfo][lane] = 0u;
     __syncwarp();
     const int piece = (lane & 8) * (kTile) + (lane & 7);      // 16-byte piece lane & 15 of a row: its half, its place
@@ -175,106 +180,147 @@ __device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const It
   }
 }
 
-__device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int lane) {
+// Where the CTA is in the ring of stages.
+struct Ring {
+  uint32_t slot = 0, parity = 0;
+  __device__ __forceinline__ void step() {
+    if (++slot == kStages) slot = 0, parity ^= 1;
+  }
+};
+
+// The products of one stream, by a warp of its own.  A buffer's are issued in the order S, O, next S: the tensor pipe runs them
+// in that order, so S may take the columns that O reads P from without waiting for it.  Both streams' warps follow every
+// stage of the ring and give it back, whether they use it or not.
+__device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int s, int lane) {
   Walk k;
   k.start(a.w, sm.plan);
-  uint32_t n_use = 0, n_items = 0, n_tiles = 0, n_p[2] = {0, 0};
-  const uint32_t q_lo[2] = {desc_lo(smem_u32(sm.q[0]), 16), desc_lo(smem_u32(sm.q[1]), 16)};
-  const uint32_t kv0 = smem_u32(sm.kv[0]);
-  auto full = [&](uint32_t n) { return wait_warp(smem_u32(&sm.full[n % kStages]), (n / kStages) & 1, w, 3); };
-  auto release = [&](uint32_t n) {
-    if (elect()) tc_commit(smem_u32(&sm.empty[n % kStages]));
-  };
-  auto qk = [&](int s, int q_tile, uint32_t n) {   // S_s = Q K^T
-    if (elect()) {
-      const uint32_t b = desc_lo(kv0 + (n % kStages) * kTileBytes, 16);
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {   // 16 dimensions = 32 bytes of a 128-byte swizzled row; the second half is 16 KB on
-        const uint32_t off = (kk & 3) * 2 + (kk >> 2) * (kHalf >> 4);
-        mma_ss(tmem + kColS + s * 128, desc_of(q_lo[q_tile] + off), desc_of(b + off), a.idesc_qk, kk > 0);
-      }
-      tc_commit(smem_u32(&sm.s_full[s]));
-    }
-  };
-  auto pv = [&](int s, uint32_t n, bool accumulate) {   // O_s += P_s V, once P_s is there
-    if (!wait_warp(smem_u32(&sm.p_full[s]), n_p[s] & 1, w, 5)) return false;
-    ++n_p[s];
-    tc_fence_after();
-    if (elect()) {
-      const uint32_t b = desc_lo(kv0 + (n % kStages) * kTileBytes, kHalf);   // 64-dimension halves 16 KB apart
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)     // 16 keys = 16 rows of 128 bytes
-        mma_ts(tmem + kColO + s * 128, tmem + kColS + s * 128 + kk * 8, desc_of(b + kk * (2048 >> 4)), kIdescPV,
-               accumulate || kk > 0);
-      tc_commit(smem_u32(&sm.pv_done[s]));
-    }
-    return true;
-  };
-  // The products of one stream are issued in the order S(j), O(j), S(j + 1): the tensor pipe runs them in that order, so S(j + 1)
-  // may take the columns that O(j) reads P from without waiting for it.
+  uint32_t n_items = 0, n_tiles = 0, n_p = 0, n_clean = 0;
+  Ring ring;                              // of the next key tile to look at
+  const uint32_t kv0 = smem_u32(sm.kv[0]), full0 = smem_u32(&sm.full[0]), empty0 = smem_u32(&sm.empty[0]);
+  const uint32_t s_cols = tmem + kColS + s * 128, o_cols = tmem + kColO + s * 128;
+  const uint32_t bar_s = smem_u32(&sm.s_full[s][0]), bar_p = smem_u32(&sm.p_full[s][0]), bar_o = smem_u32(&sm.pv_done[s]);
+  auto full = [&](const Ring& r) { return wait_warp(full0 + r.slot * 8, r.parity, w, 3); };
   for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
     const bool pair = paired(it);
-    const int ahead = pair ? 1 : 2;      // a stream's next key tile
+    const int first = pair ? 0 : s, ahead = pair ? 1 : 2;      // the stream's first key tile, and the distance to its next
+    const uint32_t q_lo = desc_lo(smem_u32(sm.q[pair ? s : 0]), 16);
+    int j_clean = 0;                                           // first tile whose values have to be looked at
+    while (j_clean < n && late_row(a, it, j_clean) == kTile && it.visible - (it.t0 + j_clean) * kTile >= kTile) ++j_clean;
     if (!wait_warp(smem_u32(&sm.q_full), n_items & 1, w, 4)) return;
-    for (int j = 0; j < min(ahead, n); ++j) {
-      if (!full(n_use + 2 * j)) return;
+    auto qk = [&](uint32_t slot, int h, bool last) {   // S = Q K^T for half a tile
       tc_fence_after();
-      qk(j, 0, n_use + 2 * j);
-      if (pair) qk(1, 1, n_use + 2 * j);
-      release(n_use + 2 * j);
-      if (j == n - 1 && elect()) tc_commit(smem_u32(&sm.q_empty));
+      if (elect()) {
+        const uint32_t b = desc_lo(kv0 + slot * kTileBytes + h * (kStep * 128), 16);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {   // 16 dimensions = 32 bytes of a 128-byte swizzled row; the second half is 16 KB on
+          const uint32_t off = (kk & 3) * 2 + (kk >> 2) * (kHalf >> 4);
+          mma_ss(s_cols + h * kStep, desc_of(q_lo + off), desc_of(b + off), a.idesc_qk, kk > 0);
+        }
+        tc_commit(bar_s + h * 8);
+        if (h == 1) tc_commit(empty0 + slot * 8);
+        if (last) tc_commit(smem_u32(&sm.q_empty));
+      }
+    };
+    auto pass = [&](uint32_t slot) {            // a stage the stream has no use for
+      if (lane == 0) bar_arrive(empty0 + slot * 8);
+    };
+    if (n <= first && lane == 0) bar_arrive(smem_u32(&sm.q_empty));
+    // the stage of key tile j is looked at `ahead` tiles before the values of j are (two stages per tile: K, V)
+    Ring kr = ring;
+    for (int j = 0; j < min(ahead, n); ++j) {
+      if (!full(kr)) return;
+      if (j == first) qk(kr.slot, 0, false), qk(kr.slot, 1, j + ahead >= n);
+      else pass(kr.slot);
+      kr.step(), kr.step();
     }
     for (int j = 0; j < n; ++j, ++n_tiles) {
-      const uint32_t nv = n_use + 2 * j + 1, nk = n_use + 2 * (j + ahead);
-      const bool more = j + ahead < n;
-      if (!full(nv)) return;
-      clean_values(a, sm, it, j, nv, n_tiles, lane);
-      const int s = pair ? 0 : j & 1;
-      if (!pv(s, nv, j >= ahead)) return;
-      if (!pair) release(nv);
-      if (more) {
-        if (!full(nk)) return;
-        tc_fence_after();
-        qk(s, 0, nk);
-        if (!pair) release(nk);
+      Ring vr = ring;
+      vr.step();
+      ring = vr, ring.step();
+      const bool mine = pair || (j & 1) == s, more = j + ahead < n;
+      if (!full(vr)) return;
+      if (more && pair && !full(kr)) return;   // ahead of P, so that nothing stands between the two products
+      if (j >= j_clean || *(volatile uint32_t*)&sm.bad[n_tiles % kInfo]) {
+        if (pair ? s == 0 : mine) {
+          clean_values(a, sm, it, j, vr.slot, n_tiles, lane);
+          if (pair && lane == 0) bar_arrive(smem_u32(&sm.clean));
+        } else if (pair) {
+          if (!wait_warp(smem_u32(&sm.clean), n_clean & 1, w, 9)) return;
+        }
+        if (pair) ++n_clean;
       }
-      if (pair) {
-        if (!pv(1, nv, j > 0)) return;
-        release(nv);
+      if (mine) {
+        const uint32_t b = desc_lo(kv0 + vr.slot * kTileBytes, kHalf);   // 64-dimension halves 16 KB apart
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {     // O += P V for half a tile, then the buffer's next logits
+          if (!wait_warp(bar_p + h * 8, n_p & 1, w, 5)) return;
+          tc_fence_after();
+          if (elect()) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)     // 16 keys = 16 rows of 128 bytes = 8 columns
+              mma_ts(o_cols, s_cols + h * kStep + kk * 8, desc_of(b + (h * 4 + kk) * (2048 >> 4)), kIdescPV, j > first || h > 0 || kk > 0);
+            tc_commit(bar_o);
+            if (h == 1) tc_commit(empty0 + vr.slot * 8);
+          }
+          if (more && pair) qk(kr.slot, h, h == 1 && j + 2 >= n);
+        }
+        if (more && !pair) {   // the stage only comes free with the other stream's tile
+          if (!full(kr)) return;
+          qk(kr.slot, 0, false), qk(kr.slot, 1, j + 4 >= n);
+        }
+        ++n_p;
+      } else {
+        pass(vr.slot);
         if (more) {
-          qk(1, 1, nk);
-          release(nk);
+          if (!full(kr)) return;
+          pass(kr.slot);
         }
       }
-      if (more && j + ahead == n - 1 && elect()) tc_commit(smem_u32(&sm.q_empty));
+      if (more) kr.step(), kr.step();
     }
-    n_use += 2 * n;
     ++n_items;
   }
 }
 
-// The exponentials of one tile of one row, to TMEM as bf16; returns their sum.
-__device__ __forceinline__ float softmax_tile(float (&s)[kTile], float scale, float ref, uint32_t p_addr) {
-  uint64_t sum[4] = {0, 0, 0, 0};
+// The exponentials of a row's 64 logits, to TMEM as bf16; returns their sum.
+__device__ __forceinline__ float softmax_step(const uint32_t (&s)[kStep], float scale, float ref, uint32_t p_addr) {
+  uint64_t sum[2] = {0, 0};
   const uint64_t sc = pack2(scale, scale), mr = pack2(-ref, -ref);
+  uint32_t p[32];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    uint32_t p[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      float a, b;
-      unpack2(fma2(pack2(s[c * 64 + 2 * i], s[c * 64 + 2 * i + 1]), sc, mr), a, b);
-      a = ex2(a), b = ex2(b);
-      sum[i & 3] = add2(sum[i & 3], pack2(a, b));
-      p[i] = bf16x2(a, b);
-    }
-    tmem_st32(p_addr + c * 32, p);
+  for (int i = 0; i < 32; ++i) {
+    float a, b;
+    unpack2(fma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc, mr), a, b);
+    a = ex2(a), b = ex2(b);
+    sum[i & 1] = add2(sum[i & 1], pack2(a, b));
+    p[i] = bf16x2(a, b);
   }
+  tmem_st32(p_addr, p);
   float a, b;
-  unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), a, b);
+  unpack2(add2(sum[0], sum[1]), a, b);
   return a + b;
+}
+__device__ __forceinline__ float row_max(const uint32_t (&s)[kStep]) {
+  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < kStep; i += 8) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) mx[c] = max3(mx[c], __uint_as_float(s[i + 2 * c]), __uint_as_float(s[i + 2 * c + 1]));
+  }
+  return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+}
+__device__ __forceinline__ void scale_output(uint32_t o_addr, float f) {
+#pragma unroll 1
+  for (int c = 0; c < 8; ++c) {
+    uint32_t o[16];
+    tmem_ld16(o_addr + c * 16, o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+    tmem_st16(o_addr + c * 16, o);
+  }
+  tmem_wait_st();
 }
 
 // O += 2^(x - m) v for one cache row, with the logit from the rows as they lie in memory; rows of the tile that do
@@ -306,11 +352,11 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
                                              int lane) {
   Walk k;
   k.start(a.w, sm.plan);
-  uint32_t n_s = 0, n_all = 0, n_join = 0;   // tiles of this stream so far; key tiles of the CTA; joins of the streams
+  uint32_t n_s = 0, n_all = 0, n_join = 0;   // tiles of this stream so far; of the CTA; joins of the streams
   const int r = quarter * 32 + lane;                        // row of the query tile
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const uint32_t s_addr = tmem + lanes + kColS + stream * 128, o_addr = tmem + lanes + kColO + stream * 128;
-  const uint32_t bar_s = smem_u32(&sm.s_full[stream]), bar_p = smem_u32(&sm.p_full[stream]), bar_o = smem_u32(&sm.pv_done[stream]);
+  const uint32_t bar_s = smem_u32(&sm.s_full[stream][0]), bar_p = smem_u32(&sm.p_full[stream][0]), bar_o = smem_u32(&sm.pv_done[stream]);
   for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
@@ -322,55 +368,53 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     auto limit_of = [&](int tk) { return a.w.causal ? min(max(it.len - it.n + tk + 1, 0), it.len) : it.len; };
     const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
     float m = -INFINITY, l = 0.f;
+    bool open = true;                                         // some row of the warp has no reference yet
     for (int j = j0; j < n; j += step, ++n_s) {
-      const int key0 = (it.t0 + j) * kTile;
-      if (!wait_warp(bar_s, n_s & 1, w, 6)) return;
-      tc_fence_after();
-      uint32_t raw[kTile];
-      tmem_ld128(s_addr, raw);
-      float s[kTile];
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        const int key0 = (it.t0 + j) * kTile + h * kStep;
+        const uint32_t buf = s_addr + h * kStep;
+        if (!wait_warp(bar_s + h * 8, n_s & 1, w, 6)) return;
+        tc_fence_after();
+        uint32_t s[kStep];
+        tmem_ld64(buf, s);
+        const uint32_t bad = *(volatile uint32_t*)&sm.bad[(n_all + j) % kInfo];
+        if (key0 + kStep > least || bad) {
 #pragma unroll
-      for (int i = 0; i < kTile; ++i) s[i] = __uint_as_float(raw[i]);
-      const uint32_t bad = *(volatile uint32_t*)&sm.bad[(n_all + j) % kInfo];
-      if (key0 + kTile > least || bad) {
-#pragma unroll
-        for (int i = 0; i < kTile; ++i)
-          if (key0 + i >= limit || (bad >> (i >> a.w.log_p) & 1)) s[i] = -INFINITY;
-      }
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int i = 0; i < kTile; i += 8) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = max3(mx[c], s[i + 2 * c], s[i + 2 * c + 1]);
-      }
-      const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.x_scale;
-      const bool raise = top > m + kRaise;                    // the first visible key: m is -infinity
-      if (__any_sync(0xffffffffu, raise)) {
-        const float f = raise ? ex2(m - top) : 1.0f;
-        if (raise) m = top;
-        l *= f;
-        if (j > j0) {
-          if (!wait_warp(bar_o, (n_s - 1) & 1, w, 7)) return;
-          tc_fence_after();
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t o[32];
-            tmem_ld32(o_addr + c * 32, o);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(o_addr + c * 32, o);
+          for (int i = 0; i < kStep; ++i)
+            if (key0 + i >= limit || (bad >> ((h * kStep + i) >> a.w.log_p) & 1)) s[i] = 0xff800000u;
+        }
+        // Rows that have seen nothing yet take their reference here; what O holds for them is zero.
+        if (open) {
+          const float top = row_max(s) * a.x_scale;
+          if (m == -INFINITY) m = top;
+          open = __any_sync(0xffffffffu, m == -INFINITY);
+        }
+        // Done again with the row's maximum as the reference where the sum has left the range (once: logits past 2^30 differ
+        // from their own rounded maximum by more than that).
+        float sum;
+        for (int again = 0;; ++again) {
+          sum = softmax_step(s, a.x_scale, m == -INFINITY ? 0.f : m, buf);
+          if (again == 1 || !__any_sync(0xffffffffu, sum > kOverflow)) break;
+          const float top = fmaxf(m, row_max(s) * a.x_scale);
+          const float f = top == -INFINITY ? 1.0f : ex2(m - top);
+          m = top, l *= f;
+          if (j > j0 || h > 0) {   // steps are counted from the stream's first: this one is 2 n_s + h
+            if (!wait_warp(bar_o, (h + 1) & 1, w, 7)) return;
+            tc_fence_after();
+            scale_output(o_addr, f);
           }
         }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar_p + h * 8);
+        l += sum;
       }
-      l += softmax_tile(s, a.x_scale, m == -INFINITY ? 0.f : m, s_addr);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(bar_p);
     }
     // the item's output: normalised, or a partial result for the join
     if (j0 < n) {
-      if (!wait_warp(bar_o, (n_s - 1) & 1, w, 7)) return;
+      if (!wait_warp(bar_o, 0, w, 7) || !wait_warp(bar_o, 1, w, 7)) return;   // the last two steps, in order
       tc_fence_after();
     }
     // value rows that were left out because they are not finite, for the tokens that see them
@@ -469,10 +513,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) bar_init(smem_u32(&sm.full[i]), 1), bar_init(smem_u32(&sm.empty[i]), 1);
-    bar_init(smem_u32(&sm.q_full), 1), bar_init(smem_u32(&sm.q_empty), 1);
-    for (int s = 0; s < 2; ++s)
-      bar_init(smem_u32(&sm.s_full[s]), 1), bar_init(smem_u32(&sm.p_full[s]), 4), bar_init(smem_u32(&sm.pv_done[s]), 1);
+    for (int i = 0; i < kStages; ++i) bar_init(smem_u32(&sm.full[i]), 1), bar_init(smem_u32(&sm.empty[i]), 2);
+    bar_init(smem_u32(&sm.q_full), 1), bar_init(smem_u32(&sm.q_empty), 2), bar_init(smem_u32(&sm.clean), 1);
+    for (int s = 0; s < 2; ++s) {
+      bar_init(smem_u32(&sm.pv_done[s]), 1);
+      for (int b = 0; b < 2; ++b) bar_init(smem_u32(&sm.s_full[s][b]), 1), bar_init(smem_u32(&sm.p_full[s][b]), 4);
+    }
     bar_init(smem_u32(&sm.join_full), 4), bar_init(smem_u32(&sm.join_done), 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -487,14 +533,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   if (threadIdx.x == 0) a.w.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
   __syncthreads();
   const Waiter w{&sm.abort_flag, a.w.status, a.wait_ns};
-  if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    softmax_role(a, sm, tmem, w, warp >> 2, warp & 3, lane);
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 8) mma_role(a, sm, tmem, w, lane);
-    if (warp == 9) load_role(a, sm, &qm, &km, &vm, w, lane);
-  }
+  if (warp < 8) softmax_role(a, sm, tmem, w, warp >> 2, warp & 3, lane);
+  else if (warp < 10) mma_role(a, sm, tmem, w, warp - 8, lane);
+  else load_role(a, sm, &qm, &km, &vm, w, lane);
   tc_fence_before();
   __syncthreads();
   if (sm.abort_flag) {   // a wait gave up: let copies and products in flight land before the memory is given back
@@ -565,12 +606,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
     return cudaErrorInvalidValue;
   static PerDevice ready;
   cudaError_t e = ready.once([] {
-    cudaError_t r = cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
-    // setmaxnreg hands out what the launch holds: a build with fewer registers would wait for ever
-    cudaFuncAttributes attrs;
-    if (r == cudaSuccess) r = cudaFuncGetAttributes(&attrs, attend_tc_kernel);
-    if (r == cudaSuccess && attrs.numRegs * kThreads < kSoftmaxRegs * 256 + kOtherRegs * 128) r = cudaErrorLaunchOutOfResources;
-    return r;
+    return cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
