@@ -61,8 +61,8 @@ struct __align__(1024) Smem {
   uint8_t q[2][kTileBytes];
   uint64_t full[kStages], empty[kStages];
   uint64_t q_full, q_empty;
-  uint64_t clean;                               // a value tile of a pair of streams has been looked at
-  uint64_t s_full[2][2], p_full[2][2], pv_done[2];   // [stream][buffer]
+  uint64_t clean;                               // a value tile has been looked at
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2], item_done[2];   // [stream][buffer]
   uint64_t join_full, join_done;                // stream 1's result is there; stream 0 has read it
   float2 other[kTile];                          // stream 1's maximum and sum per row
   uint32_t bad[kInfo];                          // which pages of a key tile are missing (bit per page)
@@ -84,8 +84,8 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
   return __all_sync(0xffffffffu, bar_wait(bar, parity, w, code));
 }
 
-// How an item is cut up.  Two query tiles: each stream has one, and takes every key tile.  One query tile (the tokens
-// fill no more than half of the block): both streams work on it, on every other key tile, and join at the end.
+// How an item is cut up.  Two query tiles: each stream has one, and takes both halves of every key tile.  One query tile (the
+// tokens fill no more than half of the block): both streams work on it, each on its half of every key tile, and join at the end.
 __device__ __forceinline__ bool paired(const Item& it) { return it.weight == 2; }
 
 // First row of the item's j-th key tile that the block's first token does not see (128: it sees them all).  Where every
@@ -114,11 +114,14 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
       tma_load_4d(qm, smem_u32(&sm.q[lane >> 1][(lane & 1) * kHalf]), smem_u32(&sm.q_full), 0, it.g * a.w.G,
                   it.first + it.block * a.w.tokens + (lane >> 1) * a.TQ, lane & 1);
     const int32_t* table = a.w.table + ((int64_t)it.u * a.w.Hkv + it.g) * a.w.max_pages;
+    // the pages that hold visible rows of a tile, looked up a tile ahead
+    auto row_of = [&](int t) { return t * kTile + slot_of_lane * (a.w.P < kTile ? a.w.P : kTile); };
+    auto wants = [&](int t) { return copies && t < it.t1 && row_of(t) < it.visible; };
+    int next_page = wants(it.t0) ? table[row_of(it.t0) >> a.w.log_p] : 0;
     for (int t = it.t0; t < it.t1; ++t, ++n_tiles) {
-      // the pages of this tile that hold visible rows
-      const int first_row = t * kTile + slot_of_lane * (a.w.P < kTile ? a.w.P : kTile);
-      const bool wanted = copies && first_row < it.visible;
-      const int page = wanted ? table[first_row >> a.w.log_p] : 0;
+      const bool wanted = wants(t);
+      const int page = next_page;
+      if (wants(t + 1)) next_page = table[row_of(t + 1) >> a.w.log_p];
       const bool fine = (unsigned)page < (unsigned)a.w.n_pages;
       if (wanted && !fine && half == 0) report_status(a.w.status, kStatusPage);
       const bool copy = wanted && fine;
@@ -188,98 +191,81 @@ struct Ring {
   }
 };
 
-// The products of one stream, by a warp of its own.  A buffer's are issued in the order S, O, next S: the tensor pipe runs them
-// in that order, so S may take the columns that O reads P from without waiting for it.  Both streams' warps follow every
-// stage of the ring and give it back, whether they use it or not.
+// The products of one stream, by a warp of its own, step by step (64 keys) through two buffers.  A buffer's are issued in the
+// order S, O, next S: the tensor pipe runs them in that order, so S may take the columns that O reads P from without
+// waiting for it.
 __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int s, int lane) {
   Walk k;
   k.start(a.w, sm.plan);
-  uint32_t n_items = 0, n_tiles = 0, n_p = 0, n_clean = 0;
-  Ring ring;                              // of the next key tile to look at
+  uint32_t n_items = 0, n_tiles = 0, n_steps = 0, n_clean = 0;
+  Ring ring;                              // of the item's first key tile; two stages per tile: K, V
   const uint32_t kv0 = smem_u32(sm.kv[0]), full0 = smem_u32(&sm.full[0]), empty0 = smem_u32(&sm.empty[0]);
   const uint32_t s_cols = tmem + kColS + s * 128, o_cols = tmem + kColO + s * 128;
-  const uint32_t bar_s = smem_u32(&sm.s_full[s][0]), bar_p = smem_u32(&sm.p_full[s][0]), bar_o = smem_u32(&sm.pv_done[s]);
-  auto full = [&](const Ring& r) { return wait_warp(full0 + r.slot * 8, r.parity, w, 3); };
+  const uint32_t bar_s = smem_u32(&sm.s_full[s][0]), bar_p = smem_u32(&sm.p_full[s][0]);
+  const uint32_t bar_o = smem_u32(&sm.pv_done[s]), bar_item = smem_u32(&sm.item_done[s]);
   for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
     const bool pair = paired(it);
-    const int first = pair ? 0 : s, ahead = pair ? 1 : 2;      // the stream's first key tile, and the distance to its next
+    const int steps = pair ? 2 * n : n;
     const uint32_t q_lo = desc_lo(smem_u32(sm.q[pair ? s : 0]), 16);
     int j_clean = 0;                                           // first tile whose values have to be looked at
     while (j_clean < n && late_row(a, it, j_clean) == kTile && it.visible - (it.t0 + j_clean) * kTile >= kTile) ++j_clean;
     if (!wait_warp(smem_u32(&sm.q_full), n_items & 1, w, 4)) return;
-    auto qk = [&](uint32_t slot, int h, bool last) {   // S = Q K^T for half a tile
+    Ring kr = ring, vr = ring;
+    vr.step();
+    auto qk = [&](int g) {   // S = Q K^T of step g
+      const int h = pair ? g & 1 : s;                          // which half of the tile's keys
+      if ((!pair || h == 0) && !wait_warp(full0 + kr.slot * 8, kr.parity, w, 3)) return false;
       tc_fence_after();
+      const uint32_t buf = (n_steps + g) & 1;
       if (elect()) {
-        const uint32_t b = desc_lo(kv0 + slot * kTileBytes + h * (kStep * 128), 16);
+        const uint32_t b = desc_lo(kv0 + kr.slot * kTileBytes + h * (kStep * 128), 16);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {   // 16 dimensions = 32 bytes of a 128-byte swizzled row; the second half is 16 KB on
           const uint32_t off = (kk & 3) * 2 + (kk >> 2) * (kHalf >> 4);
-          mma_ss(s_cols + h * kStep, desc_of(q_lo + off), desc_of(b + off), a.idesc_qk, kk > 0);
+          mma_ss(s_cols + buf * kStep, desc_of(q_lo + off), desc_of(b + off), a.idesc_qk, kk > 0);
         }
-        tc_commit(bar_s + h * 8);
-        if (h == 1) tc_commit(empty0 + slot * 8);
-        if (last) tc_commit(smem_u32(&sm.q_empty));
+        tc_commit(bar_s + buf * 8);
+        if (!pair || h == 1) tc_commit(empty0 + kr.slot * 8);
+        if (g == steps - 1) tc_commit(smem_u32(&sm.q_empty));
       }
+      if (!pair || h == 1) kr.step(), kr.step();
+      return true;
     };
-    auto pass = [&](uint32_t slot) {            // a stage the stream has no use for
-      if (lane == 0) bar_arrive(empty0 + slot * 8);
-    };
-    if (n <= first && lane == 0) bar_arrive(smem_u32(&sm.q_empty));
-    // the stage of key tile j is looked at `ahead` tiles before the values of j are (two stages per tile: K, V)
-    Ring kr = ring;
-    for (int j = 0; j < min(ahead, n); ++j) {
-      if (!full(kr)) return;
-      if (j == first) qk(kr.slot, 0, false), qk(kr.slot, 1, j + ahead >= n);
-      else pass(kr.slot);
-      kr.step(), kr.step();
-    }
-    for (int j = 0; j < n; ++j, ++n_tiles) {
-      Ring vr = ring;
-      vr.step();
-      ring = vr, ring.step();
-      const bool mine = pair || (j & 1) == s, more = j + ahead < n;
-      if (!full(vr)) return;
-      if (more && pair && !full(kr)) return;   // ahead of P, so that nothing stands between the two products
-      if (j >= j_clean || *(volatile uint32_t*)&sm.bad[n_tiles % kInfo]) {
-        if (pair ? s == 0 : mine) {
-          clean_values(a, sm, it, j, vr.slot, n_tiles, lane);
-          if (pair && lane == 0) bar_arrive(smem_u32(&sm.clean));
-        } else if (pair) {
-          if (!wait_warp(smem_u32(&sm.clean), n_clean & 1, w, 9)) return;
-        }
-        if (pair) ++n_clean;
-      }
-      if (mine) {
-        const uint32_t b = desc_lo(kv0 + vr.slot * kTileBytes, kHalf);   // 64-dimension halves 16 KB apart
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {     // O += P V for half a tile, then the buffer's next logits
-          if (!wait_warp(bar_p + h * 8, n_p & 1, w, 5)) return;
-          tc_fence_after();
-          if (elect()) {
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)     // 16 keys = 16 rows of 128 bytes = 8 columns
-              mma_ts(o_cols, s_cols + h * kStep + kk * 8, desc_of(b + (h * 4 + kk) * (2048 >> 4)), kIdescPV, j > first || h > 0 || kk > 0);
-            tc_commit(bar_o);
-            if (h == 1) tc_commit(empty0 + vr.slot * 8);
+    if (!qk(0) || (steps > 1 && !qk(1))) return;
+    for (int g = 0; g < steps; ++g) {
+      const int h = pair ? g & 1 : s, j = pair ? g >> 1 : g;
+      if (!pair || h == 0) {   // a new tile of values
+        if (!wait_warp(full0 + vr.slot * 8, vr.parity, w, 3)) return;
+        if (j >= j_clean || *(volatile uint32_t*)&sm.bad[n_tiles % kInfo]) {
+          if (s == 0) {
+            clean_values(a, sm, it, j, vr.slot, n_tiles, lane);
+            if (lane == 0) bar_arrive(smem_u32(&sm.clean));
+          } else if (!wait_warp(smem_u32(&sm.clean), n_clean & 1, w, 9)) {
+            return;
           }
-          if (more && pair) qk(kr.slot, h, h == 1 && j + 2 >= n);
+          ++n_clean;
         }
-        if (more && !pair) {   // the stage only comes free with the other stream's tile
-          if (!full(kr)) return;
-          qk(kr.slot, 0, false), qk(kr.slot, 1, j + 4 >= n);
-        }
-        ++n_p;
-      } else {
-        pass(vr.slot);
-        if (more) {
-          if (!full(kr)) return;
-          pass(kr.slot);
-        }
+        ++n_tiles;
       }
-      if (more) kr.step(), kr.step();
+      const uint32_t step = n_steps + g, buf = step & 1;
+      if (!wait_warp(bar_p + buf * 8, (step >> 1) & 1, w, 5)) return;
+      tc_fence_after();
+      if (elect()) {           // O += P V
+        const uint32_t b = desc_lo(kv0 + vr.slot * kTileBytes, kHalf) + h * 4 * (2048 >> 4);   // 64-dimension halves 16 KB apart
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)     // 16 keys = 16 rows of 128 bytes = 8 columns
+          mma_ts(o_cols, s_cols + buf * kStep + kk * 8, desc_of(b + kk * (2048 >> 4)), kIdescPV, g > 0 || kk > 0);
+        tc_commit(bar_o);
+        if (!pair || h == 1) tc_commit(empty0 + vr.slot * 8);
+        if (g == steps - 1) tc_commit(bar_item);
+      }
+      if (!pair || h == 1) vr.step(), vr.step();
+      if (g + 2 < steps && !qk(g + 2)) return;
     }
+    n_steps += steps;
+    ring = kr;
     ++n_items;
   }
 }
@@ -352,7 +338,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
                                              int lane) {
   Walk k;
   k.start(a.w, sm.plan);
-  uint32_t n_s = 0, n_all = 0, n_join = 0;   // tiles of this stream so far; of the CTA; joins of the streams
+  uint32_t n_steps = 0, n_all = 0, n_items = 0, n_join = 0;   // steps of this stream so far; tiles, items; joins of the streams
   const int r = quarter * 32 + lane;                        // row of the query tile
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const uint32_t s_addr = tmem + lanes + kColS + stream * 128, o_addr = tmem + lanes + kColO + stream * 128;
@@ -361,7 +347,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
     const bool pair = paired(it);
-    const int j0 = pair ? 0 : stream, step = pair ? 1 : 2, q_tile = pair ? stream : 0;
+    const int steps = pair ? 2 * n : n, q_tile = pair ? stream : 0;
     const int tok0 = it.block * a.w.tokens + q_tile * a.TQ;   // first token of the tile
     const int token = tok0 + r / a.w.G;
     const bool live = r < a.TQ * a.w.G && token < it.n;
@@ -369,58 +355,55 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
     float m = -INFINITY, l = 0.f;
     bool open = true;                                         // some row of the warp has no reference yet
-    for (int j = j0; j < n; j += step, ++n_s) {
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
-        const int key0 = (it.t0 + j) * kTile + h * kStep;
-        const uint32_t buf = s_addr + h * kStep;
-        if (!wait_warp(bar_s + h * 8, n_s & 1, w, 6)) return;
-        tc_fence_after();
-        uint32_t s[kStep];
-        tmem_ld64(buf, s);
-        const uint32_t bad = *(volatile uint32_t*)&sm.bad[(n_all + j) % kInfo];
-        if (key0 + kStep > least || bad) {
+    for (int g = 0; g < steps; ++g, ++n_steps) {
+      const int j = pair ? g >> 1 : g, h = pair ? g & 1 : stream;
+      const int key0 = (it.t0 + j) * kTile + h * kStep;
+      const uint32_t buf = n_steps & 1, s_buf = s_addr + buf * kStep;
+      if (!wait_warp(bar_s + buf * 8, (n_steps >> 1) & 1, w, 6)) return;
+      tc_fence_after();
+      uint32_t s[kStep];
+      tmem_ld64(s_buf, s);
+      const uint32_t bad = *(volatile uint32_t*)&sm.bad[(n_all + j) % kInfo];
+      if (key0 + kStep > least || bad) {
 #pragma unroll
-          for (int i = 0; i < kStep; ++i)
-            if (key0 + i >= limit || (bad >> ((h * kStep + i) >> a.w.log_p) & 1)) s[i] = 0xff800000u;
-        }
-        // Rows that have seen nothing yet take their reference here; what O holds for them is zero.
-        if (open) {
-          const float top = row_max(s) * a.x_scale;
-          if (m == -INFINITY) m = top;
-          open = __any_sync(0xffffffffu, m == -INFINITY);
-        }
-        // Done again with the row's maximum as the reference where the sum has left the range (once: logits past 2^30 differ
-        // from their own rounded maximum by more than that).
-        float sum;
-        for (int again = 0;; ++again) {
-          sum = softmax_step(s, a.x_scale, m == -INFINITY ? 0.f : m, buf);
-          if (again == 1 || !__any_sync(0xffffffffu, sum > kOverflow)) break;
-          const float top = fmaxf(m, row_max(s) * a.x_scale);
-          const float f = top == -INFINITY ? 1.0f : ex2(m - top);
-          m = top, l *= f;
-          if (j > j0 || h > 0) {   // steps are counted from the stream's first: this one is 2 n_s + h
-            if (!wait_warp(bar_o, (h + 1) & 1, w, 7)) return;
-            tc_fence_after();
-            scale_output(o_addr, f);
-          }
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(bar_p + h * 8);
-        l += sum;
+        for (int i = 0; i < kStep; ++i)
+          if (key0 + i >= limit || (bad >> ((h * kStep + i) >> a.w.log_p) & 1)) s[i] = 0xff800000u;
       }
+      // Rows that have seen nothing yet take their reference here; what O holds for them is zero.
+      if (open) {
+        const float top = row_max(s) * a.x_scale;
+        if (m == -INFINITY) m = top;
+        open = __any_sync(0xffffffffu, m == -INFINITY);
+      }
+      // Done again with the row's maximum as the reference where the sum has left the range (once: logits past 2^30 differ
+      // from their own rounded maximum by more than that).
+      float sum;
+      for (int again = 0;; ++again) {
+        sum = softmax_step(s, a.x_scale, m == -INFINITY ? 0.f : m, s_buf);
+        if (again == 1 || !__any_sync(0xffffffffu, sum > kOverflow)) break;
+        const float top = fmaxf(m, row_max(s) * a.x_scale);
+        const float f = top == -INFINITY ? 1.0f : ex2(m - top);
+        m = top, l *= f;
+        if (g > 0) {   // the product of the step before; the one before that is done, or S would not be here
+          if (!wait_warp(bar_o, (n_steps - 1) & 1, w, 7)) return;
+          tc_fence_after();
+          scale_output(o_addr, f);
+        }
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar_p + buf * 8);
+      l += sum;
     }
     // the item's output: normalised, or a partial result for the join
-    if (j0 < n) {
-      if (!wait_warp(bar_o, 0, w, 7) || !wait_warp(bar_o, 1, w, 7)) return;   // the last two steps, in order
-      tc_fence_after();
-    }
+    if (!wait_warp(smem_u32(&sm.item_done[stream]), n_items & 1, w, 7)) return;
+    ++n_items;
+    tc_fence_after();
     // value rows that were left out because they are not finite, for the tokens that see them
     for (int j = n - 1; j >= 0 && late_row(a, it, j) < kTile; --j) {
-      if (!pair && (j & 1) != stream) continue;
-      for (int x = 0; x < 4; ++x) {
+      for (int x = pair ? 0 : 2 * stream; x < (pair ? 4 : 2 * stream + 2); ++x) {   // the stream's keys
         uint32_t odd = *(volatile uint32_t*)&sm.odd[(n_all + j) % kInfo][x];
         for (; odd; odd &= odd - 1) add_row(a, it, o_addr, (it.t0 + j) * kTile + x * 32 + __ffs(odd) - 1, limit, token, r % a.w.G, m);
       }
@@ -428,7 +411,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     n_all += n;
     // one query tile: stream 1 leaves its maximum and sum, stream 0 takes its output from TMEM (the same lanes, other columns)
     float f0 = 1.0f, f1 = 0.f;
-    if (!pair && n > 1) {
+    if (!pair) {
       if (stream == 1) {
         sm.other[r] = make_float2(m, l);
         tc_fence_before();
@@ -446,10 +429,8 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
       f0 = ex2(m - ref), f1 = ex2(x.x - ref);
       l = l * f0 + x.y * f1, m = top;
-    } else if (!pair && stream == 1) {
-      continue;
     }
-    const bool joined = !pair && n > 1;
+    const bool joined = !pair;
     const bool whole = it.t0 == 0 && it.t1 == it.tiles;
     const int which = it.t0 > 0 ? 0 : 1;
     const int br = q_tile * a.TQ * a.w.G + r;                // row of the block
@@ -516,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     for (int i = 0; i < kStages; ++i) bar_init(smem_u32(&sm.full[i]), 1), bar_init(smem_u32(&sm.empty[i]), 2);
     bar_init(smem_u32(&sm.q_full), 1), bar_init(smem_u32(&sm.q_empty), 2), bar_init(smem_u32(&sm.clean), 1);
     for (int s = 0; s < 2; ++s) {
-      bar_init(smem_u32(&sm.pv_done[s]), 1);
+      bar_init(smem_u32(&sm.pv_done[s]), 1), bar_init(smem_u32(&sm.item_done[s]), 1);
       for (int b = 0; b < 2; ++b) bar_init(smem_u32(&sm.s_full[s][b]), 1), bar_init(smem_u32(&sm.p_full[s][b]), 4);
     }
     bar_init(smem_u32(&sm.join_full), 4), bar_init(smem_u32(&sm.join_done), 4);
