@@ -189,7 +189,7 @@ ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k
   CKV_TRY(check_pages(paged));
   CKV_TRY(check_paged_ws(paged_ws(*paged).total, ws, ws_bytes));
   if (paged->n_tokens == 0) return CKV_OK;
-  if (!good({q, k_pages, v_pages, out}, 16) || !good({page_table, lengths, token_starts}, 4)) return CKV_ERR_INVALID_ARG;
+  if (!good({q, k_pages, v_pages}, 16) || !good({out}, 32) || !good({page_table, lengths, token_starts}, 4)) return CKV_ERR_INVALID_ARG;
   if (lse_or_null && !aligned(lse_or_null, 4)) return CKV_ERR_INVALID_ARG;
   if (!token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, paged->n_q_heads)) return CKV_ERR_INVALID_ARG;
   const int64_t T = paged->n_tokens, H = paged->n_q_heads, e = esize(*paged);

@@ -171,35 +171,41 @@ constexpr int kJoinRows = 8;
 template <bool BF16>
 __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int workers, void* __restrict__ out,
                                                               float* __restrict__ lse) {
+  const int w = blockIdx.x, lane = threadIdx.x & 31;
+  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), d = lane * 4;   // a warp per row
   pdl_wait();
-  const int w = blockIdx.x;
+  // Who has a part, the first part and the three after it (which may turn out to be none of ours, but are there to be read): where
+  // blocks are small all of it is asked for at once, where they are large only what is used.
+  constexpr int kBatch = 4;
+  const bool early = gridDim.y <= 4;
+  const int4 next = w + 1 + lane < workers ? a.split[w + 1 + lane] : make_int4(-1, -1, -1, -1);
   const int4 mine = a.split[w];
-  if (mine.z < 0) return;
-  const Item it = make_item(a, mine.z, mine.w, 0, 1ll << 40);
-  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), d = (threadIdx.x & 31) * 4;   // a warp per row
-  if (r >= block_rows(a, it)) return;
-  // the workers after w that have a part: the lanes look at 32 of them at once
-  const int lane = threadIdx.x & 31;
-  int parts = 0;
-  for (int w0 = w + 1;; w0 += 32) {
-    const int x = w0 + lane;
-    const int4 s = x < workers ? a.split[x] : make_int4(-1, -1, -1, -1);
-    const unsigned no = ~__ballot_sync(0xffffffffu, s.x == mine.z && s.y == mine.w);
-    parts += no ? __ffs(no) - 1 : 32;
-    if (no) break;
-  }
-  float2 ml = a.ml[((int64_t)w * 2 + 1) * a.slot_rows + r];
-  float4 o = *reinterpret_cast<const float4*>(a.o + (((int64_t)w * 2 + 1) * a.slot_rows + r) * kHeadDim + d);
-  constexpr int kBatch = 4;                       // parts in flight
-  for (int p0 = 1; p0 <= parts; p0 += kBatch) {
-    float2 x[kBatch];
-    float4 y[kBatch];
+  auto slot_of = [&](int part) { return (int64_t)(part == 0 ? w * 2 + 1 : min(w + part, workers - 1) * 2) * a.slot_rows + r; };
+  float2 x[kBatch];
+  float4 y[kBatch];
+  auto fetch = [&](int p0, int last) {
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      const int64_t slot = (int64_t)(w + min(p0 + b, parts)) * 2 * a.slot_rows + r;
+      const int64_t slot = slot_of(min(p0 + b, last));
       x[b] = a.ml[slot];
       y[b] = *reinterpret_cast<const float4*>(a.o + slot * kHeadDim + d);
     }
+  };
+  if (early && r < a.slot_rows) fetch(0, kBatch);
+  if (mine.z < 0) return;
+  const Item it = make_item(a, mine.z, mine.w, 0, 1ll << 40);
+  if (r >= block_rows(a, it)) return;
+  unsigned no = ~__ballot_sync(0xffffffffu, next.x == mine.z && next.y == mine.w);
+  int parts = no ? __ffs(no) - 1 : 32;            // workers after w that have one
+  for (int w0 = w + 33; !no; w0 += 32) {
+    const int4 s = w0 + lane < workers ? a.split[w0 + lane] : make_int4(-1, -1, -1, -1);
+    no = ~__ballot_sync(0xffffffffu, s.x == mine.z && s.y == mine.w);
+    parts += no ? __ffs(no) - 1 : 32;
+  }
+  if (!early) fetch(0, parts);
+  float2 ml = make_float2(-INFINITY, 0.f);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 <= parts; p0 += kBatch) {
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
       if (p0 + b > parts) break;
@@ -208,10 +214,12 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int wo
       ml = make_float2(top, ml.y * ca + x[b].y * cb);
       o.x = o.x * ca + y[b].x * cb, o.y = o.y * ca + y[b].y * cb, o.z = o.z * ca + y[b].z * cb, o.w = o.w * ca + y[b].w * cb;
     }
+    if (p0 + kBatch <= parts) fetch(p0 + kBatch, parts);
   }
   const bool none = ml.x == -INFINITY;
   const float inv = none ? 0.f : 1.0f / ml.y;
   const int64_t at = out_row(a, it, r);
+  if (none) o = make_float4(0.f, 0.f, 0.f, 0.f);   // a part that saw nothing may hold anything times zero
   if (BF16) {
     const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
     const uint2 v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
@@ -232,9 +240,9 @@ int log2_of(int p) {
 }  // namespace
 
 template <bool BF16>
-cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, cudaStream_t st) {
+cudaError_t launch_join(const WorkArgs& a, int workers, int rows, void* out, float* lse, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(workers, (a.slot_rows + kJoinRows - 1) / kJoinRows), cfg.blockDim = dim3(32 * kJoinRows), cfg.stream = st;
+  cfg.gridDim = dim3(workers, (rows + kJoinRows - 1) / kJoinRows), cfg.blockDim = dim3(32 * kJoinRows), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel<BF16>, a, workers, out, lse);
@@ -242,14 +250,16 @@ cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, c
   return e;
 }
 
-template cudaError_t launch_join<true>(const WorkArgs&, int, void*, float*, cudaStream_t);
-template cudaError_t launch_join<false>(const WorkArgs&, int, void*, float*, cudaStream_t);
+template cudaError_t launch_join<true>(const WorkArgs&, int, int, void*, float*, cudaStream_t);
+template cudaError_t launch_join<false>(const WorkArgs&, int, int, void*, float*, cudaStream_t);
 
-// Up to this many query rows per KV head in every unit, the call goes to the kernel for few rows, else to the tensor cores.
-constexpr int kFewRows = 32;
+// bf16 calls go to the kernel for few rows while every unit has at most so many query rows per KV head, else to the tensor
+// cores: with 16 rows a long cache streams at the memory's rate, with 32 the matrix instructions of that kernel take longer
+// than the bytes; a short cache is all latency, where it stays ahead for longer.
+constexpr int kFewRows = 16, kFewRowsShort = 32;
 static bool wants_tc(const ckv_paged& pg) {
   const int64_t G = pg.n_q_heads / pg.n_kv_heads, most = pg.max_new > 0 ? pg.max_new : pg.n_tokens;
-  return pg.dtype == CKV_BF16 && G <= 128 && most * G > kFewRows;
+  return pg.dtype == CKV_BF16 && G <= 128 && most * G > (mma_cluster(pg) ? kFewRowsShort : kFewRows);
 }
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -294,7 +304,7 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   cudaError_t e = cudaLaunchKernelEx(&cfg, attend_rows_kernel, a, pg, scale * kLog2e, (const char*)q, (const char*)k_pages,
                                      (const char*)v_pages, (float*)out, lse);
   count_launch();
-  if (e == cudaSuccess) e = launch_join<false>(a, kWorkers, out, lse, st);
+  if (e == cudaSuccess) e = launch_join<false>(a, kWorkers, kRowsM, out, lse, st);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -384,28 +384,30 @@ cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, int grid, int n_cta, 
 
 }  // namespace
 
+// Short caches go to clusters: as many CTAs per head as the heads leave room for, as long as each has keys to read and none has
+// more than kClusterRows.  0: the cache is not short.
+int mma_cluster(const ckv_paged& pg) {
+  const int64_t pairs = (int64_t)pg.n_units * pg.n_kv_heads, capacity = (int64_t)pg.max_pages * pg.page_size;
+  int n_cta = 1;
+  while (n_cta < 8 && pairs * n_cta * 2 <= kWorkers && n_cta * kCtaKeys < capacity) n_cta *= 2;
+  return capacity <= (int64_t)n_cta * kClusterRows ? n_cta : 0;
+}
+
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st) {
   WorkArgs a = base;
   a.tokens = 0, a.tile = kMmaTile, a.granule = 2;
   a.M = rows <= 16 ? 16 : 32;
   const float x_scale = scale * kLog2e;
-  // Short caches go to clusters: as many CTAs per head as the heads leave room for, as long as each has rows to read and none has
-  // more than kClusterRows.
-  const int64_t pairs = (int64_t)a.Nu * a.Hkv, capacity = (int64_t)a.max_pages * a.P;
-  int n_cta = 1;
-  while (n_cta < 8 && pairs * n_cta * 2 <= kWorkers && n_cta * kCtaKeys < capacity) n_cta *= 2;
-  cudaError_t e;
-  if (capacity <= (int64_t)n_cta * kClusterRows) {
-    int64_t clusters = 2 * kWorkers / n_cta;
-    if (pairs < clusters) clusters = pairs;
-    const int grid = (int)clusters * n_cta;
+  if (const int n_cta = mma_cluster(pg)) {
+    const int64_t pairs = (int64_t)a.Nu * a.Hkv, most = 2 * kWorkers / n_cta;
+    const int grid = (int)(pairs < most ? pairs : most) * n_cta;
     return rows <= 16 ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
                       : launch<2, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st);
   }
-  e = rows <= 16 ? launch<1, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
-                 : launch<2, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st);
-  return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, out, lse, st);
+  const cudaError_t e = rows <= 16 ? launch<1, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
+                                   : launch<2, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st);
+  return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, a.M, out, lse, st);
 }
 
 }  // namespace ckv

@@ -450,19 +450,22 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       }
       if (!live) continue;
       if (whole) {
-        uint4* dst = reinterpret_cast<uint4*>(a.out + at * kHeadDim + c * 32);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t p[4];
+        for (int i = 0; i < 2; ++i) {
+          uint32_t p[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            p[e] = bf16x2(none ? 0.f : __uint_as_float(o[8 * i + 2 * e]) * inv, none ? 0.f : __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
-          dst[i] = make_uint4(p[0], p[1], p[2], p[3]);
+          for (int e = 0; e < 8; ++e)
+            p[e] = none ? 0u : bf16x2(__uint_as_float(o[16 * i + 2 * e]) * inv, __uint_as_float(o[16 * i + 2 * e + 1]) * inv);
+          st_global32(a.out + at * kHeadDim + c * 32 + i * 16, p);
         }
       } else {
-        uint4* dst = reinterpret_cast<uint4*>(a.w.o + slot * kHeadDim + c * 32);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = o[8 * i + e];
+          st_global32(a.w.o + slot * kHeadDim + c * 32 + i * 8, p);
+        }
       }
     }
     if (live) {
@@ -505,6 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     fence_async_smem();
     sm.abort_flag = 0;
   }
+  if (warp == 10 && lane == 0) prefetch_map(&qm), prefetch_map(&km), prefetch_map(&vm);
   tc_fence_before();
   pdl_wait();
   make_plan<kThreads>(a.w, blockIdx.x, gridDim.x, sm.plan);
@@ -596,7 +600,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   cfg.attrs = &attr, cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, attend_tc_kernel, qm, km, vm, a);
   count_launch();
-  return e != cudaSuccess ? e : launch_join<true>(a.w, kWorkers, out, lse, st);
+  return e != cudaSuccess ? e : launch_join<true>(a.w, kWorkers, a.w.M, out, lse, st);
 }
 
 }  // namespace ckv

@@ -65,25 +65,91 @@ struct Plan {           // in shared memory
   int pair, block;      // that item
 };
 
-// All threads of the CTA.  Returns with the worker's share in `plan`.
+__device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p) {
+  int first, n;
+  unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
+  const int len = head_length(a, p), nb = unit_blocks(a, n);
+  long long c = 0;
+  for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
+  return c;
+}
+// The share [begin, end) of a worker.
+__device__ __forceinline__ void share_of(const WorkArgs& a, long long total, int worker, int n_workers, long long& begin,
+                                         long long& end) {
+  // rounded down: every share is at least `granule` >= 2 wide, so that a tile begins in each (the join follows an item from one
+  // worker to the next and stops at the first that has no part in it)
+  const long long most = max(total / a.granule, 1ll);
+  const int workers = (int)(most < n_workers ? most : n_workers);
+  begin = end = total;
+  if (worker < workers) {
+    if (total < (1 << 24)) {   // 32-bit divisions where they do: the plan is all latency
+      begin = (unsigned)total * (unsigned)worker / (unsigned)workers;
+      end = (unsigned)total * (unsigned)(worker + 1) / (unsigned)workers;
+    } else {
+      begin = total * worker / workers, end = total * (worker + 1) / workers;
+    }
+  }
+}
+// Where in pair p's cost offset `at` falls, for a share of `width`.
+__device__ __forceinline__ void settle_plan(const WorkArgs& a, int p, long long at, long long width, Plan& plan) {
+  int first, n, b = 0;
+  unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
+  const int len = head_length(a, p);
+  for (;; ++b) {
+    const int t = tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
+    if (at < t) break;
+    at -= t;
+  }
+  plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + width;
+}
+
+// All threads of the CTA.  Returns with the worker's share in `plan`.  Up to kWarpPairs (unit, KV head) pairs one warp does it
+// alone, without barriers; beyond, every thread has its pairs.
+constexpr int kWarpPairs = 128;
 template <int NT>
 __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& plan) {
   const int pairs = a.Nu * a.Hkv;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (pairs <= kWarpPairs) {
+    if (warp == 0) {
+      constexpr int kPer = kWarpPairs / 32;
+      const int per = (pairs + 31) / 32;
+      int c[kPer], mine = 0;   // a pair's cost fits 31 bits: fewer than 2^13 blocks of at most 2^18 tiles
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        c[i] = i < per && lane * per + i < pairs ? (int)pair_cost(a, lane * per + i) : 0;
+        mine += c[i];
+      }
+      int incl = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      long long begin, end;
+      share_of(a, __shfl_sync(0xffffffffu, incl, 31), worker, n_workers, begin, end);
+      long long at = begin - (incl - mine);
+      if (begin >= end) {
+        if (lane == 0) plan.begin = plan.end = 0;
+      } else if (at >= 0 && at < mine) {
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (!found && at < c[i]) {
+            settle_plan(a, lane * per + i, at, end - begin, plan);
+            found = true;
+          }
+          at -= c[i];
+        }
+      }
+    }
+    __syncthreads();
+    return;
+  }
   const int per = (pairs + NT - 1) / NT;
   const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  auto cost_of = [&](int p) {
-    int first, n;
-    unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
-    const int nb = unit_blocks(a, n);
-    if (nb == 0) return 0ll;
-    const int len = head_length(a, p);
-    long long c = 0;
-    for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
-    return c;
-  };
   long long mine = 0;
-  for (int p = p0; p < p1; ++p) mine += cost_of(p);
+  for (int p = p0; p < p1; ++p) mine += pair_cost(a, p);
   long long incl = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -102,40 +168,19 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
     plan.total = s;
   }
   __syncthreads();
-  const long long total = plan.total;
-  // rounded down: every share is at least `granule` >= 2 wide, so that a tile begins in each (the join follows an item from one
-  // worker to the next and stops at the first that has no part in it)
-  const long long most = max(total / a.granule, 1ll);
-  const int workers = (int)(most < n_workers ? most : n_workers);
-  long long begin = total, end = total;
-  if (worker < workers) {
-    if (total < (1 << 24)) {   // 32-bit divisions where they do: the plan is all latency
-      begin = (unsigned)total * (unsigned)worker / (unsigned)workers;
-      end = (unsigned)total * (unsigned)(worker + 1) / (unsigned)workers;
-    } else {
-      begin = total * worker / workers, end = total * (worker + 1) / workers;
-    }
-  }
+  long long begin, end;
+  share_of(a, plan.total, worker, n_workers, begin, end);
   if (threadIdx.x == 0 && begin >= end) plan.begin = plan.end = 0;
   const long long before = plan.warp_sum[warp] + incl - mine;
   if (end > begin && begin >= before && begin < before + mine) {
     long long at = begin - before;
     for (int p = p0; p < p1; ++p) {
-      const long long c = cost_of(p);
-      if (at >= c) {
-        at -= c;
-        continue;
+      const long long c = pair_cost(a, p);
+      if (at < c) {
+        settle_plan(a, p, at, end - begin, plan);
+        break;
       }
-      int first, n, b = 0;
-      unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
-      const int len = head_length(a, p);
-      for (;; ++b) {
-        const int t = tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
-        if (at < t) break;
-        at -= t;
-      }
-      plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + (end - begin);
-      break;
+      at -= c;
     }
   }
   __syncthreads();
@@ -230,10 +275,12 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
                              const void* v_pages, void* out, float* lse, cudaStream_t st);
 constexpr int kMmaRows = 32;         // most query rows of a block of the bf16 kernel for few rows
 constexpr int kMmaTile = 64;         // keys per tile of its schedule
+int mma_cluster(const ckv_paged& pg);   // CTAs per cluster where the cache is short, else 0
 // rows: the most query rows per KV head that a unit is expected to have.
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
+// rows: the most query rows a block has.
 template <bool BF16>
-cudaError_t launch_join(const WorkArgs& a, int workers, void* out, float* lse, cudaStream_t st);
+cudaError_t launch_join(const WorkArgs& a, int workers, int rows, void* out, float* lse, cudaStream_t st);
 
 }  // namespace ckv
