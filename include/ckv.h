@@ -317,7 +317,7 @@ ckv_status ckv_score_noalloc(const ckv_shape* shape, const ckv_params* params, c
  *
  * Tokens are packed: unit u (a sequence in one layer) owns the rows token_starts[u] .. token_starts[u+1]-1 of the token
  * arrays (token_starts [Nu+1] int32, ascending; a unit may own none).  Rows outside token_starts[0] .. token_starts[Nu]-1
- * are padding: not read, and nothing is written for them.
+ * are padding: they may hold anything, and nothing is written for them.
  * The cache is two pools k_pages, v_pages [n_pages, page_size, d]; row j of KV head g of unit u is row j % page_size of
  * page page_table[u, g, j / page_size] (page_table [Nu, Hkv, max_pages] int32), and lengths [Nu, Hkv] int32 counts
  * the rows each head holds: the heads of a unit keep different numbers of rows, so table and lengths are per head.  Only

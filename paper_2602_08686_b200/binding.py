@@ -197,8 +197,10 @@ def make_shape(q: torch.Tensor, k: torch.Tensor) -> ckv_shape:
         raise ValueError("q_win and k must be 4-D with a contiguous last dimension")
     Nu, H, W, d = q.shape
     _, Hkv, L, _ = k.shape
-    return ckv_shape(Nu, H, Hkv, d, L, W, _dtype_code(k), 0, q.stride(0), q.stride(1), q.stride(2),
-                     k.stride(0), k.stride(1), k.stride(2))
+    shape = ckv_shape(Nu, H, Hkv, d, L, W, _dtype_code(k), 0, q.stride(0), q.stride(1), q.stride(2),
+                      k.stride(0), k.stride(1), k.stride(2))
+    shape._k = (k.shape, k.stride(), k.dtype)
+    return shape
 
 
 def make_params(p: Params, head_w: torch.Tensor | None, sens: torch.Tensor | None, H: int = 0,
@@ -569,12 +571,16 @@ def ckv_append(paged, rotary, k, v, positions, token_starts, lengths, page_table
 def ckv_gather_pages(shape, params, paged, k, v, indices, budgets, offsets, page_table, k_pages, v_pages, lengths, ws, stream=None):
     """The rows the retention pass kept of k, v, into the pages of a cache; lengths receives the heads' budgets."""
     dev, i32 = paged._device, torch.int32
-    _check_kv(shape, k, "k"), _check_kv(shape, v, "v")
-    if k.get_device() != dev or v.get_device() != dev:
-        raise ValueError(f"k and v must be on device {dev}")
+    made_for = getattr(shape, "_k", None)
+    for t, name in ((k, "k"), (v, "v")):
+        if (t.shape, t.stride(), t.dtype) != made_for:
+            _check_kv(shape, t, name)
+        if t.get_device() != dev:
+            raise ValueError(f"{name} must be on device {dev}")
     Nu, Hkv = paged._heads
+    rows = Hkv * min(params.budget_per_head, shape.seq_len)
     _paged_call(lib().ckv_gather_pages, "ckv_gather_pages", dev, stream, C.byref(shape), C.byref(params), paged._ref,
-                k.data_ptr(), v.data_ptr(), _dense(indices, (Nu, rows_per_unit(shape, params)), i32, dev, "indices"),
+                k.data_ptr(), v.data_ptr(), _dense(indices, (Nu, rows), i32, dev, "indices"),
                 _dense(budgets, paged._heads, i32, dev, "budgets"), _dense(offsets, (Nu, Hkv + 1), i32, dev, "offsets"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _same(k_pages, paged._pages, "k_pages"),
                 _same(v_pages, paged._pages, "v_pages"), _dense(lengths, paged._heads, i32, dev, "lengths"), _ws_of(paged, ws),
