@@ -34,23 +34,32 @@ struct RowsSmem {
   Plan plan;
   float2 ml[kRowsWarps][kRowsM];
   float o[kRowsWarps][kRowsM][kHeadDim];
+  float2 cta_ml[kRowsM];                       // the CTA's result, for the others of its cluster
+  float cta_o[kRowsM][kHeadDim];
 };
 
+// kCluster: every pair of (unit, KV head) is one cluster's, as in the bf16 kernel for few rows.
+template <bool kCluster>
 __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a, ckv_paged pg, float x_scale,
                                                                       const char* __restrict__ q,
                                                                       const char* __restrict__ kp,
                                                                       const char* __restrict__ vp, float* __restrict__ out,
-                                                                      float* __restrict__ lse) {
+                                                                      float* __restrict__ lse, int n_cta) {
   constexpr int E = 4;
   __shared__ RowsSmem sm;
   pdl_wait();
-  make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
-  pdl_launch_dependents();
-  if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
   Walk walk;
-  walk.start(a, sm.plan);
+  const int rank = kCluster ? (int)blockIdx.x % n_cta : 0, n_ranks = kCluster ? n_cta : 1;
+  if (kCluster) {
+    walk.cluster_next(a, blockIdx.x / n_cta, 0, gridDim.x / n_cta);
+  } else {
+    make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
+    walk.start(a, sm.plan);
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
-  for (; walk.live; walk.next(a)) {
+  while (walk.live) {
     const Item& it = walk.it;
     const int rows = block_rows(a, it);
     float qr[kRowsM][16], acc[kRowsM][16], m[kRowsM], l[kRowsM];
@@ -67,7 +76,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       }
     }
     const int end = min(it.t1 * a.tile, it.visible);
-    for (int j0 = it.t0 * a.tile; j0 < end; j0 += a.tile) {
+    for (int j0 = it.t0 * a.tile + rank * a.tile; j0 < end; j0 += n_ranks * a.tile) {
       float x[2][kRowsM], kv[2][16], vv[2][16];
       int key[2];
 #pragma unroll
@@ -137,6 +146,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
     const bool whole = it.t0 == 0 && it.t1 == it.tiles;
     const int which = it.t0 > 0 ? 0 : 1;
     const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.slot_rows;
+    auto finish = [&](int r, int d, float top, float sum, float o) {
+      const int64_t at = out_row(a, it, r);
+      out[at * kHeadDim + d] = top == -INFINITY ? 0.f : o / sum;
+      if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    };
     for (int e = threadIdx.x; e < rows * kHeadDim; e += kRowsThreads) {
       const int r = e / kHeadDim, d = e - r * kHeadDim;
       float top = -INFINITY;
@@ -147,54 +161,81 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         sum = fmaf(sm.ml[w][r].y, c, sum);
         o = fmaf(sm.o[w][r][d], c, o);
       }
-      if (whole) {
-        const int64_t at = out_row(a, it, r);
-        o = top == -INFINITY ? 0.f : o / sum;
-        out[at * kHeadDim + d] = o;
-        if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      if (kCluster && n_cta > 1) {
+        sm.cta_o[r][d] = o;
+        if (d == 0) sm.cta_ml[r] = make_float2(top, sum);
+      } else if (kCluster || whole) {
+        finish(r, d, top, sum, o);
       } else {
         a.o[(slot + r) * kHeadDim + d] = o;
         if (d == 0) a.ml[slot + r] = make_float2(top, sum);
       }
     }
-    if (!whole && threadIdx.x == 0) {
-      int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
-      sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
+    if (kCluster) {
+      if (n_cta > 1) {
+        cluster_sync();
+        for (int e = rank * kRowsThreads + threadIdx.x; e < rows * (kHeadDim / 2); e += n_cta * kRowsThreads) {
+          const int r = e / (kHeadDim / 2), d = (e - r * (kHeadDim / 2)) * 2;
+          float2 ml[8], y[8], x = make_float2(0.f, 0.f);
+          float top = -INFINITY, sum = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k < n_cta) ml[k] = ld_peer(&sm.cta_ml[r], k), y[k] = ld_peer(&sm.cta_o[r][d], k), top = fmaxf(top, ml[k].x);
+          const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k < n_cta) {
+              const float f = exp2f(ml[k].x - ref);
+              sum = fmaf(ml[k].y, f, sum);
+              x.x = fmaf(y[k].x, f, x.x), x.y = fmaf(y[k].y, f, x.y);
+            }
+          finish(r, d, top, sum, x.x);
+          finish(r, d + 1, top, sum, x.y);
+        }
+        cluster_sync();   // nobody's memory is written again or given back while it is read
+      }
+      walk.cluster_next(a, walk.pair, walk.block + 1, gridDim.x / n_cta);
+    } else {
+      if (!whole && threadIdx.x == 0) {
+        int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
+        sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
+      }
+      walk.next(a);
     }
     __syncthreads();
   }
 }
 
 // Worker w's slot 1 holds the beginning of an item that the workers after it went on with (their slots 0): the parts are
-// added up in worker order.  One CTA per (worker, eight rows), 32 threads per row.
-constexpr int kJoinRows = 8;
+// added up in worker order.  A CTA per worker and share of the rows, a warp per row and round; no more CTAs than run at once.
+constexpr int kJoinRows = 8, kJoinCtas = 8;
 template <bool BF16>
-__global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int workers, void* __restrict__ out,
+__global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int workers, int rows, void* __restrict__ out,
                                                               float* __restrict__ lse) {
-  const int w = blockIdx.x, lane = threadIdx.x & 31;
-  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), d = lane * 4;   // a warp per row
+  const int w = blockIdx.x, lane = threadIdx.x & 31, d = lane * 4;
+  int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5);
   pdl_wait();
   // Who has a part, the first part and the three after it (which may turn out to be none of ours, but are there to be read): where
   // blocks are small all of it is asked for at once, where they are large only what is used.
   constexpr int kBatch = 4;
-  const bool early = gridDim.y <= 4;
+  const bool early = rows <= 32;
   const int4 next = w + 1 + lane < workers ? a.split[w + 1 + lane] : make_int4(-1, -1, -1, -1);
   const int4 mine = a.split[w];
-  auto slot_of = [&](int part) { return (int64_t)(part == 0 ? w * 2 + 1 : min(w + part, workers - 1) * 2) * a.slot_rows + r; };
   float2 x[kBatch];
   float4 y[kBatch];
   auto fetch = [&](int p0, int last) {
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      const int64_t slot = slot_of(min(p0 + b, last));
+      const int part = min(p0 + b, last);
+      const int64_t slot = (int64_t)(part == 0 ? w * 2 + 1 : min(w + part, workers - 1) * 2) * a.slot_rows + r;
       x[b] = a.ml[slot];
       y[b] = *reinterpret_cast<const float4*>(a.o + slot * kHeadDim + d);
     }
   };
-  if (early && r < a.slot_rows) fetch(0, kBatch);
+  if (early && r < rows) fetch(0, kBatch);
   if (mine.z < 0) return;
   const Item it = make_item(a, mine.z, mine.w, 0, 1ll << 40);
-  if (r >= block_rows(a, it)) return;
+  const int have = block_rows(a, it);
   unsigned no = ~__ballot_sync(0xffffffffu, next.x == mine.z && next.y == mine.w);
   int parts = no ? __ffs(no) - 1 : 32;            // workers after w that have one
   for (int w0 = w + 33; !no; w0 += 32) {
@@ -202,33 +243,36 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int wo
     no = ~__ballot_sync(0xffffffffu, s.x == mine.z && s.y == mine.w);
     parts += no ? __ffs(no) - 1 : 32;
   }
-  if (!early) fetch(0, parts);
-  float2 ml = make_float2(-INFINITY, 0.f);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p0 = 0; p0 <= parts; p0 += kBatch) {
+  bool asked = early;
+  for (; r < have; r += gridDim.y * kJoinRows, asked = false) {
+    if (!asked) fetch(0, parts);
+    float2 ml = make_float2(-INFINITY, 0.f);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 <= parts; p0 += kBatch) {
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      if (p0 + b > parts) break;
-      const float top = fmaxf(ml.x, x[b].x), ref = top == -INFINITY ? 0.f : top;
-      const float ca = exp2f(ml.x - ref), cb = exp2f(x[b].x - ref);
-      ml = make_float2(top, ml.y * ca + x[b].y * cb);
-      o.x = o.x * ca + y[b].x * cb, o.y = o.y * ca + y[b].y * cb, o.z = o.z * ca + y[b].z * cb, o.w = o.w * ca + y[b].w * cb;
+      for (int b = 0; b < kBatch; ++b) {
+        if (p0 + b > parts) break;
+        const float top = fmaxf(ml.x, x[b].x), ref = top == -INFINITY ? 0.f : top;
+        const float ca = exp2f(ml.x - ref), cb = exp2f(x[b].x - ref);
+        ml = make_float2(top, ml.y * ca + x[b].y * cb);
+        o.x = o.x * ca + y[b].x * cb, o.y = o.y * ca + y[b].y * cb, o.z = o.z * ca + y[b].z * cb, o.w = o.w * ca + y[b].w * cb;
+      }
+      if (p0 + kBatch <= parts) fetch(p0 + kBatch, parts);
     }
-    if (p0 + kBatch <= parts) fetch(p0 + kBatch, parts);
+    const bool none = ml.x == -INFINITY;
+    const float inv = none ? 0.f : 1.0f / ml.y;
+    const int64_t at = out_row(a, it, r);
+    if (none) o = make_float4(0.f, 0.f, 0.f, 0.f);   // a part that saw nothing may hold anything times zero
+    if (BF16) {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+      const uint2 v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + at * kHeadDim + d) = v;
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(out) + at * kHeadDim + d) =
+          make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    }
+    if (lse && d == 0) lse[at] = none ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
   }
-  const bool none = ml.x == -INFINITY;
-  const float inv = none ? 0.f : 1.0f / ml.y;
-  const int64_t at = out_row(a, it, r);
-  if (none) o = make_float4(0.f, 0.f, 0.f, 0.f);   // a part that saw nothing may hold anything times zero
-  if (BF16) {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-    const uint2 v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + at * kHeadDim + d) = v;
-  } else {
-    *reinterpret_cast<float4*>(static_cast<float*>(out) + at * kHeadDim + d) =
-        make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  }
-  if (lse && d == 0) lse[at] = none ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
 }
 
 int log2_of(int p) {
@@ -242,10 +286,11 @@ int log2_of(int p) {
 template <bool BF16>
 cudaError_t launch_join(const WorkArgs& a, int workers, int rows, void* out, float* lse, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(workers, (rows + kJoinRows - 1) / kJoinRows), cfg.blockDim = dim3(32 * kJoinRows), cfg.stream = st;
+  const int shares = (rows + kJoinRows - 1) / kJoinRows;
+  cfg.gridDim = dim3(workers, shares < kJoinCtas ? shares : kJoinCtas), cfg.blockDim = dim3(32 * kJoinRows), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel<BF16>, a, workers, out, lse);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, join_kernel<BF16>, a, workers, rows, out, lse);
   count_launch();
   return e;
 }
@@ -259,7 +304,17 @@ template cudaError_t launch_join<false>(const WorkArgs&, int, int, void*, float*
 constexpr int kFewRows = 16, kFewRowsShort = 32;
 static bool wants_tc(const ckv_paged& pg) {
   const int64_t G = pg.n_q_heads / pg.n_kv_heads, most = pg.max_new > 0 ? pg.max_new : pg.n_tokens;
-  return pg.dtype == CKV_BF16 && G <= 128 && most * G > (mma_cluster(pg) ? kFewRowsShort : kFewRows);
+  return pg.dtype == CKV_BF16 && G <= 128 && most * G > (cluster_size(pg, kMmaCtaKeys) ? kFewRowsShort : kFewRows);
+}
+
+// Short caches go to clusters: as many CTAs per head as the heads leave room for, as long as each has a step's keys to read and
+// none has more than kClusterRows.  0: the cache is not short.
+int cluster_size(const ckv_paged& pg, int cta_keys) {
+  constexpr int kClusterRows = 1024;
+  const int64_t pairs = (int64_t)pg.n_units * pg.n_kv_heads, capacity = (int64_t)pg.max_pages * pg.page_size;
+  int n_cta = 1;
+  while (n_cta < 8 && pairs * n_cta * 2 <= kWorkers && (int64_t)n_cta * cta_keys < capacity) n_cta *= 2;
+  return capacity <= (int64_t)n_cta * kClusterRows ? n_cta : 0;
 }
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -297,14 +352,19 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   }
   a.slot_rows = kRowsM;
   a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4;
+  const int n_cta = cluster_size(pg, kRowsTile);
+  const int64_t pairs = (int64_t)a.Nu * a.Hkv, most = n_cta ? 2 * kWorkers / n_cta : 0;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
-  cudaLaunchAttribute attr = pdl_attribute();
-  cfg.attrs = &attr, cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, attend_rows_kernel, a, pg, scale * kLog2e, (const char*)q, (const char*)k_pages,
-                                     (const char*)v_pages, (float*)out, lse);
+  cfg.gridDim = dim3(n_cta ? (int)(pairs < most ? pairs : most) * n_cta : kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0] = pdl_attribute();
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = n_cta, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr, cfg.numAttrs = n_cta > 1 ? 2 : 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, n_cta ? attend_rows_kernel<true> : attend_rows_kernel<false>, a, pg, scale * kLog2e, (const char*)q,
+                                     (const char*)k_pages, (const char*)v_pages, (float*)out, lse, n_cta);
   count_launch();
-  if (e == cudaSuccess) e = launch_join<false>(a, kWorkers, kRowsM, out, lse, st);
+  if (e == cudaSuccess && !n_cta) e = launch_join<false>(a, kWorkers, kRowsM, out, lse, st);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -19,9 +19,8 @@ namespace ckv {
 namespace {
 
 constexpr int kMmaWarps = 8;
-constexpr int kClusterRows = 1024;  // rows of a cache per CTA up to which clusters take it
 constexpr int kGroup = 16;          // keys per warp and step
-constexpr int kCtaKeys = kMmaWarps * kGroup;
+static_assert(kMmaCtaKeys == kMmaWarps * kGroup, "keys of a step");
 constexpr float kRaise = 8.0f;      // powers of two a row may exceed its reference before the output is rescaled
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -54,19 +53,6 @@ struct Smem {
   float2 cta_ml[16 * MT];                      // the CTA's result, for the others of its cluster
   float cta_o[16 * MT][kHeadDim];
 };
-
-__device__ __forceinline__ void cluster_sync() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float2 ld_peer(const void* mine, int rank) {   // the same place in another CTA's shared memory
-  uint32_t at;
-  float2 x;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
-  return x;
-}
 
 // kCluster: every item is one cluster's (of n_cta CTAs), whose warps share its keys and whose results join through distributed
 // shared memory; no schedule, no second kernel.  Otherwise the items are split evenly over the grid.
@@ -384,22 +370,13 @@ cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, int grid, int n_cta, 
 
 }  // namespace
 
-// Short caches go to clusters: as many CTAs per head as the heads leave room for, as long as each has keys to read and none has
-// more than kClusterRows.  0: the cache is not short.
-int mma_cluster(const ckv_paged& pg) {
-  const int64_t pairs = (int64_t)pg.n_units * pg.n_kv_heads, capacity = (int64_t)pg.max_pages * pg.page_size;
-  int n_cta = 1;
-  while (n_cta < 8 && pairs * n_cta * 2 <= kWorkers && n_cta * kCtaKeys < capacity) n_cta *= 2;
-  return capacity <= (int64_t)n_cta * kClusterRows ? n_cta : 0;
-}
-
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st) {
   WorkArgs a = base;
   a.tokens = 0, a.tile = kMmaTile, a.granule = 2;
   a.M = rows <= 16 ? 16 : 32;
   const float x_scale = scale * kLog2e;
-  if (const int n_cta = mma_cluster(pg)) {
+  if (const int n_cta = cluster_size(pg, kMmaCtaKeys)) {
     const int64_t pairs = (int64_t)a.Nu * a.Hkv, most = 2 * kWorkers / n_cta;
     const int grid = (int)(pairs < most ? pairs : most) * n_cta;
     return rows <= 16 ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)

@@ -41,8 +41,11 @@ struct Item {
 __device__ __forceinline__ int unit_blocks(const WorkArgs& a, int n) {
   return a.tokens ? (n + a.tokens - 1) / a.tokens : (int)(((int64_t)n * a.G + a.M - 1) / a.M);
 }
+// Rows the head holds; a length that the table has no pages for, or below zero, is reported and cut.
 __device__ __forceinline__ int head_length(const WorkArgs& a, int pair) {
-  return min(max(a.lengths[pair], 0), a.max_pages << a.log_p);
+  const int len = a.lengths[pair], cut = min(max(len, 0), a.max_pages << a.log_p);
+  if (cut != len) report_status(a.status, kStatusPage);
+  return cut;
 }
 // rows that the last token of a block sees
 __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, int block) {
@@ -58,11 +61,29 @@ __device__ __forceinline__ int weight_of(const WorkArgs& a, int n, int block) {
   return a.tokens && 2 * (n - block * a.tokens) > a.tokens ? 2 : 1;
 }
 
+// The item at (pair, block) of a unit whose tokens and a head whose length are known: its tiles whose cost begins in [begin, end),
+// relative to the cost before the item.
+__device__ __forceinline__ Item item_of(const WorkArgs& a, int pair, int block, int first, int n, int len, long long begin,
+                                        long long end) {
+  Item it;
+  it.u = pair / a.Hkv, it.g = pair - it.u * a.Hkv, it.block = block;
+  it.first = first, it.n = n, it.len = len;
+  it.rows = n * a.G;
+  it.visible = block_visible(a, n, len, block);
+  it.tiles = tiles_of(a, it.visible);
+  it.weight = weight_of(a, n, block);
+  const long long cost = (long long)it.tiles * it.weight;
+  const int from = (int)(begin < cost ? begin : cost), to = (int)(end < cost ? end : cost);
+  it.t0 = (from + it.weight - 1) / it.weight, it.t1 = (to + it.weight - 1) / it.weight;
+  return it;
+}
+
 struct Plan {           // in shared memory
   long long warp_sum[32];
   long long total;
   long long begin, end; // the worker's share, relative to the cost before the item it starts in
-  int pair, block;      // that item
+  int pair, block;      // that item ...
+  Item it;              // ... and what is known of it
 };
 
 __device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p) {
@@ -101,6 +122,7 @@ __device__ __forceinline__ void settle_plan(const WorkArgs& a, int p, long long 
     at -= t;
   }
   plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + width;
+  plan.it = item_of(a, p, b, first, n, len, at, at + width);
 }
 
 // All threads of the CTA.  Returns with the worker's share in `plan`.  Up to kWarpPairs (unit, KV head) pairs one warp does it
@@ -186,21 +208,10 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
   __syncthreads();
 }
 
-// The item at (pair, block): its tiles whose cost begins in [begin, end), relative to the cost before the item.
 __device__ __forceinline__ Item make_item(const WorkArgs& a, int pair, int block, long long begin, long long end) {
-  Item it;
-  it.u = pair / a.Hkv, it.g = pair - it.u * a.Hkv, it.block = block;
-  unit_tokens(a.starts, it.u, a.T, it.first, it.n);
-  it.len = head_length(a, pair);
-  if (it.len != a.lengths[pair] && threadIdx.x == 0) report_status(a.status, kStatusPage);
-  it.rows = it.n * a.G;
-  it.visible = block_visible(a, it.n, it.len, block);
-  it.tiles = tiles_of(a, it.visible);
-  it.weight = weight_of(a, it.n, block);
-  const long long cost = (long long)it.tiles * it.weight;
-  const int from = (int)(begin < cost ? begin : cost), to = (int)(end < cost ? end : cost);
-  it.t0 = (from + it.weight - 1) / it.weight, it.t1 = (to + it.weight - 1) / it.weight;
-  return it;
+  int first, n;
+  unit_tokens(a.starts, pair / a.Hkv, a.T, first, n);
+  return item_of(a, pair, block, first, n, head_length(a, pair), begin, end);
 }
 // Moves to the next item that has rows; false behind the last one.
 __device__ __forceinline__ bool next_item(const WorkArgs& a, int& pair, int& block, int n) {
@@ -217,6 +228,19 @@ __device__ __forceinline__ bool next_item(const WorkArgs& a, int& pair, int& blo
   }
   return false;
 }
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float2 ld_peer(const void* mine, int rank) {   // the same place in another CTA's shared memory
+  uint32_t at;
+  float2 x;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
+  return x;
+}
+
 // Walks a worker's items: for (Walk k(...); k.more(); k.next()) ... k.it
 struct Walk {
   int pair, block;
@@ -236,7 +260,22 @@ struct Walk {
   }
   __device__ __forceinline__ void start(const WorkArgs& a, const Plan& p) {
     pair = p.pair, block = p.block, begin = p.begin, end = p.end, live = end > begin;
+    if (!live) return;
+    it = p.it;
+    if (it.t1 > it.t0) return;
+    step(a);
     settle(a);
+  }
+  // Where every pair is one cluster's: from (p, b) on, the first item that has rows; clusters are `stride` pairs apart.
+  __device__ __forceinline__ void cluster_next(const WorkArgs& a, int p, int b, int stride) {
+    live = false;
+    for (; p < a.Nu * a.Hkv; p += stride, b = 0) {
+      it = make_item(a, p, b, 0, 1ll << 40);
+      if (b < unit_blocks(a, it.n)) {
+        pair = p, block = b, live = true;
+        return;
+      }
+    }
   }
   __device__ __forceinline__ bool next(const WorkArgs& a) {
     step(a);
@@ -275,7 +314,8 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
                              const void* v_pages, void* out, float* lse, cudaStream_t st);
 constexpr int kMmaRows = 32;         // most query rows of a block of the bf16 kernel for few rows
 constexpr int kMmaTile = 64;         // keys per tile of its schedule
-int mma_cluster(const ckv_paged& pg);   // CTAs per cluster where the cache is short, else 0
+constexpr int kMmaCtaKeys = 128;     // keys a CTA of it takes per step
+int cluster_size(const ckv_paged& pg, int cta_keys);   // CTAs per cluster where the cache is short, else 0
 // rows: the most query rows per KV head that a unit is expected to have.
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
