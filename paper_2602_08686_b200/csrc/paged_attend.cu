@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
 
 // Worker w's slot 1 holds the beginning of an item that the workers after it went on with (their slots 0): the parts are
 // added up in worker order.  A CTA per worker and share of the rows, a warp per row and round; no more CTAs than run at once.
-constexpr int kJoinRows = 8, kJoinCtas = 8;
+constexpr int kJoinRows = 8, kJoinCtas = 16;
 template <bool BF16>
 __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int workers, int rows, void* __restrict__ out,
                                                               float* __restrict__ lse) {
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int wo
     no = ~__ballot_sync(0xffffffffu, s.x == mine.z && s.y == mine.w);
     parts += no ? __ffs(no) - 1 : 32;
   }
-  bool asked = early;
+  bool asked = early && r < rows;
   for (; r < have; r += gridDim.y * kJoinRows, asked = false) {
     if (!asked) fetch(0, parts);
     float2 ml = make_float2(-INFINITY, 0.f);

@@ -88,12 +88,14 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
 // tokens fill no more than half of the block): both streams work on it, each on its half of every key tile, and join at the end.
 __device__ __forceinline__ bool paired(const Item& it) { return it.weight == 2; }
 
+// Rows that every token of the block sees: those its first token does.
+__device__ __forceinline__ int all_see(const TcArgs& a, const Item& it) {
+  return a.w.causal ? min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len) : it.len;
+}
 // First row of the item's j-th key tile that the block's first token does not see (128: it sees them all).  Where every
 // token sees every row there is none.
 __device__ __forceinline__ int late_row(const TcArgs& a, const Item& it, int j) {
-  if (!a.w.causal) return kTile;
-  const int sees = min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len);
-  return min(max(sees - (it.t0 + j) * kTile, 0), kTile);
+  return a.w.causal ? min(max(all_see(a, it) - (it.t0 + j) * kTile, 0), kTile) : kTile;
 }
 
 __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUtensorMap* qm, const CUtensorMap* km,
@@ -209,8 +211,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
     const bool pair = paired(it);
     const int steps = pair ? 2 * n : n;
     const uint32_t q_lo = desc_lo(smem_u32(sm.q[pair ? s : 0]), 16);
-    int j_clean = 0;                                           // first tile whose values have to be looked at
-    while (j_clean < n && late_row(a, it, j_clean) == kTile && it.visible - (it.t0 + j_clean) * kTile >= kTile) ++j_clean;
+    const int j_clean = max(all_see(a, it) / kTile - it.t0, 0);   // first tile whose values have to be looked at
     if (!wait_warp(smem_u32(&sm.q_full), n_items & 1, w, 4)) return;
     Ring kr = ring, vr = ring;
     vr.step();
@@ -600,7 +601,9 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   cfg.attrs = &attr, cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, attend_tc_kernel, qm, km, vm, a);
   count_launch();
-  return e != cudaSuccess ? e : launch_join<true>(a.w, kWorkers, a.w.M, out, lse, st);
+  if (e != cudaSuccess) return e;
+  const int64_t most = (int64_t)(pg.max_new > 0 && pg.max_new < pg.n_tokens ? pg.max_new : pg.n_tokens) * base.G;
+  return launch_join<true>(a.w, kWorkers, (int)(most < a.w.M ? most : a.w.M), out, lse, st);
 }
 
 }  // namespace ckv

@@ -39,7 +39,8 @@ struct Item {
 };
 
 __device__ __forceinline__ int unit_blocks(const WorkArgs& a, int n) {
-  return a.tokens ? (n + a.tokens - 1) / a.tokens : (int)(((int64_t)n * a.G + a.M - 1) / a.M);
+  const int per = a.tokens ? a.tokens : a.M, units = a.tokens ? n : n * a.G;   // at most 2^26 rows
+  return units <= per ? (units > 0) : (units + per - 1) / per;
 }
 // Rows the head holds; a length that the table has no pages for, or below zero, is reported and cut.
 __device__ __forceinline__ int head_length(const WorkArgs& a, int pair) {
@@ -50,9 +51,8 @@ __device__ __forceinline__ int head_length(const WorkArgs& a, int pair) {
 // rows that the last token of a block sees
 __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, int block) {
   if (!a.causal) return len;
-  const int64_t end = a.tokens ? (int64_t)(block + 1) * a.tokens : ((int64_t)(block + 1) * a.M + a.G - 1) / a.G;
-  const int last = (int)(end < n ? end : n) - 1;
-  return min(max(len - n + last + 1, 0), len);
+  const int end = a.tokens ? (block + 1) * a.tokens : ((block + 1) * a.M >= n * a.G ? n : ((block + 1) * a.M + a.G - 1) / a.G);
+  return min(max(len - n + min(end, n), 0), len);
 }
 __device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) / a.tile, 1); }
 
