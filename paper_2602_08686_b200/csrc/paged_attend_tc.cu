@@ -31,6 +31,7 @@ constexpr int kStages = 5;
 constexpr int kTile = 128, kStep = 64;         // keys of a tile, and of a step
 constexpr uint32_t kHalf = 128 * 128;          // 128 rows x 64 bf16
 constexpr uint32_t kTileBytes = 2 * kHalf;
+constexpr int kTcGranule = kBothTiles;         // least cost a CTA takes on (twice that: 31 us instead of 27 for 40 tokens on 2048 rows)
 constexpr int kInfo = 8;                       // ring of per-tile notes from the loader
 constexpr float kOverflow = 1.8446744e19f;     // 2^64: a step's sum above it is done again with a new reference
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);   // fp32 += bf16 * bf16, M = 128
@@ -86,7 +87,7 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
 
 // How an item is cut up.  Two query tiles: each stream has one, and takes both halves of every key tile.  One query tile (the
 // tokens fill no more than half of the block): both streams work on it, each on its half of every key tile, and join at the end.
-__device__ __forceinline__ bool paired(const Item& it) { return it.weight == 2; }
+__device__ __forceinline__ bool paired(const Item& it) { return it.weight == kBothTiles; }
 
 // Rows that every token of the block sees: those its first token does.
 __device__ __forceinline__ int all_see(const TcArgs& a, const Item& it) {
@@ -108,7 +109,7 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
   const int tiles_per_page = a.w.P > kTile ? a.w.P / kTile : 1;
   for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
-    const int ns = it.weight;
+    const int ns = paired(it) ? 2 : 1;
     if (!wait_warp(smem_u32(&sm.q_empty), (n_items & 1) ^ 1, w, 1)) return;
     if (lane == 0) bar_arrive_tx(smem_u32(&sm.q_full), ns * a.q_bytes);
     __syncwarp();
@@ -573,7 +574,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   TcArgs a{};
   a.w = base;
   a.TQ = kTile / base.G;
-  a.w.tokens = 2 * a.TQ, a.w.M = a.w.tokens * base.G, a.w.tile = kTile, a.w.granule = 2;
+  a.w.tokens = 2 * a.TQ, a.w.M = a.w.tokens * base.G, a.w.tile = kTile, a.w.granule = kTcGranule;
   a.x_scale = (scale < 0.f ? -scale : scale) * kLog2e;
   a.idesc_qk = kIdescQK | (scale < 0.f ? kNegateA : 0u);
   a.q_bytes = 2u * (uint32_t)(a.TQ * base.G) * 128u;

@@ -2,7 +2,7 @@
 //
 // An item is one block of query rows of one (unit, KV head): the rows r = token * G + head of the unit's tokens and the
 // group's G query heads, `M` of them.  Its cost is the number of key tiles its last token sees (at least one, so that rows
-// that see nothing are written too), times two where the block fills more than half of its rows.  Lengths and token counts
+// that see nothing are written too), times what a tile of it takes.  Lengths and token counts
 // live on the device, so the split is made there: every worker (CTA) adds up the costs, takes an equal share of the total
 // and works through the items in it; a tile belongs to the share its cost begins in.  The first item may have been begun by the
 // worker before, the last may be finished by the next: those two
@@ -18,7 +18,7 @@ struct WorkArgs {
   int M;            // query rows of a block
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
   int tile;         // keys per tile
-  int granule;      // least cost per worker, at least 2
+  int granule;      // least cost per worker, at least that of a tile
   int P, log_p, n_pages, max_pages;
   const int32_t *starts, *lengths, *table;
   int* status;
@@ -56,9 +56,11 @@ __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, 
 }
 __device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) / a.tile, 1); }
 
-// 2: the block fills both of the query tiles of whole tokens that make it up
+// Cost of a key tile: one, where blocks are one tile of query rows.  Where they are two tiles of whole tokens, a key tile takes
+// 2 us if the tokens fill both and 1.35 us if they fill one: 3 and 2.
+constexpr int kBothTiles = 3, kOneTile = 2;
 __device__ __forceinline__ int weight_of(const WorkArgs& a, int n, int block) {
-  return a.tokens && 2 * (n - block * a.tokens) > a.tokens ? 2 : 1;
+  return !a.tokens ? 1 : (2 * (n - block * a.tokens) > a.tokens ? kBothTiles : kOneTile);
 }
 
 // The item at (pair, block) of a unit whose tokens and a head whose length are known: its tiles whose cost begins in [begin, end),
@@ -97,7 +99,7 @@ __device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p) {
 // The share [begin, end) of a worker.
 __device__ __forceinline__ void share_of(const WorkArgs& a, long long total, int worker, int n_workers, long long& begin,
                                          long long& end) {
-  // rounded down: every share is at least `granule` >= 2 wide, so that a tile begins in each (the join follows an item from one
+  // rounded down: every share is at least `granule` wide, no less than a tile, so that a tile begins in each (the join follows an item from one
   // worker to the next and stops at the first that has no part in it)
   const long long most = max(total / a.granule, 1ll);
   const int workers = (int)(most < n_workers ? most : n_workers);

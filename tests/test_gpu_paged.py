@@ -142,6 +142,30 @@ def test_append(B, dtype, H, Hkv, page, counts, lens, rot, norm):
     assert torch.equal(again[0], c.pools[0]) and torch.equal(again[1], c.pools[1])
 
 
+@pytest.mark.parametrize("Nu,per", [(600, 1), (520, 5), (33, 100), (3, 0)])
+def test_append_many_units(B, Nu, per):
+    """Units found among many starts, empty ones among them; a call without tokens still hands the lengths on."""
+    counts = [(u * 7) % (per + 1) if per != 1 else 1 for u in range(Nu)]
+    st = starts_of(counts)
+    lens = [[(u * 5) % 40] for u in range(Nu)]
+    c = R.Cache(lens, 16, max_extra=max(max(counts), 1), dtype=torch.float32, device="cuda", poison=3.0)
+    k = torch.randn(st[-1], 1, D, device="cuda")
+    v = torch.randn(st[-1], 1, D, device="cuda")
+    pg = B.make_paged(c.k_pages, c.table, k_new=k)
+    ws = B.alloc_paged_workspace(pg)
+    new = torch.full((Nu, 1), -1, dtype=torch.int32, device="cuda")
+    B.ckv_append(pg, None, k, v, None, i32(st), c.lengths, c.table, c.k_pages, c.v_pages, ws, new_lengths=new)
+    assert torch.equal(new, c.lengths + i32(counts)[:, None]) and B.ckv_device_status(ws) == B.OK
+    for u in range(Nu):
+        for i in range(counts[u]):
+            j = lens[u][0] + i
+            assert torch.equal(c.k_pages[int(c.table[u, 0, j // 16]), j % 16], k[st[u] + i, 0]), (u, i)
+            assert torch.equal(c.v_pages[int(c.table[u, 0, j // 16]), j % 16], v[st[u] + i, 0]), (u, i)
+            if u > 40:
+                break
+    assert int((c.pools[0] != 3.0).any(-1).sum()) == sum(x[0] for x in lens) + sum(counts)
+
+
 def test_append_leaves_out_rows_that_have_no_page_and_says_so(B):
     c = R.Cache([[20, 3]], 16, max_extra=4, dtype=torch.float32, device="cuda", poison=3.0)
     k = torch.randn(4, 2, D, device="cuda")
@@ -270,6 +294,30 @@ def test_attend(B, dtype, causal, H, Hkv, page, counts, lens):
         check_attend(c, q, starts, out, lse, causal)
 
 
+MANY = {
+    # more (unit, KV head) pairs than one warp schedules, units without tokens among them, short and long caches
+    "decode short": (40, 8, 8, 16, lambda u: 1 if u % 7 else 0, lambda u, g: 3 + (37 * u + 11 * g) % 200),
+    "decode long": (33, 4, 8, 64, lambda u: u % 2, lambda u, g: 1200 + (97 * u + 501 * g) % 1500),
+    "verify": (50, 3, 9, 32, lambda u: (u * 5) % 4, lambda u, g: 4 + (61 * u + 17 * g) % 1300),
+    "chunks": (36, 4, 8, 16, lambda u: (0, 1, 40, 3)[u % 4], lambda u, g: 40 + (53 * u + 29 * g) % 300),
+    "one head": (700, 1, 4, 16, lambda u: 1, lambda u, g: 1 + (u * 13) % 90),
+}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("name", list(MANY))
+def test_attend_many_heads(B, dtype, name):
+    Nu, Hkv, H, page, count, length = MANY[name]
+    counts = [count(u) for u in range(Nu)]
+    lens = [[length(u, g) for g in range(Hkv)] for u in range(Nu)]
+    c = R.Cache(lens, page, dtype=dtype, device="cuda", seed=Nu)
+    st = starts_of(counts)
+    q = torch.randn(st[-1] + 1, H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)).to(dtype)
+    for max_new in (0, max(counts), 1):          # the last one may be less than the truth: it only picks kernels
+        out, lse = run_attend(B, c, q, st, max_new=max_new)
+        check_attend(c, q, st, out, lse)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("counts,length", [([1], 40000), ([1, 1], 9000), ([6], 20000), ([100], 9000), ([700], 3000)])
 def test_attend_long(B, dtype, counts, length):
@@ -368,6 +416,38 @@ def test_attend_same_bits_again_and_on_two_streams(B):
             torch.cuda.synchronize()
             first = outs[0].clone() if first is None else first
             assert torch.equal(outs[0], first) and torch.equal(outs[1], first)
+
+
+def test_two_graphs_share_a_work_space(B):
+    """Two captured steps of different shapes on one work space, replayed in turn: neither leaves anything the other trips over."""
+    cases = []
+    for counts, lens in (([1, 1], [[3000, 100], [777, 2500]]), ([60], [[2000, 333]]), ([1], [[40, 17]])):
+        c = R.Cache(lens, 64, dtype=torch.bfloat16, device="cuda", seed=sum(counts))
+        q = torch.randn(sum(counts), 16, D, device="cuda").bfloat16()
+        pg = B.make_paged(c.k_pages, c.table, q=q, max_new=max(counts))
+        cases.append((c, q, pg, i32(starts_of(counts)), torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda"), counts))
+    ws = torch.randint(0, 255, (max(B.ckv_paged_workspace_bytes(x[2]) for x in cases),), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for c, q, pg, st, out, lse, _ in cases:
+        B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, c.lengths, st, out, ws, lse=lse)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, c.lengths, st, out, ws, lse=lse)
+        graphs.append(g)
+    first = []
+    for c, q, pg, st, out, lse, counts in cases:
+        want, want_lse = R.attend(q, starts_of(counts), c.rows)
+        assert (out.double() - want).norm() <= 2 * 2.0 ** -8 * want.norm() and (lse.double() - want_lse).abs().max() <= 1e-3
+        first.append(out.clone())
+        out.fill_(5.0)
+    for turn in range(6):
+        for g in (graphs if turn % 2 else graphs[::-1]):
+            g.replay()
+    torch.cuda.synchronize()
+    for x, want in zip(cases, first):
+        assert torch.equal(x[4], want)
+    assert B.ckv_device_status(ws) == B.OK
 
 
 def test_offsets_past_32_bits(B):
