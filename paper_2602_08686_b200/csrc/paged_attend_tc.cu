@@ -105,11 +105,15 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
   k.start(a.w, sm.plan);
   uint32_t n_loads = 0, n_items = 0, n_tiles = 0;
   const int slot_of_lane = lane >> 1, half = lane & 1;
+  const uint64_t first = evict_first();
   const bool copies = slot_of_lane < a.pages_per_tile;
   const int tiles_per_page = a.w.P > kTile ? a.w.P / kTile : 1;
   for (; k.live; k.next(a.w)) {
     const Item& it = k.it;
     const int ns = paired(it) ? 2 : 1;
+    // Keys and values that one block alone reads leave L2 first: what every call needs again (code, tables, lengths) is then not
+    // streamed out of it, and the next call does not start with misses (49 us instead of 62 for 8 x 5 tokens on 16k).
+    const bool once = it.n <= a.w.tokens;
     if (!wait_warp(smem_u32(&sm.q_empty), (n_items & 1) ^ 1, w, 1)) return;
     if (lane == 0) bar_arrive_tx(smem_u32(&sm.q_full), ns * a.q_bytes);
     __syncwarp();
@@ -144,9 +148,11 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
           bar_arrive_tx(smem_u32(&sm.full[s]), bytes);
         }
         __syncwarp();
-        if (copy)
-          tma_load_4d(kv ? vm : km, smem_u32(&sm.kv[s][half * kHalf + slot_of_lane * a.page_bytes]), smem_u32(&sm.full[s]), 0,
-                      row_in_page, half, page);
+        if (copy) {
+          const uint32_t dst = smem_u32(&sm.kv[s][half * kHalf + slot_of_lane * a.page_bytes]);
+          if (once) tma_load_4d_hint(kv ? vm : km, dst, smem_u32(&sm.full[s]), 0, row_in_page, half, page, first);
+          else tma_load_4d(kv ? vm : km, dst, smem_u32(&sm.full[s]), 0, row_in_page, half, page);
+        }
       }
     }
     ++n_items;
