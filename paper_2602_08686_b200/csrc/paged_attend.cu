@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
         sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
       }
-      walk.next(a);
+      walk.next(a, sm.plan);
     }
     __syncthreads();
   }

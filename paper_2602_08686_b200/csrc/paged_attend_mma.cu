@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
         sp[2 * which] = walk.pair, sp[2 * which + 1] = walk.block;
       }
-      walk.next(a);
+      walk.next(a, sm.plan);
     }
     __syncthreads();
   }

@@ -108,7 +108,7 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
   const uint64_t first = evict_first();
   const bool copies = slot_of_lane < a.pages_per_tile;
   const int tiles_per_page = a.w.P > kTile ? a.w.P / kTile : 1;
-  for (; k.live; k.next(a.w)) {
+  for (; k.live; k.next(a.w, sm.plan)) {
     const Item& it = k.it;
     const int ns = paired(it) ? 2 : 1;
     // Keys and values that one block alone reads leave L2 first: what every call needs again (code, tables, lengths) is then not
@@ -212,7 +212,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
   const uint32_t s_cols = tmem + kColS + s * 128, o_cols = tmem + kColO + s * 128;
   const uint32_t bar_s = smem_u32(&sm.s_full[s][0]), bar_p = smem_u32(&sm.p_full[s][0]);
   const uint32_t bar_o = smem_u32(&sm.pv_done[s]), bar_item = smem_u32(&sm.item_done[s]);
-  for (; k.live; k.next(a.w)) {
+  for (; k.live; k.next(a.w, sm.plan)) {
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
     const bool pair = paired(it);
@@ -351,7 +351,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const uint32_t s_addr = tmem + lanes + kColS + stream * 128, o_addr = tmem + lanes + kColO + stream * 128;
   const uint32_t bar_s = smem_u32(&sm.s_full[stream][0]), bar_p = smem_u32(&sm.p_full[stream][0]), bar_o = smem_u32(&sm.pv_done[stream]);
-  for (; k.live; k.next(a.w)) {
+  for (; k.live; k.next(a.w, sm.plan)) {
     const Item& it = k.it;
     const int n = it.t1 - it.t0;
     const bool pair = paired(it);
@@ -581,6 +581,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   a.w = base;
   a.TQ = kTile / base.G;
   a.w.tokens = 2 * a.TQ, a.w.M = a.w.tokens * base.G, a.w.tile = kTile, a.w.granule = kTcGranule;
+  a.w.rounds = (pg.max_new > 0 ? pg.max_new : pg.n_tokens) > a.w.tokens;
   a.x_scale = (scale < 0.f ? -scale : scale) * kLog2e;
   a.idesc_qk = kIdescQK | (scale < 0.f ? kNegateA : 0u);
   a.q_bytes = 2u * (uint32_t)(a.TQ * base.G) * 128u;
