@@ -41,7 +41,7 @@ bool token_strides(const ckv_paged& pg, int64_t tok, int64_t head, int heads) {
   const int64_t e = esize(pg);
   if (tok < 0 || head < 0 || (tok * e) % 16 || (head * e) % 16) return false;
   if ((heads > 1 && head < kHeadDim) || (pg.n_tokens > 1 && tok < kHeadDim)) return false;
-  return tok < ((int64_t)1 << 40) && head < ((int64_t)1 << 40);
+  return tok < ((int64_t)1 << 38) && head < ((int64_t)1 << 38);   // a tensor map's strides end at 2^40 bytes
 }
 ckv_status check_pages(const ckv_paged* pg) {
   if (pg->page_size < 1 || pg->n_pages < 1 || pg->max_pages < 1) return CKV_ERR_INVALID_ARG;
@@ -193,8 +193,11 @@ ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k
   if (lse_or_null && !aligned(lse_or_null, 4)) return CKV_ERR_INVALID_ARG;
   if (!token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, paged->n_q_heads)) return CKV_ERR_INVALID_ARG;
   const int64_t T = paged->n_tokens, H = paged->n_q_heads, e = esize(*paged);
-  if (overlap(range_of(out, T, H, H * kHeadDim, kHeadDim, e), range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e)))
-    return CKV_ERR_INVALID_ARG;
+  const Range o = range_of(out, T, H, H * kHeadDim, kHeadDim, e);
+  if (overlap(o, range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e))) return CKV_ERR_INVALID_ARG;
+  for (const void* pool : {k_pages, v_pages})
+    if (overlap(o, range_of(pool, paged->n_pages, paged->page_size, paged->page_stride, paged->page_stride_row, e)))
+      return CKV_ERR_INVALID_ARG;
   CKV_CUDA(launch_paged_attend(*paged, q, k_pages, v_pages, page_table, lengths, token_starts, out, lse_or_null,
                                static_cast<char*>(ws), (cudaStream_t)stream));
   return CKV_OK;

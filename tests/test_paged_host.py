@@ -115,6 +115,8 @@ def test_bad_pointers_and_work_space():
     assert call("append", pg, rot, new_lengths=FAKE + 6 * (1 << 30)) == B.ERR_INVALID_ARG
     assert call("append", pg, rot, new_lengths=FAKE + 6 * (1 << 30) + 60) == B.ERR_INVALID_ARG
     assert call("attend", pg, out=FAKE + 1 * (1 << 30)) == B.ERR_INVALID_ARG
+    assert call("attend", pg, out=FAKE + 10 * (1 << 30) + 64) == B.ERR_INVALID_ARG       # the pages
+    assert call("attend", pg, out=FAKE + (1 << 36) + 16) == B.ERR_INVALID_ARG            # off its 32-byte boundary
     assert call("rotate", pg, rot, q_out=FAKE + 1 * (1 << 30) + 16) == B.ERR_INVALID_ARG
     assert call("rotate", pg, rot, q_out=FAKE + 2 * (1 << 30)) == B.ERR_INVALID_ARG      # the keys' input
     assert call("rotate", pg, rot, q_out=FAKE + 9 * (1 << 30) + 256) == B.ERR_INVALID_ARG  # the keys' output
