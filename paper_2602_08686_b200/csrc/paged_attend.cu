@@ -335,6 +335,7 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
                                 char* ws, cudaStream_t st) {
   const PagedWs w = paged_ws(pg);
   const bool bf16 = pg.dtype == CKV_BF16, tc = wants_tc(pg);
+  const int64_t most = pg.max_new > 0 && pg.max_new < pg.n_tokens ? pg.max_new : pg.n_tokens;   // tokens of a unit
   const float scale = pg.scale != 0.f ? pg.scale : 0.08838834764831845f;
   WorkArgs a{};
   a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = pg.causal;
@@ -343,19 +344,18 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   a.split = reinterpret_cast<int4*>(ws + w.split), a.ml = reinterpret_cast<float2*>(ws + w.ml), a.o = reinterpret_cast<float*>(ws + w.o);
   if (tc) {
     a.slot_rows = kTcRows;
-    return launch_attend_tc(pg, a, scale, q, k_pages, v_pages, out, lse, st);
+    return launch_attend_tc(pg, a, most, scale, q, k_pages, v_pages, out, lse, st);
   }
   if (bf16) {
     a.slot_rows = kMmaRows;
-    const int64_t most = (int64_t)(pg.max_new > 0 ? pg.max_new : pg.n_tokens) * a.G;
-    return launch_attend_mma(pg, a, (int)(most < kMmaRows ? most : kMmaRows), scale, q, k_pages, v_pages, out, lse, st);
+    return launch_attend_mma(pg, a, most, scale, q, k_pages, v_pages, out, lse, st);
   }
   a.slot_rows = kRowsM;
-  a.M = kRowsM, a.tokens = 0, a.tile = kRowsTile, a.granule = 4;
+  set_blocks(a, most, kRowsM, 0, kRowsTile, 4);
   const int n_cta = cluster_size(pg, kRowsTile);
-  const int64_t pairs = (int64_t)a.Nu * a.Hkv, most = n_cta ? 2 * kWorkers / n_cta : 0;
+  const int64_t pairs = (int64_t)a.Nu * a.Hkv, fit = n_cta ? 2 * kWorkers / n_cta : 0;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(n_cta ? (int)(pairs < most ? pairs : most) * n_cta : kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
+  cfg.gridDim = dim3(n_cta ? (int)(pairs < fit ? pairs : fit) * n_cta : kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0] = pdl_attribute();
   attr[1].id = cudaLaunchAttributeClusterDimension;

@@ -370,19 +370,19 @@ cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, int grid, int n_cta, 
 
 }  // namespace
 
-cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
+cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st) {
   WorkArgs a = base;
-  a.tokens = 0, a.tile = kMmaTile, a.granule = 2;
-  a.M = rows <= 16 ? 16 : 32;
+  const bool few = most * a.G <= 16;
+  set_blocks(a, most, few ? 16 : 32, 0, kMmaTile, 2);
   const float x_scale = scale * kLog2e;
   if (const int n_cta = cluster_size(pg, kMmaCtaKeys)) {
-    const int64_t pairs = (int64_t)a.Nu * a.Hkv, most = 2 * kWorkers / n_cta;
-    const int grid = (int)(pairs < most ? pairs : most) * n_cta;
-    return rows <= 16 ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
+    const int64_t pairs = (int64_t)a.Nu * a.Hkv, fit = 2 * kWorkers / n_cta;
+    const int grid = (int)(pairs < fit ? pairs : fit) * n_cta;
+    return few ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
                       : launch<2, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st);
   }
-  const cudaError_t e = rows <= 16 ? launch<1, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
+  const cudaError_t e = few ? launch<1, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
                                    : launch<2, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st);
   return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, a.M, out, lse, st);
 }

@@ -588,13 +588,12 @@ bool make_map(CUtensorMap* map, const void* base, cuuint64_t n1, int64_t s1, cuu
 
 }  // namespace
 
-cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float scale, const void* q, const void* k_pages,
+cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                              const void* v_pages, void* out, float* lse, cudaStream_t st) {
   TcArgs a{};
   a.w = base;
   a.TQ = kTile / base.G;
-  a.w.tokens = 2 * a.TQ, a.w.M = a.w.tokens * base.G, a.w.tile = kTile, a.w.granule = kTcGranule;
-  a.w.rounds = (pg.max_new > 0 ? pg.max_new : pg.n_tokens) > a.w.tokens;
+  set_blocks(a.w, most, 2 * a.TQ * base.G, 2 * a.TQ, kTile, kTcGranule);
   a.x_scale = (scale < 0.f ? -scale : scale) * kLog2e;
   a.idesc_qk = kIdescQK | (scale < 0.f ? kNegateA : 0u);
   a.q_bytes = 2u * (uint32_t)(a.TQ * base.G) * 128u;
@@ -623,8 +622,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float sc
   e = cudaLaunchKernelEx(&cfg, attend_tc_kernel, qm, km, vm, a);
   count_launch();
   if (e != cudaSuccess) return e;
-  const int64_t most = (int64_t)(pg.max_new > 0 && pg.max_new < pg.n_tokens ? pg.max_new : pg.n_tokens) * base.G;
-  return launch_join<true>(a.w, kWorkers, (int)(most < a.w.M ? most : a.w.M), out, lse, st);
+  return launch_join<true>(a.w, kWorkers, (int)(most * base.G < a.w.M ? most * base.G : a.w.M), out, lse, st);
 }
 
 }  // namespace ckv

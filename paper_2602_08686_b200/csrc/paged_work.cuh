@@ -17,9 +17,10 @@ struct WorkArgs {
   int Nu, H, Hkv, G, T, causal;
   int M;            // query rows of a block
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
-  int tile;         // keys per tile
+  int tile, log_tile;   // keys per tile
   int granule;      // least cost per worker, at least that of a tile
   int rounds;       // whether to hand out whole items first (units may have several blocks, which share keys and values)
+  int one_warp;     // few pairs of few blocks each: one warp makes the schedule
   int P, log_p, n_pages, max_pages;
   const int32_t *starts, *lengths, *table;
   int* status;
@@ -28,6 +29,15 @@ struct WorkArgs {
   float* o;         // [workers][2][slot_rows][128]
   int slot_rows;
 };
+
+// Block and tile sizes of a kernel; units have at most `most` tokens.
+constexpr int kWarpPairs = 128, kWarpBlocks = 8;
+inline void set_blocks(WorkArgs& a, int64_t most, int M, int tokens, int tile, int granule) {
+  a.M = M, a.tokens = tokens, a.tile = tile, a.granule = granule;
+  for (a.log_tile = 0; (1 << a.log_tile) < tile;) ++a.log_tile;
+  a.rounds = tokens > 0 && most > tokens;
+  a.one_warp = (int64_t)a.Nu * a.Hkv <= kWarpPairs && !a.rounds && most * a.G <= (int64_t)kWarpBlocks * M;
+}
 
 struct Item {
   int u, g, block;       // block of rows
@@ -55,7 +65,7 @@ __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, 
   const int end = a.tokens ? (block + 1) * a.tokens : ((block + 1) * a.M >= n * a.G ? n : ((block + 1) * a.M + a.G - 1) / a.G);
   return min(max(len - n + min(end, n), 0), len);
 }
-__device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) / a.tile, 1); }
+__device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) >> a.log_tile, 1); }
 
 // Cost of a key tile: one, where blocks are one tile of query rows.  Where they are two tiles of whole tokens, a key tile takes
 // 2 us if the tokens fill both and 1.35 us if they fill one: 3 and 2.
@@ -84,7 +94,7 @@ __device__ __forceinline__ Item item_of(const WorkArgs& a, int pair, int block, 
 constexpr int kMaxRounds = 8;
 struct Plan {           // in shared memory
   long long warp_sum[16];
-  long long total;
+  int warp_items[16], warp_most[16];
   long long begin, end; // the worker's share, relative to the cost before the item it starts in
   int pair, block;      // that item
   Item it;              // what is known of the worker's first item
@@ -93,7 +103,6 @@ struct Plan {           // in shared memory
   int2 round[kMaxRounds];                      // (pair, block) of the worker's
   long long before[kMaxRounds + 1];            // cost of the items before round k
   long long mine[kMaxRounds], cost[kMaxRounds]; // cost of the items before the worker's of the round, and its own
-  int warp_items[16], n_items, max_cost;
 };
 
 __device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p) {
@@ -104,6 +113,10 @@ __device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p) {
   for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
   return c;
 }
+// 32-bit divisions where they do: the plan is all latency.
+__device__ __forceinline__ long long part_of(long long total, int worker, int workers) {
+  return total < (1 << 24) ? (long long)((unsigned)total * (unsigned)worker / (unsigned)workers) : total * worker / workers;
+}
 // The share [begin, end) of a worker.
 __device__ __forceinline__ void share_of(const WorkArgs& a, long long total, int worker, int n_workers, long long& begin,
                                          long long& end) {
@@ -113,12 +126,7 @@ __device__ __forceinline__ void share_of(const WorkArgs& a, long long total, int
   const int workers = (int)(most < n_workers ? most : n_workers);
   begin = end = total;
   if (worker < workers) {
-    if (total < (1 << 24)) {   // 32-bit divisions where they do: the plan is all latency
-      begin = (unsigned)total * (unsigned)worker / (unsigned)workers;
-      end = (unsigned)total * (unsigned)(worker + 1) / (unsigned)workers;
-    } else {
-      begin = total * worker / workers, end = total * (worker + 1) / workers;
-    }
+    begin = part_of(total, worker, workers), end = part_of(total, worker + 1, workers);
   }
 }
 // Where in pair p's cost offset `at` falls, for a share of `width`.
@@ -135,20 +143,19 @@ __device__ __forceinline__ void settle_plan(const WorkArgs& a, int p, long long 
   plan.it = item_of(a, p, b, first, n, len, at, at + width);
 }
 
-// All threads of the CTA.  Returns with the worker's share in `plan`.  Up to kWarpPairs (unit, KV head) pairs one warp does it
-// alone, without barriers; beyond, and with rounds, every thread has its pairs.
+// All threads of the CTA.  Returns with the worker's share in `plan`.  Few (unit, KV head) pairs of few blocks one warp does
+// alone, without barriers; else every thread has its pairs or, where there are more threads, its blocks of a pair (one thread a
+// pair: 22 us for the 32 blocks of 2048 tokens, 4 this way).
 //
 // With rounds: while the most expensive item costs less than a fair share, the first items go out whole, one to each worker and
 // round, and only the rest is split, so that the shares even out.  In a round all workers start at the first key of
 // neighbouring blocks: they read the same keys and values at the same time, from L2 (shares cut end to end start all over
 // the cache: 2.65 GB from memory instead of 0.17 for four 2048-token chunks on 8192 rows).
-constexpr int kWarpPairs = 128;
 template <int NT>
 __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& plan) {
   const int pairs = a.Nu * a.Hkv;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) plan.n_rounds = 0, plan.max_cost = 0;
-  if (pairs <= kWarpPairs && !a.rounds) {
+  if (a.one_warp) {
     if (warp == 0) {
       constexpr int kPer = kWarpPairs / 32;
       const int per = (pairs + 31) / 32;
@@ -167,6 +174,7 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
       long long begin, end;
       share_of(a, __shfl_sync(0xffffffffu, incl, 31), worker, n_workers, begin, end);
       long long at = begin - (incl - mine), off = -1;
+      if (lane == 0) plan.n_rounds = 0;
       if (begin >= end) {
         if (lane == 0) plan.begin = plan.end = 0;
       } else if (at >= 0 && at < mine) {
@@ -183,20 +191,27 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
     return;
   }
   static_assert(NT <= 512, "one entry of warp_sum per warp");
-  const int per = (pairs + NT - 1) / NT;
-  const int p0 = min((int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
+  // the thread's items, in order: all blocks of the pairs p0 to p1, or part of the blocks of pair p0
+  int log_group = 0;
+  while (log_group < 5 && (pairs << (log_group + 1)) <= NT) ++log_group;
+  const int per = (pairs + NT - 1) / NT, sub = threadIdx.x & ((1 << log_group) - 1);
+  const int p0 = min(log_group ? (int)threadIdx.x >> log_group : (int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
+  auto each = [&](auto&& f) {   // f(pair, block, first, n, len, cost) until it says stop
+    for (int p = p0; p < p1; ++p) {
+      int first, n;
+      unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
+      const int len = head_length(a, p), nb = unit_blocks(a, n);
+      const int b1 = (nb * (sub + 1)) >> log_group;
+      for (int b = (nb * sub) >> log_group; b < b1; ++b)
+        if (f(p, b, first, n, len, tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b))) return;
+    }
+  };
   long long mine = 0;
   int items = 0, most = 0;
-  for (int p = p0; p < p1; ++p) {
-    int first, n;
-    unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
-    const int len = head_length(a, p), nb = unit_blocks(a, n);
-    for (int b = 0; b < nb; ++b) {
-      const int c = tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
-      mine += c, most = max(most, c);
-    }
-    items += nb;
-  }
+  each([&](int, int, int, int, int, int c) {
+    mine += c, most = max(most, c), ++items;
+    return false;
+  });
   long long incl = mine;
   int incl_items = items;
 #pragma unroll
@@ -205,61 +220,41 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
     const int i = __shfl_up_sync(0xffffffffu, incl_items, d);
     if (lane >= d) incl += o, incl_items += i;
   }
-  if (lane == 31) plan.warp_sum[warp] = incl, plan.warp_items[warp] = incl_items;
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 31) plan.warp_sum[warp] = incl, plan.warp_items[warp] = incl_items, plan.warp_most[warp] = most;
   __syncthreads();
-  if (a.rounds) atomicMax(&plan.max_cost, most);
-  if (threadIdx.x == 0) {
-    long long s = 0;
-    int n = 0;
-    for (int w = 0; w < NT / 32; ++w) {
-      const long long x = plan.warp_sum[w];
-      const int i = plan.warp_items[w];
-      plan.warp_sum[w] = s, plan.warp_items[w] = n;
-      s += x, n += i;
-    }
-    plan.total = s, plan.n_items = n;
+  long long before = incl - mine, total = 0;
+  int items_before = incl_items - items, n_items = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    if (w < warp) before += plan.warp_sum[w], items_before += plan.warp_items[w];
+    total += plan.warp_sum[w], n_items += plan.warp_items[w], most = max(most, plan.warp_most[w]);
   }
-  __syncthreads();
-  const long long before = plan.warp_sum[warp] + incl - mine, total = plan.total;
-  const int items_before = plan.warp_items[warp] + incl_items - items, n_items = plan.n_items;
   int rounds = 0;
   if (a.rounds && total / a.granule >= n_workers)   // every worker keeps at least `granule` of the rest
-    rounds = (int)min(min((total / n_workers - a.granule) / plan.max_cost, (long long)(n_items / n_workers)), (long long)kMaxRounds);
+    rounds = (int)min(min((total / n_workers - a.granule) / most, (long long)(n_items / n_workers)), (long long)kMaxRounds);
   long long begin, end;
   if (rounds > 0) {
     // the thread that has an item says which it is and what comes before it
-    auto look_up = [&](int index, int k, bool own) {
-      if (index < items_before || index >= items_before + items) return;
-      int i = index - items_before;
-      long long c = before;
-      for (int p = p0; p < p1; ++p) {
-        int first, n;
-        unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
-        const int len = head_length(a, p), nb = unit_blocks(a, n);
-        for (int b = 0; b < min(i, nb); ++b) c += tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
-        if (i < nb) {
-          if (!own) {
-            plan.before[k] = c;
-          } else {
-            const Item it = item_of(a, p, i, first, n, len, 0, 1ll << 40);
-            plan.mine[k] = c, plan.cost[k] = (long long)it.tiles * it.weight, plan.round[k] = make_int2(p, i);
-            if (k == 0) plan.it = it;
-          }
-          return;
-        }
-        i -= nb;
-      }
-    };
     for (int k = 0; k <= rounds; ++k) {
-      look_up(k * n_workers, k, false);
-      if (k < rounds) look_up(k * n_workers + worker, k, true);
+      const int head = k * n_workers - items_before, own = k < rounds ? head + worker : -1;   // of the thread's items
+      if ((head < 0 || head >= items) && (own < 0 || own >= items)) continue;
+      int i = 0;
+      long long c = before;
+      each([&](int p, int b, int first, int n, int len, int cost) {
+        if (i == head) plan.before[k] = c;
+        if (i == own) {
+          plan.mine[k] = c, plan.cost[k] = cost, plan.round[k] = make_int2(p, b);
+          if (k == 0) plan.it = item_of(a, p, b, first, n, len, 0, 1ll << 40);
+        }
+        ++i, c += cost;
+        return false;
+      });
     }
-    if (threadIdx.x == 0) {
-      plan.n_rounds = rounds;
-      if (rounds * n_workers == n_items) plan.before[rounds] = total;
-    }
+    if (threadIdx.x == 0 && rounds * n_workers == n_items) plan.before[rounds] = total;
     __syncthreads();
-    begin = plan.before[rounds] + total * worker / n_workers, end = plan.before[rounds] + total * (worker + 1) / n_workers;
+    const long long rest = plan.before[rounds];
+    begin = rest + part_of(total, worker, n_workers), end = rest + part_of(total, worker + 1, n_workers);
     for (int k = 0; k < rounds; ++k) {
       const long long handed = plan.mine[k] - plan.before[k];
       begin -= handed, end -= handed + plan.cost[k];
@@ -267,19 +262,21 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
   } else {
     share_of(a, total, worker, n_workers, begin, end);
   }
-  if (threadIdx.x == 0 && begin >= end) plan.begin = plan.end = 0;
+  if (threadIdx.x == 0) {
+    plan.n_rounds = rounds;
+    if (begin >= end) plan.begin = plan.end = 0;
+  }
   if (end > begin && begin >= before && begin < before + mine) {
     long long at = begin - before;
-    for (int p = p0; p < p1; ++p) {
-      const long long c = pair_cost(a, p);
-      if (at < c) {
-        const Item first = plan.it;
-        settle_plan(a, p, at, end - begin, plan);
-        if (rounds > 0) plan.it = first;
-        break;
+    each([&](int p, int b, int first, int n, int len, int cost) {
+      if (at >= cost) {
+        at -= cost;
+        return false;
       }
-      at -= c;
-    }
+      plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + (end - begin);
+      if (rounds == 0) plan.it = item_of(a, p, b, first, n, len, at, at + (end - begin));
+      return true;
+    });
   }
   __syncthreads();
 }
@@ -395,15 +392,14 @@ __device__ __forceinline__ int page_of(const WorkArgs& a, const Item& it, int sl
 constexpr int kWorkers = 148;        // CTAs of every attention kernel, one per SM
 constexpr int kTcRows = 256;         // query rows of a block of the tensor-core kernel
 
-// `base`: everything but the block and tile sizes; scale not 0.
-cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, float scale, const void* q, const void* k_pages,
+// `base`: everything but the block and tile sizes; most: the tokens a unit is expected to have at most; scale not 0.
+cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                              const void* v_pages, void* out, float* lse, cudaStream_t st);
 constexpr int kMmaRows = 32;         // most query rows of a block of the bf16 kernel for few rows
 constexpr int kMmaTile = 64;         // keys per tile of its schedule
 constexpr int kMmaCtaKeys = 128;     // keys a CTA of it takes per step
 int cluster_size(const ckv_paged& pg, int cta_keys);   // CTAs per cluster where the cache is short, else 0
-// rows: the most query rows per KV head that a unit is expected to have.
-cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int rows, float scale, const void* q, const void* k_pages,
+cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
 // rows: the most query rows a block has.
 template <bool BF16>
