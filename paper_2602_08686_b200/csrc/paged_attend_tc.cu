@@ -16,7 +16,7 @@
 // common factor costs none of their bits.  So a row keeps the reference of its first visible step, and the sums tell
 // whether an exponential left the range (2^64: then, and only then, the maximum is taken, O is rescaled in TMEM and
 // the step is done again).
-// Warps 0-3 and 4-7: softmax of stream 0 and 1; warps 8, 9: their MMAs; warp 10: TMA.
+// Warps 0-3 and 4-7: softmax of stream 0 and 1; warps 8, 9: their MMAs; warp 10: TMA; warp 11 walks the items ahead of the others.
 // Every wait is bounded and reports CKV_ERR_TIMEOUT through the status word.
 #include "paged_work.cuh"
 #include "tc_ptx.cuh"
@@ -26,13 +26,14 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 352;
+constexpr int kThreads = 384;
 constexpr int kStages = 5;
 constexpr int kTile = 128, kStep = 64;         // keys of a tile, and of a step
 constexpr uint32_t kHalf = 128 * 128;          // 128 rows x 64 bf16
 constexpr uint32_t kTileBytes = 2 * kHalf;
 constexpr int kTcGranule = kBothTiles;         // least cost a CTA takes on (twice that: 31 us instead of 27 for 40 tokens on 2048 rows)
 constexpr int kInfo = 8;                       // ring of per-tile notes from the loader
+constexpr int kJobs = 4;                       // ring of items
 constexpr float kOverflow = 1.8446744e19f;     // 2^64: a step's sum above it is done again with a new reference
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);   // fp32 += bf16 * bf16, M = 128
 constexpr uint32_t kIdescQK = kIdesc | ((64u >> 3) << 17);
@@ -57,6 +58,17 @@ struct TcArgs {
   float* lse;
 };
 
+// An item, as the roles need it.
+struct Job {
+  Item it;
+  int pair, block;       // where it comes from
+  int n;                 // key tiles (0: there are no more items)
+  int tiles2;            // whether it has two query tiles
+  int steps;             // of each stream
+  int see;               // rows that every token of the block sees: those its first token does
+  int whole;             // not a part
+};
+
 struct __align__(1024) Smem {
   uint8_t kv[kStages][kTileBytes];
   uint8_t q[2][kTileBytes];
@@ -65,9 +77,11 @@ struct __align__(1024) Smem {
   uint64_t clean;                               // a value tile has been looked at
   uint64_t s_full[2][2], p_full[2][2], pv_done[2], item_done[2];   // [stream][buffer]
   uint64_t join_full, join_done;                // stream 1's result is there; stream 0 has read it
+  uint64_t job_full[kJobs], job_empty[kJobs];
+  Job jobs[kJobs];
   float2 other[kTile];                          // stream 1's maximum and sum per row
   uint32_t bad[kInfo];                          // which pages of a key tile are missing (bit per page)
-  uint32_t odd[kInfo][4];                       // which rows of a value tile were not finite and have been zeroed
+  __align__(16) uint32_t odd[kInfo][4];                       // which rows of a value tile were not finite and have been zeroed
   Plan plan;
   uint32_t tmem_base;
   int abort_flag;
@@ -87,30 +101,59 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
 
 // How an item is cut up.  Two query tiles: each stream has one, and takes both halves of every key tile.  One query tile (the
 // tokens fill no more than half of the block): both streams work on it, each on its half of every key tile, and join at the end.
-__device__ __forceinline__ bool paired(const Item& it) { return it.weight == kBothTiles; }
-
-// Rows that every token of the block sees: those its first token does.
-__device__ __forceinline__ int all_see(const TcArgs& a, const Item& it) {
-  return a.w.causal ? min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len) : it.len;
+//
+// One warp looks the items up for all (lengths, token counts, divisions: 2000 to 6000 clocks each where every warp did it between
+// two items).
+__device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter& w, int lane) {
+  Walk k;
+  k.start(a.w, sm.plan);
+  // this wait takes as long as an item does; the others are for one step's work
+  const Waiter patient{w.abort_flag, w.status, 64 * w.limit_ns};
+  for (uint32_t i = 0;; ++i) {
+    if (!wait_warp(smem_u32(&sm.job_empty[i % kJobs]), ((i / kJobs) & 1) ^ 1, patient, 10)) return;
+    if (lane == 0) {
+      Job& job = sm.jobs[i % kJobs];
+      job.n = 0;
+      if (k.live) {
+        const Item& it = k.it;
+        job.it = it, job.pair = k.pair, job.block = k.block;
+        job.n = it.t1 - it.t0, job.tiles2 = it.weight == kBothTiles, job.steps = job.tiles2 ? 2 * job.n : job.n;
+        job.see = a.w.causal ? min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len) : it.len;
+        job.whole = it.t0 == 0 && it.t1 == it.tiles;
+      }
+      bar_arrive(smem_u32(&sm.job_full[i % kJobs]));
+    }
+    if (!k.live) return;
+    k.next(a.w, sm.plan);
+  }
 }
+// The i-th item, for a warp that arrives on its `job_empty` when it is done with it; null: a wait has given up.
+__device__ __forceinline__ const Job* job_of(Smem& sm, uint32_t i, const Waiter& w) {
+  return wait_warp(smem_u32(&sm.job_full[i % kJobs]), (i / kJobs) & 1, w, 11) ? &sm.jobs[i % kJobs] : nullptr;
+}
+__device__ __forceinline__ void job_done(Smem& sm, uint32_t i, int lane) {
+  __syncwarp();
+  if (lane == 0) bar_arrive(smem_u32(&sm.job_empty[i % kJobs]));
+}
+
 // First row of the item's j-th key tile that the block's first token does not see (128: it sees them all).  Where every
 // token sees every row there is none.
-__device__ __forceinline__ int late_row(const TcArgs& a, const Item& it, int j) {
-  return a.w.causal ? min(max(all_see(a, it) - (it.t0 + j) * kTile, 0), kTile) : kTile;
+__device__ __forceinline__ int late_row(const TcArgs& a, const Job& job, int j) {
+  return a.w.causal ? min(max(job.see - (job.it.t0 + j) * kTile, 0), kTile) : kTile;
 }
 
 __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUtensorMap* qm, const CUtensorMap* km,
                                           const CUtensorMap* vm, const Waiter& w, int lane) {
-  Walk k;
-  k.start(a.w, sm.plan);
-  uint32_t n_loads = 0, n_items = 0, n_tiles = 0;
+  uint32_t n_loads = 0, n_tiles = 0;
   const int slot_of_lane = lane >> 1, half = lane & 1;
   const uint64_t first = evict_first();
   const bool copies = slot_of_lane < a.pages_per_tile;
   const int tiles_per_page = a.w.P > kTile ? a.w.P / kTile : 1;
-  for (; k.live; k.next(a.w, sm.plan)) {
-    const Item& it = k.it;
-    const int ns = paired(it) ? 2 : 1;
+  for (uint32_t n_items = 0;; ++n_items) {
+    const Job* job = job_of(sm, n_items, w);
+    if (!job || job->n == 0) return;
+    const Item& it = job->it;
+    const int ns = job->tiles2 ? 2 : 1, t0 = it.t0, t1 = it.t1, visible = it.visible;
     // Keys and values that one block alone reads leave L2 first: what every call needs again (code, tables, lengths) is then not
     // streamed out of it, and the next call does not start with misses (49 us instead of 62 for 8 x 5 tokens on 16k).
     const bool once = it.n <= a.w.tokens;
@@ -123,9 +166,9 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
     const int32_t* table = a.w.table + ((int64_t)it.u * a.w.Hkv + it.g) * a.w.max_pages;
     // the pages that hold visible rows of a tile, looked up a tile ahead
     auto row_of = [&](int t) { return t * kTile + slot_of_lane * (a.w.P < kTile ? a.w.P : kTile); };
-    auto wants = [&](int t) { return copies && t < it.t1 && row_of(t) < it.visible; };
-    int next_page = wants(it.t0) ? table[row_of(it.t0) >> a.w.log_p] : 0;
-    for (int t = it.t0; t < it.t1; ++t, ++n_tiles) {
+    auto wants = [&](int t) { return copies && t < t1 && row_of(t) < visible; };
+    int next_page = wants(t0) ? table[row_of(t0) >> a.w.log_p] : 0;
+    for (int t = t0; t < t1; ++t, ++n_tiles) {
       const bool wanted = wants(t);
       const int page = next_page;
       if (wants(t + 1)) next_page = table[row_of(t + 1) >> a.w.log_p];
@@ -155,16 +198,16 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
         }
       }
     }
-    ++n_items;
+    job_done(sm, n_items, lane);
   }
 }
 
 // 0 * NaN is not 0: value rows that no query sees are zeroed, and so are rows with an infinity or a NaN that some of the
 // block's tokens do not see yet (the softmax threads add those to the tokens that do).  Each MMA warp has half of the tile's
 // rows; reads go out eight at a time (one warp, row by row: 3400 clocks, most of them ahead of the item's last product).
-__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Item& it, int j, uint32_t slot, uint32_t n_tiles,
+__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Job& job, int j, uint32_t slot, uint32_t n_tiles,
                                              int s, int lane) {
-  const int lo = s * kStep, hi = lo + kStep, valid = it.visible - (it.t0 + j) * kTile;
+  const int lo = s * kStep, hi = lo + kStep, valid = job.it.visible - (job.it.t0 + j) * kTile;
   const uint32_t bad = *(volatile uint32_t*)&sm.bad[n_tiles % kInfo];
   uint4* v = reinterpret_cast<uint4*>(sm.kv[slot]);
   uint32_t* odd = sm.odd[n_tiles % kInfo];
@@ -173,7 +216,7 @@ __device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const It
   const int piece = (lane & 8) * kTile + (lane & 7);          // 16-byte piece lane & 15 of a row: its half, its place
   const int end = min(valid, hi);
 #pragma unroll 1
-  for (int r0 = max(late_row(a, it, j), lo); r0 < end; r0 += 16) {
+  for (int r0 = max(late_row(a, job, j), lo); r0 < end; r0 += 16) {
     uint32_t hit = 0;                                         // bit i: the piece of row r0 + 2 i (+ 1) has an exponent of all ones
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -214,21 +257,19 @@ struct Ring {
 // order S, O, next S: the tensor pipe runs them in that order, so S may take the columns that O reads P from without
 // waiting for it.
 __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int s, int lane) {
-  Walk k;
-  k.start(a.w, sm.plan);
-  uint32_t n_items = 0, n_tiles = 0, n_steps = 0, n_clean = 0;
+  uint32_t n_tiles = 0, n_steps = 0, n_clean = 0;
   Ring ring;                              // of the item's first key tile; two stages per tile: K, V
   const uint32_t kv0 = smem_u32(sm.kv[0]), full0 = smem_u32(&sm.full[0]), empty0 = smem_u32(&sm.empty[0]);
   const uint32_t s_cols = tmem + kColS + s * 128, o_cols = tmem + kColO + s * 128;
   const uint32_t bar_s = smem_u32(&sm.s_full[s][0]), bar_p = smem_u32(&sm.p_full[s][0]);
   const uint32_t bar_o = smem_u32(&sm.pv_done[s]), bar_item = smem_u32(&sm.item_done[s]);
-  for (; k.live; k.next(a.w, sm.plan)) {
-    const Item& it = k.it;
-    const int n = it.t1 - it.t0;
-    const bool pair = paired(it);
-    const int steps = pair ? 2 * n : n;
+  for (uint32_t n_items = 0;; ++n_items) {
+    const Job* job = job_of(sm, n_items, w);
+    if (!job || job->n == 0) return;
+    const bool pair = job->tiles2;
+    const int steps = job->steps;
     const uint32_t q_lo = desc_lo(smem_u32(sm.q[pair ? s : 0]), 16);
-    const int j_clean = max(all_see(a, it) / kTile - it.t0, 0);   // first tile whose values have to be looked at
+    const int j_clean = max(job->see / kTile - job->it.t0, 0);   // first tile whose values have to be looked at
     if (!wait_warp(smem_u32(&sm.q_full), n_items & 1, w, 4)) return;
     Ring kr = ring, vr = ring;
     vr.step();
@@ -257,7 +298,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
       if (!pair || h == 0) {   // a new tile of values
         if (!wait_warp(full0 + vr.slot * 8, vr.parity, w, 3)) return;
         if (j >= j_clean || *(volatile uint32_t*)&sm.bad[n_tiles % kInfo]) {
-          clean_values(a, sm, it, j, vr.slot, n_tiles, s, lane);
+          clean_values(a, sm, *job, j, vr.slot, n_tiles, s, lane);
           if (lane == 0) bar_arrive(smem_u32(&sm.clean));
           if (!wait_warp(smem_u32(&sm.clean), n_clean & 1, w, 9)) return;
           ++n_clean;
@@ -281,7 +322,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
     }
     n_steps += steps;
     ring = kr;
-    ++n_items;
+    job_done(sm, n_items, lane);
   }
 }
 
@@ -349,26 +390,23 @@ __device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o
   tmem_wait_st();
 }
 
-// The softmax threads' next item.  A call, so that the walk stays out of the step loop's registers (inlined: 975 us instead of
-// 925 for 2048 tokens over 32k rows).
-__device__ __noinline__ void advance(Walk& k, const WorkArgs& w, const Plan& plan) { k.next(w, plan); }
-
 __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int stream, int quarter,
                                              int lane) {
-  Walk k;
-  k.start(a.w, sm.plan);
-  uint32_t n_steps = 0, n_all = 0, n_items = 0, n_join = 0;   // steps of this stream so far; tiles, items; joins of the streams
-  const int r = quarter * 32 + lane;                        // row of the query tile
+  uint32_t n_steps = 0, n_all = 0, n_join = 0;              // steps of this stream so far; tiles; joins of the streams
+  const int r = quarter * 32 + lane;                        // row of the query tile: token, head
+  const int r_tok = r / a.w.G, r_head = r - r_tok * a.w.G;
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const uint32_t s_addr = tmem + lanes + kColS + stream * 128, o_addr = tmem + lanes + kColO + stream * 128;
   const uint32_t bar_s = smem_u32(&sm.s_full[stream][0]), bar_p = smem_u32(&sm.p_full[stream][0]), bar_o = smem_u32(&sm.pv_done[stream]);
-  while (k.live) {
-    const Item it = k.it;
-    const int n = it.t1 - it.t0;
-    const bool pair = paired(it);
-    const int steps = pair ? 2 * n : n, q_tile = pair ? stream : 0;
+  for (uint32_t n_items = 0;; ++n_items) {
+    const Job* job = job_of(sm, n_items, w);
+    if (!job || job->n == 0) return;
+    const Item& it = job->it;
+    const int n = job->n, t0 = it.t0;
+    const bool pair = job->tiles2;
+    const int steps = job->steps, q_tile = pair ? stream : 0;
     const int tok0 = it.block * a.w.tokens + q_tile * a.TQ;   // first token of the tile
-    const int token = tok0 + r / a.w.G;
+    const int token = tok0 + r_tok;
     const bool live = r < a.TQ * a.w.G && token < it.n;
     auto limit_of = [&](int tk) { return a.w.causal ? min(max(it.len - it.n + tk + 1, 0), it.len) : it.len; };
     const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
@@ -377,7 +415,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
 #pragma unroll 1
     for (int g = 0; g < steps; ++g, ++n_steps) {
       const int j = pair ? g >> 1 : g, h = pair ? g & 1 : stream;
-      const int key0 = (it.t0 + j) * kTile + h * kStep;
+      const int key0 = (t0 + j) * kTile + h * kStep;
       const uint32_t buf = n_steps & 1, s_buf = s_addr + buf * kStep;
       if (!wait_warp(bar_s + buf * 8, (n_steps >> 1) & 1, w, 6)) return;
       tc_fence_after();
@@ -416,17 +454,22 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       if (lane == 0) bar_arrive(bar_p + buf * 8);
       l += sum;
     }
-    // the item's output: normalised, or a partial result for the join (the next item's lengths are on their way meanwhile)
-    const int pair_of = k.pair, block_of = k.block;
-    advance(k, a.w, sm.plan);
+    // the item's output: normalised, or a partial result for the join
+    const bool whole = job->whole;
+    const int which = t0 > 0 ? 0 : 1;
+    const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.w.slot_rows + q_tile * a.TQ * a.w.G + r;   // its row of the block
+    const int64_t at = (int64_t)(it.first + token) * a.w.H + it.g * a.w.G + r_head;
+    __nv_bfloat16* out = a.out + at * kHeadDim;
+    float* part = a.w.o + slot * kHeadDim;
     if (!wait_warp(smem_u32(&sm.item_done[stream]), n_items & 1, w, 7)) return;
-    ++n_items;
     tc_fence_after();
     // value rows that were left out because they are not finite, for the tokens that see them
-    for (int j = n - 1; j >= 0 && late_row(a, it, j) < kTile; --j) {
+    for (int j = n - 1; j >= 0 && late_row(a, *job, j) < kTile; --j) {
+      const uint4 some = *reinterpret_cast<const uint4*>(sm.odd[(n_all + j) % kInfo]);
+      if (!(some.x | some.y | some.z | some.w)) continue;
       for (int x = pair ? 0 : 2 * stream; x < (pair ? 4 : 2 * stream + 2); ++x) {   // the stream's keys
-        uint32_t odd = *(volatile uint32_t*)&sm.odd[(n_all + j) % kInfo][x];
-        for (; odd; odd &= odd - 1) add_row(a, it, o_addr, (it.t0 + j) * kTile + x * 32 + __ffs(odd) - 1, limit, token, r % a.w.G, m);
+        uint32_t odd = sm.odd[(n_all + j) % kInfo][x];
+        for (; odd; odd &= odd - 1) add_row(a, it, o_addr, (t0 + j) * kTile + x * 32 + __ffs(odd) - 1, limit, token, r_head, m);
       }
     }
     n_all += n;
@@ -441,6 +484,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
         if (!wait_warp(smem_u32(&sm.join_done), n_join & 1, w, 8)) return;
         tc_fence_after();
         ++n_join;
+        job_done(sm, n_items, lane);
         continue;
       }
       if (!wait_warp(smem_u32(&sm.join_full), n_join & 1, w, 8)) return;
@@ -452,13 +496,8 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       l = l * f0 + x.y * f1, m = top;
     }
     const bool joined = !pair;
-    const bool whole = it.t0 == 0 && it.t1 == it.tiles;
-    const int which = it.t0 > 0 ? 0 : 1;
-    const int br = q_tile * a.TQ * a.w.G + r;                // row of the block
     const bool none = m == -INFINITY;
     const float inv = none ? 0.f : 1.0f / l;
-    const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.w.slot_rows + br;
-    const int64_t at = (int64_t)(it.first + token) * a.w.H + it.g * a.w.G + r % a.w.G;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       uint32_t o[32];
@@ -477,7 +516,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             p[e] = none ? 0u : bf16x2(__uint_as_float(o[16 * i + 2 * e]) * inv, __uint_as_float(o[16 * i + 2 * e + 1]) * inv);
-          st_global32(a.out + at * kHeadDim + c * 32 + i * 16, p);
+          st_global32(out + c * 32 + i * 16, p);
         }
       } else {
 #pragma unroll
@@ -485,7 +524,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
           uint32_t p[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) p[e] = o[8 * i + e];
-          st_global32(a.w.o + slot * kHeadDim + c * 32 + i * 8, p);
+          st_global32(part + c * 32 + i * 8, p);
         }
       }
     }
@@ -500,8 +539,9 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     }
     if (!whole && r == 0 && stream == 0) {
       int* sp = reinterpret_cast<int*>(a.w.split + blockIdx.x);
-      sp[2 * which] = pair_of, sp[2 * which + 1] = block_of;
+      sp[2 * which] = job->pair, sp[2 * which + 1] = job->block;
     }
+    job_done(sm, n_items, lane);
   }
 }
 
@@ -525,6 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       for (int b = 0; b < 2; ++b) bar_init(smem_u32(&sm.s_full[s][b]), 1), bar_init(smem_u32(&sm.p_full[s][b]), 4);
     }
     bar_init(smem_u32(&sm.join_full), 4), bar_init(smem_u32(&sm.join_done), 4);
+    for (int i = 0; i < kJobs; ++i) bar_init(smem_u32(&sm.job_full[i]), 1), bar_init(smem_u32(&sm.job_empty[i]), 11);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
     sm.abort_flag = 0;
@@ -541,7 +582,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   const Waiter w{&sm.abort_flag, a.w.status, a.wait_ns};
   if (warp < 8) softmax_role(a, sm, tmem, w, warp >> 2, warp & 3, lane);
   else if (warp < 10) mma_role(a, sm, tmem, w, warp - 8, lane);
-  else load_role(a, sm, &qm, &km, &vm, w, lane);
+  else if (warp == 10) load_role(a, sm, &qm, &km, &vm, w, lane);
+  else job_role(a, sm, w, lane);
   tc_fence_before();
   __syncthreads();
   if (sm.abort_flag) {   // a wait gave up: let copies and products in flight land before the memory is given back
