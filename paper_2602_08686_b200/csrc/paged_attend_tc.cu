@@ -67,6 +67,7 @@ struct Job {
   int steps;             // of each stream
   int see;               // rows that every token of the block sees: those its first token does
   int whole;             // not a part
+  int odd;               // some value rows have been zeroed that tokens see
 };
 
 struct __align__(1024) Smem {
@@ -81,7 +82,7 @@ struct __align__(1024) Smem {
   Job jobs[kJobs];
   float2 other[kTile];                          // stream 1's maximum and sum per row
   uint32_t bad[kInfo];                          // which pages of a key tile are missing (bit per page)
-  __align__(16) uint32_t odd[kInfo][4];                       // which rows of a value tile were not finite and have been zeroed
+  uint32_t odd[kInfo][4];                       // which rows of a value tile were not finite and have been zeroed
   Plan plan;
   uint32_t tmem_base;
   int abort_flag;
@@ -120,6 +121,7 @@ __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter
         job.n = it.t1 - it.t0, job.tiles2 = it.weight == kBothTiles, job.steps = job.tiles2 ? 2 * job.n : job.n;
         job.see = a.w.causal ? min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len) : it.len;
         job.whole = it.t0 == 0 && it.t1 == it.tiles;
+        job.odd = 0;
       }
       bar_arrive(smem_u32(&sm.job_full[i % kJobs]));
     }
@@ -128,7 +130,7 @@ __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter
   }
 }
 // The i-th item, for a warp that arrives on its `job_empty` when it is done with it; null: a wait has given up.
-__device__ __forceinline__ const Job* job_of(Smem& sm, uint32_t i, const Waiter& w) {
+__device__ __forceinline__ Job* job_of(Smem& sm, uint32_t i, const Waiter& w) {
   return wait_warp(smem_u32(&sm.job_full[i % kJobs]), (i / kJobs) & 1, w, 11) ? &sm.jobs[i % kJobs] : nullptr;
 }
 __device__ __forceinline__ void job_done(Smem& sm, uint32_t i, int lane) {
@@ -150,7 +152,7 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
   const bool copies = slot_of_lane < a.pages_per_tile;
   const int tiles_per_page = a.w.P > kTile ? a.w.P / kTile : 1;
   for (uint32_t n_items = 0;; ++n_items) {
-    const Job* job = job_of(sm, n_items, w);
+    Job* job = job_of(sm, n_items, w);
     if (!job || job->n == 0) return;
     const Item& it = job->it;
     const int ns = job->tiles2 ? 2 : 1, t0 = it.t0, t1 = it.t1, visible = it.visible;
@@ -205,7 +207,7 @@ __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUten
 // 0 * NaN is not 0: value rows that no query sees are zeroed, and so are rows with an infinity or a NaN that some of the
 // block's tokens do not see yet (the softmax threads add those to the tokens that do).  Each MMA warp has half of the tile's
 // rows; reads go out eight at a time (one warp, row by row: 3400 clocks, most of them ahead of the item's last product).
-__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Job& job, int j, uint32_t slot, uint32_t n_tiles,
+__device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, Job& job, int j, uint32_t slot, uint32_t n_tiles,
                                              int s, int lane) {
   const int lo = s * kStep, hi = lo + kStep, valid = job.it.visible - (job.it.t0 + j) * kTile;
   const uint32_t bad = *(volatile uint32_t*)&sm.bad[n_tiles % kInfo];
@@ -232,7 +234,7 @@ __device__ __forceinline__ void clean_values(const TcArgs& a, Smem& sm, const Jo
       const uint32_t any = __ballot_sync(0xffffffffu, hit >> i & 1u);
       if ((any >> (lane & 16)) & 0xffffu) {
         v[piece + row * 8] = make_uint4(0u, 0u, 0u, 0u);
-        if ((lane & 15) == 0) atomicOr(&odd[row >> 5], 1u << (row & 31));
+        if ((lane & 15) == 0) atomicOr(&odd[row >> 5], 1u << (row & 31)), job.odd = 1;
       }
     }
   }
@@ -264,7 +266,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
   const uint32_t bar_s = smem_u32(&sm.s_full[s][0]), bar_p = smem_u32(&sm.p_full[s][0]);
   const uint32_t bar_o = smem_u32(&sm.pv_done[s]), bar_item = smem_u32(&sm.item_done[s]);
   for (uint32_t n_items = 0;; ++n_items) {
-    const Job* job = job_of(sm, n_items, w);
+    Job* job = job_of(sm, n_items, w);
     if (!job || job->n == 0) return;
     const bool pair = job->tiles2;
     const int steps = job->steps;
@@ -320,6 +322,7 @@ __device__ __forceinline__ void mma_role(const TcArgs& a, Smem& sm, uint32_t tme
       if (!pair || h == 1) vr.step(), vr.step();
       if (g + 2 < steps && !qk(g + 2)) return;
     }
+    if (lane == 0) bar_arrive(bar_item);   // releases what clean_values wrote
     n_steps += steps;
     ring = kr;
     job_done(sm, n_items, lane);
@@ -399,7 +402,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
   const uint32_t s_addr = tmem + lanes + kColS + stream * 128, o_addr = tmem + lanes + kColO + stream * 128;
   const uint32_t bar_s = smem_u32(&sm.s_full[stream][0]), bar_p = smem_u32(&sm.p_full[stream][0]), bar_o = smem_u32(&sm.pv_done[stream]);
   for (uint32_t n_items = 0;; ++n_items) {
-    const Job* job = job_of(sm, n_items, w);
+    Job* job = job_of(sm, n_items, w);
     if (!job || job->n == 0) return;
     const Item& it = job->it;
     const int n = job->n, t0 = it.t0;
@@ -464,9 +467,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     if (!wait_warp(smem_u32(&sm.item_done[stream]), n_items & 1, w, 7)) return;
     tc_fence_after();
     // value rows that were left out because they are not finite, for the tokens that see them
-    for (int j = n - 1; j >= 0 && late_row(a, *job, j) < kTile; --j) {
-      const uint4 some = *reinterpret_cast<const uint4*>(sm.odd[(n_all + j) % kInfo]);
-      if (!(some.x | some.y | some.z | some.w)) continue;
+    for (int j = n - 1; job->odd && j >= 0 && late_row(a, *job, j) < kTile; --j) {
       for (int x = pair ? 0 : 2 * stream; x < (pair ? 4 : 2 * stream + 2); ++x) {   // the stream's keys
         uint32_t odd = sm.odd[(n_all + j) % kInfo][x];
         for (; odd; odd &= odd - 1) add_row(a, it, o_addr, (t0 + j) * kTile + x * 32 + __ffs(odd) - 1, limit, token, r_head, m);
@@ -561,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     for (int i = 0; i < kStages; ++i) bar_init(smem_u32(&sm.full[i]), 1), bar_init(smem_u32(&sm.empty[i]), 2);
     bar_init(smem_u32(&sm.q_full), 1), bar_init(smem_u32(&sm.q_empty), 2), bar_init(smem_u32(&sm.clean), 2);
     for (int s = 0; s < 2; ++s) {
-      bar_init(smem_u32(&sm.pv_done[s]), 1), bar_init(smem_u32(&sm.item_done[s]), 1);
+      bar_init(smem_u32(&sm.pv_done[s]), 1), bar_init(smem_u32(&sm.item_done[s]), 2);
       for (int b = 0; b < 2; ++b) bar_init(smem_u32(&sm.s_full[s][b]), 1), bar_init(smem_u32(&sm.p_full[s][b]), 4);
     }
     bar_init(smem_u32(&sm.join_full), 4), bar_init(smem_u32(&sm.join_done), 4);
