@@ -31,7 +31,7 @@ constexpr int kStages = 5;
 constexpr int kTile = 128, kStep = 64;         // keys of a tile, and of a step
 constexpr uint32_t kHalf = 128 * 128;          // 128 rows x 64 bf16
 constexpr uint32_t kTileBytes = 2 * kHalf;
-constexpr int kTcGranule = kBothTiles;         // least cost a CTA takes on (twice that: 31 us instead of 27 for 40 tokens on 2048 rows)
+constexpr int kTcGranule = kBothTiles;         // least cost a CTA takes on (two tiles: 31 us instead of 27 for 40 tokens on 2048 rows)
 constexpr int kInfo = 8;                       // ring of per-tile notes from the loader
 constexpr int kJobs = 4;                       // ring of items
 constexpr float kOverflow = 1.8446744e19f;     // 2^64: a step's sum above it is done again with a new reference
@@ -118,7 +118,7 @@ __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter
       if (k.live) {
         const Item& it = k.it;
         job.it = it, job.pair = k.pair, job.block = k.block;
-        job.n = it.t1 - it.t0, job.tiles2 = it.weight == kBothTiles, job.steps = job.tiles2 ? 2 * job.n : job.n;
+        job.n = it.t1 - it.t0, job.tiles2 = both_tiles(a.w, it.n, it.block), job.steps = job.tiles2 ? 2 * job.n : job.n;
         job.see = a.w.causal ? min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len) : it.len;
         job.whole = it.t0 == 0 && it.t1 == it.tiles;
         job.odd = 0;

@@ -18,7 +18,7 @@ struct WorkArgs {
   int M;            // query rows of a block
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
   int tile, log_tile;   // keys per tile
-  int granule;      // least cost per worker, at least that of a tile
+  int granule;      // least cost per worker (a tile, where that costs more)
   int rounds;       // whether to hand out whole items first (units may have several blocks, which share keys and values)
   int one_warp;     // few pairs of few blocks each: one warp makes the schedule
   int P, log_p, n_pages, max_pages;
@@ -67,11 +67,16 @@ __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, 
 }
 __device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) >> a.log_tile, 1); }
 
-// Cost of a key tile: one, where blocks are one tile of query rows.  Where they are two tiles of whole tokens, a key tile takes
-// 2 us if the tokens fill both and 1.35 us if they fill one: 3 and 2.
-constexpr int kBothTiles = 3, kOneTile = 2;
-__device__ __forceinline__ int weight_of(const WorkArgs& a, int n, int block) {
-  return !a.tokens ? 1 : (2 * (n - block * a.tokens) > a.tokens ? kBothTiles : kOneTile);
+// Whether a block of two tiles of query rows has rows in both.
+__device__ __forceinline__ bool both_tiles(const WorkArgs& a, int n, int block) { return 2 * (n - block * a.tokens) > a.tokens; }
+// Cost of one of an item's key tiles: one, where blocks are one tile of query rows.  Where they are two tiles of whole tokens, a key
+// tile takes 2.1 us if the tokens fill both and 1.15 us if they fill one: 9 and 5.  What an item takes besides (its last
+// product, its output: 4.8 and 2.7 us) is spread over its tiles.
+constexpr int kBothTiles = 9, kOneTile = 5, kBothItem = 20, kOneItem = 12;
+__device__ __forceinline__ int weight_of(const WorkArgs& a, int n, int block, int tiles) {
+  if (!a.tokens) return 1;
+  const bool both = both_tiles(a, n, block);
+  return (both ? kBothTiles : kOneTile) + (int)((unsigned)(both ? kBothItem : kOneItem) / (unsigned)tiles);
 }
 
 // The item at (pair, block) of a unit whose tokens and a head whose length are known: its tiles whose cost begins in [begin, end),
@@ -84,7 +89,7 @@ __device__ __forceinline__ Item item_of(const WorkArgs& a, int pair, int block, 
   it.rows = n * a.G;
   it.visible = block_visible(a, n, len, block);
   it.tiles = tiles_of(a, it.visible);
-  it.weight = weight_of(a, n, block);
+  it.weight = weight_of(a, n, block, it.tiles);
   const long long cost = (long long)it.tiles * it.weight;
   const int from = (int)(begin < cost ? begin : cost), to = (int)(end < cost ? end : cost);
   it.t0 = (from + it.weight - 1) / it.weight, it.t1 = (to + it.weight - 1) / it.weight;
@@ -94,7 +99,8 @@ __device__ __forceinline__ Item item_of(const WorkArgs& a, int pair, int block, 
 constexpr int kMaxRounds = 8;
 struct Plan {           // in shared memory
   long long warp_sum[16];
-  int warp_items[16], warp_most[16];
+  int warp_items[16];
+  int2 warp_most[16];
   long long begin, end; // the worker's share, relative to the cost before the item it starts in
   int pair, block;      // that item
   Item it;              // what is known of the worker's first item
@@ -105,12 +111,16 @@ struct Plan {           // in shared memory
   long long mine[kMaxRounds], cost[kMaxRounds]; // cost of the items before the worker's of the round, and its own
 };
 
-__device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p) {
+// Cost of a pair's blocks; `most`: the greatest weight of a tile.
+__device__ __forceinline__ long long pair_cost(const WorkArgs& a, int p, int& most) {
   int first, n;
   unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
   const int len = head_length(a, p), nb = unit_blocks(a, n);
   long long c = 0;
-  for (int b = 0; b < nb; ++b) c += tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
+  for (int b = 0; b < nb; ++b) {
+    const int t = tiles_of(a, block_visible(a, n, len, b)), w = weight_of(a, n, b, t);
+    c += t * w, most = max(most, w);
+  }
   return c;
 }
 // 32-bit divisions where they do: the plan is all latency.
@@ -118,11 +128,10 @@ __device__ __forceinline__ long long part_of(long long total, int worker, int wo
   return total < (1 << 24) ? (long long)((unsigned)total * (unsigned)worker / (unsigned)workers) : total * worker / workers;
 }
 // The share [begin, end) of a worker.
-__device__ __forceinline__ void share_of(const WorkArgs& a, long long total, int worker, int n_workers, long long& begin,
-                                         long long& end) {
+__device__ __forceinline__ void share_of(long long total, int granule, int worker, int n_workers, long long& begin, long long& end) {
   // rounded down: every share is at least `granule` wide, no less than a tile, so that a tile begins in each (the join follows an item from one
   // worker to the next and stops at the first that has no part in it)
-  const long long most = max(total / a.granule, 1ll);
+  const long long most = max(total / granule, 1ll);
   const int workers = (int)(most < n_workers ? most : n_workers);
   begin = end = total;
   if (worker < workers) {
@@ -135,9 +144,9 @@ __device__ __forceinline__ void settle_plan(const WorkArgs& a, int p, long long 
   unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
   const int len = head_length(a, p);
   for (;; ++b) {
-    const int t = tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b);
-    if (at < t) break;
-    at -= t;
+    const int t = tiles_of(a, block_visible(a, n, len, b)), c = t * weight_of(a, n, b, t);
+    if (at < c) break;
+    at -= c;
   }
   plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + width;
   plan.it = item_of(a, p, b, first, n, len, at, at + width);
@@ -160,9 +169,10 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
       constexpr int kPer = kWarpPairs / 32;
       const int per = (pairs + 31) / 32;
       long long c[kPer], mine = 0;
+      int heaviest = a.granule;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        c[i] = i < per && lane * per + i < pairs ? pair_cost(a, lane * per + i) : 0;
+        c[i] = i < per && lane * per + i < pairs ? pair_cost(a, lane * per + i, heaviest) : 0;
         mine += c[i];
       }
       long long incl = mine;
@@ -172,7 +182,7 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
         if (lane >= d) incl += o;
       }
       long long begin, end;
-      share_of(a, __shfl_sync(0xffffffffu, incl, 31), worker, n_workers, begin, end);
+      share_of(__shfl_sync(0xffffffffu, incl, 31), __reduce_max_sync(0xffffffffu, heaviest), worker, n_workers, begin, end);
       long long at = begin - (incl - mine), off = -1;
       if (lane == 0) plan.n_rounds = 0;
       if (begin >= end) {
@@ -196,20 +206,22 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
   while (log_group < 5 && (pairs << (log_group + 1)) <= NT) ++log_group;
   const int per = (pairs + NT - 1) / NT, sub = threadIdx.x & ((1 << log_group) - 1);
   const int p0 = min(log_group ? (int)threadIdx.x >> log_group : (int)threadIdx.x * per, pairs), p1 = min(p0 + per, pairs);
-  auto each = [&](auto&& f) {   // f(pair, block, first, n, len, cost) until it says stop
+  auto each = [&](auto&& f) {   // f(pair, block, first, n, len, tiles, weight) until it says stop
     for (int p = p0; p < p1; ++p) {
       int first, n;
       unit_tokens(a.starts, p / a.Hkv, a.T, first, n);
       const int len = head_length(a, p), nb = unit_blocks(a, n);
       const int b1 = (nb * (sub + 1)) >> log_group;
-      for (int b = (nb * sub) >> log_group; b < b1; ++b)
-        if (f(p, b, first, n, len, tiles_of(a, block_visible(a, n, len, b)) * weight_of(a, n, b))) return;
+      for (int b = (nb * sub) >> log_group; b < b1; ++b) {
+        const int t = tiles_of(a, block_visible(a, n, len, b));
+        if (f(p, b, first, n, len, t, weight_of(a, n, b, t))) return;
+      }
     }
   };
   long long mine = 0;
-  int items = 0, most = 0;
-  each([&](int, int, int, int, int, int c) {
-    mine += c, most = max(most, c), ++items;
+  int items = 0, most = 0, heaviest = a.granule;
+  each([&](int, int, int, int, int, int t, int w) {
+    mine += t * w, most = max(most, t * w), heaviest = max(heaviest, w), ++items;
     return false;
   });
   long long incl = mine;
@@ -220,19 +232,20 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
     const int i = __shfl_up_sync(0xffffffffu, incl_items, d);
     if (lane >= d) incl += o, incl_items += i;
   }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if (lane == 31) plan.warp_sum[warp] = incl, plan.warp_items[warp] = incl_items, plan.warp_most[warp] = most;
+  most = __reduce_max_sync(0xffffffffu, most), heaviest = __reduce_max_sync(0xffffffffu, heaviest);
+  if (lane == 31) plan.warp_sum[warp] = incl, plan.warp_items[warp] = incl_items, plan.warp_most[warp] = make_int2(most, heaviest);
   __syncthreads();
   long long before = incl - mine, total = 0;
   int items_before = incl_items - items, n_items = 0;
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) {
     if (w < warp) before += plan.warp_sum[w], items_before += plan.warp_items[w];
-    total += plan.warp_sum[w], n_items += plan.warp_items[w], most = max(most, plan.warp_most[w]);
+    total += plan.warp_sum[w], n_items += plan.warp_items[w];
+    most = max(most, plan.warp_most[w].x), heaviest = max(heaviest, plan.warp_most[w].y);
   }
   int rounds = 0;
-  if (a.rounds && total / a.granule >= n_workers)   // every worker keeps at least `granule` of the rest
-    rounds = (int)min(min((total / n_workers - a.granule) / most, (long long)(n_items / n_workers)), (long long)kMaxRounds);
+  if (a.rounds && total / heaviest >= n_workers)   // every worker keeps at least a tile of the rest
+    rounds = (int)min(min((total / n_workers - heaviest) / most, (long long)(n_items / n_workers)), (long long)kMaxRounds);
   long long begin, end;
   if (rounds > 0) {
     // the thread that has an item says which it is and what comes before it
@@ -241,7 +254,8 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
       if ((head < 0 || head >= items) && (own < 0 || own >= items)) continue;
       int i = 0;
       long long c = before;
-      each([&](int p, int b, int first, int n, int len, int cost) {
+      each([&](int p, int b, int first, int n, int len, int t, int w) {
+        const int cost = t * w;
         if (i == head) plan.before[k] = c;
         if (i == own) {
           plan.mine[k] = c, plan.cost[k] = cost, plan.round[k] = make_int2(p, b);
@@ -260,7 +274,7 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
       begin -= handed, end -= handed + plan.cost[k];
     }
   } else {
-    share_of(a, total, worker, n_workers, begin, end);
+    share_of(total, heaviest, worker, n_workers, begin, end);
   }
   if (threadIdx.x == 0) {
     plan.n_rounds = rounds;
@@ -268,9 +282,9 @@ __device__ void make_plan(const WorkArgs& a, int worker, int n_workers, Plan& pl
   }
   if (end > begin && begin >= before && begin < before + mine) {
     long long at = begin - before;
-    each([&](int p, int b, int first, int n, int len, int cost) {
-      if (at >= cost) {
-        at -= cost;
+    each([&](int p, int b, int first, int n, int len, int t, int w) {
+      if (at >= t * w) {
+        at -= t * w;
         return false;
       }
       plan.pair = p, plan.block = b, plan.begin = at, plan.end = at + (end - begin);
