@@ -24,6 +24,9 @@ Range range_of(const void* p, int64_t T, int64_t heads, int64_t tok, int64_t hea
   return {lo, lo + (uintptr_t)(((T - 1) * tok + (heads - 1) * head + kHeadDim) * esz)};
 }
 bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+Range pool_of(const ckv_paged& pg, const void* pool) {
+  return range_of(pool, pg.n_pages, pg.page_size, pg.page_stride, pg.page_stride_row, esize(pg));
+}
 
 ckv_status check_tokens(const ckv_paged* pg) {
   if (!pg) return CKV_ERR_INVALID_ARG;
@@ -148,14 +151,16 @@ ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const vo
     if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
     if ((rotary && rotary->rot_dim) && !good({positions}, 4)) return CKV_ERR_INVALID_ARG;
     if (!token_strides(*paged, paged->kv_stride_tok, paged->kv_stride_head, Hkv)) return CKV_ERR_INVALID_ARG;
+    const int64_t T = paged->n_tokens, e = esize(*paged);
+    const Range kr = range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
+    const Range vr = range_of(v, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
+    const Range kp = pool_of(*paged, k_pages), vp = pool_of(*paged, v_pages);
+    if (overlap(kr, kp) || overlap(kr, vp) || overlap(vr, kp) || overlap(vr, vp)) return CKV_ERR_INVALID_ARG;
     if (q_or_null) {
       if (!aligned(q_or_null, 16) || !token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, H))
         return CKV_ERR_INVALID_ARG;
-      const int64_t T = paged->n_tokens, e = esize(*paged);
-      const Range kr = range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
-      const Range vr = range_of(v, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
-      if (!out_ok(*paged, q_out, q_or_null, H, {range_of(q_or_null, T, H, paged->q_stride_tok, paged->q_stride_head, e), kr, vr}))
-        return CKV_ERR_INVALID_ARG;
+      const Range qr = range_of(q_or_null, T, H, paged->q_stride_tok, paged->q_stride_head, e);
+      if (overlap(qr, kp) || overlap(qr, vp) || !out_ok(*paged, q_out, q_or_null, H, {qr, kr, vr, kp, vp})) return CKV_ERR_INVALID_ARG;
     }
   }
   CKV_CUDA(launch_rotate(*paged, rotary, any ? q_or_null : nullptr, any ? k : nullptr, any ? v : nullptr, positions,
@@ -176,6 +181,13 @@ ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, co
   if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
   if (!good({indices, budgets, offsets, page_table, lengths}, 4) || lengths == budgets) return CKV_ERR_INVALID_ARG;
   CKV_TRY(check_paged_ws(kStatusBytes, ws, ws_bytes));
+  const int64_t e = esize(*paged);
+  for (const void* in : {k, v}) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(in);
+    const Range r{lo, lo + (uintptr_t)(((shape->n_units - 1) * shape->kv_stride_unit + (shape->n_kv_heads - 1) * shape->kv_stride_head +
+                                        (shape->seq_len - 1) * shape->kv_stride_tok + kHeadDim) * e)};
+    if (overlap(r, pool_of(*paged, k_pages)) || overlap(r, pool_of(*paged, v_pages))) return CKV_ERR_INVALID_ARG;
+  }
   CKV_CUDA(launch_gather_pages(*shape, *params, *paged, k, v, indices, budgets, offsets, page_table, k_pages, v_pages, lengths,
                                reinterpret_cast<int*>(static_cast<char*>(ws) + paged_ws(*paged).status),
                                (cudaStream_t)stream));
@@ -195,9 +207,10 @@ ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k
   const int64_t T = paged->n_tokens, H = paged->n_q_heads, e = esize(*paged);
   const Range o = range_of(out, T, H, H * kHeadDim, kHeadDim, e);
   if (overlap(o, range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e))) return CKV_ERR_INVALID_ARG;
-  for (const void* pool : {k_pages, v_pages})
-    if (overlap(o, range_of(pool, paged->n_pages, paged->page_size, paged->page_stride, paged->page_stride_row, e)))
-      return CKV_ERR_INVALID_ARG;
+  const uintptr_t l = reinterpret_cast<uintptr_t>(lse_or_null);
+  if (overlap(o, pool_of(*paged, k_pages)) || overlap(o, pool_of(*paged, v_pages)) ||
+      (l && overlap(o, {l, l + (uintptr_t)(T * H) * sizeof(float)})))
+    return CKV_ERR_INVALID_ARG;
   CKV_CUDA(launch_paged_attend(*paged, q, k_pages, v_pages, page_table, lengths, token_starts, out, lse_or_null,
                                static_cast<char*>(ws), (cudaStream_t)stream));
   return CKV_OK;

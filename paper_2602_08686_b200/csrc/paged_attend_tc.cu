@@ -9,9 +9,14 @@
 //                     bf16 over the columns S came from (the rounding tensor cores want; the sum l is of the unrounded values)
 //   O_s += P V        A = P from TMEM, V as it lies in memory ([keys][dims], MN-major B), into 128 TMEM columns
 // With two buffers a stream's logits are a step ahead of its softmax, so that the softmax threads do not wait for the tensor
-// cores (512 TMEM columns hold two streams' outputs and four 64-column buffers, or two of 128: with those the two took turns
-// and a pair of 128-key tiles took 3500 clocks).  N = 64 costs the first product half as much again (48 clocks for 32 of
-// arithmetic: A and B are read from shared memory at 128 bytes a clock), 2600 clocks per pair of 128-key tiles in all.
+// cores (512 TMEM columns hold two streams' outputs and four 64-column buffers, or two of 128: with those the two took turns).
+// N = 64 costs the first product half as much again (48 clocks for 32 of arithmetic: A and B are read from shared memory at 128
+// bytes a clock), 2600 clocks per key tile and pair of query tiles; the exponentials alone take 2050 (16 a clock).
+// Bound: those two together, at the clocks the power limit leaves under them (1.4 to 1.6 GHz).  2048 tokens over 32k rows:
+// 2.0 us per key tile, 900 to 925 us, 1.23 PFLOP/s (76 % of the measured rate of a plain matrix product); at 8192 rows the
+// tensor pipe is active 55 % of the time, and as much the exponentials' one.  An item takes 5 us besides its tiles: its last
+// product, and its output, whose 32-byte pieces of 128 rows keep the store path busy (gathered to lines by shuffles
+// they take 0.5 us less on two query tiles and more on one).
 // No maximum is taken per step.  Any reference m gives the same softmax, up to overflow: P, l and O are floating-point, and a
 // common factor costs none of their bits.  So a row keeps the reference of its first visible step, and the sums tell
 // whether an exponential left the range (2^64: then, and only then, the maximum is taken, O is rescaled in TMEM and

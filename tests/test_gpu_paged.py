@@ -332,6 +332,62 @@ def test_attend_long(B, dtype, counts, length):
     assert torch.equal(out, out2)
 
 
+@pytest.mark.parametrize("Nu,Hkv,H,counts,extra", [
+    (1, 1, 4, [1100], 40),                                   # the blocks of one head spread over the threads
+    (3, 2, 8, [257, 0, 600], 300),
+    (30, 8, 16, [0, 70, 129, 1, 260], 20),                   # a few hundred heads of up to three blocks
+    (60, 8, 8, [300, 1, 0, 33], 0),                          # more heads than threads
+    (5, 4, 32, [512, 64, 65, 1, 200], 700),                  # whole items first, then shares
+    (4, 8, 32, [700, 650, 800, 1], 0),                       # items of one key tile and of many
+])
+def test_attend_schedules(B, Nu, Hkv, H, counts, extra):
+    """Long chunks of many shapes: whatever max_new says, the same rows come out."""
+    counts = [counts[u % len(counts)] for u in range(Nu)]
+    lens = [[n + (extra * (u + 3 * g)) % (2 * extra + 1) for g in range(Hkv)] for u, n in enumerate(counts)]
+    c = R.Cache(lens, 32, device="cuda", seed=Nu + Hkv)
+    st = starts_of(counts)
+    q = torch.randn(st[-1], H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).bfloat16()
+    for max_new in (0, max(counts), 40):
+        out, lse = run_attend(B, c, q, st, max_new=max_new)
+        check_attend(c, q, st, out, lse)
+
+
+@pytest.mark.parametrize("n", [5, 20, 64, 90, 300])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_attend_infinite_values_inside_a_chunk(B, n, bad):
+    """A value row with one element that is not finite reaches the tokens that see it, in that element, and no others."""
+    lens = [[n + 200, n + 61]]
+    c = R.Cache(lens, 32, device="cuda", seed=n)
+    rows = []
+    for g in range(2):
+        k, v = c.rows[0][g]
+        hit = sorted({lens[0][g] - x for x in (1, 2, n // 2 + 1, n // 3 + 1, 3 * n // 4 + 1, n - 1)})
+        v = v.clone()
+        for j in hit:
+            v[j, 7 * g + 3] = bad
+            c.v_pages[int(c.table[0, g, j // 32]), j % 32, 7 * g + 3] = bad
+        rows.append((k, v, hit[0]))
+    q = torch.randn(n, 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).bfloat16()
+    for max_new in (0, n):
+        out, lse = run_attend(B, c, q, [0, n], max_new=max_new)
+        for g in range(2):
+            first = rows[g][2] - (lens[0][g] - n)              # the first token that sees a bad row
+            mine = out[:, 4 * g:4 * g + 4]
+            assert not torch.isfinite(mine[first:, :, 7 * g + 3]).any()
+            mine[first:, :, 7 * g + 3] = 0.0
+            assert torch.isfinite(mine).all()
+        # the element aside, the outputs are those of the clean cache
+        want, want_lse = R.attend(q, [0, n], c.rows)
+        for g in range(2):
+            first = rows[g][2] - (lens[0][g] - n)
+            want[first:, 4 * g:4 * g + 4, 7 * g + 3] = 0.0
+        vmax = max(float(v.double().abs().max()) for _, v in c.rows[0])
+        kmax = max(float(k.double().norm(dim=-1).max()) for k, _ in c.rows[0])
+        r = 132 * EPS * float(q.double().norm(dim=-1).max()) * kmax / math.sqrt(D) + 2.0 ** -20 + (lens[0][0] / 8 + 256) * EPS
+        assert ((out.double() - want).abs() <= 2.0 ** -8 * (vmax + want.abs()) + 2 * r * vmax).all()
+        assert ((lse.double() - want_lse).abs() <= r + 2 * EPS * want_lse.abs()).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("counts", [[1], [40], [200]])
 def test_attend_large_logits_and_scales(B, dtype, counts):

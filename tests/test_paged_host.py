@@ -184,3 +184,17 @@ def test_the_binding_compares_layouts():
         B.make_rotary(torch.zeros(64, dtype=torch.float64), q_norm_w=torch.zeros(64))
     with pytest.raises(TypeError):
         B.make_packed(q.half(), k.half(), 1)
+
+
+def test_outputs_and_pages_apart_from_inputs():
+    pg, rot = paged(), rotary()
+    far = lambda i: FAKE + i * (1 << 30)
+    for x in ("q", "k", "v", "q_out"):
+        for pool in (10, 11):
+            assert call("append", pg, rot, **{x: far(pool) + 99 * 64 * 256}) == B.ERR_INVALID_ARG, (x, pool)   # the last page
+    assert call("attend", pg, lse=far(13) + 10 * 32 * 256 - 4) == B.ERR_INVALID_ARG
+    s = B.ckv_shape(2, 32, 8, 128, 4096, 32, B.BF16, 0, 32 * 32 * 128, 32 * 128, 128, 8 * 4096 * 128, 4096 * 128, 128)
+    p = B.make_params(B.Params(), None, None)
+    for k, v in ((far(6) - 256, far(2)), (far(1), far(7) + 99 * 64 * 256), (far(6) - 2 * 8 * 4096 * 256 + 256, far(2))):
+        assert B.lib().ckv_gather_pages(C.byref(s), C.byref(p), C.byref(pg), k, v, far(3), far(4), far(5), far(9), far(6), far(7),
+                                        far(8), far(10), BIG, None) == B.ERR_INVALID_ARG
