@@ -19,6 +19,7 @@ constexpr int kRowsM = 4;            // query rows of a block
 constexpr int kRowsThreads = 256;
 constexpr int kRowsWarps = kRowsThreads / 32;
 constexpr int kRowsTile = kRowsWarps * 8;   // keys a CTA takes per step
+constexpr ShortRule kShortRows{kRowsTile, 100, 300};
 
 // the 16 dimensions of lane l8 of 8: 16-byte pieces l8, l8 + 8, ... of the row (coalesced over the eight lanes)
 __device__ __forceinline__ void load16(const char* row, int l8, float (&x)[16]) {
@@ -299,22 +300,26 @@ template cudaError_t launch_join<true>(const WorkArgs&, int, int, void*, float*,
 template cudaError_t launch_join<false>(const WorkArgs&, int, int, void*, float*, cudaStream_t);
 
 // bf16 calls go to the kernel for few rows while every unit has at most so many query rows per KV head, else to the tensor
-// cores: with 16 rows a long cache streams at the memory's rate, with 32 the matrix instructions of that kernel take longer
-// than the bytes; a short cache is all latency, where it stays ahead for longer.
-constexpr int kFewRows = 16, kFewRowsShort = 32;
+// cores.  With up to 16 rows it is ahead (one sequence on 16k rows 27 us against 33; 16 x 32k are read at the memory's rate by either), with
+// 32 on a long cache its matrix instructions take longer than the bytes (8 x 8 tokens on 16k rows 159 us against 101); a
+// short cache is all latency, where it stays ahead for longer (8 tokens on 1000 rows 13 us against 20).
+constexpr int kFewRows = 16;
 static bool wants_tc(const ckv_paged& pg) {
   const int64_t G = pg.n_q_heads / pg.n_kv_heads, most = pg.max_new > 0 ? pg.max_new : pg.n_tokens;
-  return pg.dtype == CKV_BF16 && G <= 128 && most * G > (cluster_size(pg, kMmaCtaKeys) ? kFewRowsShort : kFewRows);
+  return pg.dtype == CKV_BF16 && G <= 128 && most * G > kFewRows && (most * G > kMmaRows || !cluster_size(pg, kShortMore));
 }
 
-// Short caches go to clusters: as many CTAs per head as the heads leave room for, as long as each has a step's keys to read and
-// none has more than kClusterRows.  0: the cache is not short.
-int cluster_size(const ckv_paged& pg, int cta_keys) {
-  constexpr int kClusterRows = 1024;
+// Short caches go to clusters, one per head: as many CTAs as the heads leave room for, as long as each has a step's keys to read.
+// Clusters do not cross the GPCs, so that of eight CTAs 15 run at a time, of four 33, of two 74 (148 SMs, one CTA each; 16 heads
+// of 2000 rows in clusters of eight: 18 us, of four: 13).  0: the cache is not short: a cluster's CTA has more rows to read
+// than the split's even share and what the split's schedule and join take besides.
+int cluster_size(const ckv_paged& pg, const ShortRule& rule) {
+  constexpr int kFit[] = {kWorkers, 74, 33, 15};
   const int64_t pairs = (int64_t)pg.n_units * pg.n_kv_heads, capacity = (int64_t)pg.max_pages * pg.page_size;
-  int n_cta = 1;
-  while (n_cta < 8 && pairs * n_cta * 2 <= kWorkers && (int64_t)n_cta * cta_keys < capacity) n_cta *= 2;
-  return capacity <= (int64_t)n_cta * kClusterRows ? n_cta : 0;
+  int log = 0;
+  while (log < 3 && pairs <= kFit[log + 1] && ((int64_t)rule.cta_keys << log) < capacity) ++log;
+  const int64_t rows = (pairs + kFit[log] - 1) / kFit[log] * capacity >> log, share = pairs * capacity / kWorkers;
+  return rows <= share * rule.share_percent / 100 + rule.rows ? 1 << log : 0;
 }
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -352,7 +357,7 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   }
   a.slot_rows = kRowsM;
   set_blocks(a, most, kRowsM, 0, kRowsTile, 4);
-  const int n_cta = cluster_size(pg, kRowsTile);
+  const int n_cta = cluster_size(pg, kShortRows);
   const int64_t pairs = (int64_t)a.Nu * a.Hkv, fit = n_cta ? 2 * kWorkers / n_cta : 0;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(n_cta ? (int)(pairs < fit ? pairs : fit) * n_cta : kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;

@@ -376,7 +376,7 @@ cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t
   const bool few = most * a.G <= 16;
   set_blocks(a, most, few ? 16 : 32, 0, kMmaTile, 2);
   const float x_scale = scale * kLog2e;
-  if (const int n_cta = cluster_size(pg, kMmaCtaKeys)) {
+  if (const int n_cta = cluster_size(pg, few ? kShortFew : kShortMore)) {
     const int64_t pairs = (int64_t)a.Nu * a.Hkv, fit = 2 * kWorkers / n_cta;
     const int grid = (int)(pairs < fit ? pairs : fit) * n_cta;
     return few ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)

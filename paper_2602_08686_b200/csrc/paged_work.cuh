@@ -412,7 +412,14 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, int64_t 
 constexpr int kMmaRows = 32;         // most query rows of a block of the bf16 kernel for few rows
 constexpr int kMmaTile = 64;         // keys per tile of its schedule
 constexpr int kMmaCtaKeys = 128;     // keys a CTA of it takes per step
-int cluster_size(const ckv_paged& pg, int cta_keys);   // CTAs per cluster where the cache is short, else 0
+// When a cache is short: a CTA of a cluster takes `cta_keys` per step, and reads no more than the given part of the split's even share
+// and `rows` more.  (A row takes such a CTA 13 ns with up to 16 query rows, 21 with 32, 32 in fp32; the split's schedule and
+// join take 10 us.  With 32 query rows the other side is the tensor-core kernel: 9 ns a row.)
+struct ShortRule {
+  int cta_keys, share_percent, rows;
+};
+constexpr ShortRule kShortFew{kMmaCtaKeys, 100, 800}, kShortMore{kMmaCtaKeys, 50, 450};
+int cluster_size(const ckv_paged& pg, const ShortRule& rule);   // CTAs per cluster where the cache is short, else 0
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
 // rows: the most query rows a block has.
