@@ -76,27 +76,32 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         limit[r] = row_limit(a, it, r);
       }
     }
-    const int end = min(it.t1 * a.tile, it.visible);
-    for (int j0 = it.t0 * a.tile + rank * a.tile; j0 < end; j0 += n_ranks * a.tile) {
-      float x[2][kRowsM], kv[2][16], vv[2][16];
-      int key[2];
+    const int end = min(it.t1 * a.tile, it.visible), step = n_ranks * a.tile;
+    // a warp's eight keys are in one page
+    auto page_at = [&](int j) { return j + warp * 8 < end ? page_of(a, it, (j + warp * 8) >> a.log_p) : -1; };
+    auto key_at = [&](int j, int s) { return j + warp * 8 + s * 4 + grp; };
+    auto load = [&](const char* pool, int j, int page, float (&x)[2][16]) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        key[s] = j0 + warp * 8 + s * 4 + grp;
-        int page = -1;
-        if (key[s] < end) page = page_of(a, it, key[s] >> a.log_p);
+        const int key = key_at(j, s);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) kv[s][i] = 0.f, vv[s][i] = 0.f;
-        if (page >= 0) {
-          const int64_t at = (page * pg.page_stride + (key[s] & (a.P - 1)) * pg.page_stride_row) * E;
-          load16(kp + at, l8, kv[s]);
-          load16(vp + at, l8, vv[s]);
-        } else {
-          key[s] = 0x7fffffff;   // hidden from every row
-        }
+        for (int i = 0; i < 16; ++i) x[s][i] = 0.f;
+        if (page >= 0 && key < end) load16(pool + (page * pg.page_stride + (key & (a.P - 1)) * pg.page_stride_row) * E, l8, x[s]);
       }
+    };
+    int j0 = it.t0 * a.tile + rank * a.tile;
+    int page = page_at(j0), next = page_at(j0 + step);
+    float kv[2][16], vv[2][16];
+    load(kp, j0, page, kv);
+    load(vp, j0, page, vv);
+    // The next keys are asked for when the logits are done, the next values when the output is.
+    for (; j0 < end; j0 += step) {
+      float x[2][kRowsM];
+      int key[2];
+      bool raise = false;
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s) {
+        key[s] = page >= 0 && key_at(j0, s) < end ? key_at(j0, s) : 0x7fffffff;   // hidden from every row
 #pragma unroll
         for (int r = 0; r < kRowsM; ++r) {
           float d = 0.f;
@@ -105,24 +110,38 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
 #pragma unroll
           for (int b = 1; b < 8; b <<= 1) d += __shfl_xor_sync(0xffffffffu, d, b);
           x[s][r] = key[s] < limit[r] ? d * x_scale : -INFINITY;
+          raise |= x[s][r] > m[r];
         }
+      }
+      load(kp, j0 + step, next, kv);
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int r = 0; r < kRowsM; ++r) {
+          const float top = fmaxf(m[r], fmaxf(x[0][r], x[1][r]));
+          const float c = exp2f(m[r] - (top == -INFINITY ? 0.f : top));
+          m[r] = top, l[r] *= c;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[r][i] *= c;
+        }
+      }
 #pragma unroll
       for (int r = 0; r < kRowsM; ++r) {
-        const float top = fmaxf(m[r], fmaxf(x[0][r], x[1][r]));
-        const float ref = top == -INFINITY ? 0.f : top;
-        const float c = exp2f(m[r] - ref), p0 = exp2f(x[0][r] - ref), p1 = exp2f(x[1][r] - ref);
-        m[r] = top;
-        l[r] = fmaf(l[r], c, p0 + p1);
+        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+        const float p0 = exp2f(x[0][r] - ref), p1 = exp2f(x[1][r] - ref);
+        l[r] += p0 + p1;
         // a hidden key's value may be anything: its row is skipped, not multiplied by zero
         const bool s0 = key[0] < limit[r], s1 = key[1] < limit[r];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          float o = acc[r][i] * c;
+          float o = acc[r][i];
           if (s0) o = fmaf(p0, vv[0][i], o);
           if (s1) o = fmaf(p1, vv[1][i], o);
           acc[r][i] = o;
         }
       }
+      page = next;
+      load(vp, j0 + step, page, vv);
+      next = page_at(j0 + 2 * step);
     }
     // join the four groups of the warp, then the warps
 #pragma unroll
