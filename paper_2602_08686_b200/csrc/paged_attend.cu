@@ -51,8 +51,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
   pdl_wait();
   Walk walk;
   const int rank = kCluster ? (int)blockIdx.x % n_cta : 0, n_ranks = kCluster ? n_cta : 1;
+  auto cluster_item = [&](int i, int more) {                   // the next item of this cluster that has rows
+    walk.live = false;
+    for (; i < a.Nu * a.Hkv * a.blocks; i += gridDim.x / n_cta, more = 0)
+      if (walk.cluster_item(a, i, more)) return;
+  };
   if (kCluster) {
-    walk.cluster_next(a, blockIdx.x / n_cta, 0, gridDim.x / n_cta);
+    cluster_item(blockIdx.x / n_cta, 0);
   } else {
     make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
     pdl_launch_dependents();
@@ -214,7 +219,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         }
         cluster_sync();   // nobody's memory is written again or given back while it is read
       }
-      walk.cluster_next(a, walk.pair, walk.block + 1, gridDim.x / n_cta);
+      cluster_item(walk.round, walk.cluster_more(a));
     } else {
       if (!whole && threadIdx.x == 0) {
         int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
@@ -325,19 +330,19 @@ template cudaError_t launch_join<false>(const WorkArgs&, int, int, void*, float*
 constexpr int kFewRows = 16;
 static bool wants_tc(const ckv_paged& pg) {
   const int64_t G = pg.n_q_heads / pg.n_kv_heads, most = pg.max_new > 0 ? pg.max_new : pg.n_tokens;
-  return pg.dtype == CKV_BF16 && G <= 128 && most * G > kFewRows && (most * G > kMmaRows || !cluster_size(pg, kShortMore));
+  return pg.dtype == CKV_BF16 && G <= 128 && most * G > kFewRows && (most * G > kMmaRows || !cluster_size(pg, kShortMore, 1));
 }
 
-// Short caches go to clusters, one per head: as many CTAs as the heads leave room for, as long as each has a step's keys to read.
+// Short caches go to clusters, one per block of a head's query rows: as many CTAs as the blocks leave room for, as long as each has a step's keys to read.
 // Clusters do not cross the GPCs, so that of eight CTAs 15 run at a time, of four 33, of two 74 (148 SMs, one CTA each; 16 heads
 // of 2000 rows in clusters of eight: 18 us, of four: 13).  0: the cache is not short: a cluster's CTA has more rows to read
 // than the split's even share and what the split's schedule and join take besides.
-int cluster_size(const ckv_paged& pg, const ShortRule& rule) {
+int cluster_size(const ckv_paged& pg, const ShortRule& rule, int64_t blocks) {
   constexpr int kFit[] = {kWorkers, 74, 33, 15};
-  const int64_t pairs = (int64_t)pg.n_units * pg.n_kv_heads, capacity = (int64_t)pg.max_pages * pg.page_size;
+  const int64_t items = (int64_t)pg.n_units * pg.n_kv_heads * blocks, capacity = (int64_t)pg.max_pages * pg.page_size;
   int log = 0;
-  while (log < 3 && pairs <= kFit[log + 1] && ((int64_t)rule.cta_keys << log) < capacity) ++log;
-  const int64_t rows = (pairs + kFit[log] - 1) / kFit[log] * capacity >> log, share = pairs * capacity / kWorkers;
+  while (log < 3 && items <= kFit[log + 1] && ((int64_t)rule.cta_keys << log) < capacity) ++log;
+  const int64_t rows = (items + kFit[log] - 1) / kFit[log] * capacity >> log, share = items * capacity / kWorkers;
   return rows <= share * rule.share_percent / 100 + rule.rows ? 1 << log : 0;
 }
 
@@ -376,10 +381,10 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   }
   a.slot_rows = kRowsM;
   set_blocks(a, most, kRowsM, 0, kRowsTile, 4);
-  const int n_cta = cluster_size(pg, kShortRows);
-  const int64_t pairs = (int64_t)a.Nu * a.Hkv, fit = n_cta ? 2 * kWorkers / n_cta : 0;
+  const int n_cta = cluster_size(pg, kShortRows, a.blocks);
+  const int64_t items = (int64_t)a.Nu * a.Hkv * a.blocks, fit = n_cta ? 2 * kWorkers / n_cta : 0;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(n_cta ? (int)(pairs < fit ? pairs : fit) * n_cta : kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
+  cfg.gridDim = dim3(n_cta ? (int)(items < fit ? items : fit) * n_cta : kWorkers), cfg.blockDim = dim3(kRowsThreads), cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0] = pdl_attribute();
   attr[1].id = cudaLaunchAttributeClusterDimension;

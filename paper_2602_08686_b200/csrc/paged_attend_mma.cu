@@ -71,16 +71,12 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
   const int rank = kCluster ? (int)blockIdx.x % n_cta : 0;
   const int stride = (kCluster ? n_cta : 1) * NW * kGroup;     // keys all warps take per step
   int early_page = 0;                                          // table entry of the warp's first group, asked for ahead of the lengths
-  auto cluster_item = [&](int pair, int block) {               // the next item of this cluster that has rows
+  auto cluster_item = [&](int i, int more) {                   // the next item of this cluster that has rows
     walk.live = false;
-    for (; pair < a.Nu * a.Hkv; pair += gridDim.x / n_cta, block = 0) {
+    for (; i < a.Nu * a.Hkv * a.blocks; i += gridDim.x / n_cta, more = 0) {
       const int slot = (rank * NW + warp) * kGroup >> a.log_p;
-      if (slot < a.max_pages) early_page = a.table[(int64_t)pair * a.max_pages + slot];
-      walk.it = make_item(a, pair, block, 0, 1ll << 40);
-      if (block < unit_blocks(a, walk.it.n)) {
-        walk.pair = pair, walk.block = block, walk.live = true;
-        return;
-      }
+      if (slot < a.max_pages) early_page = a.table[(int64_t)Walk::cluster_pair(a, i) * a.max_pages + slot];
+      if (walk.cluster_item(a, i, more)) return;
     }
   };
   if (kCluster) {
@@ -335,7 +331,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         }
         cluster_sync();   // nobody's memory is written again or given back while it is read
       }
-      cluster_item(walk.pair, walk.block + 1);
+      cluster_item(walk.round, walk.cluster_more(a));
     } else {
       if (!whole && threadIdx.x == 0) {
         int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);
@@ -376,9 +372,9 @@ cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t
   const bool few = most * a.G <= 16;
   set_blocks(a, most, few ? 16 : 32, 0, kMmaTile, 2);
   const float x_scale = scale * kLog2e;
-  if (const int n_cta = cluster_size(pg, few ? kShortFew : kShortMore)) {
-    const int64_t pairs = (int64_t)a.Nu * a.Hkv, fit = 2 * kWorkers / n_cta;
-    const int grid = (int)(pairs < fit ? pairs : fit) * n_cta;
+  if (const int n_cta = cluster_size(pg, few ? kShortFew : kShortMore, a.blocks)) {
+    const int64_t items = (int64_t)a.Nu * a.Hkv * a.blocks, fit = 2 * kWorkers / n_cta;
+    const int grid = (int)(items < fit ? items : fit) * n_cta;
     return few ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
                       : launch<2, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st);
   }

@@ -16,6 +16,7 @@ namespace ckv {
 struct WorkArgs {
   int Nu, H, Hkv, G, T, causal;
   int M;            // query rows of a block
+  int blocks;       // blocks a pair is expected to have (clusters)
   int tokens;       // 0, or the whole tokens a block holds (then M is tokens * G)
   int tile, log_tile;   // keys per tile
   int granule;      // least cost per worker (a tile, where that costs more)
@@ -35,6 +36,8 @@ constexpr int kWarpPairs = 128, kWarpBlocks = 8;
 inline void set_blocks(WorkArgs& a, int64_t most, int M, int tokens, int tile, int granule) {
   a.M = M, a.tokens = tokens, a.tile = tile, a.granule = granule;
   for (a.log_tile = 0; (1 << a.log_tile) < tile;) ++a.log_tile;
+  const int64_t blocks = (most * a.G + M - 1) / M;
+  a.blocks = (int)(blocks < 1 ? 1 : blocks > 4096 ? 4096 : blocks);
   a.rounds = tokens > 0 && most > tokens;
   a.one_warp = (int64_t)a.Nu * a.Hkv <= kWarpPairs && !a.rounds && most * a.G <= (int64_t)kWarpBlocks * M;
 }
@@ -368,17 +371,15 @@ struct Walk {
     }
     settle(a);
   }
-  // Where every pair is one cluster's: from (p, b) on, the first item that has rows; clusters are `stride` pairs apart.
-  __device__ __forceinline__ void cluster_next(const WorkArgs& a, int p, int b, int stride) {
-    live = false;
-    for (; p < a.Nu * a.Hkv; p += stride, b = 0) {
-      it = make_item(a, p, b, 0, 1ll << 40);
-      if (b < unit_blocks(a, it.n)) {
-        pair = p, block = b, live = true;
-        return;
-      }
-    }
+  // Where an item is one cluster's: the i-th of (pair, expected block), and `more` times as many blocks on where a unit has more
+  // than expected.
+  __device__ __forceinline__ static int cluster_pair(const WorkArgs& a, int i) { return a.blocks == 1 ? i : i / a.blocks; }
+  __device__ __forceinline__ bool cluster_item(const WorkArgs& a, int i, int more) {
+    round = i, pair = cluster_pair(a, i), block = i + (more - pair) * a.blocks;
+    it = make_item(a, pair, block, 0, 1ll << 40);
+    return live = block < unit_blocks(a, it.n);
   }
+  __device__ __forceinline__ int cluster_more(const WorkArgs& a) const { return block / a.blocks + 1; }
 };
 // Rows of the block, and where query row r of it (token, head) lives.
 __device__ __forceinline__ int block_rows(const WorkArgs& a, const Item& it) {
@@ -419,7 +420,8 @@ struct ShortRule {
   int cta_keys, share_percent, rows;
 };
 constexpr ShortRule kShortFew{kMmaCtaKeys, 100, 800}, kShortMore{kMmaCtaKeys, 50, 450};
-int cluster_size(const ckv_paged& pg, const ShortRule& rule);   // CTAs per cluster where the cache is short, else 0
+// CTAs per cluster where the cache is short, else 0.  blocks: of query rows of a pair.
+int cluster_size(const ckv_paged& pg, const ShortRule& rule, int64_t blocks);
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
 // rows: the most query rows a block has.
