@@ -37,9 +37,10 @@ struct RowsSmem {
   float o[kRowsWarps][kRowsM][kHeadDim];
   float2 cta_ml[kRowsM];                       // the CTA's result, for the others of its cluster
   float cta_o[kRowsM][kHeadDim];
+  Item it;                                     // of the cluster
 };
 
-// kCluster: every pair of (unit, KV head) is one cluster's, as in the bf16 kernel for few rows.
+// kCluster: every item is one cluster's, as in the bf16 kernel for few rows.
 template <bool kCluster>
 __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a, ckv_paged pg, float x_scale,
                                                                       const char* __restrict__ q,
@@ -51,23 +52,23 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
   pdl_wait();
   Walk walk;
   const int rank = kCluster ? (int)blockIdx.x % n_cta : 0, n_ranks = kCluster ? n_cta : 1;
-  auto cluster_item = [&](int i, int more) {                   // the next item of this cluster that has rows
-    walk.live = false;
-    for (; i < a.Nu * a.Hkv * a.blocks; i += gridDim.x / n_cta, more = 0)
-      if (walk.cluster_item(a, i, more)) return;
-  };
-  if (kCluster) {
-    cluster_item(blockIdx.x / n_cta, 0);
-  } else {
+  int index = blockIdx.x / n_cta, more = 0;   // of the cluster's item
+  if (!kCluster) {
     make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
     pdl_launch_dependents();
     if (threadIdx.x == 0) a.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
     walk.start(a, sm.plan);
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
-  while (walk.live) {
-    const Item& it = walk.it;
-    const int rows = block_rows(a, it);
+  for (;;) {
+    if (kCluster) {   // the next item that has rows
+      walk.live = false;
+      for (; index < a.Nu * a.Hkv * a.blocks && !walk.cluster_item(a, index, more); more = 0) index += gridDim.x / n_cta;
+    }
+    if (!walk.live) break;
+    const Item& now = walk.it;
+    if (kCluster && threadIdx.x == 0) sm.it = now;
+    const int rows = block_rows(a, now);
     float qr[kRowsM][16], acc[kRowsM][16], m[kRowsM], l[kRowsM];
     int limit[kRowsM];
 #pragma unroll
@@ -76,14 +77,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[r][i] = 0.f, qr[r][i] = 0.f;
       if (r < rows) {
-        const int row = it.block * a.M + r, token = row / a.G, h = it.g * a.G + (row - token * a.G);
-        load16(q + ((it.first + token) * pg.q_stride_tok + h * pg.q_stride_head) * E, l8, qr[r]);
-        limit[r] = row_limit(a, it, r);
+        const int row = now.block * a.M + r, token = row / a.G, h = now.g * a.G + (row - token * a.G);
+        load16(q + ((now.first + token) * pg.q_stride_tok + h * pg.q_stride_head) * E, l8, qr[r]);
+        limit[r] = row_limit(a, now, r);
       }
     }
-    const int end = min(it.t1 * a.tile, it.visible), step = n_ranks * a.tile;
+    const int end = min(now.t1 * a.tile, now.visible), step = n_ranks * a.tile;
     // a warp's eight keys are in one page
-    auto page_at = [&](int j) { return j + warp * 8 < end ? page_of(a, it, (j + warp * 8) >> a.log_p) : -1; };
+    auto page_at = [&](int j) { return j + warp * 8 < end ? page_of(a, now, (j + warp * 8) >> a.log_p) : -1; };
     auto key_at = [&](int j, int s) { return j + warp * 8 + s * 4 + grp; };
     auto load = [&](const char* pool, int j, int page, float (&x)[2][16]) {
 #pragma unroll
@@ -94,7 +95,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         if (page >= 0 && key < end) load16(pool + (page * pg.page_stride + (key & (a.P - 1)) * pg.page_stride_row) * E, l8, x[s]);
       }
     };
-    int j0 = it.t0 * a.tile + rank * a.tile;
+    int j0 = now.t0 * a.tile + rank * a.tile;
     int page = page_at(j0), next = page_at(j0 + step);
     float kv[2][16], vv[2][16];
     load(kp, j0, page, kv);
@@ -168,6 +169,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       }
     }
     __syncthreads();
+    const Item& it = kCluster ? sm.it : walk.it;   // out of registers, which the loop over the keys has no more of
     const bool whole = it.t0 == 0 && it.t1 == it.tiles;
     const int which = it.t0 > 0 ? 0 : 1;
     const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.slot_rows;
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         }
         cluster_sync();   // nobody's memory is written again or given back while it is read
       }
-      cluster_item(walk.round, walk.cluster_more(a));
+      index = Walk::cluster_index(a, it), more = Walk::cluster_more(a, it) + 1;
     } else {
       if (!whole && threadIdx.x == 0) {
         int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);

@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         }
         cluster_sync();   // nobody's memory is written again or given back while it is read
       }
-      cluster_item(walk.round, walk.cluster_more(a));
+      cluster_item(Walk::cluster_index(a, walk.it), Walk::cluster_more(a, walk.it) + 1);
     } else {
       if (!whole && threadIdx.x == 0) {
         int* sp = reinterpret_cast<int*>(a.split + blockIdx.x);

@@ -375,11 +375,15 @@ struct Walk {
   // than expected.
   __device__ __forceinline__ static int cluster_pair(const WorkArgs& a, int i) { return a.blocks == 1 ? i : i / a.blocks; }
   __device__ __forceinline__ bool cluster_item(const WorkArgs& a, int i, int more) {
-    round = i, pair = cluster_pair(a, i), block = i + (more - pair) * a.blocks;
-    it = make_item(a, pair, block, 0, 1ll << 40);
-    return live = block < unit_blocks(a, it.n);
+    const int p = cluster_pair(a, i), b = i + (more - p) * a.blocks;
+    it = make_item(a, p, b, 0, 1ll << 40);
+    return live = b < unit_blocks(a, it.n);
   }
-  __device__ __forceinline__ int cluster_more(const WorkArgs& a) const { return block / a.blocks + 1; }
+  // i and `more` of an item
+  __device__ __forceinline__ static int cluster_more(const WorkArgs& a, const Item& it) { return it.block / a.blocks; }
+  __device__ __forceinline__ static int cluster_index(const WorkArgs& a, const Item& it) {
+    return (it.u * a.Hkv + it.g - cluster_more(a, it)) * a.blocks + it.block;
+  }
 };
 // Rows of the block, and where query row r of it (token, head) lives.
 __device__ __forceinline__ int block_rows(const WorkArgs& a, const Item& it) {

@@ -332,6 +332,7 @@ def test_attend_long(B, dtype, counts, length):
     assert torch.equal(out, out2)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("Nu,Hkv,H,counts,extra", [
     (1, 1, 4, [1100], 40),                                   # the blocks of one head spread over the threads
     (3, 2, 8, [257, 0, 600], 300),
@@ -339,15 +340,17 @@ def test_attend_long(B, dtype, counts, length):
     (60, 8, 8, [300, 1, 0, 33], 0),                          # more heads than threads
     (5, 4, 32, [512, 64, 65, 1, 200], 700),                  # whole items first, then shares
     (4, 8, 32, [700, 650, 800, 1], 0),                       # items of one key tile and of many
+    (1, 1, 200, [21], 300),                                  # more query heads than a tensor-core block has rows
+    (7, 2, 8, [16, 3, 0, 9], 250),                           # a head's blocks shared out to clusters
 ])
-def test_attend_schedules(B, Nu, Hkv, H, counts, extra):
+def test_attend_schedules(B, dtype, Nu, Hkv, H, counts, extra):
     """Long chunks of many shapes: whatever max_new says, the same rows come out."""
     counts = [counts[u % len(counts)] for u in range(Nu)]
     lens = [[n + (extra * (u + 3 * g)) % (2 * extra + 1) for g in range(Hkv)] for u, n in enumerate(counts)]
-    c = R.Cache(lens, 32, device="cuda", seed=Nu + Hkv)
+    c = R.Cache(lens, 32, dtype=dtype, device="cuda", seed=Nu + Hkv)
     st = starts_of(counts)
-    q = torch.randn(st[-1], H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).bfloat16()
-    for max_new in (0, max(counts), 40):
+    q = torch.randn(st[-1], H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).to(dtype)
+    for max_new in (0, max(counts), 40, 1):
         out, lse = run_attend(B, c, q, st, max_new=max_new)
         check_attend(c, q, st, out, lse)
 
