@@ -37,7 +37,7 @@ struct RotArgs {
   const int32_t *lengths, *table;
   char *k_pages, *v_pages;
   int32_t* new_lengths;
-  int P, n_pages, max_pages;
+  int log_p, n_pages, max_pages;
   int64_t page_stride, page_row;
   int* status;
 };
@@ -189,9 +189,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotate_kernel(const __grid_co
   int ahead = 0;
   auto place = [&](int h) -> int64_t {
     const int64_t row = (int64_t)a.lengths[pair0 + h] + ahead;
-    const bool in_table = row >= 0 && row < (int64_t)a.max_pages * a.P;
-    const int page = in_table ? a.table[(pair0 + h) * a.max_pages + (int)row / a.P] : -1;
-    if ((unsigned)page < (unsigned)a.n_pages) return (page * a.page_stride + ((int)row % a.P) * a.page_row) * E;
+    const bool in_table = row >= 0 && row < (int64_t)a.max_pages << a.log_p;
+    const int page = in_table ? a.table[(pair0 + h) * a.max_pages + ((int)row >> a.log_p)] : -1;
+    if ((unsigned)page < (unsigned)a.n_pages) return (page * a.page_stride + ((int)row & ((1 << a.log_p) - 1)) * a.page_row) * E;
     if (lane == 0) report_status(a.status, kStatusPage);
     return -1;
   };
@@ -272,7 +272,8 @@ cudaError_t launch_rotate(const ckv_paged& pg, const ckv_rotary* rot, const void
     a.interleaved = rot->interleaved, a.rot_scale = rot->rot_scale, a.eps = rot->norm_eps;
   }
   a.lengths = lengths, a.table = table, a.k_pages = (char*)k_pages, a.v_pages = (char*)v_pages;
-  a.new_lengths = new_lengths, a.P = pg.page_size, a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
+  a.new_lengths = new_lengths, a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
+  while ((1 << a.log_p) < pg.page_size) ++a.log_p;
   a.page_stride = pg.page_stride, a.page_row = pg.page_stride_row, a.status = status;
   // Tokens of a CTA share its set-up (the reads before the first row, the angles): as many as leave kWaves rounds of CTAs.
   int per = kMaxTokens;
