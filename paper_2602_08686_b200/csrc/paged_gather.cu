@@ -3,7 +3,7 @@
 // both sides are coalesced (a page holds whole rows of 256 or 512 bytes).  The threads of a row look its head up together
 // (offsets compared side by side) and no index is divided by anything but a power of two: with 64-bit divisions per
 // thread the copy was bound by instruction issue.  Bound: HBM, 4 rows' bytes per kept position; the launch and four
-// dependent reads (offset, index, page, row) when small.
+// dependent reads (offset, index, page, row) when small (8 layers of 512 rows: 7.2 us, from L2 5.2; one layer: 2).
 #include "paged.cuh"
 
 namespace ckv {

@@ -8,7 +8,8 @@
 // dimensions and its token over all the rows it takes, its cosines stay in registers.  (With one 16-byte piece, the
 // partner's by shuffles and the cosines from shared memory per row, the 32k prompt took 243 us: instruction issue.)  The
 // row's sum of squares is a shuffle tree.  Everything between the load and the store is fp32, rounded once.
-// Bound: HBM for long inputs (each row is read and written once), the launch and three dependent reads for a decode step.
+// Bound: HBM for long inputs (each row is read and written once; the 32k prompt in 118 us, 0.87 of the measured copy rate), the
+// launch and three dependent reads for a decode step (16 sequences: 4 us).
 #include <cuda_bf16.h>
 
 #include "paged.cuh"
