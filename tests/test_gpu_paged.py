@@ -332,6 +332,16 @@ def test_attend_long(B, dtype, counts, length):
     assert torch.equal(out, out2)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_wide_group_on_a_long_cache(B, causal):
+    """More query heads per KV head than a tensor-core block has rows: blocks of 32 rows, split along the keys."""
+    c = R.Cache([[12000], [9001]], 64, device="cuda", seed=4)
+    q = torch.randn(4, 150, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).bfloat16()
+    for max_new in (0, 3, 1):
+        out, lse = run_attend(B, c, q, [0, 1, 4], causal, max_new=max_new)
+        check_attend(c, q, [0, 1, 4], out, lse, causal)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("Nu,Hkv,H,counts,extra", [
     (1, 1, 4, [1100], 40),                                   # the blocks of one head spread over the threads
