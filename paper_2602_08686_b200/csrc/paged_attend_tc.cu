@@ -418,7 +418,8 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     const bool live = r < a.TQ * a.w.G && token < it.n;
     auto limit_of = [&](int tk) { return a.w.causal ? min(max(it.len - it.n + tk + 1, 0), it.len) : it.len; };
     const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
-    float m = -INFINITY, l = 0.f;
+    // rows of no token hold what shared memory held, or another unit's queries: above everything, they ask for no step again
+    float m = live ? -INFINITY : INFINITY, l = 0.f;
     bool open = true;                                         // some row of the warp has no reference yet
 #pragma unroll 1
     for (int g = 0; g < steps; ++g, ++n_steps) {

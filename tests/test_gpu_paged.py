@@ -487,6 +487,22 @@ def test_attend_same_bits_again_and_on_two_streams(B):
             assert torch.equal(outs[0], first) and torch.equal(outs[1], first)
 
 
+def test_attend_same_bits_whatever_ran_before(B):
+    """Groups that do not fill a tensor-core block leave rows of it to what shared memory held: no token's bits depend on it."""
+    n = 100
+    c = R.Cache([[n + 900] * 4], 32, device="cuda", seed=8)
+    other = R.Cache([[n + 900] * 4], 32, device="cuda", seed=9)
+    q = torch.randn(n, 28, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(6)).bfloat16()
+    big = torch.randn(n, 32, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).bfloat16()
+    seen = []
+    for factor in (0.0, 300.0, 1.0, 3e4):
+        run_attend(B, other, big * factor, [0, n])
+        seen.append(run_attend(B, c, q, [0, n]))
+    for out, lse in seen[1:]:
+        assert torch.equal(out, seen[0][0]) and torch.equal(lse, seen[0][1])
+    check_attend(c, q, [0, n], *seen[0])
+
+
 def test_two_graphs_share_a_work_space(B):
     """Two captured steps of different shapes on one work space, replayed in turn: neither leaves anything the other trips over."""
     cases = []
