@@ -93,9 +93,9 @@ struct Turn {
 
 // One token's heads of one kind: rows src + head * in_stride, head = r0, r0 + step, ... < heads, normed (kNorm, weight w), turned
 // and handed to store(head, whether in the first batch, index in the batch, pieces).  kBatch rows are under way at a time; `raw` are the ones already asked for.  All threads
-// of a warp go as many rounds (the shuffles want them all).
+// of a warp go as many rounds (the shuffles want them all); where there is no such token (the last CTA's end) nothing is read.
 template <bool BF16, int kBatch, bool kNorm, class Store>
-__device__ __forceinline__ void do_heads(const char* src, int64_t in_stride, int heads, int r0, int step, bool live, const Turn<BF16>& q,
+__device__ __forceinline__ void do_heads(const char* src, int64_t in_stride, int heads, int r0, int step, bool token, bool live, const Turn<BF16>& q,
                                          const float* w, Two (&raw)[kBatch], Store&& store) {
   constexpr int N = Piece<BF16>::N, E = BF16 ? 2 : 4;
   float wa[N], wb[N];
@@ -104,6 +104,7 @@ __device__ __forceinline__ void do_heads(const char* src, int64_t in_stride, int
     for (int i = 0; i < N; ++i) wa[i] = __ldg(w + q.off_a / E + i), wb[i] = __ldg(w + q.off_b / E + i);
   }
   const char* at = src + (r0 + (int64_t)kBatch * step) * in_stride;
+  const int readable = token ? heads : 0;
   for (int r = r0; r - r0 < heads; r += kBatch * step) {
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
@@ -144,7 +145,7 @@ __device__ __forceinline__ void do_heads(const char* src, int64_t in_stride, int
     }
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      if (r + (kBatch + b) * step < heads)
+      if (r + (kBatch + b) * step < readable)
         raw[b].a = *reinterpret_cast<const uint2*>(at + q.off_a), raw[b].b = *reinterpret_cast<const uint2*>(at + q.off_b);
       at += step * in_stride;
     }
@@ -231,8 +232,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotate_kernel(const __grid_co
       char* at = dst + h * a.qo_head * E;
       *reinterpret_cast<uint2*>(at + turn.off_a) = x.a, *reinterpret_cast<uint2*>(at + turn.off_b) = x.b;
     };
-    if (a.qw) do_heads<BF16, kBatch, true>(q_src, a.q_head * E, a.H, r0, step, live, turn, a.qw, raw, store);
-    else do_heads<BF16, kBatch, false>(q_src, a.q_head * E, a.H, r0, step, live, turn, nullptr, raw, store);
+    if (a.qw) do_heads<BF16, kBatch, true>(q_src, a.q_head * E, a.H, r0, step, t < a.T, live, turn, a.qw, raw, store);
+    else do_heads<BF16, kBatch, false>(q_src, a.q_head * E, a.H, r0, step, t < a.T, live, turn, nullptr, raw, store);
   }
   if (!a.k) return;
   auto store_k = [&](int h, bool first, int b, const Two& x) {
@@ -241,8 +242,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotate_kernel(const __grid_co
     char* dst = (a.k_pages ? a.k_pages : a.k_out) + to;
     *reinterpret_cast<uint2*>(dst + turn.off_a) = x.a, *reinterpret_cast<uint2*>(dst + turn.off_b) = x.b;
   };
-  if (a.kw) do_heads<BF16, kBatch, true>(k_src, a.kv_head * E, a.Hkv, r0, step, live, turn, a.kw, raw_k, store_k);
-  else do_heads<BF16, kBatch, false>(k_src, a.kv_head * E, a.Hkv, r0, step, live, turn, nullptr, raw_k, store_k);
+  if (a.kw) do_heads<BF16, kBatch, true>(k_src, a.kv_head * E, a.Hkv, r0, step, t < a.T, live, turn, a.kw, raw_k, store_k);
+  else do_heads<BF16, kBatch, false>(k_src, a.kv_head * E, a.Hkv, r0, step, t < a.T, live, turn, nullptr, raw_k, store_k);
   if (!a.v || !live) return;
   const char* v_src = a.v + t * a.kv_tok * E + lane * 16;
 #pragma unroll

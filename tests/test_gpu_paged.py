@@ -91,6 +91,24 @@ def test_rotate_one_side_only_and_plain_copies(B):
     assert torch.equal(out, x)                              # no norm, no rotation: the same bits
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,Hkv,norm", [(889, 12, 12, False), (1783, 32, 8, True), (3553, 28, 4, True), (4575, 32, 8, False)])
+def test_rotate_where_the_last_cta_is_not_full(B, dtype, T, H, Hkv, norm):
+    """Two, four and eight tokens a CTA with one to seven in the last, more heads than the first batch of rows."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    qkv = torch.randn(T, H + 2 * Hkv, D, generator=g, device="cuda").to(dtype)
+    q, k = qkv[:, :H], qkv[:, H:H + Hkv]
+    pos = torch.randint(0, 1 << 17, (T,), generator=g, device="cuda", dtype=torch.int32)
+    inv = 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+    w = [1 + 0.2 * torch.randn(D, generator=g, device="cuda") if norm else None for _ in range(2)]
+    outs = torch.zeros(T, H, D, device="cuda", dtype=dtype), torch.zeros(T, Hkv, D, device="cuda", dtype=dtype)
+    B.ckv_rotate(B.make_packed(q, k, 2), B.make_rotary(inv, q_norm_w=w[0], k_norm_w=w[1]), q, k, pos, i32([0, T // 2, T]), *outs)
+    for x, wt, out in ((q, w[0], outs[0]), (k, w[1], outs[1])):
+        want = R.turn(x, pos, inv, wt)
+        tol = 80 * EPS * want.abs().amax(-1, keepdim=True) + (2.0 ** -8 if dtype == torch.bfloat16 else 2 * EPS) * want.abs()
+        assert ((out.double() - want).abs() <= tol).all()
+
+
 # ------------------------------------------------------------------------------------------------ append
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("H,Hkv,page,counts,lens,rot,norm", [
