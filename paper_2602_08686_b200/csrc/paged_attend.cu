@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
   pdl_wait();
   Walk walk;
   const int rank = kCluster ? (int)blockIdx.x % n_cta : 0, n_ranks = kCluster ? n_cta : 1;
-  int index = blockIdx.x / n_cta, more = 0;   // of the cluster's item
+  int index = kCluster ? (int)blockIdx.x / n_cta : 0, more = 0;   // of the cluster's item
   if (!kCluster) {
     make_plan<kRowsThreads>(a, blockIdx.x, gridDim.x, sm.plan);
     pdl_launch_dependents();

@@ -1,5 +1,6 @@
 // Runs a CUDA kernel's own source on the host, a block at a time: every thread is a fibre, block barriers and warp
-// exchanges are where fibres wait for one another.  Enough for kernels of plain loads and stores; test infrastructure only.
+// exchanges are where fibres wait for one another.  Enough for kernels of plain loads and stores, one block at a time (no
+// clusters); PTX is taken out of the source beforehand (tests/host_cuda.py).  Test infrastructure only.
 // Arrays come from `guarded`: they end (or begin) where memory that may not be touched begins, so that a read or write
 // beside them ends the process.
 #pragma once
@@ -24,7 +25,6 @@
 #define __shared__ static
 #undef __forceinline__
 #define __forceinline__ inline
-#define asm if (0) __asm__   // PTX has no meaning here
 
 namespace host_cuda {
 
@@ -33,7 +33,7 @@ struct Fibre {
   ucontext_t at;
   std::vector<char> stack;
   int waits = 0;            // 0: runs, 1: for its warp, 2: for its block, 3: done
-  unsigned value = 0, peers[32];
+  unsigned long long value = 0, peers[32];
 };
 inline Fibre fibres[kMostThreads];
 inline ucontext_t scheduler;
@@ -87,7 +87,7 @@ inline void run_block(int threads) {
     if (!moved) fprintf(stderr, "threads wait for others that never come\n"), exit(3);
   }
 }
-inline const unsigned* exchange(unsigned mask, unsigned value) {
+inline const unsigned long long* exchange(unsigned mask, unsigned long long value) {
   if (mask != 0xffffffffu) fprintf(stderr, "exchanges of part of a warp are not covered\n"), exit(3);
   fibres[now].value = value;
   yield(1);
@@ -108,18 +108,37 @@ inline void __syncthreads() { host_cuda::yield(2); }
 inline void __syncwarp() { host_cuda::exchange(0xffffffffu, 0); }
 inline void __threadfence() {}
 inline unsigned __ballot_sync(unsigned mask, bool x) {
-  const unsigned* all = host_cuda::exchange(mask, x);
+  const unsigned long long* all = host_cuda::exchange(mask, x);
   unsigned r = 0;
-  for (int l = 0; l < 32; ++l) r |= (all[l] & 1u) << l;
+  for (int l = 0; l < 32; ++l) r |= (unsigned)(all[l] & 1) << l;
   return r;
 }
-inline float __shfl_xor_sync(unsigned mask, float x, int m) {
-  unsigned u;
-  memcpy(&u, &x, 4);
-  const unsigned r = host_cuda::exchange(mask, u)[(host_cuda::now & 31) ^ m];
-  memcpy(&x, &r, 4);
+inline bool __any_sync(unsigned mask, bool x) { return __ballot_sync(mask, x) != 0; }
+template <class T>
+T host_shuffle(unsigned mask, T x, int from) {
+  static_assert(sizeof(T) <= 8, "one word");
+  unsigned long long u = 0;
+  memcpy(&u, &x, sizeof(T));
+  u = host_cuda::exchange(mask, u)[from];
+  memcpy(&x, &u, sizeof(T));
   return x;
 }
+template <class T>
+T __shfl_sync(unsigned mask, T x, int from) { return host_shuffle(mask, x, from & 31); }
+template <class T>
+T __shfl_xor_sync(unsigned mask, T x, int m) { return host_shuffle(mask, x, (host_cuda::now & 31) ^ m); }
+template <class T>
+T __shfl_up_sync(unsigned mask, T x, int d) {
+  const int lane = host_cuda::now & 31;
+  return host_shuffle(mask, x, lane >= d ? lane - d : lane);
+}
+inline int __reduce_max_sync(unsigned mask, int x) {
+  const unsigned long long* all = host_cuda::exchange(mask, (unsigned)x);
+  int r = x;
+  for (int l = 0; l < 32; ++l) r = (int)(unsigned)all[l] > r ? (int)(unsigned)all[l] : r;
+  return r;
+}
+inline int __ffs(unsigned x) { return __builtin_ffs(x); }
 inline float __uint_as_float(unsigned u) {
   float f;
   memcpy(&f, &u, 4);

@@ -1,12 +1,10 @@
 """rotate_kernel's own source run on the host (tests/host_cuda.h): every array ends where memory that may not be touched begins, so a
 read or write behind it ends the process.  No GPU needed."""
-import os
 import subprocess
 
 import pytest
 
-HERE = os.path.dirname(os.path.abspath(__file__))
-CSRC = os.path.join(os.path.dirname(HERE), "paper_2602_08686_b200", "csrc")
+import host_cuda
 
 MAIN = r"""
 #include "host_cuda.h"
@@ -135,11 +133,7 @@ int main(int, char** v) {
 
 @pytest.fixture(scope="module")
 def program(tmp_path_factory):
-    d = tmp_path_factory.mktemp("rotate")
-    (d / "main.cpp").write_text(MAIN)
-    cuda = os.path.join(os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"))), "include")
-    subprocess.check_call(["g++", "-std=c++17", "-O1", "-w", "-I", HERE, "-I", CSRC, "-I", cuda, str(d / "main.cpp"), "-o", str(d / "main")])
-    return str(d / "main")
+    return host_cuda.build(str(tmp_path_factory.mktemp("rotate")), MAIN)
 
 
 @pytest.mark.parametrize("append", [0, 1])
