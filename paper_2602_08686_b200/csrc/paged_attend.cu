@@ -2,6 +2,8 @@
 // keys with a running maximum m and sum l per query row,
 //   m' = max(m, x),  l' = l 2^(m - m') + 2^(x - m'),  o' = o 2^(m - m') + 2^(x - m') v,   x = scale log2(e) q.k,
 // which can be cut anywhere along the keys: partial (m, l, o) of any two ranges join by the same rule.
+// A row that saw nothing is one whose sum is exactly zero: the largest logit adds one to it, and a NaN, which no maximum notices, a
+// NaN, which goes on to the output and the lse.
 //
 // This file has the kernel for fp32 inputs, the join of split items and the choice of kernels.
 //
@@ -157,7 +159,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       float top = m[r];
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-      const float c = top == -INFINITY ? 0.f : exp2f(m[r] - top);
+      const float c = exp2f(m[r] - (top == -INFINITY ? 0.f : top));
       float sum = l[r] * c;
       sum += __shfl_xor_sync(0xffffffffu, sum, 8);
       sum += __shfl_xor_sync(0xffffffffu, sum, 16);
@@ -177,8 +179,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
     const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.slot_rows;
     auto finish = [&](int r, int d, float top, float sum, float o) {
       const int64_t at = out_row(a, it, r);
-      out[at * kHeadDim + d] = top == -INFINITY ? 0.f : o / sum;
-      if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      out[at * kHeadDim + d] = sum == 0.f ? 0.f : o / sum;
+      if (lse && d == 0) lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
     };
     for (int e = threadIdx.x; e < rows * kHeadDim; e += kRowsThreads) {
       const int r = e / kHeadDim, d = e - r * kHeadDim;
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       for (int w = 0; w < kRowsWarps; ++w) top = fmaxf(top, sm.ml[w][r].x);
       float sum = 0.f, o = 0.f;
       for (int w = 0; w < kRowsWarps; ++w) {
-        const float c = top == -INFINITY ? 0.f : exp2f(sm.ml[w][r].x - top);
+        const float c = exp2f(sm.ml[w][r].x - (top == -INFINITY ? 0.f : top));
         sum = fmaf(sm.ml[w][r].y, c, sum);
         o = fmaf(sm.o[w][r][d], c, o);
       }
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) join_kernel(WorkArgs a, int wo
       }
       if (p0 + kBatch <= parts) fetch(p0 + kBatch, parts);
     }
-    const bool none = ml.x == -INFINITY;
+    const bool none = ml.y == 0.f;
     const float inv = none ? 0.f : 1.0f / ml.y;
     const int64_t at = out_row(a, it, r);
     if (none) o = make_float4(0.f, 0.f, 0.f, 0.f);   // a part that saw nothing may hold anything times zero

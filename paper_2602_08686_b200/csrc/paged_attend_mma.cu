@@ -279,9 +279,9 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
     const int64_t slot = ((int64_t)blockIdx.x * 2 + which) * a.slot_rows;
     auto finish = [&](int r, int d, float top, float sum, float2 x) {
       const int64_t at = out_row(a, it, r);
-      const float inv = top == -INFINITY ? 0.f : 1.0f / sum;
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       *reinterpret_cast<uint32_t*>(out + at * kHeadDim + d) = bf16x2(x.x * inv, x.y * inv);
-      if (lse && d == 0) lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      if (lse && d == 0) lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
     };
     for (int e = threadIdx.x; e < rows * (kHeadDim / 2); e += kThreads) {
       const int r = e / (kHeadDim / 2), d = (e - r * (kHeadDim / 2)) * 2;

@@ -503,7 +503,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       l = l * f0 + x.y * f1, m = top;
     }
     const bool joined = !pair;
-    const bool none = m == -INFINITY;
+    const bool none = l == 0.f;   // nothing seen (a NaN sum is not nothing)
     const float inv = none ? 0.f : 1.0f / l;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {

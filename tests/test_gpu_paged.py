@@ -460,6 +460,59 @@ def test_attend_masked_infinities(B, counts):
         assert (lse.double() - want_lse).abs()[:seen].max() <= 1e-3
 
 
+@pytest.mark.parametrize("where", ["query", "keys"])
+@pytest.mark.parametrize("counts,rows,width", [
+    ([1], [[300, 90]], 0), ([1], [[9000, 700]], 0), ([1, 1, 1], [[500, 40], [33, 1], [600, 600]], 900),    # clusters, split, wide tables
+    ([5], [[400, 77]], 0), ([5, 2], [[16000, 3000], [900, 2]], 0), ([7], [[400, 77]], 900),
+    ([30], [[300, 31]], 0), ([100], [[100, 700]], 0), ([90], [[9000, 8000]], 0), ([400, 3], [[3000, 400], [70, 3]], 0)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attend_carries_nan(B, dtype, counts, rows, width, where):
+    """A NaN in a query, or in every key a token sees, reaches that token's output and lse, and nobody else's: only a token that
+    sees no row gets zeros.  More tokens than rows among them, whose first see nothing."""
+    H, Hkv = 8, 2
+    c = R.Cache(rows, 32, dtype=dtype, device="cuda", seed=sum(counts), max_extra=0)
+    if width:
+        wide = torch.full((len(rows), Hkv, width), 0x7ffffff0, dtype=torch.int32, device="cuda")
+        wide[:, :, :c.max_pages] = c.table
+        c.table, c.max_pages = wide, width
+    st = starts_of(counts)
+    q = torch.randn(st[-1], H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5)).to(dtype)
+    sick = torch.zeros(st[-1], H, dtype=torch.bool, device="cuda")
+    clean = q.clone()
+    if where == "query":
+        for t in {0, st[-1] // 2, st[-1] - 1}:
+            for h in (1, 6):
+                q[t, h, (7 * t + h) % D] = float("nan")
+                sick[t, h] = True
+    else:                                              # unit 0, head 0: every key
+        k, v = c.rows[0][0]
+        c.rows[0][0] = (torch.full_like(k, float("nan")), v)
+        for j in range(0, k.shape[0], 32):
+            c.k_pages[int(c.table[0, 0, j // 32]), :min(32, k.shape[0] - j)] = float("nan")
+        sick[:st[1], :H // Hkv] = True
+    for causal in (True, False):
+        out, lse = run_attend(B, c, q, st, causal, max_new=max(counts))
+        want, want_lse = R.attend(q, st, c.rows, causal)
+        ill = sick.clone()
+        for u in range(len(counts)):                   # tokens that see nothing stay as they are
+            for g in range(Hkv):
+                for i in range(max(0, min(counts[u], counts[u] - rows[u][g])) if causal else 0):
+                    ill[st[u] + i, g * (H // Hkv):(g + 1) * (H // Hkv)] = False
+        assert torch.equal(torch.isnan(lse), ill)
+        assert torch.equal(torch.isnan(out).all(-1), ill) and torch.equal(torch.isnan(out).any(-1), ill)
+        well = ~ill
+        assert torch.equal((lse == -math.inf)[well], torch.isinf(want_lse)[well])
+        seen = well & ~torch.isinf(want_lse)
+        # (as check_attend, for the tokens that are well)
+        kmax = max(float(k.double().nan_to_num().norm(dim=-1).max()) for row in c.rows for k, _ in row)
+        vmax = max(float(v.double().abs().max()) for row in c.rows for _, v in row)
+        r = 132 * EPS * float(clean.double().norm(dim=-1).max()) * kmax / math.sqrt(D) + 2.0 ** -20 + (max(map(max, rows)) / 8 + 256) * EPS
+        assert ((lse.double() - want_lse).abs() <= r + 2 * EPS * want_lse.abs())[seen].all()
+        tol = 2 * r * vmax + (2.0 ** -8 * (vmax + want.abs()) if dtype == torch.bfloat16 else EPS * want.abs())
+        assert ((out.double() - want).abs() <= tol)[seen].all()
+        assert (out[well & torch.isinf(want_lse)] == 0).all()
+
+
 @pytest.mark.parametrize("dtype,counts", [(torch.float32, [2]), (torch.bfloat16, [2]), (torch.bfloat16, [90])])
 def test_attend_leaves_out_bad_pages_and_says_so(B, dtype, counts):
     n = counts[0]
