@@ -396,7 +396,8 @@ ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, co
  * Attention of the units' tokens over the cache; with `causal`, lengths count the tokens' own rows (append first).  With n
  * tokens in unit u, its token i sees rows j <= lengths[u,g] - n + i of head g (causal), or every row j < lengths[u,g].
  *   out [T,H,d] = softmax(scale q k^T) v in the dtype of `paged`, on a 32-byte boundary;  lse_or_null [T,H] fp32 = ln sum_j exp(scale q . k_j).
- * A token that sees no row gets zeros and -infinity; one that sees a NaN logit, NaN for both.  Each sum is 32-bit and taken in an order that the shapes,
+ * A token that sees no row gets zeros and -infinity; one that sees a NaN logit, NaN for both.  Values up to 2^94 in size stay
+ * in range whatever the logits (sums run against a reference that may lag behind the largest by 2^16).  Each sum is 32-bit and taken in an order that the shapes,
  * lengths and token counts alone decide.
  */
 ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k_pages, const void* v_pages,

@@ -19,7 +19,7 @@
 // they take 0.5 us less on two query tiles and more on one).
 // No maximum is taken per step.  Any reference m gives the same softmax, up to overflow: P, l and O are floating-point, and a
 // common factor costs none of their bits.  So a row keeps the reference of its first visible step, and the sums tell
-// whether an exponential left the range (2^64: then, and only then, the maximum is taken, O is rescaled in TMEM and
+// whether an exponential left the range (2^16: then, and only then, the maximum is taken, O is rescaled in TMEM and
 // the step is done again).
 // Warps 0-3 and 4-7: softmax of stream 0 and 1; warps 8, 9: their MMAs; warp 10: TMA; warp 11 walks the items ahead of the others.
 // Every wait is bounded and reports CKV_ERR_TIMEOUT through the status word.
@@ -39,7 +39,9 @@ constexpr uint32_t kTileBytes = 2 * kHalf;
 constexpr int kTcGranule = kBothTiles;         // least cost a CTA takes on (two tiles: 31 us instead of 27 for 40 tokens on 2048 rows)
 constexpr int kInfo = 8;                       // ring of per-tile notes from the loader
 constexpr int kJobs = 4;                       // ring of items
-constexpr float kOverflow = 1.8446744e19f;     // 2^64: a step's sum above it is done again with a new reference
+// A step's sum above it is done again with a new reference.  Sums and outputs of up to 2^24 rows (2^18 steps) then stay below 2^34 and
+// 2^34 max|v|, in range for values up to 2^94 (the largest fp32 is 2^128).
+constexpr float kOverflow = 65536.0f;
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);   // fp32 += bf16 * bf16, M = 128
 constexpr uint32_t kIdescQK = kIdesc | ((64u >> 3) << 17);
 constexpr uint32_t kIdescPV = kIdesc | ((128u >> 3) << 17) | (1u << 16);                // B (the values) is MN-major

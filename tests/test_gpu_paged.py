@@ -439,6 +439,35 @@ def test_attend_large_logits_and_scales(B, dtype, counts):
         check_attend(c, q, [0, n], out, lse, scale=scale or None, spread=False)
 
 
+@pytest.mark.parametrize("size", [1e21, 4e27])
+@pytest.mark.parametrize("dtype,counts,rows", [
+    (torch.float32, [3], 1500), (torch.bfloat16, [1], 700), (torch.bfloat16, [4], 12000), (torch.bfloat16, [40], 20000),
+    (torch.bfloat16, [90], 20000), (torch.bfloat16, [300], 9000), (torch.bfloat16, [700], 800)])
+def test_attend_large_values_under_rising_logits(B, dtype, counts, rows, size):
+    """Values up to 2^94 stay in range in every kernel while the logits climb by 41 (a factor of 2^59) over 256 keys and fall again,
+    over and over, so that each of the parts a cache is cut into sees a rise."""
+    n = counts[0]
+    c = R.Cache([[n + rows, n + rows // 3]], 32, dtype=dtype, device="cuda", seed=n)
+    q = torch.randn(n, 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).mul_(0.1)
+    q[..., 0] = 8.0
+    q = q.to(dtype)
+    for g in range(2):
+        k, v = c.rows[0][g]
+        L = k.shape[0]
+        k = k.clone()
+        wave = torch.cat((torch.zeros(128), torch.linspace(0.0, 41.0 * math.sqrt(D) / 8.0, 256), torch.zeros(128)))
+        k[:, 0] = wave.repeat(L // 512 + 1)[:L].to(dtype)
+        v = (v.double() * size).clamp(-2.0 ** 94, 2.0 ** 94).to(dtype)
+        c.rows[0][g] = (k, v)
+        for pool, x in ((c.k_pages, k), (c.v_pages, v)):
+            for j in range(0, L, 32):
+                pool[int(c.table[0, g, j // 32]), :min(32, L - j)] = x[j:j + 32].cuda()
+    for causal in (True, False):
+        out, lse = run_attend(B, c, q, [0, n], causal)
+        assert torch.isfinite(out).all()
+        check_attend(c, q, [0, n], out, lse, causal, spread=False)
+
+
 @pytest.mark.parametrize("counts", [[1], [5], [150]])
 def test_attend_masked_infinities(B, counts):
     """Infinite and NaN keys and values behind what a token sees do not reach it."""
