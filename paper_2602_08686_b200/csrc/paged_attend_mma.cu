@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
       }
       sm.q[mt][hh][i][ln] = x;
     }
-    int limit[MT][2], least = it.len;
+    int limit[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
         const int r = mt * 16 + hh * 8 + p;
         limit[mt][hh] = r < rows ? row_limit(a, it, r) : it.visible;   // rows that do not exist mask nothing
       }
-    least = row_limit(a, it, 0);
+    const int least = row_limit(a, it, 0);
     float o[MT][16][4], m[MT][2], l[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {

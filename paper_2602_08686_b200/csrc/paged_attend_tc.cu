@@ -126,7 +126,7 @@ __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter
         const Item& it = k.it;
         job.it = it, job.pair = k.pair, job.block = k.block;
         job.n = it.t1 - it.t0, job.tiles2 = both_tiles(a.w, it.n, it.block), job.steps = job.tiles2 ? 2 * job.n : job.n;
-        job.see = a.w.causal ? min(max(it.len - it.n + it.block * a.w.tokens + 1, 0), it.len) : it.len;
+        job.see = rows_seen(a.w, it.n, it.len, it.block * a.w.tokens + 1);
         job.whole = it.t0 == 0 && it.t1 == it.tiles;
         job.odd = 0;
       }
@@ -418,7 +418,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     const int tok0 = it.block * a.w.tokens + q_tile * a.TQ;   // first token of the tile
     const int token = tok0 + r_tok;
     const bool live = r < a.TQ * a.w.G && token < it.n;
-    auto limit_of = [&](int tk) { return a.w.causal ? min(max(it.len - it.n + tk + 1, 0), it.len) : it.len; };
+    auto limit_of = [&](int tk) { return rows_seen(a.w, it.n, it.len, tk + 1); };
     const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
     // rows of no token hold what shared memory held, or another unit's queries: above everything, they ask for no step again
     float m = live ? -INFINITY : INFINITY, l = 0.f;

@@ -44,7 +44,7 @@ inline void set_blocks(WorkArgs& a, int64_t most, int M, int tokens, int tile, i
 
 struct Item {
   int u, g, block;       // block of rows
-  int first, n, len;     // the unit's first token and token count; rows the head holds
+  int first, n, len;     // the unit's first token and token count; the head's length
   int rows;              // query rows of the unit (n * G)
   int visible;           // rows the block's last token sees
   int tiles;             // tiles of the whole item
@@ -56,17 +56,20 @@ __device__ __forceinline__ int unit_blocks(const WorkArgs& a, int n) {
   const int per = a.tokens ? a.tokens : a.M, units = a.tokens ? n : n * a.G;   // at most 2^26 rows
   return units <= per ? (units > 0) : (units + per - 1) / per;
 }
-// Rows the head holds; a length that the table has no pages for, or below zero, is reported and cut.
+// The head's length; one that the table has no pages for is reported (the rows without a page are left out, see rows_seen), and so
+// is one below zero, which counts as zero.
 __device__ __forceinline__ int head_length(const WorkArgs& a, int pair) {
-  const int len = a.lengths[pair], cut = min(max(len, 0), a.max_pages << a.log_p);
-  if (cut != len) report_status(a.status, kStatusPage);
-  return cut;
+  const int len = a.lengths[pair];
+  if (len < 0 || len > a.max_pages << a.log_p) report_status(a.status, kStatusPage);
+  return max(len, 0);
+}
+// Rows of the cache that the unit's first `tokens` tokens see between them: those that the last of them sees.
+__device__ __forceinline__ int rows_seen(const WorkArgs& a, int n, int len, int tokens) {
+  return min(a.causal ? max(len - n + min(tokens, n), 0) : len, a.max_pages << a.log_p);
 }
 // rows that the last token of a block sees
 __device__ __forceinline__ int block_visible(const WorkArgs& a, int n, int len, int block) {
-  if (!a.causal) return len;
-  const int end = a.tokens ? (block + 1) * a.tokens : ((block + 1) * a.M >= n * a.G ? n : ((block + 1) * a.M + a.G - 1) / a.G);
-  return min(max(len - n + min(end, n), 0), len);
+  return rows_seen(a, n, len, a.tokens ? (block + 1) * a.tokens : ((block + 1) * a.M >= n * a.G ? n : ((block + 1) * a.M + a.G - 1) / a.G));
 }
 __device__ __forceinline__ int tiles_of(const WorkArgs& a, int visible) { return max((visible + a.tile - 1) >> a.log_tile, 1); }
 
@@ -396,9 +399,7 @@ __device__ __forceinline__ int64_t out_row(const WorkArgs& a, const Item& it, in
 }
 // Rows of the cache that query row r of the block sees.
 __device__ __forceinline__ int row_limit(const WorkArgs& a, const Item& it, int r) {
-  if (!a.causal) return it.len;
-  const int token = (it.block * a.M + r) / a.G;
-  return min(max(it.len - it.n + token + 1, 0), it.len);
+  return rows_seen(a, it.n, it.len, (it.block * a.M + r) / a.G + 1);
 }
 // Pool row (page * page_size + row within) is not formed: the pool's strides are free.  A bad page gives -1.
 __device__ __forceinline__ int page_of(const WorkArgs& a, const Item& it, int slot) {

@@ -165,6 +165,8 @@ T max(T a, T b) { return a > b ? a : b; }
 
 template <class... P, class... A>
 cudaError_t host_launch(const cudaLaunchConfig_t* cfg, void (*kernel)(P...), A... args) {
+  for (unsigned i = 0; i < cfg->numAttrs; ++i)
+    if (cfg->attrs[i].id == cudaLaunchAttributeClusterDimension) fprintf(stderr, "clusters are not covered\n"), exit(3);
   gridDim = cfg->gridDim, blockDim = cfg->blockDim;
   host_cuda::body = [=] { kernel(P(args)...); };
   for (unsigned y = 0; y < gridDim.y; ++y)

@@ -103,3 +103,11 @@ def go(program, H, Hkv, width, causal, counts, lens):
 def test_split_form(program, counts, lens, causal):
     """A table too wide for clusters: the schedule splits the work, the join adds the parts."""
     assert go(program, 8, 2, 1200, causal, counts, lens) == 0
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+def test_rows_past_the_table(program, causal):
+    """Rows the table has no pages for are left out; the others are seen by the tokens that the lengths say see them."""
+    for width, H, counts, more in ((3, 8, [6], (4, 0)), (3, 2, [1, 9], (1, 12, 3, 30)), (3, 2, [40], (39, 2)), (700, 2, [1, 9], (1, 12, 3, 30))):
+        lens = [[16 * width + more[u * 2 + g] for g in range(2)] for u in range(len(counts))]
+        assert go(program, H, 2, width, causal, counts, lens) == 4096, (width, counts)

@@ -568,6 +568,38 @@ def test_attend_leaves_out_bad_pages_and_says_so(B, dtype, counts):
     assert B.ckv_device_status(ws) == B.OK
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("counts,pages", [([1], 4), ([5], 4), ([5], 400), ([40], 20), ([300], 30), ([90, 7], 300)])
+def test_attend_leaves_out_rows_past_the_table(B, dtype, causal, counts, pages):
+    """Lengths past the table's last page (an append that ran out of pages): the rows it has no place for are left out, every
+    other row is seen by the tokens that the lengths say see it."""
+    room = 32 * pages
+    c = R.Cache([[room, room] for _ in counts], 32, dtype=dtype, device="cuda", seed=pages)
+    q = torch.randn(sum(counts), 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)).to(dtype)
+    st = starts_of(counts)
+    more = [[max(1, n // 2), max(1, n - 1)] for n in counts]
+    pg = B.make_paged(c.k_pages, c.table, q=q, causal=causal)
+    ws = B.alloc_paged_workspace(pg)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    B.ckv_paged_attend(pg, q, c.k_pages, c.v_pages, c.table, i32([[room + x for x in m] for m in more]), i32(st), out, ws, lse=lse)
+    assert B.ckv_device_status(ws) == B.ERR_PAGE and B.ckv_device_status(ws) == B.OK
+    for u, n in enumerate(counts):
+        for g in range(2):
+            k, v = (x.cuda().double() for x in c.rows[u][g])
+            qs = q[st[u]:st[u + 1], 4 * g:4 * g + 4].double()
+            x = torch.einsum("nhd,ld->nhl", qs, k) / math.sqrt(D)
+            if causal:
+                sees = room + more[u][g] - n + torch.arange(n, device="cuda")
+                x = x.masked_fill((torch.arange(room, device="cuda")[None] > sees[:, None])[:, None], -math.inf)
+            want = torch.einsum("nhl,ld->nhd", torch.softmax(x, -1), v)
+            r = 132 * EPS * float(q.double().norm(dim=-1).max()) * float(k.norm(dim=-1).max()) / math.sqrt(D) + 2.0 ** -20 + (room / 8 + 256) * EPS
+            tol = 2 * r * v.abs().max() + (2.0 ** -8 * (v.abs().max() + want.abs()) if dtype == torch.bfloat16 else EPS * want.abs())
+            assert ((out[st[u]:st[u + 1], 4 * g:4 * g + 4].double() - want).abs() <= tol).all()
+            want_lse = torch.logsumexp(x, -1)
+            assert ((lse[st[u]:st[u + 1], 4 * g:4 * g + 4].double() - want_lse).abs() <= r + 2 * EPS * want_lse.abs()).all()
+
+
 def test_attend_same_bits_again_and_on_two_streams(B):
     for counts in ([1, 1], [60, 3]):
         c = R.Cache([[3000, 100], [777, 2500]], 64, dtype=torch.bfloat16, device="cuda")
