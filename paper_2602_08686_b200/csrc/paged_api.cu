@@ -39,12 +39,56 @@ ckv_status check_tokens(const ckv_paged* pg) {
   if ((int64_t)pg->n_units * pg->n_kv_heads > 65536) return CKV_ERR_UNSUPPORTED;
   return CKV_OK;
 }
-// Strides of a token array: rows on 16-byte boundaries that do not overlap one another.
+// Strides of a token array: rows on 16-byte boundaries (that they do not overlap is asked where they are written, see in_place_ok).
 bool token_strides(const ckv_paged& pg, int64_t tok, int64_t head, int heads) {
   const int64_t e = esize(pg);
   if (tok < 0 || head < 0 || (tok * e) % 16 || (head * e) % 16) return false;
   if ((heads > 1 && head < kHeadDim) || (pg.n_tokens > 1 && tok < kHeadDim)) return false;
   return tok < ((int64_t)1 << 38) && head < ((int64_t)1 << 38);   // a tensor map's strides end at 2^40 bytes
+}
+// Rows of 128 elements at base + i * outer + j * inner, i < n_outer, j < n_inner (strides in elements).
+struct Rows {
+  const void* base;
+  int64_t n_outer, outer, n_inner, inner, esz;
+  Range range() const { return range_of(base, n_outer, n_inner, outer, inner, esz); }
+  // no row shares memory with another: one stride steps over all that the other reaches
+  bool apart_from_itself() const {
+    return n_outer == 1 || n_inner == 1 || outer >= (n_inner - 1) * inner + kHeadDim || inner >= (n_outer - 1) * outer + kHeadDim;
+  }
+};
+// Whether no row of a is on one of b's.  Arrays that are interleaved (views of a fused projection) have one outer stride; with two
+// different ones over the same memory they count as overlapping.
+bool apart(const Rows& a, const Rows& b) {
+  if (!overlap(a.range(), b.range())) return true;
+  const int64_t row = kHeadDim * a.esz, s = a.outer * a.esz;
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.base) - reinterpret_cast<uintptr_t>(a.base));
+  const bool steps = a.n_outer > 1 || b.n_outer > 1;
+  if (steps && (a.n_outer != b.n_outer || a.outer != b.outer || s < row)) return false;
+  // each within an outer step, and beside the other there
+  const int64_t at = steps ? ((d % s) + s) % s : 0;
+  if (steps && at >= (a.n_inner - 1) * a.inner * a.esz + row && at + (b.n_inner - 1) * b.inner * b.esz + row <= s) return true;
+  // row j of a against row k of b, whichever outer steps bring them closest
+  auto meet = [&](int64_t x) {   // x: from one to the other within the same step
+    if (!steps) return -row < x && x < row;
+    const int64_t r = ((x % s) + s) % s, i = (r - x) / s;   // i steps on it is r away, one step less r - s
+    return (r < row && i > -a.n_outer && i < a.n_outer) || (s - r < row && i - 1 > -a.n_outer && i - 1 < a.n_outer);
+  };
+  if (a.inner == b.inner) {      // only the difference of the two matters
+    for (int64_t k = -(a.n_inner - 1); k < b.n_inner; ++k)
+      if (meet(d + k * a.inner * a.esz)) return false;
+    return true;
+  }
+  for (int64_t j = 0; j < a.n_inner; ++j)
+    for (int64_t k = 0; k < b.n_inner; ++k)
+      if (meet(d + (k * b.inner - j * a.inner) * a.esz)) return false;
+  return true;
+}
+// Rows that are turned in place: each is one (token, head) pair's, and none is among the other arrays'.
+bool in_place_ok(const Rows& x, std::initializer_list<Rows> others) {
+  if (!x.apart_from_itself()) return false;
+  for (const Rows& o : others)
+    if (o.base && !apart(x, o)) return false;
+  return true;
 }
 ckv_status check_pages(const ckv_paged* pg) {
   if (pg->page_size < 1 || pg->n_pages < 1 || pg->max_pages < 1) return CKV_ERR_INVALID_ARG;
@@ -122,6 +166,8 @@ ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const vo
   const Range kr = k ? range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e) : Range{0, 0};
   if (q && !out_ok(*paged, q_out, q, H, {qr, kr})) return CKV_ERR_INVALID_ARG;
   if (k && !out_ok(*paged, k_out, k, Hkv, {qr, kr})) return CKV_ERR_INVALID_ARG;
+  const Rows q_rows{q, T, paged->q_stride_tok, H, paged->q_stride_head, e}, k_rows{k, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e};
+  if ((q && q_out == q && !in_place_ok(q_rows, {k_rows})) || (k && k_out == k && !in_place_ok(k_rows, {q_rows}))) return CKV_ERR_INVALID_ARG;
   if (q && k && q_out != q && k_out != k &&
       overlap(range_of(q_out, T, H, (int64_t)H * kHeadDim, kHeadDim, e), range_of(k_out, T, Hkv, (int64_t)Hkv * kHeadDim, kHeadDim, e)))
     return CKV_ERR_INVALID_ARG;
@@ -161,6 +207,9 @@ ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const vo
         return CKV_ERR_INVALID_ARG;
       const Range qr = range_of(q_or_null, T, H, paged->q_stride_tok, paged->q_stride_head, e);
       if (overlap(qr, kp) || overlap(qr, vp) || !out_ok(*paged, q_out, q_or_null, H, {qr, kr, vr, kp, vp})) return CKV_ERR_INVALID_ARG;
+      const Rows k_rows{k, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e}, v_rows{v, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e};
+      if (q_out == q_or_null && !in_place_ok({q_or_null, T, paged->q_stride_tok, H, paged->q_stride_head, e}, {k_rows, v_rows}))
+        return CKV_ERR_INVALID_ARG;
     }
   }
   CKV_CUDA(launch_rotate(*paged, rotary, any ? q_or_null : nullptr, any ? k : nullptr, any ? v : nullptr, positions,

@@ -91,6 +91,26 @@ def test_rotate_one_side_only_and_plain_copies(B):
     assert torch.equal(out, x)                              # no norm, no rotation: the same bits
 
 
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("layout", ["token, kind, head", "token, head, kind", "kind, token, head", "kind, head, token", "head, kind, token"])
+def test_rotate_in_place_in_any_layout(B, layout, T):
+    """Queries and keys as views of one projection, turned where they lie, whatever the order of its dimensions."""
+    H = 4
+    sizes = dict(token=T, kind=3, head=H)
+    order = layout.split(", ")
+    x = torch.randn(*[sizes[n] for n in order], D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(T))
+    was = x.clone()
+    view = lambda y, i: y.permute(*[order.index(n) for n in ("token", "kind", "head")], 3)[:, i]
+    q, k = view(x, 0), view(x, 1)
+    inv = 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") + 5
+    B.ckv_rotate(B.make_packed(q, k, 1), B.make_rotary(inv), q, k, pos, i32([0, T]), q, k)
+    for i in range(2):
+        want = R.turn(view(was, i), pos, inv)
+        assert ((view(x, i).double() - want).abs() <= 80 * EPS * want.abs().amax(-1, keepdim=True) + 2 * EPS * want.abs()).all()
+    assert torch.equal(view(x, 2), view(was, 2))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,H,Hkv,norm", [(889, 12, 12, False), (1783, 32, 8, True), (3553, 28, 4, True), (4575, 32, 8, False)])
 def test_rotate_where_the_last_cta_is_not_full(B, dtype, T, H, Hkv, norm):

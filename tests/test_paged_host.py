@@ -1,10 +1,12 @@
 """The paged-cache entry points on the host: argument errors are reported before anything is launched, the binding
 compares every tensor with the layout its struct was made for.  No GPU needed: no call below passes validation."""
 import ctypes as C
+import subprocess
 
 import pytest
 import torch
 
+import host_cuda
 from paper_2602_08686_b200 import binding as B
 from paper_2602_08686_b200 import build as ckv_build
 
@@ -198,3 +200,81 @@ def test_outputs_and_pages_apart_from_inputs():
     for k, v in ((far(6) - 256, far(2)), (far(1), far(7) + 99 * 64 * 256), (far(6) - 2 * 8 * 4096 * 256 + 256, far(2))):
         assert B.lib().ckv_gather_pages(C.byref(s), C.byref(p), C.byref(pg), k, v, far(3), far(4), far(5), far(9), far(6), far(7),
                                         far(8), far(10), BIG, None) == B.ERR_INVALID_ARG
+
+
+def test_rows_written_in_place_are_apart():
+    """A row that is two (token, head) pairs', or a query's and a key's, would be turned twice at once."""
+    far = lambda i: FAKE + i * (1 << 30)
+    rot = rotary()
+    in_place = dict(rotate=dict(q_out=far(1), k_out=far(2)), append=dict(q_out=far(1)))
+    for name, outs in in_place.items():
+        for strides in (dict(q_stride_tok=128), dict(q_stride_tok=31 * 128), dict(q_stride_head=9 * 128, q_stride_tok=128),
+                        dict(q_stride_head=256, q_stride_tok=384)):
+            assert call(name, paged(**strides), rot, **outs) == B.ERR_INVALID_ARG, (name, strides)
+    for strides in (dict(kv_stride_tok=128), dict(kv_stride_tok=7 * 128), dict(kv_stride_head=9 * 128, kv_stride_tok=128)):
+        assert call("rotate", paged(**strides), rot, k_out=far(2)) == B.ERR_INVALID_ARG, strides
+    # the keys (append: or the values) start inside the queries' rows, or are the queries
+    for shift in (0, 256, 31 * 256, 48 * 256, -7 * 256, 3 * 48 * 256 + 64, -9 * 48 * 256):
+        at = far(1) + shift
+        assert call("rotate", paged(), rot, q_out=far(1), k=at) == B.ERR_INVALID_ARG, shift
+        assert call("rotate", paged(), rot, k=at, k_out=at) == B.ERR_INVALID_ARG, shift
+        assert call("append", paged(), rot, q_out=far(1), k=at) == B.ERR_INVALID_ARG, shift
+        assert call("append", paged(), rot, q_out=far(1), v=at) == B.ERR_INVALID_ARG, shift
+    pg = paged(kv_stride_tok=50 * 128)                 # other token strides over the same memory
+    assert call("rotate", pg, rot, q_out=far(1), k=far(1) + 32 * 256) == B.ERR_INVALID_ARG
+
+
+APART = r"""
+#include "host_cuda.h"
+#include <random>
+#include "paged_api.cu"
+namespace ckv {
+PagedWs paged_ws(const ckv_paged&) { return {}; }
+cudaError_t launch_rotate(const ckv_paged&, const ckv_rotary*, const void*, const void*, const void*, const int32_t*, const int32_t*, void*, void*,
+                          const int32_t*, const int32_t*, void*, void*, int32_t*, int*, cudaStream_t) { return cudaErrorUnknown; }
+cudaError_t launch_gather_pages(const ckv_shape&, const ckv_params&, const ckv_paged&, const void*, const void*, const int32_t*, const int32_t*,
+                                const int32_t*, const int32_t*, void*, void*, int32_t*, int*, cudaStream_t) { return cudaErrorUnknown; }
+cudaError_t launch_paged_attend(const ckv_paged&, const void*, const void*, const void*, const int32_t*, const int32_t*, const int32_t*, void*,
+                                float*, char*, cudaStream_t) { return cudaErrorUnknown; }
+}
+extern "C" size_t ckv_workspace_bytes(const ckv_shape*, const ckv_params*) { return 0; }
+int main() {
+  std::mt19937 rng(1);
+  auto any = [&](int lo, int hi) { return (int64_t)(lo + rng() % (hi - lo + 1)); };
+  int yes = 0, no = 0, careful = 0;
+  for (int c = 0; c < 200000; ++c) {
+    const int64_t esz = any(0, 1) ? 2 : 4, n = any(1, 5), outer = any(16, 16 * 14) * 8, q = 128;
+    auto heads = [&] { return any(0, 2) ? q * any(1, 4) : any(16, 60) * 8; };
+    const int64_t inner = heads();
+    Rows a{(char*)0 + (1 << 20), n, outer, any(1, 5), inner, esz}, b{(char*)0 + (1 << 20) + 16 * any(-900, 900), n, outer, any(1, 5), inner, esz};
+    if (any(0, 3) == 0) b.inner = heads();
+    const bool alike = any(0, 9) != 0;
+    if (!alike) b.outer = any(16, 16 * 14) * 8;
+    auto at = [](const Rows& x, int64_t i, int64_t j) { return (int64_t)(intptr_t)x.base + (i * x.outer + j * x.inner) * x.esz; };
+    bool meet = false, self = false;
+    for (int64_t i = 0; i < a.n_outer; ++i)
+      for (int64_t j = 0; j < a.n_inner; ++j) {
+        for (int64_t k = 0; k < b.n_outer; ++k)
+          for (int64_t l = 0; l < b.n_inner; ++l) meet |= llabs(at(a, i, j) - at(b, k, l)) < 128 * esz;
+        for (int64_t k = 0; k < a.n_outer; ++k)
+          for (int64_t l = 0; l < a.n_inner; ++l) self |= (i != k || j != l) && llabs(at(a, i, j) - at(a, k, l)) < 128 * esz;
+      }
+    const bool said = apart(a, b);
+    if (said && meet) return printf("said apart\n"), 1;
+    if (!said && !meet) {
+      if (alike && outer >= 128) return printf("said not apart\n"), 1;
+      ++careful;
+    }
+    if (a.apart_from_itself() && self) return printf("said apart from itself\n"), 1;
+    said ? ++yes : ++no;
+  }
+  printf("%d apart, %d not, %d of them only to be careful\n", yes, no, careful);
+  return yes < 10000 || no < 10000;
+}
+"""
+
+
+def test_which_arrays_count_as_apart(tmp_path):
+    """The host's check of overlapping rows against every row of small arrays."""
+    p = subprocess.run([host_cuda.build(str(tmp_path), APART)], stdout=subprocess.PIPE)
+    assert p.returncode == 0, p.stdout.decode()
