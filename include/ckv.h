@@ -318,7 +318,7 @@ ckv_status ckv_score_noalloc(const ckv_shape* shape, const ckv_params* params, c
  * Tokens are packed: unit u (a sequence in one layer) owns the rows token_starts[u] .. token_starts[u+1]-1 of the token
  * arrays (token_starts [Nu+1] int32, ascending; a unit may own none).  Rows outside token_starts[0] .. token_starts[Nu]-1
  * are padding: they may hold anything, and nothing is written for them.
- * The cache is two pools k_pages, v_pages [n_pages, page_size, d]; row j of KV head g of unit u is row j % page_size of
+ * The cache is two pools k_pages, v_pages [n_pages, page_size, d] that share no row (they may be interleaved); row j of KV head g of unit u is row j % page_size of
  * page page_table[u, g, j / page_size] (page_table [Nu, Hkv, max_pages] int32), and lengths [Nu, Hkv] int32 counts
  * the rows each head holds: the heads of a unit keep different numbers of rows, so table and lengths are per head.  Only
  * the table entries of pages that hold rows are read; a page may be shared by several readers.
@@ -362,7 +362,7 @@ typedef struct {
  *   y = x * w / sqrt(mean(x^2) + norm_eps)   (where there is a weight),
  *   (y_a, y_b) -> rot_scale * (y_a cos - y_b sin, y_b cos + y_a sin),  angle = position * inv_freq[pair] in 64 bits.
  * positions [T] int32.  q_out [T,H,d], k_out [T,Hkv,d]: dense, or q_out == q / k_out == k (in place, the inputs'
- * strides).  Either pair may be NULL.  Of `paged` only the token fields are read (the page fields may be 0).
+ * strides; rows that share memory with one another or with the other array's are refused).  Either pair may be NULL.  Of `paged` only the token fields are read (the page fields may be 0).
  */
 ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const void* q, const void* k,
                       const int32_t* positions, const int32_t* token_starts, void* q_out, void* k_out, void* stream);

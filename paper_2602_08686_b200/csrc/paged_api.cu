@@ -67,6 +67,11 @@ bool apart(const Rows& a, const Rows& b) {
   // each within an outer step, and beside the other there
   const int64_t at = steps ? ((d % s) + s) % s : 0;
   if (steps && at >= (a.n_inner - 1) * a.inner * a.esz + row && at + (b.n_inner - 1) * b.inner * b.esz + row <= s) return true;
+  // or their rows take turns: a[0] b[0] a[1] b[1] ...
+  if (a.inner == b.inner && a.inner > 0 && (!steps || a.outer % a.inner == 0)) {
+    const int64_t i = a.inner * a.esz, between = ((d % i) + i) % i;
+    if (between >= row && between + row <= i) return true;
+  }
   // row j of a against row k of b, whichever outer steps bring them closest
   auto meet = [&](int64_t x) {   // x: from one to the other within the same step
     if (!steps) return -row < x && x < row;
@@ -104,6 +109,12 @@ ckv_status check_pages(const ckv_paged* pg) {
   if (pg->page_stride_row >= ((int64_t)1 << 32) || pg->page_stride < 0 || pg->page_stride >= ((int64_t)1 << 38))
     return CKV_ERR_UNSUPPORTED;
   return CKV_OK;
+}
+// Keys and values go to pools that share no row (they may be interleaved).
+bool pools_apart(const ckv_paged& pg, const void* k_pages, const void* v_pages) {
+  const int64_t e = esize(pg);
+  return apart({k_pages, pg.n_pages, pg.page_stride, pg.page_size, pg.page_stride_row, e},
+               {v_pages, pg.n_pages, pg.page_stride, pg.page_size, pg.page_stride_row, e});
 }
 ckv_status check_rotary(const ckv_rotary* r) {
   if (r->rot_dim < 0 || r->rot_dim > kHeadDim) return CKV_ERR_INVALID_ARG;
@@ -194,7 +205,7 @@ ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const vo
   const bool any = paged->n_tokens > 0;
   if (any) {
     const int H = paged->n_q_heads, Hkv = paged->n_kv_heads;
-    if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
+    if (!good({k, v, k_pages, v_pages}, 16) || !pools_apart(*paged, k_pages, v_pages)) return CKV_ERR_INVALID_ARG;
     if ((rotary && rotary->rot_dim) && !good({positions}, 4)) return CKV_ERR_INVALID_ARG;
     if (!token_strides(*paged, paged->kv_stride_tok, paged->kv_stride_head, Hkv)) return CKV_ERR_INVALID_ARG;
     const int64_t T = paged->n_tokens, e = esize(*paged);
@@ -227,7 +238,7 @@ ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, co
   CKV_TRY(check_pages(paged));
   if (shape->n_units != paged->n_units || shape->n_kv_heads != paged->n_kv_heads || shape->dtype != paged->dtype)
     return CKV_ERR_INVALID_ARG;
-  if (!good({k, v, k_pages, v_pages}, 16) || k_pages == v_pages) return CKV_ERR_INVALID_ARG;
+  if (!good({k, v, k_pages, v_pages}, 16) || !pools_apart(*paged, k_pages, v_pages)) return CKV_ERR_INVALID_ARG;
   if (!good({indices, budgets, offsets, page_table, lengths}, 4) || lengths == budgets) return CKV_ERR_INVALID_ARG;
   CKV_TRY(check_paged_ws(kStatusBytes, ws, ws_bytes));
   const int64_t e = esize(*paged);

@@ -223,6 +223,30 @@ def test_append_leaves_out_rows_that_have_no_page_and_says_so(B):
     assert torch.equal(c.k_pages[c.table[0, 1, 0].long(), 3:7], k[:, 1])
 
 
+@pytest.mark.parametrize("layout", ["page, kind, row", "page, row, kind", "kind, page, row"])
+@pytest.mark.parametrize("n", [1, 60])
+def test_interleaved_pools(B, layout, n):
+    """Keys and values as views of one pool."""
+    P, pages = 32, 9
+    order = layout.split(", ")
+    sizes = dict(page=pages, row=P, kind=2)
+    pool = torch.full([sizes[x] for x in order] + [D], float("nan"), dtype=torch.bfloat16, device="cuda")
+    kp, vp = (pool.permute(*[order.index(x) for x in ("kind", "page", "row")], 3)[i] for i in range(2))
+    table = torch.arange(8, dtype=torch.int32, device="cuda").flip(0).view(1, 2, 4).contiguous()
+    x, v = (torch.randn(n + 50, 2, D, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(n, 8, D, device="cuda").bfloat16()
+    grown = torch.zeros(1, 2, dtype=torch.int32, device="cuda")
+    pk, pq = B.make_paged(kp, table, k_new=x), B.make_paged(kp, table, q=q)
+    ws = B.alloc_paged_workspace(pq)
+    B.ckv_append(pk, None, x, v, None, i32([0, n + 50]), i32([[0, 0]]), table, kp, vp, ws, new_lengths=grown)
+    out, lse = torch.zeros_like(q), torch.zeros(n, 8, device="cuda")
+    B.ckv_paged_attend(pq, q, kp, vp, table, grown, i32([0, n]), out, ws, lse=lse)
+    assert B.ckv_device_status(ws) == B.OK
+    want, want_lse = R.attend(q, [0, n], [[(x[:, g], v[:, g]) for g in range(2)]])
+    assert (out.double() - want).norm() <= 2 * 2.0 ** -8 * want.norm() and (lse.double() - want_lse).abs().max() <= 1e-3
+    assert torch.isnan(kp[8]).all() and torch.isnan(vp[8]).all()
+
+
 # ---------------------------------------------------------------------------------------- gather into pages
 @pytest.mark.parametrize("cfg_name,page,L", [("c1", 16, 2048), ("c2", 64, 4096), ("c5", 256, 1111)])
 def test_gather_pages(B, cfg_name, page, L):

@@ -224,6 +224,26 @@ def test_rows_written_in_place_are_apart():
     assert call("rotate", pg, rot, q_out=far(1), k=far(1) + 32 * 256) == B.ERR_INVALID_ARG
 
 
+def test_the_two_pools_are_apart():
+    """A page row that is both pools' would take a key and a value at once."""
+    far = lambda i: FAKE + i * (1 << 30)
+    s = B.ckv_shape(2, 32, 8, 128, 4096, 32, B.BF16, 0, 32 * 32 * 128, 32 * 128, 128, 8 * 4096 * 128, 4096 * 128, 128)
+    p = B.make_params(B.Params(), None, None)
+
+    def gather(pg, v_pages):
+        return B.lib().ckv_gather_pages(C.byref(s), C.byref(p), C.byref(pg), far(1), far(2), far(3), far(4), far(5), far(9), far(10),
+                                        v_pages, far(8), far(15), BIG, None)
+
+    page = 64 * 256
+    for layout, shifts in ((dict(), (0, 256, page, 99 * page, -page, 64, -99 * page - 16)),
+                           (dict(page_stride=2 * 64 * 128), (256, page - 16, 2 * page, 2 * page - 256)),
+                           (dict(page_stride=2 * 64 * 128, page_stride_row=256), (512, 16, 128, 2 * page + 512, -512)),
+                           (dict(page_stride=64 * 136, page_stride_row=136), (16, 64 * 272, 272))):
+        for shift in shifts:
+            assert call("append", paged(**layout), rotary(), v_pages=far(10) + shift) == B.ERR_INVALID_ARG, (layout, shift)
+            assert gather(paged(**layout), far(10) + shift) == B.ERR_INVALID_ARG, (layout, shift)
+
+
 APART = r"""
 #include "host_cuda.h"
 #include <random>
