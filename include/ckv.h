@@ -324,8 +324,9 @@ ckv_status ckv_score_noalloc(const ckv_shape* shape, const ckv_params* params, c
  * the table entries of pages that hold rows are read; a page may be shared by several readers.
  * A page number outside the pool, or a row past the table's last page, is never followed: the row is left out, and
  * ckv_device_status(ws) reports CKV_ERR_PAGE.  Cache rows behind a head's length may hold anything, NaN included.
- * The calls use only the current device's memory and are capturable; a work space serves one call at a time.  Outputs
- * and pages are apart from what a call reads (but for the outputs that may be written in place); CKV_ERR_INVALID_ARG where not.
+ * The calls use only the current device's memory and are capturable; a work space serves one call at a time.  Outputs,
+ * pages and the work space are apart from what a call reads and from one another (but for the outputs that may be written in
+ * place); CKV_ERR_INVALID_ARG where not.
  */
 typedef struct {
   int32_t n_units;     /* Nu >= 1; Nu * Hkv <= 65536 */

@@ -15,15 +15,29 @@ bool good(std::initializer_list<const void*> ps, size_t a) {
 }
 int64_t esize(const ckv_paged& pg) { return pg.dtype == CKV_BF16 ? 2 : 4; }
 
-// What a token array [T, heads, d] with these strides covers, in bytes.
+// The bytes an array covers (none: {0, 0}).
 struct Range {
-  uintptr_t lo, hi;
+  uintptr_t lo = 0, hi = 0;
 };
-Range range_of(const void* p, int64_t T, int64_t heads, int64_t tok, int64_t head, int64_t esz) {
+Range bytes_of(const void* p, int64_t bytes) {
+  if (!p) return {};
   const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return {lo, lo + (uintptr_t)(((T - 1) * tok + (heads - 1) * head + kHeadDim) * esz)};
+  return {lo, lo + (uintptr_t)bytes};
+}
+Range ints_of(const void* p, int64_t n) { return bytes_of(p, n * 4); }   // or floats
+// A token array [T, heads, d] with these strides; what would leave the address space ends with it.
+Range range_of(const void* p, int64_t T, int64_t heads, int64_t tok, int64_t head, int64_t esz) {
+  if (!p) return {};
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  const __int128 hi = (__int128)lo + ((__int128)(T - 1) * tok + (__int128)(heads - 1) * head + kHeadDim) * esz;
+  return {lo, hi < (__int128)UINTPTR_MAX ? (uintptr_t)hi : UINTPTR_MAX};
 }
 bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+bool clear_of(const Range& written, std::initializer_list<Range> others) {
+  for (const Range& o : others)
+    if (overlap(written, o)) return false;
+  return true;
+}
 Range pool_of(const ckv_paged& pg, const void* pool) {
   return range_of(pool, pg.n_pages, pg.page_size, pg.page_stride, pg.page_stride_row, esize(pg));
 }
@@ -130,15 +144,16 @@ ckv_status check_paged_ws(size_t need, const void* ws, size_t ws_bytes) {
   return ws && aligned(ws, 256) && ws_bytes >= need ? CKV_OK : CKV_ERR_WORKSPACE;
 }
 constexpr size_t kStatusBytes = 256;   // all that the calls without partial results use
-// An output is either its own input (in place) or dense and apart from everything that is read.
-bool out_ok(const ckv_paged& pg, const void* out, const void* in, int heads, std::initializer_list<Range> read) {
-  if (!good({out}, 16)) return false;
-  if (out == in) return true;
-  const Range o = range_of(out, pg.n_tokens, heads, (int64_t)heads * kHeadDim, kHeadDim, esize(pg));
-  for (const Range& r : read)
-    if (overlap(o, r)) return false;
-  return true;
+// Where the turned tokens go: over the input (in place) or to a dense array.
+Range out_range(const ckv_paged& pg, const void* out, const void* in, const Range& in_range, int heads) {
+  return out == in ? in_range : range_of(out, pg.n_tokens, heads, (int64_t)heads * kHeadDim, kHeadDim, esize(pg));
 }
+Range freq_of(const ckv_rotary* r) { return r ? bytes_of(r->inv_freq, r->rot_dim / 2 * 8) : Range{}; }
+Range q_norm_of(const ckv_rotary* r) { return r ? ints_of(r->q_norm_w, kHeadDim) : Range{}; }
+Range k_norm_of(const ckv_rotary* r) { return r ? ints_of(r->k_norm_w, kHeadDim) : Range{}; }
+Range starts_of(const ckv_paged& pg, const void* starts) { return ints_of(starts, (int64_t)pg.n_units + 1); }
+Range heads_of(const ckv_paged& pg, const void* per_head) { return ints_of(per_head, (int64_t)pg.n_units * pg.n_kv_heads); }
+Range table_of(const ckv_paged& pg, const void* table) { return ints_of(table, (int64_t)pg.n_units * pg.n_kv_heads * pg.max_pages); }
 
 #define CKV_TRY(expr)                  \
   do {                                 \
@@ -173,15 +188,16 @@ ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const vo
   if (k && (!aligned(k, 16) || !token_strides(*paged, paged->kv_stride_tok, paged->kv_stride_head, Hkv)))
     return CKV_ERR_INVALID_ARG;
   const int64_t T = paged->n_tokens, e = esize(*paged);
-  const Range qr = q ? range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e) : Range{0, 0};
-  const Range kr = k ? range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e) : Range{0, 0};
-  if (q && !out_ok(*paged, q_out, q, H, {qr, kr})) return CKV_ERR_INVALID_ARG;
-  if (k && !out_ok(*paged, k_out, k, Hkv, {qr, kr})) return CKV_ERR_INVALID_ARG;
+  const Range qr = range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e), kr = range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
+  if ((q && !good({q_out}, 16)) || (k && !good({k_out}, 16))) return CKV_ERR_INVALID_ARG;
   const Rows q_rows{q, T, paged->q_stride_tok, H, paged->q_stride_head, e}, k_rows{k, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e};
-  if ((q && q_out == q && !in_place_ok(q_rows, {k_rows})) || (k && k_out == k && !in_place_ok(k_rows, {q_rows}))) return CKV_ERR_INVALID_ARG;
-  if (q && k && q_out != q && k_out != k &&
-      overlap(range_of(q_out, T, H, (int64_t)H * kHeadDim, kHeadDim, e), range_of(k_out, T, Hkv, (int64_t)Hkv * kHeadDim, kHeadDim, e)))
-    return CKV_ERR_INVALID_ARG;
+  const bool q_here = q && q_out == q, k_here = k && k_out == k;
+  if ((q_here && !in_place_ok(q_rows, {k_rows})) || (k_here && !in_place_ok(k_rows, {q_rows}))) return CKV_ERR_INVALID_ARG;
+  const Range qo = q ? out_range(*paged, q_out, q, qr, H) : Range{}, ko = k ? out_range(*paged, k_out, k, kr, Hkv) : Range{};
+  if ((!q_here && !clear_of(qo, {qr, kr, ko})) || (!k_here && !clear_of(ko, {qr, kr, qo}))) return CKV_ERR_INVALID_ARG;
+  for (const Range& o : {qo, ko})
+    if (!clear_of(o, {ints_of(positions, T), starts_of(*paged, token_starts), freq_of(rotary), q_norm_of(rotary), k_norm_of(rotary)}))
+      return CKV_ERR_INVALID_ARG;
   CKV_CUDA(launch_rotate(*paged, rotary, q, k, nullptr, positions, token_starts, q_out, k_out, nullptr, nullptr, nullptr,
                          nullptr, nullptr, nullptr, (cudaStream_t)stream));
   return CKV_OK;
@@ -195,33 +211,38 @@ ckv_status ckv_append(const ckv_paged* paged, const ckv_rotary* rotary, const vo
   CKV_TRY(check_pages(paged));
   if (rotary) CKV_TRY(check_rotary(rotary));
   if (!good({token_starts, lengths, page_table}, 4)) return CKV_ERR_INVALID_ARG;
-  if (new_lengths_or_null) {
-    const uintptr_t n = (uintptr_t)paged->n_units * paged->n_kv_heads * sizeof(int32_t);
-    const uintptr_t a = reinterpret_cast<uintptr_t>(lengths), b = reinterpret_cast<uintptr_t>(new_lengths_or_null);
-    if (b % 4 || (a < b + n && b < a + n)) return CKV_ERR_INVALID_ARG;
-  }
+  if (new_lengths_or_null && !aligned(new_lengths_or_null, 4)) return CKV_ERR_INVALID_ARG;
   CKV_TRY(check_paged_ws(kStatusBytes, ws, ws_bytes));
   if (paged->n_tokens == 0 && !new_lengths_or_null) return CKV_OK;
   const bool any = paged->n_tokens > 0;
+  const Range st = starts_of(*paged, token_starts), len = heads_of(*paged, lengths), tab = table_of(*paged, page_table);
+  const Range grown = heads_of(*paged, new_lengths_or_null), work = bytes_of(ws, kStatusBytes);
+  if (!clear_of(grown, {st, len, tab, work}) || !clear_of(work, {st, len, tab})) return CKV_ERR_INVALID_ARG;
   if (any) {
     const int H = paged->n_q_heads, Hkv = paged->n_kv_heads;
     if (!good({k, v, k_pages, v_pages}, 16) || !pools_apart(*paged, k_pages, v_pages)) return CKV_ERR_INVALID_ARG;
-    if ((rotary && rotary->rot_dim) && !good({positions}, 4)) return CKV_ERR_INVALID_ARG;
+    const bool turns = rotary && rotary->rot_dim;
+    if (turns && !good({positions}, 4)) return CKV_ERR_INVALID_ARG;
     if (!token_strides(*paged, paged->kv_stride_tok, paged->kv_stride_head, Hkv)) return CKV_ERR_INVALID_ARG;
     const int64_t T = paged->n_tokens, e = esize(*paged);
-    const Range kr = range_of(k, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
-    const Range vr = range_of(v, T, Hkv, paged->kv_stride_tok, paged->kv_stride_head, e);
-    const Range kp = pool_of(*paged, k_pages), vp = pool_of(*paged, v_pages);
-    if (overlap(kr, kp) || overlap(kr, vp) || overlap(vr, kp) || overlap(vr, vp)) return CKV_ERR_INVALID_ARG;
+    const Rows k_rows{k, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e}, v_rows{v, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e};
+    const Rows q_rows{q_or_null, T, paged->q_stride_tok, H, paged->q_stride_head, e};
+    const Range kr = k_rows.range(), vr = v_rows.range(), qr = q_rows.range();
+    const bool q_here = q_or_null && q_out == q_or_null;
     if (q_or_null) {
-      if (!aligned(q_or_null, 16) || !token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, H))
+      if (!aligned(q_or_null, 16) || !good({q_out}, 16) || !token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, H))
         return CKV_ERR_INVALID_ARG;
-      const Range qr = range_of(q_or_null, T, H, paged->q_stride_tok, paged->q_stride_head, e);
-      if (overlap(qr, kp) || overlap(qr, vp) || !out_ok(*paged, q_out, q_or_null, H, {qr, kr, vr, kp, vp})) return CKV_ERR_INVALID_ARG;
-      const Rows k_rows{k, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e}, v_rows{v, T, paged->kv_stride_tok, Hkv, paged->kv_stride_head, e};
-      if (q_out == q_or_null && !in_place_ok({q_or_null, T, paged->q_stride_tok, H, paged->q_stride_head, e}, {k_rows, v_rows}))
-        return CKV_ERR_INVALID_ARG;
+      if (q_here && !in_place_ok(q_rows, {k_rows, v_rows})) return CKV_ERR_INVALID_ARG;
     }
+    const Range qo = q_or_null ? out_range(*paged, q_out, q_or_null, qr, H) : Range{};
+    if (!q_here && !clear_of(qo, {qr, kr, vr})) return CKV_ERR_INVALID_ARG;
+    const Range pos = turns ? ints_of(positions, T) : Range{}, freq = freq_of(rotary), qn = q_norm_of(rotary), kn = k_norm_of(rotary);
+    for (const Range& o : {pool_of(*paged, k_pages), pool_of(*paged, v_pages)})
+      if (!clear_of(o, {qr, kr, vr, qo})) return CKV_ERR_INVALID_ARG;
+    for (const Range& o : {pool_of(*paged, k_pages), pool_of(*paged, v_pages), qo})
+      if (!clear_of(o, {pos, freq, qn, kn, st, len, tab, grown, work})) return CKV_ERR_INVALID_ARG;
+    for (const Range& o : {grown, work})
+      if (!clear_of(o, {qr, kr, vr, pos, freq, qn, kn})) return CKV_ERR_INVALID_ARG;
   }
   CKV_CUDA(launch_rotate(*paged, rotary, any ? q_or_null : nullptr, any ? k : nullptr, any ? v : nullptr, positions,
                          token_starts, q_out, nullptr, lengths, page_table, k_pages, v_pages, new_lengths_or_null,
@@ -239,15 +260,23 @@ ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, co
   if (shape->n_units != paged->n_units || shape->n_kv_heads != paged->n_kv_heads || shape->dtype != paged->dtype)
     return CKV_ERR_INVALID_ARG;
   if (!good({k, v, k_pages, v_pages}, 16) || !pools_apart(*paged, k_pages, v_pages)) return CKV_ERR_INVALID_ARG;
-  if (!good({indices, budgets, offsets, page_table, lengths}, 4) || lengths == budgets) return CKV_ERR_INVALID_ARG;
+  if (!good({indices, budgets, offsets, page_table, lengths}, 4)) return CKV_ERR_INVALID_ARG;
   CKV_TRY(check_paged_ws(kStatusBytes, ws, ws_bytes));
-  const int64_t e = esize(*paged);
-  for (const void* in : {k, v}) {
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(in);
-    const Range r{lo, lo + (uintptr_t)(((shape->n_units - 1) * shape->kv_stride_unit + (shape->n_kv_heads - 1) * shape->kv_stride_head +
-                                        (shape->seq_len - 1) * shape->kv_stride_tok + kHeadDim) * e)};
-    if (overlap(r, pool_of(*paged, k_pages)) || overlap(r, pool_of(*paged, v_pages))) return CKV_ERR_INVALID_ARG;
-  }
+  const int64_t kept = (int64_t)shape->n_units * shape->n_kv_heads * (params->budget_per_head < shape->seq_len ? params->budget_per_head : shape->seq_len);
+  auto dense_kv = [&](const void* x) {   // [Nu, Hkv, L, d]: the last unit's rows end it
+    Range r = range_of(x, shape->n_kv_heads, shape->seq_len, shape->kv_stride_head, shape->kv_stride_tok, esize(*paged));
+    const __int128 hi = (__int128)r.hi + (__int128)(shape->n_units - 1) * shape->kv_stride_unit * esize(*paged);
+    r.hi = hi < (__int128)UINTPTR_MAX ? (uintptr_t)hi : UINTPTR_MAX;
+    return r;
+  };
+  const Range kr = dense_kv(k), vr = dense_kv(v), ind = ints_of(indices, kept), bud = heads_of(*paged, budgets);
+  const Range off = ints_of(offsets, (int64_t)shape->n_units * (shape->n_kv_heads + 1)), tab = table_of(*paged, page_table);
+  const Range len = heads_of(*paged, lengths), work = bytes_of(ws, kStatusBytes);
+  for (const Range& o : {pool_of(*paged, k_pages), pool_of(*paged, v_pages), len, work})
+    if (!clear_of(o, {kr, vr, ind, bud, off, tab})) return CKV_ERR_INVALID_ARG;
+  for (const Range& o : {pool_of(*paged, k_pages), pool_of(*paged, v_pages)})
+    if (!clear_of(o, {len, work})) return CKV_ERR_INVALID_ARG;
+  if (overlap(len, work)) return CKV_ERR_INVALID_ARG;
   CKV_CUDA(launch_gather_pages(*shape, *params, *paged, k, v, indices, budgets, offsets, page_table, k_pages, v_pages, lengths,
                                reinterpret_cast<int*>(static_cast<char*>(ws) + paged_ws(*paged).status),
                                (cudaStream_t)stream));
@@ -265,12 +294,12 @@ ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k
   if (lse_or_null && !aligned(lse_or_null, 4)) return CKV_ERR_INVALID_ARG;
   if (!token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, paged->n_q_heads)) return CKV_ERR_INVALID_ARG;
   const int64_t T = paged->n_tokens, H = paged->n_q_heads, e = esize(*paged);
-  const Range o = range_of(out, T, H, H * kHeadDim, kHeadDim, e);
-  if (overlap(o, range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e))) return CKV_ERR_INVALID_ARG;
-  const uintptr_t l = reinterpret_cast<uintptr_t>(lse_or_null);
-  if (overlap(o, pool_of(*paged, k_pages)) || overlap(o, pool_of(*paged, v_pages)) ||
-      (l && overlap(o, {l, l + (uintptr_t)(T * H) * sizeof(float)})))
-    return CKV_ERR_INVALID_ARG;
+  const Range o = range_of(out, T, H, H * kHeadDim, kHeadDim, e), l = ints_of(lse_or_null, T * H), work = bytes_of(ws, paged_ws(*paged).total);
+  for (const Range& x : {o, l, work})
+    if (!clear_of(x, {range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e), pool_of(*paged, k_pages), pool_of(*paged, v_pages),
+                      table_of(*paged, page_table), heads_of(*paged, lengths), starts_of(*paged, token_starts)}))
+      return CKV_ERR_INVALID_ARG;
+  if (overlap(o, l) || overlap(o, work) || overlap(l, work)) return CKV_ERR_INVALID_ARG;
   CKV_CUDA(launch_paged_attend(*paged, q, k_pages, v_pages, page_table, lengths, token_starts, out, lse_or_null,
                                static_cast<char*>(ws), (cudaStream_t)stream));
   return CKV_OK;

@@ -244,6 +244,51 @@ def test_the_two_pools_are_apart():
             assert gather(paged(**layout), far(10) + shift) == B.ERR_INVALID_ARG, (layout, shift)
 
 
+def test_outputs_apart_from_all_that_a_call_reads_and_writes():
+    """Every output against every input and every other output: last byte on first byte, and the other way round."""
+    far = lambda i: FAKE + i * (1 << 30)
+    pg, rot = paged(), B.ckv_rotary(far(16), far(17), far(18), 128, 0, 1.0, 1e-6)
+    at = dict(q=1, k=2, v=3, positions=4, starts=5, lengths=6, table=7, q_out=8, k_out=9, k_pages=10, v_pages=11, new_lengths=12, out=13,
+              lse=14, ws=15)
+    row, need = 256, B.ckv_paged_workspace_bytes(pg)
+    size = dict(q=(9 * 48 + 32) * row, k=(9 * 48 + 8) * row, v=(9 * 48 + 8) * row, positions=40, starts=12, lengths=64, table=2 * 8 * 9 * 4,
+                q_out=10 * 32 * row, k_out=10 * 8 * row, k_pages=100 * 64 * row, v_pages=100 * 64 * row, new_lengths=64, out=10 * 32 * row,
+                lse=10 * 32 * 4, inv_freq=512, q_norm_w=512, k_norm_w=512)
+    place = {n: far(i) for n, i in at.items()}
+    place.update(inv_freq=far(16), q_norm_w=far(17), k_norm_w=far(18))
+    turned = "inv_freq q_norm_w k_norm_w positions starts".split()
+    calls = dict(rotate=("q_out k_out", "q k".split() + turned, 0),
+                 append=("q_out k_pages v_pages new_lengths ws", "q k v lengths table".split() + turned, 256),
+                 attend=("out lse ws", "q k_pages v_pages table lengths starts".split(), need))
+    for name, (outs, ins, ws) in calls.items():
+        outs = outs.split()
+        size["ws"] = ws
+        for o in outs:
+            step = dict(ws=256, out=32, q_out=16, k_out=16, k_pages=16, v_pages=16).get(o, 4)
+            for x in ins + [y for y in outs if y != o]:
+                first = (place[x] + size[x] - 1) // step * step             # begins on x's last bytes
+                last = -(-(place[x] + 1 - size[o]) // step) * step          # ends on its first
+                for where in (first, last):
+                    assert where < place[x] + size[x] and where + size[o] > place[x]
+                    assert call(name, pg, rot, **{o: where}) == B.ERR_INVALID_ARG, (name, o, x)
+    s = B.ckv_shape(2, 32, 8, 128, 4096, 32, B.BF16, 0, 32 * 32 * 128, 32 * 128, 128, 8 * 4096 * 128, 4096 * 128, 128)
+    p = B.make_params(B.Params(), None, None)                              # 512 rows a head
+    names = "k v indices budgets offsets table k_pages v_pages lengths ws".split()
+    size = dict(k=2 * 8 * 4096 * row, v=2 * 8 * 4096 * row, indices=2 * 8 * 512 * 4, budgets=64, offsets=72, table=2 * 8 * 9 * 4,
+                k_pages=100 * 64 * row, v_pages=100 * 64 * row, lengths=64, ws=256)
+    place = {n: far(i + 1) for i, n in enumerate(names)}
+
+    def gather(**over):
+        a = dict(place, **over)
+        return B.lib().ckv_gather_pages(C.byref(s), C.byref(p), C.byref(pg), *[a[n] for n in names], BIG, None)
+
+    for o, step in dict(k_pages=16, v_pages=16, lengths=4, ws=256).items():
+        for x in names:
+            if x != o:
+                for where in ((place[x] + size[x] - 1) // step * step, -(-(place[x] + 1 - size[o]) // step) * step):
+                    assert gather(**{o: where}) == B.ERR_INVALID_ARG, (o, x)
+
+
 APART = r"""
 #include "host_cuda.h"
 #include <random>
