@@ -414,8 +414,8 @@ def _layout(t: torch.Tensor | None):
 
 def _same(t: torch.Tensor, layout, name: str) -> int:
     """The tensor's address, once its layout is the struct's (strides of extents of one do not matter)."""
-    if layout is None:
-        raise ValueError(f"{name}: the struct was made without it")
+    if layout is None or t is None:
+        raise ValueError(f"{name}: " + ("the struct was made without it" if layout is None else "missing"))
     shape, stride, dtype, device = layout
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
         raise ValueError(f"{name} must be {tuple(shape)} {dtype} on device {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
@@ -425,6 +425,8 @@ def _same(t: torch.Tensor, layout, name: str) -> int:
 
 
 def _dense(t: torch.Tensor, shape, dtype, device: int, name: str) -> int:
+    if shape is None or t is None:
+        raise ValueError(f"{name}: " + ("the struct was made without pages" if shape is None else "missing"))
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a dense {tuple(shape)} {dtype} on device {device}")
     return t.data_ptr()
@@ -457,7 +459,7 @@ def make_packed(q: torch.Tensor | None, k: torch.Tensor | None, n_units: int, ma
     if k is not None:
         pg.kv_stride_tok, pg.kv_stride_head = k.stride(0), k.stride(1)
     pg._q, pg._k, pg._pages, pg._device, pg._dtype = _layout(q), _layout(k), None, t.get_device(), t.dtype
-    pg._starts, pg._ref = (pg.n_units + 1,), C.byref(pg)
+    pg._starts, pg._heads, pg._table, pg._ref = (pg.n_units + 1,), None, None, C.byref(pg)
     return pg
 
 
@@ -531,13 +533,15 @@ def _tokens_out(pg, out, t, layout, name):
     """A token output: the input itself (in place) or a dense tensor of its shape."""
     if t is None:
         return None
+    if out is None:
+        raise ValueError(f"{name}: missing")
     if out.data_ptr() == t.data_ptr():
         return _same(out, layout, name)
     return _dense(out, layout[0], pg._dtype, pg._device, name)
 
 
 def _ws_of(pg, ws):
-    if ws.get_device() != pg._device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+    if ws is None or ws.get_device() != pg._device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise ValueError("ws must be a dense uint8 tensor on the device of the pages")
     return ws.data_ptr()
 
@@ -572,6 +576,8 @@ def ckv_gather_pages(shape, params, paged, k, v, indices, budgets, offsets, page
     """The rows the retention pass kept of k, v, into the pages of a cache; lengths receives the heads' budgets."""
     dev, i32 = paged._device, torch.int32
     made_for = getattr(shape, "_k", None)
+    if paged._heads is None:
+        raise ValueError("the struct was made without pages")
     for t, name in ((k, "k"), (v, "v")):
         if (t.shape, t.stride(), t.dtype) != made_for:
             _check_kv(shape, t, name)

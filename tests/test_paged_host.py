@@ -188,6 +188,33 @@ def test_the_binding_compares_layouts():
         B.make_packed(q.half(), k.half(), 1)
 
 
+def test_the_binding_names_what_is_missing():
+    """A struct that was made without pages, a token array without its output, or nothing at all: ValueError."""
+    kp, table = torch.zeros(6, 16, 128), torch.zeros(1, 2, 3, dtype=torch.int32)
+    x, k = torch.zeros(4, 8, 128), torch.zeros(4, 2, 128)
+    ints = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    ws, rot = torch.zeros(1 << 16, dtype=torch.uint8), B.make_rotary(torch.zeros(64, dtype=torch.float64))
+    full, tokens = B.make_paged(kp, table, q=x, k_new=k), B.make_packed(x, k, 1)
+    append = lambda pg, **kw: B.ckv_append(pg, rot, **dict(dict(k=k, v=k.clone(), positions=ints(4), token_starts=ints(2), lengths=ints(1, 2),
+                                                               page_table=table, k_pages=kp, v_pages=kp.clone(), ws=ws), **kw))
+    for call_ in (lambda: B.ckv_rotate(full, rot, x, None, ints(4), ints(2), None, None),
+                  lambda: B.ckv_rotate(full, rot, None, k, ints(4), ints(2), None, None),
+                  lambda: B.ckv_rotate(full, rot, x, None, None, ints(2), x, None),
+                  lambda: append(full, q=x), lambda: append(tokens), lambda: append(full, k=None), lambda: append(full, lengths=None),
+                  lambda: append(full, v_pages=None),
+                  lambda: append(full, ws=None),
+                  lambda: B.ckv_paged_attend(tokens, x, kp, kp.clone(), table, ints(1, 2), ints(2), x.clone(), ws),
+                  lambda: B.ckv_paged_attend(full, None, kp, kp.clone(), table, ints(1, 2), ints(2), x.clone(), ws),
+                  lambda: B.ckv_paged_attend(full, x, kp, kp.clone(), table, ints(1, 2), ints(2), None, ws),
+                  lambda: B.ckv_gather_pages(B.make_shape(torch.zeros(1, 8, 16, 128), torch.zeros(1, 2, 64, 128)),
+                                             B.make_params(B.Params(), None, None), tokens, torch.zeros(1, 2, 64, 128),
+                                             torch.zeros(1, 2, 64, 128), ints(1, 128), ints(1, 2), ints(1, 3), table, kp, kp.clone(),
+                                             ints(1, 2), ws),
+                  lambda: B.ckv_paged_workspace_bytes(tokens) or B.alloc_paged_workspace(tokens, "cpu")):
+        with pytest.raises((ValueError, B.CkvError)):
+            call_()
+
+
 def test_outputs_and_pages_apart_from_inputs():
     pg, rot = paged(), rotary()
     far = lambda i: FAKE + i * (1 << 30)
