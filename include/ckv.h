@@ -334,7 +334,7 @@ typedef struct {
   int32_t n_kv_heads;  /* Hkv <= 64 */
   int32_t head_dim;    /* d; must be 128 */
   int32_t dtype;       /* ckv_dtype of tokens, pages and outputs */
-  int32_t n_tokens;    /* T >= 0: rows of the token arrays, padding included; T <= 2^20 */
+  int32_t n_tokens;    /* T >= 0: rows of the token arrays, padding included; T <= 2^20, T * H <= 2^30 */
   int32_t max_new;     /* most tokens any unit has in a call, as far as known; 0: not known (T).  It only picks kernels:
                           the results are right whatever it says */
   int32_t causal;      /* ckv_paged_attend: 1: a unit's tokens are its heads' last rows and see no later ones;

@@ -51,6 +51,7 @@ ckv_status check_tokens(const ckv_paged* pg) {
   if (pg->head_dim != kHeadDim || pg->n_kv_heads > kMaxKvHeads || pg->n_tokens > (1 << 20) || pg->n_q_heads > 65535)
     return CKV_ERR_UNSUPPORTED;
   if ((int64_t)pg->n_units * pg->n_kv_heads > 65536) return CKV_ERR_UNSUPPORTED;
+  if ((int64_t)pg->n_tokens * pg->n_q_heads > (1 << 30)) return CKV_ERR_UNSUPPORTED;   // the kernels count query rows in 32 bits
   return CKV_OK;
 }
 // Strides of a token array: rows on 16-byte boundaries (that they do not overlap is asked where they are written, see in_place_ok).

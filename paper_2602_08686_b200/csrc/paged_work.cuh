@@ -53,7 +53,7 @@ struct Item {
 };
 
 __device__ __forceinline__ int unit_blocks(const WorkArgs& a, int n) {
-  const int per = a.tokens ? a.tokens : a.M, units = a.tokens ? n : n * a.G;   // at most 2^26 rows
+  const int per = a.tokens ? a.tokens : a.M, units = a.tokens ? n : n * a.G;   // at most 2^30 rows (checked on the host)
   return units <= per ? (units > 0) : (units + per - 1) / per;
 }
 // The head's length; one that the table has no pages for is reported (the rows without a page are left out, see rows_seen), and so

@@ -370,3 +370,12 @@ def test_which_arrays_count_as_apart(tmp_path):
     """The host's check of overlapping rows against every row of small arrays."""
     p = subprocess.run([host_cuda.build(str(tmp_path), APART)], stdout=subprocess.PIPE)
     assert p.returncode == 0, p.stdout.decode()
+
+
+@pytest.mark.parametrize("heads,kv_heads,tokens", [(65472, 64, 1 << 20), (65535, 1, 1 << 15), (2048, 8, (1 << 19) + 1)])
+def test_more_query_rows_than_any_memory_holds(heads, kv_heads, tokens):
+    """T * H above 2^30 (256 GB of bf16 rows): row indices are 32-bit."""
+    pg = paged(n_units=1, n_q_heads=heads, n_kv_heads=kv_heads, n_tokens=tokens, q_stride_tok=heads * 128)
+    assert B.ckv_paged_workspace_bytes(pg) == 0
+    for name in ("rotate", "append", "attend"):
+        assert call(name, pg, rotary()) == B.ERR_UNSUPPORTED
