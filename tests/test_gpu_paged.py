@@ -803,3 +803,32 @@ def test_prompt_to_decode(B, cfg_name, chunk):
         assert (lse.double() - want_lse).abs().max() <= (0.02 if bf else 1e-4)
     assert grown.tolist() == [[x + steps * chunk for x in r] for r in bud]
     assert B.ckv_device_status(ws) == B.OK
+
+
+def test_the_readme_s_step_of_a_decoder(B):
+    """The example as it is printed, twice, on a batch of three sequences."""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as f:
+        lines = f.read().split("A step of a decoder")[1].split("\n\n")[1].split("\n")
+    assert lines and all(x.startswith("    ") for x in lines)
+    H, Hkv, Nu = 8, 2, 3
+    c = R.Cache([[40, 33], [7, 64], [100, 1]], 32, device="cuda", max_extra=1)
+    qkv = torch.randn(Nu, H + 2 * Hkv, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).bfloat16()
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    inv = 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+    names = dict(k_pages=c.k_pages, v_pages=c.v_pages, page_table=c.table, q=q, k=k, v=v, inv_freq=inv, qw=torch.ones(D, device="cuda"),
+                 kw=torch.ones(D, device="cuda"), positions=i32([500, 600, 700]), token_starts=i32([0, 1, 2, 3]), lengths=c.lengths,
+                 new_lengths=torch.zeros_like(c.lengths), q_rot=torch.zeros(Nu, H, D, dtype=torch.bfloat16, device="cuda"),
+                 out=torch.zeros(Nu, H, D, dtype=torch.bfloat16, device="cuda"), lse=torch.zeros(Nu, H, device="cuda"))
+    for _ in range(2):
+        exec("\n".join(x[4:] for x in lines), names)
+    one = torch.ones(D, device="cuda")
+    tk = R.turn(k, names["positions"], inv, one).bfloat16()
+    rows = [[tuple(torch.cat((x.cuda(), y[u:u + 1, g])) for x, y in zip(c.rows[u][g], (tk, v))) for g in range(Hkv)] for u in range(Nu)]
+    want, want_lse = R.attend(names["q_rot"], [0, 1, 2, 3], rows)
+    assert B.ckv_device_status(names["ws"]) == B.OK
+    assert torch.equal(names["new_lengths"], c.lengths + 1)
+    # a key that rounds the other way moves a logit by 2^-8 |q| |k| / sqrt(d) at most
+    assert (names["lse"].double() - want_lse).abs().max() <= 0.05
+    assert (names["out"].double() - want).norm() <= 3 * 2.0 ** -8 * want.norm()
