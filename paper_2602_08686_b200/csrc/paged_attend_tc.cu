@@ -42,6 +42,8 @@ constexpr int kJobs = 4;                       // ring of items
 // A step's sum above it is done again with a new reference.  Sums and outputs of up to 2^24 rows (2^18 steps) then stay below 2^34 and
 // 2^34 max|v|, in range for values up to 2^94 (the largest fp32 is 2^128).
 constexpr float kOverflow = 65536.0f;
+// A logit is off its own rounded product with the scale by up to 2^-24 of it: a factor of two where the reference is this far from zero.
+constexpr float kFar = 16777216.0f;
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);   // fp32 += bf16 * bf16, M = 128
 constexpr uint32_t kIdescQK = kIdesc | ((64u >> 3) << 17);
 constexpr uint32_t kIdescPV = kIdesc | ((128u >> 3) << 17) | (1u << 16);                // B (the values) is MN-major
@@ -423,6 +425,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     // rows of no token hold what shared memory held, or another unit's queries: above everything, they ask for no step again
     float m = live ? -INFINITY : INFINITY, l = 0.f;
     bool open = true;                                         // some row of the warp has no reference yet
+    bool far = false;                                         // some row's reference is further from zero than its rounding allows
 #pragma unroll 1
     for (int g = 0; g < steps; ++g, ++n_steps) {
       const int j = pair ? g >> 1 : g, h = pair ? g & 1 : stream;
@@ -443,21 +446,24 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
         const float top = row_max(s) * a.x_scale;
         if (m == -INFINITY) m = top;
         open = __any_sync(0xffffffffu, m == -INFINITY);
+        far = __any_sync(0xffffffffu, live && m > -INFINITY && fabsf(m) > kFar);
       }
-      // Done again with the row's maximum as the reference where the sum has left the range (once: logits past 2^30 differ
-      // from their own rounded maximum by more than that).
-      float sum;
-      for (int again = 0;; ++again) {
-        sum = softmax_step(s, a.x_scale, m == -INFINITY ? 0.f : m, s_buf);
-        if (again == 1 || !__any_sync(0xffffffffu, sum > kOverflow)) break;
-        const float top = fmaxf(m, row_max(s) * a.x_scale);
+      float sum = softmax_step(s, a.x_scale, m == -INFINITY ? 0.f : m, s_buf);
+      // Done again with the row's maximum as the reference where the sum has left the range, and with products rounded as the
+      // reference is where that is far from zero.
+      if (far || __any_sync(0xffffffffu, sum > kOverflow)) {
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * a.x_scale);
+        const float top = fmaxf(m, row_max(s));
         const float f = top == -INFINITY ? 1.0f : ex2(m - top);
         m = top, l *= f;
+        far = __any_sync(0xffffffffu, live && m > -INFINITY && fabsf(m) > kFar);
         if (g > 0) {   // the product of the step before; the one before that is done, or S would not be here
           if (!wait_warp(bar_o, (n_steps - 1) & 1, w, 7)) return;
           tc_fence_after();
           scale_output(o_addr, f);
         }
+        sum = softmax_step(s, 1.0f, m == -INFINITY ? 0.f : m, s_buf);
       }
       tmem_wait_st();
       tc_fence_before();

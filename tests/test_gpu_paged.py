@@ -832,3 +832,30 @@ def test_the_readme_s_step_of_a_decoder(B):
     # a key that rounds the other way moves a logit by 2^-8 |q| |k| / sqrt(d) at most
     assert (names["lse"].double() - want_lse).abs().max() <= 0.05
     assert (names["out"].double() - want).norm() <= 3 * 2.0 ** -8 * want.norm()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("counts,rows", [([1], 500), ([1], 20000), ([4], 900), ([40], 700), ([300], 2000), ([90], 20000)])
+def test_attend_logits_of_any_size(B, dtype, counts, rows):
+    """Logits of 1e11, where one step of fp32 is thousands: the largest takes the row, as it does in 64 bits."""
+    n = counts[0]
+    c = R.Cache([[n + rows, n + rows]], 32, dtype=dtype, device="cuda", seed=n, k_scale=1e5)
+    q = (1e5 * torch.randn(n, 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))).to(dtype)
+    for causal in (True, False):
+        out, lse = run_attend(B, c, q, [0, n], causal)
+        bad = int((~torch.isfinite(out)).sum()), int((~torch.isfinite(lse)).sum())
+        assert bad == (0, 0)
+        for g in range(2):
+            k, v = (x.cuda().double() for x in c.rows[0][g])
+            x = torch.einsum("nhd,ld->nhl", q[:, 4 * g:4 * g + 4].double(), k) / math.sqrt(D)
+            if causal:
+                x = x.masked_fill((torch.arange(k.shape[0], device="cuda")[None] > rows + torch.arange(n, device="cuda")[:, None])[:, None], -math.inf)
+            two = x.topk(2, -1)
+            # a logit is off by at most 132 * 2^-24 |q| |k| / sqrt(d)
+            off = 132 * EPS * float(q.double().norm(dim=-1).max()) * float(k.norm(dim=-1).max()) / math.sqrt(D)
+            sure = two.values[..., 0] - two.values[..., 1] > 2 * off + 200
+            assert sure.float().mean() > 0.9
+            want = v[two.indices[..., 0]]
+            got = out[:, 4 * g:4 * g + 4].double()
+            assert ((got - want).abs() <= (2.0 ** -7 if dtype == torch.bfloat16 else 2 * EPS) * want.abs())[sure].all()
+            assert ((lse[:, 4 * g:4 * g + 4].double() - two.values[..., 0]).abs() <= off + 4 * EPS * two.values[..., 0].abs() + 1)[sure].all()
