@@ -834,6 +834,70 @@ def test_the_readme_s_step_of_a_decoder(B):
     assert (names["out"].double() - want).norm() <= 3 * 2.0 ** -8 * want.norm()
 
 
+# ------------------------------------------------------------------------------------- at the ends of the documented ranges
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 40])
+def test_attend_the_longest_cache(B, dtype, n):
+    """2^24 rows of one head, the same eight pages over and over: the output is that of the pages taken once, the lse larger by the
+    logarithm of how often they are taken."""
+    P, pages = 64, 8
+    c = R.Cache([[P * pages]], P, dtype=dtype, device="cuda", seed=1)
+    reps = (1 << 24) // (P * pages)
+    c.table = c.table.repeat(1, 1, reps)
+    c.lengths = i32([[1 << 24]])
+    q = torch.randn(n, 2, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(dtype)
+    out, lse = run_attend(B, c, q, [0, n], causal=False)
+    want, want_lse = R.attend(q, [0, n], c.rows, causal=False)
+    vmax = float(c.rows[0][0][1].double().abs().max())
+    # a thread adds up no more than 2^24 / 148 / 16 rows in turn (tensor cores: a row's sum, 64 of them at a time)
+    r = 132 * EPS * float(q.double().norm(dim=-1).max()) * float(c.rows[0][0][0].double().norm(dim=-1).max()) / math.sqrt(D) + 2.0 ** -20 + 7200 * EPS
+    assert ((lse.double() - want_lse - math.log(reps)).abs() <= r + 2 * EPS * (want_lse.abs() + math.log(reps))).all()
+    tol = 2 * r * vmax + (2.0 ** -8 * (vmax + want.abs()) if dtype == torch.bfloat16 else EPS * want.abs())
+    assert ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_as_many_units_as_there_may_be(B, dtype):
+    """65536 sequences of one head: a token appended and attended for each, up to 16 rows."""
+    Nu, P, H = 65536, 16, 2
+    g = torch.Generator(device="cuda").manual_seed(2)
+    kp, vp = (torch.randn(Nu + 3, P, D, device="cuda", generator=g).to(dtype) for _ in range(2))
+    table = torch.randperm(Nu + 3, device="cuda", generator=g)[:Nu].int().view(Nu, 1, 1).contiguous()
+    lengths = torch.randint(0, P, (Nu, 1), device="cuda", generator=g, dtype=torch.int32)
+    st = torch.arange(Nu + 1, device="cuda", dtype=torch.int32)
+    q, k, v = (torch.randn(Nu, h, D, device="cuda", generator=g).to(dtype) for h in (H, 1, 1))
+    pg = B.make_paged(kp, table, q=q, k_new=k, max_new=1)
+    ws, grown, out, lse = B.alloc_paged_workspace(pg), torch.zeros_like(lengths), torch.zeros_like(q), torch.zeros(Nu, H, device="cuda")
+    before = kp.clone()
+    B.ckv_append(pg, None, k, v, None, st, lengths, table, kp, vp, ws, new_lengths=grown)
+    B.ckv_paged_attend(pg, q, kp, vp, table, grown, st, out, ws, lse=lse)
+    assert B.ckv_device_status(ws) == B.OK and torch.equal(grown, lengths + 1)
+    at = table.view(Nu).long(), lengths.view(Nu).long()
+    assert torch.equal(kp[at], k[:, 0]) and torch.equal(vp[at], v[:, 0])
+    kp[at] = before[at]
+    assert torch.equal(kp, before)
+    kp[at] = k[:, 0]
+    pages = table.view(Nu).long()
+    x = torch.einsum("uhd,ujd->uhj", q.double(), kp[pages].double()) / math.sqrt(D)
+    x = x.masked_fill((torch.arange(P, device="cuda")[None] > lengths)[:, None], -math.inf)
+    want = torch.einsum("uhj,ujd->uhd", torch.softmax(x, -1), vp[pages].double())
+    vmax = vp[pages].double().abs().amax((1, 2))[:, None, None]
+    r = 132 * EPS * 20 * 20 / math.sqrt(D) + 2.0 ** -20 + 300 * EPS
+    assert ((lse.double() - torch.logsumexp(x, -1)).abs() <= r + 2 * EPS * 8).all()
+    assert ((out.double() - want).abs() <= 2 * r * vmax + (2.0 ** -8 * (vmax + want.abs()) if dtype == torch.bfloat16 else EPS * want.abs())).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 4, 30, 200])
+def test_attend_queries_head_by_head(B, dtype, n):
+    """q as a view of [H, T, d]."""
+    c = R.Cache([[n + 300, n + 31]], 64, dtype=dtype, device="cuda", seed=n)
+    q = torch.randn(8, n, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).to(dtype).transpose(0, 1)
+    for max_new in (0, n):
+        out, lse = run_attend(B, c, q, [0, n], max_new=max_new)
+        check_attend(c, q, [0, n], out, lse)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("counts,rows", [([1], 500), ([1], 20000), ([4], 900), ([40], 700), ([300], 2000), ([90], 20000)])
 def test_attend_logits_of_any_size(B, dtype, counts, rows):
@@ -859,3 +923,70 @@ def test_attend_logits_of_any_size(B, dtype, counts, rows):
             got = out[:, 4 * g:4 * g + 4].double()
             assert ((got - want).abs() <= (2.0 ** -7 if dtype == torch.bfloat16 else 2 * EPS) * want.abs())[sure].all()
             assert ((lse[:, 4 * g:4 * g + 4].double() - two.values[..., 0]).abs() <= off + 4 * EPS * two.values[..., 0].abs() + 1)[sure].all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [7, 950])
+def test_append_in_place_queries_behind_padding(B, dtype, T):
+    """q_out == q in a fused projection, rows of no unit before the first unit and behind the last, an idle unit between."""
+    H, Hkv, lead, pad = 10, 5, 2, 1
+    a = (T - lead - pad) // 2
+    starts = [lead, lead + a, lead + a, T - pad]
+    c = R.Cache([[3, 0, 31, 32, 40], [1] * 5, [64, 9, 2, 0, 5]], 32, max_extra=T, dtype=dtype, device="cuda", poison=3.0)
+    qkv = torch.randn(T, H + 2 * Hkv, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(T)).to(dtype)
+    was = qkv.clone()
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    inv = 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    pg = B.make_paged(c.k_pages, c.table, q=q, k_new=k)
+    ws, new = B.alloc_paged_workspace(pg), torch.zeros_like(c.lengths)
+    B.ckv_append(pg, B.make_rotary(inv), k, v, pos, i32(starts), c.lengths, c.table, c.k_pages, c.v_pages, ws, q=q, q_out=q, new_lengths=new)
+    assert B.ckv_device_status(ws) == B.OK
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 2 * EPS
+    tq, tk = R.turn(was[:, :H], pos, inv), R.turn(was[:, H:H + Hkv], pos, inv)
+    live = slice(lead, T - pad)
+    assert ((q.double() - tq).abs() <= 80 * EPS * tq.abs().amax(-1, keepdim=True) + half * tq.abs())[live].all()
+    assert torch.equal(qkv[:lead], was[:lead]) and torch.equal(qkv[T - pad:], was[T - pad:]) and torch.equal(qkv[:, H:], was[:, H:])
+    for u in range(3):
+        n = starts[u + 1] - starts[u]
+        for g in range(Hkv):
+            L = c.lens[u][g]
+            assert int(new[u, g]) == L + n
+            j = torch.arange(L, L + n, device="cuda")
+            at = c.table[u, g, j // 32].long(), j % 32
+            want = tk[starts[u]:starts[u + 1], g]
+            assert ((c.k_pages[at].double() - want).abs() <= 80 * EPS * want.abs().amax(-1, keepdim=True) + half * want.abs()).all()
+            assert torch.equal(c.v_pages[at], was[starts[u]:starts[u + 1], H + Hkv + g])
+
+
+@pytest.mark.parametrize("kind", ["elastic", "all"])
+def test_gather_pages_of_other_selections(B, kind):
+    """The shared elastic selection, which may keep fewer rows than its share, and a budget that keeps everything."""
+    from test_gpu_parity import params_of, problem_of
+    cfg = gen.shrink(gen.CONFIGS["c2"], n_layers=2, batch=1, seq_len=900, budget_per_head=128, n_needles=4)
+    b = gen.make_batch(cfg, "cuda")
+    P = params_of(B, problem_of(cfg, 2))
+    if kind == "elastic":
+        P.shared_elastic = True
+        b["sens"] = b["sens"] * 0 + 1e4                 # a threshold that leaves few candidates
+    else:
+        P.budget_per_head = 5000
+    out = B.compress(b["q"], b["k"], b["v"], b["head_w"], b["sens"], P)
+    shape, params = B.make_shape(b["q"], b["k"]), B.make_params(P, b["head_w"], b["sens"])
+    bud, off = out["budgets"].tolist(), out["offsets"].tolist()
+    assert (max(map(max, bud)) < 128) if kind == "elastic" else all(x == 900 for r in bud for x in r)
+    c = R.Cache(bud, 16, dtype=b["k"].dtype, device="cuda", poison=9.0)
+    for p in c.pools:
+        p.fill_(9.0)
+    pg = B.make_paged(c.k_pages, c.table, n_q_heads=cfg.n_q_heads)
+    ws, lengths = B.alloc_paged_workspace(pg), torch.full_like(out["budgets"], -1)
+    B.ckv_gather_pages(shape, params, pg, b["k"], b["v"], out["indices"], out["budgets"], out["offsets"], c.table, c.k_pages, c.v_pages,
+                       lengths, ws)
+    assert torch.equal(lengths, out["budgets"]) and B.ckv_device_status(ws) == B.OK
+    for pool, src in zip((c.k_pages, c.v_pages), ("k_out", "v_out")):
+        want = torch.full_like(pool, 9.0)
+        for u in range(2):
+            for g in range(cfg.n_kv_heads):
+                j = torch.arange(bud[u][g], device="cuda")
+                want[c.table[u, g, j // 16].long(), j % 16] = out[src][u, off[u][g]:off[u][g] + bud[u][g]]
+        assert torch.equal(pool, want)
