@@ -320,8 +320,9 @@ ckv_status ckv_score_noalloc(const ckv_shape* shape, const ckv_params* params, c
  * are padding: they may hold anything, and nothing is written for them.
  * The cache is two pools k_pages, v_pages [n_pages, page_size, d] that share no row (they may be interleaved); row j of KV head g of unit u is row j % page_size of
  * page page_table[u, g, j / page_size] (page_table [Nu, Hkv, max_pages] int32), and lengths [Nu, Hkv] int32 counts
- * the rows each head holds: the heads of a unit keep different numbers of rows, so table and lengths are per head.  Only
- * the table entries of pages that hold rows are read; a page may be shared by several readers.
+ * the rows each head holds: the heads of a unit keep different numbers of rows, so table and lengths are per head.  Table
+ * entries of pages that hold no rows may hold anything: they may be read, and are never followed.  A page may be shared by
+ * several readers.
  * A page number outside the pool, or a row past the table's last page, is never followed: the row is left out, and
  * ckv_device_status(ws) reports CKV_ERR_PAGE.  Cache rows behind a head's length may hold anything, NaN included.
  * The calls use only the current device's memory and are capturable; a work space serves one call at a time.  Outputs,
@@ -335,8 +336,8 @@ typedef struct {
   int32_t head_dim;    /* d; must be 128 */
   int32_t dtype;       /* ckv_dtype of tokens, pages and outputs */
   int32_t n_tokens;    /* T >= 0: rows of the token arrays, padding included; T <= 2^20, T * H <= 2^30 */
-  int32_t max_new;     /* most tokens any unit has in a call, as far as known; 0: not known (T).  It only picks kernels:
-                          the results are right whatever it says */
+  int32_t max_new;     /* most tokens any unit has in a call, as far as known; 0: not known (T).  It only picks kernels (so does
+                          the width of the table, max_pages): the results are right whatever it says */
   int32_t causal;      /* ckv_paged_attend: 1: a unit's tokens are its heads' last rows and see no later ones;
                           0: they see every row */
   int32_t page_size;   /* 16, 32, 64, 128 or 256 rows */
@@ -398,8 +399,10 @@ ckv_status ckv_gather_pages(const ckv_shape* shape, const ckv_params* params, co
  * tokens in unit u, its token i sees rows j <= lengths[u,g] - n + i of head g (causal), or every row j < lengths[u,g].
  *   out [T,H,d] = softmax(scale q k^T) v in the dtype of `paged`, on a 32-byte boundary;  lse_or_null [T,H] fp32 = ln sum_j exp(scale q . k_j).
  * A token that sees no row gets zeros and -infinity; one that sees a NaN logit, NaN for both.  Values up to 2^94 in size stay
- * in range whatever the logits (sums run against a reference that may lag behind the largest by 2^16).  Each sum is 32-bit and taken in an order that the shapes,
- * lengths and token counts alone decide.
+ * in range whatever the logits (sums run against a reference that may lag behind the largest by 2^16).  Logits, sums and outputs
+ * are held in 32 bits; bf16 calls round each probability to bf16 for its product with the value (not for the sum).  The order of
+ * the sums follows from the fields of `paged` (max_new and max_pages among them), the lengths and the token counts alone: the
+ * same call gives the same bits.
  */
 ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k_pages, const void* v_pages,
                             const int32_t* page_table, const int32_t* lengths, const int32_t* token_starts, void* out,

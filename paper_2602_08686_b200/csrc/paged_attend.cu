@@ -11,7 +11,7 @@
 // time, eight lanes per key with 16 dimensions each: queries, keys, values and the output all stay in registers, nothing
 // is staged, and each of the four groups of eight lanes keeps its own running (m, l, o); they join when the item ends.
 // Bound: the latency of a step at eight warps an SM (255 registers a thread), for single tokens close to HBM: 8 sequences of
-// 8192 rows in 111 us, 0.74 of the measured copy rate.
+// 8192 rows in 110 us, 0.75 of the measured copy rate.
 #include <cuda_bf16.h>
 
 #include "paged_work.cuh"
@@ -330,7 +330,7 @@ template cudaError_t launch_join<true>(const WorkArgs&, int, int, void*, float*,
 template cudaError_t launch_join<false>(const WorkArgs&, int, int, void*, float*, cudaStream_t);
 
 // bf16 calls go to the kernel for few rows while every unit has at most so many query rows per KV head, else to the tensor
-// cores.  With up to 16 rows it is ahead (one sequence on 16k rows 27 us against 33; 16 x 32k are read at the memory's rate by either), with
+// cores (lengths are on the device: a cache is as short as its table is narrow).  With up to 16 rows it is ahead (one sequence on 16k rows 27 us against 33; 16 x 32k are read at the memory's rate by either), with
 // 32 on a long cache its matrix instructions take longer than the bytes (8 x 8 tokens on 16k rows 159 us against 101); a
 // short cache is all latency, where it stays ahead for longer (8 tokens on 1000 rows 13 us against 20).
 constexpr int kFewRows = 16;
@@ -339,10 +339,13 @@ static bool wants_tc(const ckv_paged& pg) {
   return pg.dtype == CKV_BF16 && G <= 128 && most * G > kFewRows && (most * G > kMmaRows || !cluster_size(pg, kShortMore, 1));
 }
 
-// Short caches go to clusters, one per block of a head's query rows: as many CTAs as the blocks leave room for, as long as each has a step's keys to read.
+// Short caches - those whose table has room for few rows; the lengths, which may be shorter, are on the device - go to clusters, one
+// per block of a head's query rows: as many CTAs as the blocks leave room for, as long as each has a step's keys to read.
 // Clusters do not cross the GPCs, so that of eight CTAs 15 run at a time, of four 33, of two 74 (148 SMs, one CTA each; 16 heads
-// of 2000 rows in clusters of eight: 18 us, of four: 13).  0: the cache is not short: a cluster's CTA has more rows to read
-// than the split's even share and what the split's schedule and join take besides.
+// of 2000 rows in clusters of eight: 18 us, of four: 13).  0: the cache is not short: a cluster's CTA may have more rows to
+// read than the split's even share and what the split's schedule and join take besides.  A table far wider than the rows held costs the
+// cluster form: with room for 131072 rows one sequence of 512 takes 13.6 us on the device (7.9 with its own width), 16 of 1900 36 (27), 8
+// tokens on 1000 rows 19.7 (12.8); fp32, 4 sequences of 2048 rows of two heads, 19.8 (12.9).
 int cluster_size(const ckv_paged& pg, const ShortRule& rule, int64_t blocks) {
   constexpr int kFit[] = {kWorkers, 74, 33, 15};
   const int64_t items = (int64_t)pg.n_units * pg.n_kv_heads * blocks, capacity = (int64_t)pg.max_pages * pg.page_size;

@@ -11,7 +11,8 @@
 // The matrix instructions pad 4 to 8 real rows to 16, which costs nothing: a warp spends about 150 issue slots on a group
 // whose 8 KB take the SM 340 clocks to fetch.  The next keys are requested when the logits are done and the next values when
 // the output is, so a warp has 4 to 8 KB under way at any time.
-// 16 sequences of 32k rows, one token: 344 to 356 us, 0.92 to 0.95 of the measured copy rate.
+// 16 sequences of 32k rows, one token: 344 to 369 us by card, 0.89 to 0.95 of the measured copy rate.  With 32 query rows the 255
+// registers do not hold everything: 96 bytes a thread spill in the split form, 232 in clusters.
 #include <cuda_bf16.h>
 
 #include "paged_work.cuh"

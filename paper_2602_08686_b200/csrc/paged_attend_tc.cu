@@ -13,7 +13,8 @@
 // N = 64 costs the first product half as much again (48 clocks for 32 of arithmetic: A and B are read from shared memory at 128
 // bytes a clock), 2600 clocks per key tile and pair of query tiles; the exponentials alone take 2050 (16 a clock).
 // Bound: those two together, at the clocks the power limit leaves under them (1.4 to 1.6 GHz).  2048 tokens over 32k rows:
-// 2.0 us per key tile, 900 to 925 us, 1.23 PFLOP/s (76 % of the measured rate of a plain matrix product); at 8192 rows the
+// 2.0 us per key tile and 918 us after a rest (1.24 PFLOP/s, 77 % of the measured rate of a plain matrix product), 1030 to 1060 us
+// kept up (1.07 to 1.1, 80 % of that product's); at 8192 rows the
 // tensor pipe is active 58 % of the time, and as much the exponentials' one.  An item takes 5 us besides its tiles: its last
 // product, and its output, whose 32-byte pieces of 128 rows keep the store path busy (gathered to lines by shuffles
 // they take 0.5 us less on two query tiles and more on one).

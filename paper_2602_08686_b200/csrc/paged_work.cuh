@@ -418,7 +418,7 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, int64_t 
 constexpr int kMmaRows = 32;         // most query rows of a block of the bf16 kernel for few rows
 constexpr int kMmaTile = 64;         // keys per tile of its schedule
 constexpr int kMmaCtaKeys = 128;     // keys a CTA of it takes per step
-// When a cache is short: a CTA of a cluster takes `cta_keys` per step, and reads no more than the given part of the split's even share
+// When a cache (the room its table has) is short: a CTA of a cluster takes `cta_keys` per step, and reads no more than the given part of the split's even share
 // and `rows` more.  (A row takes such a CTA 13 ns with up to 16 query rows, 21 with 32, 32 in fp32; the split's schedule and
 // join take 10 us.  With 32 query rows the other side is the tensor-core kernel: 9 ns a row.)
 struct ShortRule {

@@ -1,14 +1,14 @@
 // Norms of queries and keys for each head with the position rotation, and the same on the way into a paged cache.
 //
 // A CTA takes one to eight consecutive tokens.  Cosine and sine of a token's angles are shared by its H + Hkv heads: the CTA
-// computes them once, in 64 bits where 32 would lose the angle (position * inv_freq reaches 10^6 radians; reduced to a
-// fraction of a turn in fp64 the fp32 sincospi of it is good to an ulp).  16 threads (bf16) or 32 (fp32) share a row of 128
+// computes them once, in 64 bits where 32 would lose the angle (position * inv_freq reaches 10^6 radians); its fraction of a
+// turn, at most one half, is rounded to fp32 (2^-26 of a turn: 9.4e-8 radians, 1.5 ulp of a sine) for an fp32 sincospi.  16 threads (bf16) or 32 (fp32) share a row of 128
 // elements, with two 8-byte pieces each that hold whole pairs: the same place in either half of the rotated dimensions where
 // pairs are half a rotation apart, neighbours otherwise.  So no thread needs another's elements, and since a thread keeps its
 // dimensions and its token over all the rows it takes, its cosines stay in registers.  (With one 16-byte piece, the
 // partner's by shuffles and the cosines from shared memory per row, the 32k prompt took 243 us: instruction issue.)  The
 // row's sum of squares is a shuffle tree.  Everything between the load and the store is fp32, rounded once.
-// Bound: HBM for long inputs (each row is read and written once; the 32k prompt in 118 us, 0.87 of the measured copy rate), the
+// Bound: HBM for long inputs (each row is read and written once; the 32k prompt in 118 to 123 us by card, 0.83 to 0.87 of the measured copy rate), the
 // launch and three dependent reads for a decode step (16 sequences: 4 us).
 #include <cuda_bf16.h>
 
