@@ -20,8 +20,8 @@
 // they take 0.5 us less on two query tiles and more on one).
 // No maximum is taken per step.  Any reference m gives the same softmax, up to overflow: P, l and O are floating-point, and a
 // common factor costs none of their bits.  So a row keeps the reference of its first visible step, and the sums tell
-// whether an exponential left the range (2^16: then, and only then, the maximum is taken, O is rescaled in TMEM and
-// the step is done again).
+// whether an exponential left the range (2^16: then, or where the reference itself is too far from zero to be exact, the maximum
+// is taken, O is rescaled in TMEM and the step is done again).
 // Warps 0-3 and 4-7: softmax of stream 0 and 1; warps 8, 9: their MMAs; warp 10: TMA; warp 11 walks the items ahead of the others.
 // Every wait is bounded and reports CKV_ERR_TIMEOUT through the status word.
 #include "paged_work.cuh"
