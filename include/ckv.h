@@ -408,6 +408,90 @@ ckv_status ckv_paged_attend(const ckv_paged* paged, const void* q, const void* k
                             const int32_t* page_table, const int32_t* lengths, const int32_t* token_starts, void* out,
                             float* lse_or_null, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Drafted trees.  A decoder that drafts several continuations at once appends their tokens to the cache (ckv_append, positions as
+ * below), attends with each token seeing the rows before the tree and its own ancestors, and keeps the rows of the accepted
+ * path (ckv_keep_rows).
+ */
+
+/*
+ * What each token sees of its unit's tokens, and where it stands, from the trees' parents: parents [T] int32 counts inside the unit
+ * (-1: a root; a unit may hold several trees, in any order), masks [T, words]: bit t % 32 of word t / 32 is set where the
+ * unit's token t is the token itself or an ancestor.  words 1..32; units have at most 32 * words tokens (what is past them has an
+ * empty mask and is seen by nobody).  positions_or_null [T] int32 receives the depth (roots: 0), plus
+ * first_positions_or_null [Nu].  Only token_starts as in the paged calls is needed, no cache.  A parent that is no token of the unit,
+ * a token past the words, or one that is its own ancestor is reported (CKV_ERR_PAGE): such a parent counts as none, tokens of a cycle see all
+ * of it and have depth 0.  ws: 256 bytes.
+ */
+ckv_status ckv_tree_masks(int32_t n_units, int32_t n_tokens, int32_t words, const int32_t* parents, const int32_t* token_starts,
+                          const int32_t* first_positions_or_null, uint32_t* masks, int32_t* positions_or_null, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/*
+ * ckv_paged_attend of tokens that are a unit's last rows (append first) and see each other by bits: with n tokens in unit u, its token
+ * i sees rows j < lengths[u,g] - n of head g and the rows lengths[u,g] - n + t with bit t of masks [T, words] set (any bits: a tree's
+ * ancestors, a token's own bit among them or not; words 1..2^15, tokens past 32 * words are seen by nobody).  `causal` of `paged` is
+ * not looked at.  Outputs, numerics, work space and the rest as in ckv_paged_attend.
+ */
+ckv_status ckv_tree_attend(const ckv_paged* paged, const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                           const int32_t* lengths, const int32_t* token_starts, const uint32_t* masks, int32_t words, void* out,
+                           float* lse_or_null, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rows moved together, in place: of every head's last `span` rows (tails_or_null: its list's entry; NULL: all its rows) those that its
+ * list names stay, in order: with base = lengths - span, row base + i becomes what row base + rows[begins + i] was, i < counts, and
+ * new_lengths [Nu,Hkv] = base + counts.  Rows before base stay; pages are not given back (see ckv_pages_trim).  Lists ascend strictly.
+ * n_lists is Nu * Hkv (a list per head: what a retention pass over the cache chose) or Nu / layers (a list per sequence, shared by its
+ * layers and heads: the accepted tokens of a drafted tree, tails = its tokens).  rows [n_rows] int32; begins, counts, tails [n_lists].
+ * refs_or_null [n_pages]: how many heads hold each page; rows are not moved into a page that several hold (ckv_pages_reserve makes it the
+ * head's own).  A head with such a page, a list that does not ascend or leaves its span or `rows`, or a page number outside the
+ * pool is left as it is, new_lengths = lengths, and reported (CKV_ERR_PAGE).  Units come layer by layer here and below: unit = layer
+ * * sequences + sequence.  Of `paged` the page fields, units, heads and dtype are read.  ws: 256 bytes.
+ */
+ckv_status ckv_keep_rows(const ckv_paged* paged, int32_t layers, const int32_t* rows, int32_t n_rows, const int32_t* begins,
+                         const int32_t* counts, int32_t n_lists, const int32_t* tails_or_null, const int32_t* refs_or_null,
+                         const int32_t* lengths, const int32_t* page_table, void* k_pages, void* v_pages, int32_t* new_lengths,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------
+ * Whose the pages are.  The caller keeps, next to the page table and the lengths, refs [n_pages] int32 (how many heads hold each page;
+ * 0: it is free; all zero to begin with) and held [Nu,Hkv] int32 (pages each head holds: table entries 0 .. held-1).  These
+ * calls and no others change the two; ckv_append and ckv_gather_pages write rows of pages that have been reserved.  Counts, held and
+ * table entries follow from the inputs alone.  A page number outside the pool, a count that would fall below zero, a held
+ * outside 0..max_pages or a negative length is reported (CKV_ERR_PAGE) and nothing is done for that entry.
+ */
+
+/* Bytes of work space ckv_pages_reserve needs (0 on invalid arguments); the other calls of this section use 256 of them. */
+size_t ckv_pages_workspace_bytes(const ckv_paged* paged);
+
+/*
+ * Pages for the rows to come: heads are given pages until they hold the rows lengths .. lengths + new_rows - 1, and where they
+ * share the pages they will write (slots lengths / page_size on), those are replaced by pages of their own, with copies of the
+ * rows below lengths.  new_rows [n_lists] int32, n_lists Nu * Hkv (for example a retention pass's budgets) or Nu / layers; a head of no
+ * new rows is left as it is.  Pages are the free ones of lowest number, handed out head by head, slot by slot.  All or nothing: where
+ * too few pages are free nothing is changed.  room_or_null [2] int32: the free pages there are afterwards, and how many there were too
+ * few (0: done).  Slots past the table are not reserved, and are reported (CKV_ERR_PAGE).
+ */
+ckv_status ckv_pages_reserve(const ckv_paged* paged, int32_t layers, const int32_t* new_rows, int32_t n_lists, const int32_t* lengths,
+                             int32_t* held, int32_t* page_table, int32_t* refs, void* k_pages, void* v_pages, int32_t* room_or_null,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* Gives back the pages behind each head's last row: held falls to lengths / page_size, rounded up (lengths_or_null NULL: to zero, the
+ * units end).  A page is free once nobody holds it; its rows and table entries stay as they are. */
+ckv_status ckv_pages_trim(const ckv_paged* paged, const int32_t* lengths_or_null, int32_t* held, const int32_t* page_table, int32_t* refs,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A new batch whose sequences go on from old ones, sharing their pages: new sequence s of each layer continues old sequence
+ * parents[s] (parents [n_new] int32; several may continue one, in any order; -1: an empty one).  new_lengths, new_held
+ * [layers * n_new, Hkv] and new_page_table [layers * n_new, Hkv, max_pages] receive the old ones' (table entries past held are left as
+ * they are).  keep_old 0: the old batch ends, and what no new sequence holds is free; 1: it goes on beside the new one.  `paged` is the
+ * old batch's; layers * n_new * Hkv <= 65536.  No row is copied: the first ckv_pages_reserve before a write does that.
+ */
+ckv_status ckv_pages_fork(const ckv_paged* paged, int32_t layers, int32_t n_new, const int32_t* parents, const int32_t* lengths,
+                          const int32_t* held, const int32_t* page_table, int32_t* refs, int32_t keep_old, int32_t* new_lengths,
+                          int32_t* new_held, int32_t* new_page_table, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronises `stream` and returns what device code recorded in the status word of `ws` since the last
  * such call (CKV_OK, CKV_ERR_TIMEOUT or CKV_ERR_PAGE), or CKV_ERR_CUDA if the stream is in error.  A recorded code survives
  * later calls on the work space until this function reports it, which also clears it.  ws == NULL reads the

@@ -112,6 +112,15 @@ def lib() -> C.CDLL:
         L.ckv_append.argtypes = [pgd, rty] + [vp] * 12 + [sz, vp]
         L.ckv_gather_pages.argtypes = [shp, prm, pgd] + [vp] * 10 + [sz, vp]
         L.ckv_paged_attend.argtypes = [pgd] + [vp] * 9 + [sz, vp]
+        i32 = C.c_int32
+        L.ckv_tree_masks.argtypes = [i32] * 3 + [vp] * 6 + [sz, vp]
+        L.ckv_tree_attend.argtypes = [pgd] + [vp] * 7 + [i32] + [vp] * 3 + [sz, vp]
+        L.ckv_keep_rows.argtypes = [pgd, i32, vp, i32, vp, vp, i32] + [vp] * 8 + [sz, vp]
+        L.ckv_pages_workspace_bytes.restype = sz
+        L.ckv_pages_workspace_bytes.argtypes = [pgd]
+        L.ckv_pages_reserve.argtypes = [pgd, i32, vp, i32] + [vp] * 8 + [sz, vp]
+        L.ckv_pages_trim.argtypes = [pgd] + [vp] * 5 + [sz, vp]
+        L.ckv_pages_fork.argtypes = [pgd, i32, i32] + [vp] * 5 + [i32] + [vp] * 4 + [sz, vp]
         L.ckv_device_status.argtypes = [vp, vp]
         L.ckv_gate_depth_map_host.argtypes = [fp, C.c_int, C.c_int, C.c_int64, fp]
         L.ckv_set_scan_events.argtypes = [vp, vp]
@@ -124,6 +133,7 @@ def lib() -> C.CDLL:
         L.ckv_allocate_rows_host.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int64, vp, vp]
         for name in ("ckv_score", "ckv_score_noalloc", "ckv_budget", "ckv_select", "ckv_vnorm", "ckv_unit_max", "ckv_kept_mass", "ckv_attend", "ckv_prompt_mass", "ckv_global_scores", "ckv_gather", "ckv_compress", "ckv_compress_host",
                      "ckv_rotate", "ckv_append", "ckv_gather_pages", "ckv_paged_attend",
+                     "ckv_tree_masks", "ckv_tree_attend", "ckv_keep_rows", "ckv_pages_reserve", "ckv_pages_trim", "ckv_pages_fork",
                      "ckv_device_status", "ckv_version", "ckv_allocate_rows_host"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -602,6 +612,107 @@ def ckv_paged_attend(paged, q, k_pages, v_pages, page_table, lengths, token_star
                 _dense(page_table, paged._table, i32, dev, "page_table"), _dense(lengths, paged._heads, i32, dev, "lengths"),
                 _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(out, qs[0], paged._dtype, dev, "out"),
                 None if lse is None else _dense(lse, qs[0][:2], torch.float32, dev, "lse"), _ws_of(paged, ws), ws.numel())
+
+
+def ckv_tree_masks(parents, token_starts, masks, ws, positions=None, first_positions=None, stream=None):
+    """Ancestor bits masks [T, words] int32 of the packed tokens from their trees' parents [T] (inside the unit; -1: a root), and
+    positions [T]: their depth, plus first_positions [Nu]."""
+    if masks is None or masks.dim() != 2 or token_starts is None or token_starts.dim() != 1 or token_starts.numel() < 2:
+        raise ValueError("masks must be [T, words] and token_starts [Nu + 1]")
+    dev, i32, (T, words), Nu = masks.get_device(), torch.int32, masks.shape, token_starts.numel() - 1
+    if ws is None or ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws must be a dense uint8 tensor on the device of the masks")
+    _paged_call(lib().ckv_tree_masks, "ckv_tree_masks", dev, stream, Nu, T, words, _dense(parents, (T,), i32, dev, "parents"),
+                _dense(token_starts, (Nu + 1,), i32, dev, "token_starts"),
+                None if first_positions is None else _dense(first_positions, (Nu,), i32, dev, "first_positions"),
+                _dense(masks, (T, words), i32, dev, "masks"),
+                None if positions is None else _dense(positions, (T,), i32, dev, "positions"), ws.data_ptr(), ws.numel())
+
+
+def ckv_tree_attend(paged, q, k_pages, v_pages, page_table, lengths, token_starts, masks, out, ws, lse=None, stream=None):
+    """Attention of drafted tokens, their heads' last rows: each sees the rows before them and, of the unit's tokens, those
+    whose bits are set in its row of masks [T, words] int32."""
+    dev, i32 = paged._device, torch.int32
+    qs = paged._q
+    if masks is None or masks.dim() != 2:
+        raise ValueError("masks must be [T, words]")
+    words = masks.shape[1]
+    _paged_call(lib().ckv_tree_attend, "ckv_tree_attend", dev, stream, paged._ref, _same(q, qs, "q"),
+                _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
+                _dense(page_table, paged._table, i32, dev, "page_table"), _dense(lengths, paged._heads, i32, dev, "lengths"),
+                _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(masks, (paged.n_tokens, words), i32, dev, "masks"),
+                words, _dense(out, qs[0], paged._dtype, dev, "out"),
+                None if lse is None else _dense(lse, qs[0][:2], torch.float32, dev, "lse"), _ws_of(paged, ws), ws.numel())
+
+
+# The pages' owners: refs [n_pages] (how many heads hold each page, 0: free) and held [Nu, Hkv] (pages each head holds), int32.
+def _list_of(t, n, device, name):
+    if t is None or t.dim() != 1:
+        raise ValueError(f"{name} must be a 1-D tensor")
+    return _dense(t, (t.numel() if n is None else n,), torch.int32, device, name)
+
+
+def ckv_pages_workspace_bytes(paged: ckv_paged) -> int:
+    return int(lib().ckv_pages_workspace_bytes(C.byref(paged)))
+
+
+def alloc_pages_workspace(paged: ckv_paged, device=None) -> torch.Tensor:
+    """Work space of ckv_pages_reserve; the other calls on pages and trees use its first 256 bytes."""
+    nbytes = ckv_pages_workspace_bytes(paged)
+    if nbytes == 0:
+        raise CkvError(ERR_INVALID_ARG, "ckv_pages_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", paged._device) if device is None else device)
+
+
+def ckv_keep_rows(paged, rows, begins, counts, lengths, page_table, k_pages, v_pages, new_lengths, ws, tails=None, refs=None,
+                  layers=1, stream=None):
+    """Of every head's last tails rows (None: of all) those its ascending list names - rows[begins + i], i < counts - moved together in
+    place; begins, counts and tails are per (unit, KV head) or per sequence (Nu / layers).  new_lengths receives what is left."""
+    dev, i32 = paged._device, torch.int32
+    n_lists = -1 if begins is None else begins.numel()
+    _paged_call(lib().ckv_keep_rows, "ckv_keep_rows", dev, stream, paged._ref, int(layers), _list_of(rows, None, dev, "rows"),
+                rows.numel(), _list_of(begins, n_lists, dev, "begins"), _list_of(counts, n_lists, dev, "counts"), n_lists,
+                None if tails is None else _list_of(tails, n_lists, dev, "tails"),
+                None if refs is None else _list_of(refs, paged.n_pages, dev, "refs"),
+                _dense(lengths, paged._heads, i32, dev, "lengths"), _dense(page_table, paged._table, i32, dev, "page_table"),
+                _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
+                _dense(new_lengths, paged._heads, i32, dev, "new_lengths"), _ws_of(paged, ws), ws.numel())
+
+
+def ckv_pages_reserve(paged, new_rows, lengths, held, page_table, refs, k_pages, v_pages, ws, room=None, layers=1, stream=None):
+    """Pages for the next new_rows rows (per (unit, KV head) or per sequence) of every head, all or nothing; shared pages that will be
+    written are replaced by copies.  room [2] receives the free pages left and how many there were too few."""
+    dev, i32 = paged._device, torch.int32
+    new_ptr = _list_of(new_rows, None, dev, "new_rows")
+    _paged_call(lib().ckv_pages_reserve, "ckv_pages_reserve", dev, stream, paged._ref, int(layers), new_ptr, new_rows.numel(),
+                _dense(lengths, paged._heads, i32, dev, "lengths"), _dense(held, paged._heads, i32, dev, "held"),
+                _dense(page_table, paged._table, i32, dev, "page_table"), _list_of(refs, paged.n_pages, dev, "refs"),
+                _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
+                None if room is None else _list_of(room, 2, dev, "room"), _ws_of(paged, ws), ws.numel())
+
+
+def ckv_pages_trim(paged, lengths, held, page_table, refs, ws, stream=None):
+    """Gives back the pages behind each head's lengths (None: all of them)."""
+    dev, i32 = paged._device, torch.int32
+    _paged_call(lib().ckv_pages_trim, "ckv_pages_trim", dev, stream, paged._ref,
+                None if lengths is None else _dense(lengths, paged._heads, i32, dev, "lengths"),
+                _dense(held, paged._heads, i32, dev, "held"), _dense(page_table, paged._table, i32, dev, "page_table"),
+                _list_of(refs, paged.n_pages, dev, "refs"), _ws_of(paged, ws), ws.numel())
+
+
+def ckv_pages_fork(paged, parents, lengths, held, page_table, refs, new_lengths, new_held, new_page_table, ws, layers=1,
+                   keep_old=False, stream=None):
+    """A new batch whose sequence s continues the old parents[s] (-1: empty) in every layer, on the same pages; without keep_old the
+    old batch ends."""
+    dev, i32 = paged._device, torch.int32
+    parents_ptr = _list_of(parents, None, dev, "parents")
+    n_new, (Nu, Hkv) = parents.numel(), paged._heads or (0, 0)
+    units = int(layers) * n_new
+    _paged_call(lib().ckv_pages_fork, "ckv_pages_fork", dev, stream, paged._ref, int(layers), n_new, parents_ptr,
+                _dense(lengths, paged._heads, i32, dev, "lengths"), _dense(held, paged._heads, i32, dev, "held"),
+                _dense(page_table, paged._table, i32, dev, "page_table"), _list_of(refs, paged.n_pages, dev, "refs"), int(bool(keep_old)),
+                _dense(new_lengths, (units, Hkv), i32, dev, "new_lengths"), _dense(new_held, (units, Hkv), i32, dev, "new_held"),
+                _dense(new_page_table, (units, Hkv, paged.max_pages), i32, dev, "new_page_table"), _ws_of(paged, ws), ws.numel())
 
 
 # ------------------------------------------------------------------------------------ convenience

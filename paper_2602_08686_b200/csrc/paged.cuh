@@ -67,5 +67,11 @@ cudaError_t launch_gather_pages(const ckv_shape& s, const ckv_params& p, const c
 cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
                                 const int32_t* table, const int32_t* lengths, const int32_t* starts, void* out, float* lse,
                                 char* ws, cudaStream_t st);
+constexpr int kMaxTreeWords = 32;     // of ckv_tree_masks: 1024 tokens of a unit
+cudaError_t launch_tree_masks(int Nu, int T, int words, const int32_t* parents, const int32_t* starts,
+                              const int32_t* first_positions, uint32_t* masks, int32_t* positions, int* status, cudaStream_t st);
+cudaError_t launch_tree_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
+                               const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
+                               int tree_words, void* out, float* lse, char* ws, cudaStream_t st);
 
 }  // namespace ckv

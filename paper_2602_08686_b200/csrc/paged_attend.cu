@@ -44,8 +44,8 @@ struct RowsSmem {
   Item it;                                     // of the cluster
 };
 
-// kCluster: every item is one cluster's, as in the bf16 kernel for few rows.
-template <bool kCluster>
+// kCluster: every item is one cluster's, as in the bf16 kernel for few rows.  kTree: a tree's rows are seen by the bits of its tokens.
+template <bool kCluster, bool kTree>
 __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a, ckv_paged pg, float x_scale,
                                                                       const char* __restrict__ q,
                                                                       const char* __restrict__ kp,
@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
       }
     }
     const int end = min(now.t1 * a.tile, now.visible), step = n_ranks * a.tile;
+    const int least = kTree ? rows_before_tree(now) : 0;
     // a warp's eight keys are in one page
     auto page_at = [&](int j) { return j + warp * 8 < end ? page_of(a, now, (j + warp * 8) >> a.log_p) : -1; };
     auto key_at = [&](int j, int s) { return j + warp * 8 + s * 4 + grp; };
@@ -107,11 +108,19 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
     // The next keys are asked for when the logits are done, the next values when the output is.
     for (; j0 < end; j0 += step) {
       float x[2][kRowsM];
-      int key[2];
+      int key[2] = {0x7fffffff, 0x7fffffff};
       bool raise = false;
+      uint32_t hidden = 0;                     // kTree: bit (s, r): a key of the tree that is no ancestor of the row's token
+      auto sees = [&](int s, int r) { return key[s] < limit[r] && (!kTree || !(hidden >> (s * kRowsM + r) & 1u)); };
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         key[s] = page >= 0 && key_at(j0, s) < end ? key_at(j0, s) : 0x7fffffff;   // hidden from every row
+        if (kTree && key[s] >= least && key[s] < now.visible) {
+#pragma unroll
+          for (int r = 0; r < kRowsM; ++r)
+            if (r < rows && !(tree_bits(tree_words_of(a, now, (now.block * a.M + r) / a.G), a.tree_words, key[s] - (now.len - now.n)) & 1u))
+              hidden |= 1u << (s * kRowsM + r);
+        }
 #pragma unroll
         for (int r = 0; r < kRowsM; ++r) {
           float d = 0.f;
@@ -119,7 +128,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
           for (int i = 0; i < 16; ++i) d = fmaf(qr[r][i], kv[s][i], d);
 #pragma unroll
           for (int b = 1; b < 8; b <<= 1) d += __shfl_xor_sync(0xffffffffu, d, b);
-          x[s][r] = key[s] < limit[r] ? d * x_scale : -INFINITY;
+          x[s][r] = sees(s, r) ? d * x_scale : -INFINITY;
           raise |= x[s][r] > m[r];
         }
       }
@@ -140,7 +149,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(WorkArgs a
         const float p0 = exp2f(x[0][r] - ref), p1 = exp2f(x[1][r] - ref);
         l[r] += p0 + p1;
         // a hidden key's value may be anything: its row is skipped, not multiplied by zero
-        const bool s0 = key[0] < limit[r], s1 = key[1] < limit[r];
+        const bool s0 = sees(0, r), s1 = sees(1, r);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           float o = acc[r][i];
@@ -368,15 +377,17 @@ PagedWs paged_ws(const ckv_paged& pg) {
   return w;
 }
 
-cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
-                                const int32_t* table, const int32_t* lengths, const int32_t* starts, void* out, float* lse,
-                                char* ws, cudaStream_t st) {
+// tree null: the tokens see what pg.causal says.
+static cudaError_t launch_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
+                                 const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
+                                 int tree_words, void* out, float* lse, char* ws, cudaStream_t st) {
   const PagedWs w = paged_ws(pg);
   const bool bf16 = pg.dtype == CKV_BF16, tc = wants_tc(pg);
   const int64_t most = pg.max_new > 0 && pg.max_new < pg.n_tokens ? pg.max_new : pg.n_tokens;   // tokens of a unit
   const float scale = pg.scale != 0.f ? pg.scale : 0.08838834764831845f;
   WorkArgs a{};
-  a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = pg.causal;
+  a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = tree ? 0 : pg.causal;
+  a.tree = tree, a.tree_words = tree_words;
   a.P = pg.page_size, a.log_p = log2_of(pg.page_size), a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
   a.starts = starts, a.lengths = lengths, a.table = table, a.status = reinterpret_cast<int*>(ws + w.status);
   a.split = reinterpret_cast<int4*>(ws + w.split), a.ml = reinterpret_cast<float2*>(ws + w.ml), a.o = reinterpret_cast<float*>(ws + w.o);
@@ -399,11 +410,24 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = n_cta, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr, cfg.numAttrs = n_cta > 1 ? 2 : 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, n_cta ? attend_rows_kernel<true> : attend_rows_kernel<false>, a, pg, scale * kLog2e, (const char*)q,
-                                     (const char*)k_pages, (const char*)v_pages, (float*)out, lse, n_cta);
+  auto kernel = tree ? (n_cta ? attend_rows_kernel<true, true> : attend_rows_kernel<false, true>)
+                     : (n_cta ? attend_rows_kernel<true, false> : attend_rows_kernel<false, false>);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, pg, scale * kLog2e, (const char*)q, (const char*)k_pages, (const char*)v_pages,
+                                     (float*)out, lse, n_cta);
   count_launch();
   if (e == cudaSuccess && !n_cta) e = launch_join<false>(a, kWorkers, kRowsM, out, lse, st);
   return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
+                                const int32_t* table, const int32_t* lengths, const int32_t* starts, void* out, float* lse,
+                                char* ws, cudaStream_t st) {
+  return launch_attend(pg, q, k_pages, v_pages, table, lengths, starts, nullptr, 0, out, lse, ws, st);
+}
+cudaError_t launch_tree_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
+                               const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
+                               int tree_words, void* out, float* lse, char* ws, cudaStream_t st) {
+  return launch_attend(pg, q, k_pages, v_pages, table, lengths, starts, tree, tree_words, out, lse, ws, st);
 }
 
 }  // namespace ckv

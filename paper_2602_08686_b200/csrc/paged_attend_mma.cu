@@ -58,7 +58,8 @@ struct Smem {
 
 // kCluster: every item is one cluster's (of n_cta CTAs), whose warps share its keys and whose results join through distributed
 // shared memory; no schedule, no second kernel.  Otherwise the items are split evenly over the grid.
-template <int MT, int NW, bool kCluster>
+// kTree: behind the rows that all tokens see, each sees those of its ancestors (16 bits a row and group of keys).
+template <int MT, int NW, bool kCluster, bool kTree>
 __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_paged pg, float x_scale,
                                                                 const char* __restrict__ q, const char* __restrict__ kp,
                                                                 const char* __restrict__ vp, __nv_bfloat16* __restrict__ out,
@@ -135,9 +136,9 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
         const int r = mt * 16 + hh * 8 + p;
-        limit[mt][hh] = r < rows ? row_limit(a, it, r) : it.visible;   // rows that do not exist mask nothing
+        limit[mt][hh] = !kTree && r < rows ? row_limit(a, it, r) : it.visible;   // rows that do not exist mask nothing
       }
-    const int least = row_limit(a, it, 0);
+    const int least = kTree ? rows_before_tree(it) : row_limit(a, it, 0);
     float o[MT][16][4], m[MT][2], l[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -167,6 +168,16 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
       load_k(j + stride, page);
       uint32_t pr[MT][4];
       const bool mask = j + kGroup > least || now_page < 0;
+      uint32_t sees[MT][2];                    // kTree: which of the group's keys the thread's rows see
+      if (kTree && mask) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const int r = mt * 16 + hh * 8 + p;
+            sees[mt][hh] = r < rows ? tree_bits(tree_words_of(a, it, (it.block * a.M + r) / a.G), a.tree_words, j - (it.len - it.n)) : 0xffffffffu;
+          }
+      }
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -175,6 +186,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
           for (int e = 0; e < 4; ++e) {
             s[mt][t][e] *= x_scale;
             if (mask && (now_page < 0 || j + t * 8 + 2 * c + (e & 1) >= limit[mt][e >> 1])) s[mt][t][e] = -INFINITY;
+            if (kTree && mask && !(sees[mt][e >> 1] >> (t * 8 + 2 * c + (e & 1)) & 1u)) s[mt][t][e] = -INFINITY;
           }
         bool raise = false;
         float top[2];
@@ -248,7 +260,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
             // the row's probability sits in the quad's thread (key & 7) / 2
             const uint32_t both = __shfl_sync(0xffffffffu, key < 8 ? pr[mt][hh] : pr[mt][2 + hh], (lane & 28) | ((key & 7) >> 1));
             const float w = __uint_as_float((key & 1) ? both & 0xffff0000u : both << 16);
-            if (j + key < limit[mt][hh])
+            if (j + key < limit[mt][hh] && (!kTree || (sees[mt][hh] >> key & 1u)))
 #pragma unroll
               for (int i = 0; i < 16; ++i)
 #pragma unroll
@@ -345,10 +357,10 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
   }
 }
 
-template <int MT, int NW, bool kCluster>
+template <int MT, int NW, bool kCluster, bool kTree>
 cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, int grid, int n_cta, float x_scale, const void* q, const void* kp,
                    const void* vp, void* out, float* lse, cudaStream_t st) {
-  auto kernel = attend_mma_kernel<MT, NW, kCluster>;
+  auto kernel = attend_mma_kernel<MT, NW, kCluster, kTree>;
   static PerDevice ready;
   cudaError_t e = ready.once([&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<MT, NW>));
@@ -366,10 +378,9 @@ cudaError_t launch(const ckv_paged& pg, const WorkArgs& a, int grid, int n_cta, 
   return e;
 }
 
-}  // namespace
-
-cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
-                              const void* v_pages, void* out, float* lse, cudaStream_t st) {
+template <bool kTree>
+cudaError_t launch_few(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
+                       const void* v_pages, void* out, float* lse, cudaStream_t st) {
   WorkArgs a = base;
   const bool few = most * a.G <= 16;
   set_blocks(a, most, few ? 16 : 32, 0, kMmaTile, 2);
@@ -377,12 +388,20 @@ cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t
   if (const int n_cta = cluster_size(pg, few ? kShortFew : kShortMore, a.blocks)) {
     const int64_t items = (int64_t)a.Nu * a.Hkv * a.blocks, fit = 2 * kWorkers / n_cta;
     const int grid = (int)(items < fit ? items : fit) * n_cta;
-    return few ? launch<1, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
-                      : launch<2, kMmaWarps, true>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st);
+    return few ? launch<1, kMmaWarps, true, kTree>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st)
+                      : launch<2, kMmaWarps, true, kTree>(pg, a, grid, n_cta, x_scale, q, k_pages, v_pages, out, lse, st);
   }
-  const cudaError_t e = few ? launch<1, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
-                                   : launch<2, kMmaWarps, false>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st);
+  const cudaError_t e = few ? launch<1, kMmaWarps, false, kTree>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st)
+                                   : launch<2, kMmaWarps, false, kTree>(pg, a, kWorkers, 1, x_scale, q, k_pages, v_pages, out, lse, st);
   return e != cudaSuccess ? e : launch_join<true>(a, kWorkers, a.M, out, lse, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
+                              const void* v_pages, void* out, float* lse, cudaStream_t st) {
+  return base.tree ? launch_few<true>(pg, base, most, scale, q, k_pages, v_pages, out, lse, st)
+                   : launch_few<false>(pg, base, most, scale, q, k_pages, v_pages, out, lse, st);
 }
 
 }  // namespace ckv

@@ -75,7 +75,7 @@ struct Job {
   int n;                 // key tiles (0: there are no more items)
   int tiles2;            // whether it has two query tiles
   int steps;             // of each stream
-  int see;               // rows that every token of the block sees: those its first token does
+  int see;               // rows that every token of the block sees: those its first token does, or those before the tree
   int whole;             // not a part
   int odd;               // some value rows have been zeroed that tokens see
 };
@@ -129,7 +129,7 @@ __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter
         const Item& it = k.it;
         job.it = it, job.pair = k.pair, job.block = k.block;
         job.n = it.t1 - it.t0, job.tiles2 = both_tiles(a.w, it.n, it.block), job.steps = job.tiles2 ? 2 * job.n : job.n;
-        job.see = rows_seen(a.w, it.n, it.len, it.block * a.w.tokens + 1);
+        job.see = a.w.tree ? rows_before_tree(it) : rows_seen(a.w, it.n, it.len, it.block * a.w.tokens + 1);
         job.whole = it.t0 == 0 && it.t1 == it.tiles;
         job.odd = 0;
       }
@@ -151,7 +151,7 @@ __device__ __forceinline__ void job_done(Smem& sm, uint32_t i, int lane) {
 // First row of the item's j-th key tile that the block's first token does not see (128: it sees them all).  Where every
 // token sees every row there is none.
 __device__ __forceinline__ int late_row(const TcArgs& a, const Job& job, int j) {
-  return a.w.causal ? min(max(job.see - (job.it.t0 + j) * kTile, 0), kTile) : kTile;
+  return a.w.causal || a.w.tree ? min(max(job.see - (job.it.t0 + j) * kTile, 0), kTile) : kTile;
 }
 
 __device__ __forceinline__ void load_role(const TcArgs& a, Smem& sm, const CUtensorMap* qm, const CUtensorMap* km,
@@ -379,13 +379,12 @@ __device__ __forceinline__ void scale_output(uint32_t o_addr, float f) {
 }
 
 // O += 2^(x - m) v for one cache row, with the logit from the rows as they lie in memory; rows of the tile that do
-// not see it (limit) are left as they are.
-__device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o_addr, int key, int limit, int token, int head,
+// not see it are left as they are.
+__device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o_addr, int key, bool sees, int token, int head,
                                      float m) {
   const int page = a.w.table[((int64_t)it.u * a.w.Hkv + it.g) * a.w.max_pages + (key >> a.w.log_p)];
   if ((unsigned)page >= (unsigned)a.w.n_pages) return;
   const int64_t at = page * a.page_stride + (key & (a.w.P - 1)) * a.page_row;
-  const bool sees = key < limit;
   float x = 0.f;
   if (sees) {
     const __nv_bfloat16* q = a.q + (it.first + token) * a.q_tok + (it.g * a.w.G + head) * a.q_head;
@@ -403,6 +402,7 @@ __device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o
   tmem_wait_st();
 }
 
+template <bool kTree>
 __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int stream, int quarter,
                                              int lane) {
   uint32_t n_steps = 0, n_all = 0, n_join = 0;              // steps of this stream so far; tiles; joins of the streams
@@ -422,7 +422,8 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     const int token = tok0 + r_tok;
     const bool live = r < a.TQ * a.w.G && token < it.n;
     auto limit_of = [&](int tk) { return rows_seen(a.w, it.n, it.len, tk + 1); };
-    const int limit = live ? limit_of(token) : 0, least = limit_of(tok0);
+    const int limit = live ? limit_of(token) : 0, least = kTree ? job->see : limit_of(tok0);
+    const uint32_t* const words = kTree && live ? tree_words_of(a.w, it, token) : nullptr;   // what the row's token sees of the tree
     // rows of no token hold what shared memory held, or another unit's queries: above everything, they ask for no step again
     float m = live ? -INFINITY : INFINITY, l = 0.f;
     bool open = true;                                         // some row of the warp has no reference yet
@@ -432,6 +433,11 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       const int j = pair ? g >> 1 : g, h = pair ? g & 1 : stream;
       const int key0 = (t0 + j) * kTile + h * kStep;
       const uint32_t buf = n_steps & 1, s_buf = s_addr + buf * kStep;
+      uint32_t hidden[2] = {0u, 0u};                          // kTree: the step's keys that are no ancestors; read ahead of the logits
+      if (kTree && live && key0 + kStep > least) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) hidden[i] = ~tree_bits(words, a.w.tree_words, key0 + 32 * i - (it.len - it.n));
+      }
       if (!wait_warp(bar_s + buf * 8, (n_steps >> 1) & 1, w, 6)) return;
       tc_fence_after();
       uint32_t s[kStep];
@@ -440,7 +446,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       if (key0 + kStep > least || bad) {
 #pragma unroll
         for (int i = 0; i < kStep; ++i)
-          if (key0 + i >= limit || (bad >> ((h * kStep + i) >> a.w.log_p) & 1)) s[i] = 0xff800000u;
+          if (key0 + i >= limit || (bad >> ((h * kStep + i) >> a.w.log_p) & 1) || (kTree && (hidden[i >> 5] >> (i & 31) & 1u))) s[i] = 0xff800000u;
       }
       // Rows that have seen nothing yet take their reference here; what O holds for them is zero.
       if (open) {
@@ -485,7 +491,12 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     for (int j = n - 1; job->odd && j >= 0 && late_row(a, *job, j) < kTile; --j) {
       for (int x = pair ? 0 : 2 * stream; x < (pair ? 4 : 2 * stream + 2); ++x) {   // the stream's keys
         uint32_t odd = sm.odd[(n_all + j) % kInfo][x];
-        for (; odd; odd &= odd - 1) add_row(a, it, o_addr, (t0 + j) * kTile + x * 32 + __ffs(odd) - 1, limit, token, r_head, m);
+        const int key0 = (t0 + j) * kTile + x * 32;
+        const uint32_t see = kTree && live ? tree_bits(words, a.w.tree_words, key0 - (it.len - it.n)) : 0xffffffffu;
+        for (; odd; odd &= odd - 1) {
+          const int i = __ffs(odd) - 1;
+          add_row(a, it, o_addr, key0 + i, key0 + i < limit && (see >> i & 1u), token, r_head, m);
+        }
       }
     }
     n_all += n;
@@ -561,6 +572,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
   }
 }
 
+template <bool kTree>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ CUtensorMap qm,
                                                                 const __grid_constant__ CUtensorMap km,
                                                                 const __grid_constant__ CUtensorMap vm,
@@ -596,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   if (threadIdx.x == 0) a.w.split[blockIdx.x] = make_int4(-1, -1, -1, -1);
   __syncthreads();
   const Waiter w{&sm.abort_flag, a.w.status, a.wait_ns};
-  if (warp < 8) softmax_role(a, sm, tmem, w, warp >> 2, warp & 3, lane);
+  if (warp < 8) softmax_role<kTree>(a, sm, tmem, w, warp >> 2, warp & 3, lane);
   else if (warp < 10) mma_role(a, sm, tmem, w, warp - 8, lane);
   else if (warp == 10) load_role(a, sm, &qm, &km, &vm, w, lane);
   else job_role(a, sm, w, lane);
@@ -668,16 +680,17 @@ cudaError_t launch_attend_tc(const ckv_paged& pg, const WorkArgs& base, int64_t 
       !make_map(&km, k_pages, pg.page_size, pg.page_stride_row, pg.n_pages, pg.page_stride, true, rows, 1) ||
       !make_map(&vm, v_pages, pg.page_size, pg.page_stride_row, pg.n_pages, pg.page_stride, true, rows, 1))
     return cudaErrorInvalidValue;
-  static PerDevice ready;
-  cudaError_t e = ready.once([] {
-    return cudaFuncSetAttribute(attend_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+  auto kernel = base.tree ? attend_tc_kernel<true> : attend_tc_kernel<false>;
+  static PerDevice ready[2];
+  cudaError_t e = ready[base.tree != nullptr].once([&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(kWorkers), cfg.blockDim = dim3(kThreads), cfg.dynamicSmemBytes = sizeof(Smem), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, attend_tc_kernel, qm, km, vm, a);
+  e = cudaLaunchKernelEx(&cfg, kernel, qm, km, vm, a);
   count_launch();
   if (e != cudaSuccess) return e;
   return launch_join<true>(a.w, kWorkers, (int)(most * base.G < a.w.M ? most * base.G : a.w.M), out, lse, st);

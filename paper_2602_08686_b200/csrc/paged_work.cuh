@@ -24,6 +24,8 @@ struct WorkArgs {
   int one_warp;     // few pairs of few blocks each: one warp makes the schedule
   int P, log_p, n_pages, max_pages;
   const int32_t *starts, *lengths, *table;
+  const uint32_t* tree; // ckv_tree_attend: what each token sees of its unit's tokens, tree_words words a token (causal is 0 then); else null
+  int tree_words;
   int* status;
   int4* split;      // [workers]: (pair, block) in slot 0 (begun by an earlier worker) and slot 1 (not finished), or -1
   float2* ml;       // [workers][2][slot_rows]
@@ -400,6 +402,19 @@ __device__ __forceinline__ int64_t out_row(const WorkArgs& a, const Item& it, in
 // Rows of the cache that query row r of the block sees.
 __device__ __forceinline__ int row_limit(const WorkArgs& a, const Item& it, int r) {
   return rows_seen(a, it.n, it.len, (it.block * a.M + r) / a.G + 1);
+}
+// A tree's rows are the head's last ones, row len - n + t being the unit's token t's.  The rows before them are seen by every
+// token; how many there are among those with a page:
+__device__ __forceinline__ int rows_before_tree(const Item& it) { return min(max(it.len - it.n, 0), it.visible); }
+// What a token (its words) sees of 32 rows from row `at` of the tree on, as bits; rows before the tree (at < 0) are seen, those past
+// its words are not.
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t* words, int n_words, int at) {
+  const int w = at >> 5;             // rounded down
+  auto word = [&](int i) { return i < 0 ? 0xffffffffu : i < n_words ? words[i] : 0u; };
+  return (uint32_t)(((uint64_t)word(w + 1) << 32 | word(w)) >> (at & 31));
+}
+__device__ __forceinline__ const uint32_t* tree_words_of(const WorkArgs& a, const Item& it, int token) {
+  return a.tree + (int64_t)(it.first + token) * a.tree_words;
 }
 // Pool row (page * page_size + row within) is not formed: the pool's strides are free.  A bad page gives -1.
 __device__ __forceinline__ int page_of(const WorkArgs& a, const Item& it, int slot) {
