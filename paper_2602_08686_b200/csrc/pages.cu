@@ -7,6 +7,7 @@ namespace ckv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kKeepThreads = 1024;   // most of a CTA that moves the rows of a list
 
 struct Pool {           // rows of the two pools, in bytes
   char *k, *v;
@@ -30,16 +31,11 @@ struct KeepArgs {
   int* status;
 };
 
-template <bool kWarp>
-__device__ __forceinline__ bool all_of(bool x) {
-  if (kWarp) return __all_sync(0xffffffffu, x);
-  return __syncthreads_and(x);
-}
-
 // A group is a warp (short lists) or a CTA.  slices: of a row; log_s: log2 of the 16-byte pieces in a slice.
 template <bool kWarp>
-__global__ void __launch_bounds__(kThreads) keep_rows_kernel(KeepArgs a, int slices, int log_s) {
-  constexpr int NT = kWarp ? 32 : kThreads, U = 4;
+__global__ void __launch_bounds__(kWarp ? kThreads : kKeepThreads) keep_rows_kernel(KeepArgs a, int slices, int log_s) {
+  constexpr int U = kWarp ? 4 : 8;
+  const int NT = kWarp ? 32 : blockDim.x;
   __shared__ int s_first;
   pdl_wait();
   pdl_launch_dependents();
@@ -48,61 +44,66 @@ __global__ void __launch_bounds__(kThreads) keep_rows_kernel(KeepArgs a, int sli
   const int pair = group / (2 * slices), which = group - pair * 2 * slices;
   if (pair >= a.pairs) return;
   const int list = a.lists.of(pair), len = a.lengths[pair], count = a.counts[list], begin = a.begins[list];
-  const int span = a.tails ? a.tails[list] : len, base = len - span;
+  const int span = a.tails ? a.tails[list] : len, base = len - span, log_p = a.pool.log_p;
   const int32_t* const rows = a.rows + begin;
   const int32_t* const table = a.table + (int64_t)pair * a.pool.max_pages;
   if (!kWarp) {
     if (threadIdx.x == 0) s_first = 0x7fffffff;
     __syncthreads();
   }
-  const bool sane = len >= 0 && len <= a.pool.max_pages << a.pool.log_p && span >= 0 && span <= len && count >= 0 && count <= span &&
-                    begin >= 0 && count <= a.n_rows && begin <= a.n_rows - count;
-  bool ok = sane;
+  bool ok = len >= 0 && len <= a.pool.max_pages << log_p && span >= 0 && span <= len && count >= 0 && count <= span &&
+            begin >= 0 && count <= a.n_rows && begin <= a.n_rows - count;
+  const int n = ok ? count : 0;
   int first = 0x7fffffff;      // the first entry that moves
-  if (sane)
-    for (int i = t; i < count; i += NT) {
-      const int x = rows[i];
-      if (x <= (i ? rows[i - 1] : -1) || x >= span) ok = false;
-      if (x != i) first = min(first, i);
+#pragma unroll 4
+  for (int i = t; i < n; i += NT) {
+    const int x = rows[i];
+    if (x <= (i ? rows[i - 1] : -1) || x >= span) {
+      ok = false;
+    } else if (x != i) {       // from and to pages of the pool, and to none that others hold
+      first = min(first, i);
+      const int to = table[(base + i) >> log_p];
+      if ((unsigned)table[(base + x) >> log_p] >= (unsigned)a.pool.n_pages || (unsigned)to >= (unsigned)a.pool.n_pages) ok = false;
+      else if (a.refs && a.refs[to] > 1) ok = false;
     }
+  }
   if (kWarp) {
     first = __reduce_min_sync(0xffffffffu, first);
+    ok = __all_sync(0xffffffffu, ok);
   } else {
     if (first < 0x7fffffff) atomicMin(&s_first, first);
-  }
-  ok = all_of<kWarp>(ok);
-  if (!kWarp) first = s_first;
-  if (ok && first < count) {   // the pages of the rows that move; those written are the pair's alone
-    const int to = (base + count - 1) >> a.pool.log_p, end = (base + rows[count - 1]) >> a.pool.log_p;
-    bool fine = true;
-    for (int s = ((base + first) >> a.pool.log_p) + t; s <= end; s += NT) {
-      const int page = table[s];
-      if ((unsigned)page >= (unsigned)a.pool.n_pages) fine = false;
-      else if (a.refs && s <= to && a.refs[page] > 1) fine = false;
-    }
-    ok = all_of<kWarp>(fine);
+    ok = __syncthreads_and(ok);
+    first = s_first;
   }
   if (which == 0 && t == 0) {
     a.new_lengths[pair] = ok ? base + count : len;
     if (!ok) report_status(a.status, kStatusPage);
   }
-  if (!ok) return;
+  if (!ok || first >= count) return;
   const bool values = which >= slices;
   char* const data = (values ? a.pool.v : a.pool.k) + ((((values ? which - slices : which) << log_s) + (t & ((1 << log_s) - 1))) << 4);
   auto at = [&](int row) {
-    return reinterpret_cast<uint4*>(data + table[row >> a.pool.log_p] * a.pool.page + (row & (a.pool.P - 1)) * a.pool.row);
+    return reinterpret_cast<uint4*>(data + table[row >> log_p] * a.pool.page + (row & (a.pool.P - 1)) * a.pool.row);
   };
-  const int R = NT >> log_s, r = t >> log_s;
-  for (int i0 = first; i0 < count; i0 += U * R) {
+  const int R = NT >> log_s;
+  int src[U];                  // rows to read, looked up a batch ahead
+  auto look_up = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) src[u] = i0 + u * R < count ? base + rows[i0 + u * R] : -1;
+  };
+  int i0 = first + (t >> log_s);
+  look_up(i0);
+  for (int left = count - first; left > 0; left -= U * R, i0 += U * R) {
     uint4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (i0 + u * R + r < count) x[u] = *at(base + rows[i0 + u * R + r]);
+      if (src[u] >= 0) x[u] = __ldcg(at(src[u]));
+    if (left > U * R) look_up(i0 + U * R);
     if (kWarp) __syncwarp();
     else __syncthreads();
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (i0 + u * R + r < count) *at(base + i0 + u * R + r) = x[u];
+      if (i0 + u * R < count) __stcg(at(base + i0 + u * R), x[u]);
   }
 }
 
@@ -198,45 +199,60 @@ __global__ void __launch_bounds__(kThreads) reserve_count_kernel(ReserveArgs a) 
   if (lane == 31) a.block_need[block] = sum;
 }
 
-// Sums of ints over the CTA: `before` of those with index < at, `total` of all.
-struct Sums {
-  long long before, total;
-};
-__device__ __forceinline__ Sums add_up(const int32_t* x, int n, int at, long long* s_sum) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long b = 0, t = 0;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int v = x[i];
-    t += v;
-    if (i < at) b += v;
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) b += __shfl_xor_sync(0xffffffffu, b, d), t += __shfl_xor_sync(0xffffffffu, t, d);
-  if (lane == 0) s_sum[warp * 2] = b, s_sum[warp * 2 + 1] = t;
-  __syncthreads();
-  Sums s{0, 0};
-  for (int w = 0; w < kThreads / 32; ++w) s.before += s_sum[w * 2], s.total += s_sum[w * 2 + 1];
-  __syncthreads();
-  return s;
-}
-// Exclusive prefix sums of n ints (at most kMaxChunks; sums below 2^31) in shared memory.
-__device__ __forceinline__ void prefix(const int32_t* x, int n, int32_t* out, int* s_part) {
-  const int per = (n + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int mine = 0;
-  for (int i = lo; i < hi; ++i) mine += x[i];
-  int sum = mine;
+__device__ __forceinline__ int warp_scan(int x, int lane) {   // inclusive
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, sum, d);
-    if (lane >= d) sum += y;
+    const int y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
   }
-  if (lane == 31) s_part[warp] = sum;
+  return x;
+}
+// A thread's entries [lo, hi) of an array that the CTA adds up.
+struct Part {
+  int lo, hi;
+  __device__ __forceinline__ Part(int n) {
+    const int per = (n + kThreads - 1) / kThreads;
+    lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
+  }
+};
+// What is needed and what is there; `before`: the sum ahead of entry `at` (of the needs, or of the free pages).
+struct Sums {
+  long long need, free;
+  int before;
+  int mine;       // sum ahead of this thread's entries of the other array, the one that ranks are looked up in
+};
+__device__ __forceinline__ Sums add_up(const ReserveArgs& a, bool pages, int at, int (*s_sum)[4]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Part pb(a.n_blocks), pc(a.n_chunks);
+  // a block needs less than 2^26 pages, and where a sum passes 2^31 there are not enough
+  long long need = 0;
+  int free = 0, before = 0;
+  for (int i = pb.lo; i < pb.hi; ++i) {
+    const int x = a.block_need[i];
+    need += x;
+    if (!pages && i < at) before += x;
+  }
+  for (int i = pc.lo; i < pc.hi; ++i) {
+    const int x = a.chunk_free[i];
+    free += x;
+    if (pages && i < at) before += x;
+  }
+  const int own = pages ? (int)min(need, 1ll << 30) : free, scan = warp_scan(own, lane);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    need += __shfl_xor_sync(0xffffffffu, need, d), free += __shfl_xor_sync(0xffffffffu, free, d);
+    before += __shfl_xor_sync(0xffffffffu, before, d);
+  }
+  __shared__ long long s_need[kThreads / 32];
+  if (lane == 31) s_sum[warp][0] = free, s_sum[warp][1] = before, s_sum[warp][2] = scan, s_need[warp] = need;
   __syncthreads();
-  int before = sum - mine;
-  for (int w = 0; w < warp; ++w) before += s_part[w];
-  for (int i = lo; i < hi; ++i) out[i] = before, before += x[i];
-  __syncthreads();
+  Sums s{0, 0, 0, scan - own};
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    s.need += s_need[w], s.free += s_sum[w][0], s.before += s_sum[w][1];
+    if (w < warp) s.mine += s_sum[w][2];
+  }
+  return s;
 }
 // The last i with x[i] <= r (x ascending, x[0] <= r).
 __device__ __forceinline__ int last_at_most(const int32_t* x, int n, int r) {
@@ -248,170 +264,176 @@ __device__ __forceinline__ int last_at_most(const int32_t* x, int n, int r) {
   }
   return lo;
 }
+// The rank-th free page, by a warp; starts: free pages ahead of each chunk.
+__device__ __forceinline__ int page_of_rank(const ReserveArgs& a, const int32_t* starts, int rank, int lane) {
+  const int c = last_at_most(starts, a.n_chunks, rank);
+  const uint32_t* const words = a.free_bits + (int64_t)c * (a.chunk / 32);
+  int r = rank - starts[c];
+  for (int w0 = 0; w0 < a.chunk / 32; w0 += 32) {
+    uint32_t bits = words[w0 + lane];
+    const int mine = __popc(bits), sum = warp_scan(mine, lane);
+    const uint32_t past = __ballot_sync(0xffffffffu, sum > r);
+    if (past) {
+      const int from = __ffs(past) - 1;
+      for (int k = r - (sum - mine); lane == from && k > 0; --k) bits &= bits - 1u;
+      return (int)((int64_t)c * a.chunk + (w0 + from) * 32 + __shfl_sync(0xffffffffu, (int)__ffs(bits), from) - 1);
+    }
+    r -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  return 0;    // not reached: there are enough
+}
 
-// kWarp: a group per pair is a warp, else a CTA (few pairs).
+// kWarp: a CTA has the pairs of a block, and a warp copies a page; else it has one pair, and copies with all its threads.
 template <bool kWarp>
-__global__ void __launch_bounds__(kThreads) reserve_apply_kernel(ReserveArgs a, int row_bytes) {
+__global__ void __launch_bounds__(kThreads, kWarp ? 2 : 4) reserve_apply_kernel(ReserveArgs a, int log_row) {
   __shared__ int32_t s_prefix[kMaxChunks];
-  __shared__ long long s_sum[kThreads / 32 * 2];
-  __shared__ int s_part[kThreads / 32], s_count[kThreads / 32], s_page[2];
+  __shared__ int s_sum[kThreads / 32][4], s_page, s_held[kPairBlock];
+  __shared__ int2 s_need[kPairBlock];
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool pages = (int)blockIdx.x < a.n_chunks;
-  const Sums need = add_up(a.block_need, a.n_blocks, 0, s_sum), have = add_up(a.chunk_free, a.n_chunks, blockIdx.x, s_sum);
-  const bool enough = need.total <= have.total;
+  const int group = (int)blockIdx.x - a.n_chunks, block = kWarp ? group : group / kPairBlock;
+  const int64_t page0 = (int64_t)blockIdx.x * a.chunk;
+  // asked for ahead of the sums: a thread's four pages, or its pair
+  const int pair = kWarp ? block * kPairBlock + (int)threadIdx.x : group;
+  const bool live = !pages && (kWarp ? threadIdx.x < kPairBlock && pair < a.pairs : threadIdx.x == 0);
+  uint32_t word = pages ? a.free_bits[page0 / 32 + (threadIdx.x >> 3)] : 0u;
+  int2 need = make_int2(0, 0);
+  Want w{0, 0, 0};
+  int held = 0;
+  bool bad = false;
+  if (live) need = a.need[pair], w = want_of(a, pair, bad), held = a.held[pair];
+  const Sums sum = add_up(a, pages, pages ? (int)blockIdx.x : block, s_sum);
+  const bool enough = sum.need <= sum.free;
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.room) {
-    a.room[0] = (int)(enough ? have.total - need.total : have.total);
-    a.room[1] = (int)min(enough ? 0ll : need.total - have.total, 0x7fffffffll);
+    a.room[0] = (int)(enough ? sum.free - sum.need : sum.free);
+    a.room[1] = (int)min(enough ? 0ll : sum.need - sum.free, 0x7fffffffll);
   }
   if (!enough) return;
   if (pages) {
-    if (have.before >= need.total) return;
-    prefix(a.block_need, a.n_blocks, s_prefix, s_part);
-    int rank0 = (int)have.before;
-    const int64_t begin = (int64_t)blockIdx.x * a.chunk;
-    for (int w0 = 0; w0 < a.chunk / 32; w0 += kThreads / 32) {              // a word of 32 pages a warp
-      const uint32_t bits = a.free_bits[begin / 32 + w0 + warp];
-      if (lane == 0) s_count[warp] = __popc(bits);
+    if (sum.before >= sum.need) return;
+    const Part p(a.n_blocks);
+    for (int i = p.lo, x = sum.mine; i < p.hi; ++i) s_prefix[i] = x, x += a.block_need[i];
+    int rank0 = sum.before;
+    for (int w0 = 0; rank0 < sum.need && w0 < a.chunk / 32; w0 += kThreads / 8) {
+      if (w0) word = a.free_bits[page0 / 32 + w0 + (threadIdx.x >> 3)];
+      uint32_t bits = word >> (4 * (threadIdx.x & 7)) & 15u;
+      const int mine = __popc(bits), scan = warp_scan(mine, lane);
       __syncthreads();
-      int rank = rank0 + __popc(bits & ((1u << lane) - 1u));
-      for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) rank += s_count[w];
-        rank0 += s_count[w];
-      }
-      if ((bits >> lane & 1u) && rank < need.total) {
-        const int block = last_at_most(s_prefix, a.n_blocks, rank), r = rank - s_prefix[block];
-        int lo = block * kPairBlock, hi = min(lo + kPairBlock, a.pairs) - 1;   // the first pair of the block with more than r pages up to it
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (a.need[mid].x > r) hi = mid;
-          else lo = mid + 1;
-        }
-        const int2 n = a.need[lo];
-        const int before = lo > block * kPairBlock ? a.need[lo - 1].x : 0, mine = r - before;
-        if (mine >= n.y) {
-          bool bad = false;
-          const Want w = want_of(a, lo, bad);
-          const int page = (int)(begin + (w0 + warp) * 32 + lane);
-          a.table[(int64_t)lo * a.pool.max_pages + w.slots - (n.x - before) + mine] = page;
-          a.refs[page] = 1;
-        }
-      }
+      if (lane == 31) s_sum[warp][3] = scan;
       __syncthreads();
-      if (rank0 >= need.total) return;
+      int rank = rank0 + scan - mine;
+      for (int k = 0; k < kThreads / 32; ++k) {
+        if (k < warp) rank += s_sum[k][3];
+        rank0 += s_sum[k][3];
+      }
+      for (; bits && rank < sum.need; bits &= bits - 1u, ++rank) {
+        const int b = last_at_most(s_prefix, a.n_blocks, rank), r = rank - s_prefix[b], last = a.pairs - 1;
+        // the first pair of the block with more than r pages up to it
+        int to = b * kPairBlock, some = 0;
+#pragma unroll
+        for (int k = 7; k < 31; k += 8) some += a.need[min(to + k, last)].x <= r;
+        to += 8 * some, some = 0;
+#pragma unroll
+        for (int k = 0; k < 7; ++k) some += a.need[min(to + k, last)].x <= r;
+        to += some;
+        const int2 n = a.need[to];
+        const int before = to % kPairBlock ? a.need[to - 1].x : 0, which = r - before;
+        if (which < n.y) continue;                       // a copy
+        const Want x = want_of(a, to, bad);
+        const int page = (int)(page0 + (w0 + (threadIdx.x >> 3)) * 32 + 4 * (threadIdx.x & 7) + __ffs(bits) - 1);
+        a.table[(int64_t)to * a.pool.max_pages + x.slots - (n.x - before) + which] = page;
+        a.refs[page] = 1;
+      }
     }
     return;
   }
-  // pairs
-  constexpr int NT = kWarp ? 32 : kThreads;
-  const int group = (int)blockIdx.x - a.n_chunks, t = kWarp ? lane : threadIdx.x;
-  const int pair0 = kWarp ? group * (kThreads / 32) : group, n_pairs = kWarp ? min(kThreads / 32, a.pairs - pair0) : 1;
-  int any = 0;
-  for (int p = 0; p < n_pairs; ++p) any |= a.need[pair0 + p].y;
-  const int pair = kWarp ? pair0 + warp : pair0;
-  const bool live = pair < a.pairs;
-  bool bad = false;
-  const Want w = live ? want_of(a, pair, bad) : Want{0, 0, 0};
-  const int held = live ? a.held[pair] : 0;
-  int2 n = make_int2(0, 0);
-  int rank = 0;
-  if (any) {                                                                // pages by rank
-    if (live) {
-      const int block = pair / kPairBlock;
-      n = a.need[pair];
-      for (int b = t; b < block; b += NT) rank += a.block_need[b];
-      if (t == 0 && pair % kPairBlock) rank += a.need[pair - 1].x;
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, d);
-    if (!kWarp) {
-      if (lane == 0) s_count[warp] = rank;
-      __syncthreads();
-      rank = 0;
-      for (int k = 0; k < kThreads / 32; ++k) rank += s_count[k];
-    }
-    prefix(a.chunk_free, a.n_chunks, s_prefix, s_part);
+  if (live) {
+    if (w.slots > held) a.held[pair] = w.slots;
+    // copies: pages from this rank on
+    const int at = pair % kPairBlock;
+    s_need[kWarp ? at : 0] = make_int2(sum.before + (at ? a.need[pair - 1].x : 0), need.y);
+    s_held[kWarp ? at : 0] = min(held, w.slots);
+  } else if (kWarp && threadIdx.x < kPairBlock) {
+    s_need[threadIdx.x] = make_int2(0, 0);
   }
-  int32_t* const table = a.table + (int64_t)(live ? pair : 0) * a.pool.max_pages;
-  for (int s = w.first; n.y > 0 && s < min(held, w.slots); ++s) {
-    const int old = table[s];
-    if ((unsigned)old >= (unsigned)a.pool.n_pages || !(a.shared_bits[old >> 5] >> (old & 31) & 1u)) continue;
-    // the rank-th free page: its chunk, then a word a lane
-    if (kWarp || warp == 0) {
-      const int c = last_at_most(s_prefix, a.n_chunks, rank);
-      int r = rank - s_prefix[c], page = -1;
-      const uint32_t* words = a.free_bits + (int64_t)c * (a.chunk / 32);
-      for (int w0 = 0; page < 0 && w0 < a.chunk / 32; w0 += 32) {
-        const uint32_t bits = words[w0 + lane];
-        int sum = __popc(bits);
-        const int mine = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int x = __shfl_up_sync(0xffffffffu, sum, d);
-          if (lane >= d) sum += x;
+  if (!__syncthreads_or(need.y > 0)) return;
+  const Part p(a.n_chunks);
+  for (int i = p.lo, x = sum.mine; i < p.hi; ++i) s_prefix[i] = x, x += a.chunk_free[i];
+  __syncthreads();
+  constexpr int NT = kWarp ? 32 : kThreads, U = kWarp ? 8 : 4;
+  const int t = kWarp ? lane : threadIdx.x;
+  for (int i = kWarp ? warp : 0; i < (kWarp ? kPairBlock : 1); i += kThreads / 32) {
+    if (s_need[i].y == 0) continue;
+    const int its = kWarp ? block * kPairBlock + i : group, end = s_held[i];
+    int rank = s_need[i].x;
+    const Want x = want_of(a, its, bad);
+    int32_t* const table = a.table + (int64_t)its * a.pool.max_pages;
+    for (int s = x.first; s < end; ++s) {
+      const int old = table[s];
+      if ((unsigned)old >= (unsigned)a.pool.n_pages || !(a.shared_bits[old >> 5] >> (old & 31) & 1u)) continue;
+      int page = 0;
+      if (kWarp) {
+        page = page_of_rank(a, s_prefix, rank, lane);
+      } else {
+        if (warp == 0) {
+          page = page_of_rank(a, s_prefix, rank, lane);
+          if (lane == 0) s_page = page;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, sum > r);
-        const int all = __shfl_sync(0xffffffffu, sum, 31);
-        if (past) {
-          const int from = __ffs(past) - 1;
-          uint32_t b = bits;
-          for (int k = r - (sum - mine); lane == from && k > 0; --k) b &= b - 1u;
-          page = (int)((int64_t)c * a.chunk + (w0 + from) * 32 + __shfl_sync(0xffffffffu, (int)__ffs(b), from) - 1);
-        }
-        r -= all;
+        __syncthreads();
+        page = s_page;
       }
-      if (!kWarp && lane == 0) s_page[0] = page;
-      if (kWarp && lane == 0) s_count[warp] = page;
-    }
-    if (kWarp) __syncwarp();
-    else __syncthreads();
-    const int page = kWarp ? s_count[warp] : s_page[0];
-    if (s == w.first) {
-      const int pieces = row_bytes >> 4, log_r = pieces == 16 ? 4 : 5, items = w.rows << log_r;
-      for (int which = 0; which < 2; ++which) {
-        char* const pool = which ? a.pool.v : a.pool.k;
-        const char* const from = pool + old * a.pool.page;
-        char* const to = pool + page * a.pool.page;
-#pragma unroll 8
-        for (int e = t; e < items; e += NT) {
-          const int64_t off = (e >> log_r) * a.pool.row + ((e & (pieces - 1)) << 4);
-          *reinterpret_cast<uint4*>(to + off) = *reinterpret_cast<const uint4*>(from + off);
+      if (s == x.first) {
+        const int half = x.rows << log_row;              // 16-byte pieces of the keys; the values' follow
+        const int64_t from = old * a.pool.page, to = page * a.pool.page - from;
+        auto at = [&](int e) {
+          char* const pool = e < half ? a.pool.k : a.pool.v;
+          e -= e < half ? 0 : half;
+          return pool + from + (e >> log_row) * a.pool.row + ((e & ((1 << log_row) - 1)) << 4);
+        };
+        for (int e0 = t; e0 < 2 * half; e0 += NT * U) {
+          uint4 y[U];
+#pragma unroll
+          for (int k = 0; k < U; ++k)
+            if (e0 + k * NT < 2 * half) y[k] = __ldcg(reinterpret_cast<const uint4*>(at(e0 + k * NT)));
+#pragma unroll
+          for (int k = 0; k < U; ++k)
+            if (e0 + k * NT < 2 * half) __stcg(reinterpret_cast<uint4*>(at(e0 + k * NT) + to), y[k]);
         }
       }
+      if (kWarp) __syncwarp();
+      else __syncthreads();
+      if (t == 0) table[s] = page, a.refs[page] = 1, atomicSub(&a.refs[old], 1);
+      ++rank;
     }
-    if (kWarp) __syncwarp();
-    else __syncthreads();
-    if (t == 0) table[s] = page, a.refs[page] = 1, atomicSub(&a.refs[old], 1);
-    ++rank;
   }
-  if (live && t == 0 && w.slots > held) a.held[pair] = w.slots;
 }
 
 // ------------------------------------------------------------------------------------------------ pages given back
-// Eight lanes a pair, four pages each at a time.
-__global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pairs, const int32_t* __restrict__ lengths, int32_t* __restrict__ held,
+// 2^log_t threads a pair, four pages each at a time.
+__global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pairs, int log_t, const int32_t* __restrict__ lengths, int32_t* __restrict__ held,
                                                               const int32_t* __restrict__ table, int32_t* __restrict__ refs, int* __restrict__ status) {
   pdl_wait();
   pdl_launch_dependents();
-  const int pair = blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3), l8 = threadIdx.x & 7;
+  const int pair = (int)(blockIdx.x * (kThreads >> log_t) + (threadIdx.x >> log_t)), t = threadIdx.x & ((1 << log_t) - 1);
   const bool live = pair < pairs;
   const int len = live && lengths ? lengths[pair] : 0, have = live ? held[pair] : 0;
   bool bad = len < 0 || have < 0 || have > pool.max_pages;
   const int end = min(have, pool.max_pages), keep = len < 0 ? have : (int)(((int64_t)len + pool.P - 1) >> pool.log_p);
-  for (int s0 = keep + l8; s0 < end; s0 += 32) {
+  for (int s0 = keep + t; s0 < end; s0 += 4 << log_t) {
     int page[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) page[i] = s0 + 8 * i < end ? table[(int64_t)pair * pool.max_pages + s0 + 8 * i] : 0;
+    for (int i = 0; i < 4; ++i) page[i] = s0 + (i << log_t) < end ? table[(int64_t)pair * pool.max_pages + s0 + (i << log_t)] : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (s0 + 8 * i >= end) continue;
+      if (s0 + (i << log_t) >= end) continue;
       if ((unsigned)page[i] >= (unsigned)pool.n_pages) bad = true;
       else if (atomicSub(&refs[page[i]], 1) < 1) bad = true;
     }
   }
-  __syncwarp();     // all eight have read `held`
-  if (live && l8 == 0 && keep < have) held[pair] = keep;
+  __syncthreads();     // all of the pair's threads have read `held`
+  if (live && t == 0 && keep < have) held[pair] = keep;
   if (bad) report_status(status, kStatusPage);
 }
 
@@ -470,9 +492,9 @@ Pool pool_of(const ckv_paged& pg, void* k_pages, void* v_pages) {
   return p;
 }
 template <class... P, class... A>
-cudaError_t launch(void (*kernel)(P...), int64_t grid, cudaStream_t st, A... args) {
+cudaError_t launch(void (*kernel)(P...), int64_t grid, int threads, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid), cfg.blockDim = dim3(kThreads), cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)grid), cfg.blockDim = dim3(threads), cfg.stream = st;
   cudaLaunchAttribute attr = pdl_attribute();
   cfg.attrs = &attr, cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
@@ -482,18 +504,20 @@ cudaError_t launch(void (*kernel)(P...), int64_t grid, cudaStream_t st, A... arg
 
 }  // namespace
 
-// A warp moves lists of up to a few dozen rows, a CTA longer ones: what counts is how long they are on average (n_rows is the room
-// they have).  Slices: until there are groups enough to fill the SMs.
+// A warp moves lists of up to a few dozen rows, a CTA longer ones (n_rows / n_lists: the room a list has, whatever its length).
 cudaError_t launch_keep_rows(const ckv_paged& pg, Lists lists, int n_lists, const int32_t* rows, int n_rows, const int32_t* begins,
                              const int32_t* counts, const int32_t* tails, const int32_t* refs, const int32_t* lengths,
                              const int32_t* table, void* k_pages, void* v_pages, int32_t* new_lengths, int* status, cudaStream_t st) {
   KeepArgs a{pool_of(pg, k_pages, v_pages), lists, pg.n_units * pg.n_kv_heads, n_rows, rows, begins, counts, tails, refs, lengths, table,
              new_lengths, status};
-  const bool warp = n_rows / n_lists <= 32;
+  int64_t groups = (int64_t)a.pairs * 2;
   int slices = 1, log_s = pg.dtype == CKV_BF16 ? 4 : 5;
-  if (warp) return launch(keep_rows_kernel<true>, ((int64_t)a.pairs * 2 + kThreads / 32 - 1) / (kThreads / 32), st, a, slices, log_s);
-  while (log_s > 2 && (int64_t)a.pairs * 2 * slices < 148 * 8) slices *= 2, --log_s;
-  return launch(keep_rows_kernel<false>, (int64_t)a.pairs * 2 * slices, st, a, slices, log_s);
+  if (n_rows / n_lists <= 32) return launch(keep_rows_kernel<true>, (groups + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a, slices, log_s);
+  while (log_s > 2 && groups * slices <= 148 / 2) slices *= 2, --log_s;
+  groups *= slices;
+  int threads = kKeepThreads;
+  while (threads > 128 && (groups * threads > 148 * kKeepThreads || (threads * 4 >> log_s) > n_rows / n_lists)) threads /= 2;
+  return launch(keep_rows_kernel<false>, groups, threads, st, a, slices, log_s);
 }
 
 cudaError_t launch_pages_reserve(const ckv_paged& pg, Lists lists, const int32_t* new_rows, const int32_t* lengths, int32_t* held,
@@ -510,18 +534,20 @@ cudaError_t launch_pages_reserve(const ckv_paged& pg, Lists lists, const int32_t
   a.chunk_free = reinterpret_cast<int32_t*>(ws + w.chunk_free), a.block_need = reinterpret_cast<int32_t*>(ws + w.block_need);
   a.need = reinterpret_cast<int2*>(ws + w.need);
   constexpr int kWarps = kThreads / 32;
-  cudaError_t e = launch(reserve_count_kernel, w.n_chunks + (w.n_blocks + kWarps - 1) / kWarps, st, a);
+  cudaError_t e = launch(reserve_count_kernel, w.n_chunks + (w.n_blocks + kWarps - 1) / kWarps, kThreads, st, a);
   if (e != cudaSuccess) return e;
-  const int row_bytes = kHeadDim * (pg.dtype == CKV_BF16 ? 2 : 4);
-  return pairs <= 148 * 4 ? launch(reserve_apply_kernel<false>, w.n_chunks + pairs, st, a, row_bytes)
-                          : launch(reserve_apply_kernel<true>, w.n_chunks + (pairs + kWarps - 1) / kWarps, st, a, row_bytes);
+  const int log_row = pg.dtype == CKV_BF16 ? 4 : 5;
+  return pairs <= 148 * 4 ? launch(reserve_apply_kernel<false>, w.n_chunks + pairs, kThreads, st, a, log_row)
+                          : launch(reserve_apply_kernel<true>, w.n_chunks + w.n_blocks, kThreads, st, a, log_row);
 }
 
 cudaError_t launch_pages_trim(const ckv_paged& pg, const int32_t* lengths, int32_t* held, const int32_t* table, int32_t* refs,
                               int* status, cudaStream_t st) {
   const int pairs = pg.n_units * pg.n_kv_heads;
-  return launch(pages_trim_kernel, (pairs + kThreads / 8 - 1) / (kThreads / 8), st, pool_of(pg, nullptr, nullptr), pairs, lengths, held,
-                table, refs, status);
+  int log_t = 3;       // until the SMs are full, or a pair's threads have a page each
+  while (log_t < 8 && (int64_t)pairs << log_t < 148 * 1024 && (1 << log_t) < pg.max_pages) ++log_t;
+  const int per = kThreads >> log_t;
+  return launch(pages_trim_kernel, (pairs + per - 1) / per, kThreads, st, pool_of(pg, nullptr, nullptr), pairs, log_t, lengths, held, table, refs, status);
 }
 
 cudaError_t launch_pages_fork(const ckv_paged& pg, int layers, int new_seqs, const int32_t* parents, const int32_t* lengths,
@@ -530,7 +556,7 @@ cudaError_t launch_pages_fork(const ckv_paged& pg, int layers, int new_seqs, con
   ForkArgs a{pool_of(pg, nullptr, nullptr), pg.n_kv_heads, layers, pg.n_units / layers, new_seqs, keep_old, parents, lengths, held, table,
              refs, new_lengths, new_held, new_table, status};
   const int64_t warps = (int64_t)layers * (new_seqs + a.seqs) * a.Hkv;
-  return launch(pages_fork_kernel, (warps + kThreads / 32 - 1) / (kThreads / 32), st, a);
+  return launch(pages_fork_kernel, (warps + kThreads / 32 - 1) / (kThreads / 32), kThreads, st, a);
 }
 
 }  // namespace ckv

@@ -21,6 +21,11 @@ inline bool __syncthreads_and(bool x) {
   __syncthreads();
   return all;
 }
+template <class T>
+T __ldcg(const T* p) { return *p; }
+template <class T>
+void __stcg(T* p, T x) { *p = x; }
+inline bool __syncthreads_or(bool x) { return !__syncthreads_and(!x); }
 inline void atomicMin(int* p, int x) { *p = x < *p ? x : *p; }
 inline int atomicAdd(int* p, int x) { return (*p += x) - x; }
 inline int atomicSub(int* p, int x) { return (*p -= x) + x; }
@@ -254,15 +259,14 @@ int main(int n_args, char** v) {
         auto entry = [&](int i) { return rows[begins[l] + i]; };
         int first = 0;
         while (ok && first < counts[l] && entry(first) == first) ++first;
-        if (ok && first < counts[l])
-          for (int s = (base + first) / P; s <= (base + entry(counts[l] - 1)) / P; ++s) {
-            const int page = table[(size_t)p * width + s];
-            if (!fine(page)) ok = false;
-            else if (s <= (base + counts[l] - 1) / P && refs[page] > 1) {
-              if (with_refs) ok = false;
-              else unsure = true;       // a page of several heads moved by each of them: not allowed
-            }
+        for (int i = first; ok && i < counts[l]; ++i) {
+          const int from = table[(size_t)p * width + (base + entry(i)) / P], to = table[(size_t)p * width + (base + i) / P];
+          if (!fine(from) || !fine(to)) { ok = false; break; }
+          if (refs[to] > 1) {
+            if (with_refs) ok = false;
+            else unsure = true;         // a page of several heads moved by each of them: not allowed
           }
+        }
         if (!ok) { report = true, out.want[p] = lengths[p]; continue; }
         out.want[p] = base + counts[l];
         for (int i = first; i < counts[l]; ++i)
