@@ -74,15 +74,19 @@ class ckv_rotary(C.Structure):
 
 
 _lib = None
+_m = None       # csrc/marshal.cpp: argument checks of the paged calls
+_entry = {}     # addresses of the paged calls
 
 
 def lib() -> C.CDLL:
     """Loads libckv.so; raises if it has not been built (``python -m paper_2602_08686_b200.build``)."""
-    global _lib
+    global _lib, _m
     if _lib is None:
-        if not os.path.exists(LIB_PATH):
-            raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2602_08686_b200.build` "
-                               "(there is no CPU fallback)")
+        for path in (LIB_PATH, os.path.join(_HERE, "_marshal.so")):
+            if not os.path.exists(path):
+                raise RuntimeError(f"{path} is missing: build it with `python -m paper_2602_08686_b200.build` "
+                                   "(there is no CPU fallback)")
+        from . import _marshal as _m
         L = C.CDLL(LIB_PATH)
         vp, sz, i32p, fp = C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p
         shp, prm = C.POINTER(ckv_shape), C.POINTER(ckv_params)
@@ -136,6 +140,9 @@ def lib() -> C.CDLL:
                      "ckv_tree_masks", "ckv_tree_attend", "ckv_keep_rows", "ckv_pages_reserve", "ckv_pages_trim", "ckv_pages_fork",
                      "ckv_device_status", "ckv_version", "ckv_allocate_rows_host"):
             getattr(L, name).restype = C.c_int
+        _entry.update({name: C.cast(getattr(L, name), C.c_void_p).value for name in (
+            "ckv_rotate", "ckv_append", "ckv_gather_pages", "ckv_paged_attend", "ckv_tree_masks", "ckv_tree_attend", "ckv_keep_rows",
+            "ckv_pages_reserve", "ckv_pages_trim", "ckv_pages_fork")})
         _lib = L
     return _lib
 
@@ -424,6 +431,9 @@ def _layout(t: torch.Tensor | None):
 
 def _same(t: torch.Tensor, layout, name: str) -> int:
     """The tensor's address, once its layout is the struct's (strides of extents of one do not matter)."""
+    at = _m and _m.same(t, layout)
+    if at is not None:
+        return at
     if layout is None or t is None:
         raise ValueError(f"{name}: " + ("the struct was made without it" if layout is None else "missing"))
     shape, stride, dtype, device = layout
@@ -435,6 +445,9 @@ def _same(t: torch.Tensor, layout, name: str) -> int:
 
 
 def _dense(t: torch.Tensor, shape, dtype, device: int, name: str) -> int:
+    at = _m and _m.dense(t, shape, dtype, device)
+    if at is not None:
+        return at
     if shape is None or t is None:
         raise ValueError(f"{name}: " + ("the struct was made without pages" if shape is None else "missing"))
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
@@ -442,13 +455,15 @@ def _dense(t: torch.Tensor, shape, dtype, device: int, name: str) -> int:
     return t.data_ptr()
 
 
-def _paged_call(fn, what: str, device: int, stream, *args) -> None:
+def _paged_call(what: str, device: int, stream, *args) -> None:
+    """The C entry point `what` on the tensors' device; args are integers and addresses (None: null), without the stream."""
     if device < 0:
         raise ValueError("the paged calls take CUDA tensors")
+    lib()
     if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
-            return _paged_call(fn, what, device, stream, *args)
-    status = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+            return _paged_call(what, device, stream, *args)
+    status = _m.call(_entry[what], *args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
     if status != OK:
         raise CkvError(status, what)
 
@@ -469,7 +484,7 @@ def make_packed(q: torch.Tensor | None, k: torch.Tensor | None, n_units: int, ma
     if k is not None:
         pg.kv_stride_tok, pg.kv_stride_head = k.stride(0), k.stride(1)
     pg._q, pg._k, pg._pages, pg._device, pg._dtype = _layout(q), _layout(k), None, t.get_device(), t.dtype
-    pg._starts, pg._heads, pg._table, pg._ref = (pg.n_units + 1,), None, None, C.byref(pg)
+    pg._starts, pg._heads, pg._table = (pg.n_units + 1,), None, None
     return pg
 
 
@@ -496,7 +511,7 @@ def make_paged(k_pages: torch.Tensor, page_table: torch.Tensor, q: torch.Tensor 
     pg.n_pages, pg.page_size, pg.max_pages = k_pages.shape[0], k_pages.shape[1], max_pages
     pg.page_stride, pg.page_stride_row = k_pages.stride(0), k_pages.stride(1)
     pg._pages, pg._device, pg._dtype = _layout(k_pages), k_pages.get_device(), k_pages.dtype
-    pg._table, pg._heads, pg._starts, pg._ref = tuple(page_table.shape), (Nu, Hkv), (Nu + 1,), C.byref(pg)
+    pg._table, pg._heads, pg._starts = tuple(page_table.shape), (Nu, Hkv), (Nu + 1,)
     return pg
 
 
@@ -516,7 +531,7 @@ def make_rotary(inv_freq: torch.Tensor | None, interleaved: bool = False, q_norm
         raise ValueError("inv_freq and the norm weights must be on one device")
     ptr = [None if t is None else t.data_ptr() for t in (inv_freq, q_norm_w, k_norm_w)]
     r = ckv_rotary(*ptr, 0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), float(rot_scale), float(norm_eps))
-    r._keep, r._device, r._ref = kept, kept[0].get_device() if kept else None, C.byref(r)
+    r._keep, r._device = kept, kept[0].get_device() if kept else None
     return r
 
 
@@ -536,7 +551,7 @@ def _rotary_of(pg: ckv_paged, rotary: ckv_rotary | None):
         return None
     if rotary._device is not None and rotary._device != pg._device:
         raise ValueError(f"the rotary tables are on device {rotary._device}, the tokens on {pg._device}")
-    return rotary._ref
+    return C.addressof(rotary)
 
 
 def _tokens_out(pg, out, t, layout, name):
@@ -551,6 +566,9 @@ def _tokens_out(pg, out, t, layout, name):
 
 
 def _ws_of(pg, ws):
+    at = _m and ws is not None and _m.dense(ws, ws.shape, torch.uint8, pg._device)
+    if at:
+        return at
     if ws is None or ws.get_device() != pg._device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise ValueError("ws must be a dense uint8 tensor on the device of the pages")
     return ws.data_ptr()
@@ -560,7 +578,7 @@ def ckv_rotate(paged, rotary, q, k, positions, token_starts, q_out, k_out, strea
     """Norms and rotation of q [T, H, d] and k [T, Hkv, d] (either may be None) into q_out, k_out (dense, or in place)."""
     T = paged.n_tokens
     dev = paged._device
-    _paged_call(lib().ckv_rotate, "ckv_rotate", dev, stream, paged._ref, _rotary_of(paged, rotary),
+    _paged_call("ckv_rotate", dev, stream, C.addressof(paged), _rotary_of(paged, rotary),
                 None if q is None else _same(q, paged._q, "q"), None if k is None else _same(k, paged._k, "k"),
                 _dense(positions, (T,), torch.int32, dev, "positions"),
                 _dense(token_starts, paged._starts, torch.int32, dev, "token_starts"),
@@ -572,7 +590,7 @@ def ckv_append(paged, rotary, k, v, positions, token_starts, lengths, page_table
     """Appends the tokens' keys (normed, rotated; as they are when rotary is None) and values to the cache; q goes normed and
     rotated into q_out; new_lengths receives the heads' lengths with the tokens."""
     dev, i32 = paged._device, torch.int32
-    _paged_call(lib().ckv_append, "ckv_append", dev, stream, paged._ref, _rotary_of(paged, rotary),
+    _paged_call("ckv_append", dev, stream, C.addressof(paged), _rotary_of(paged, rotary),
                 None if q is None else _same(q, paged._q, "q"), _same(k, paged._k, "k"), _same(v, paged._k, "v"),
                 None if positions is None else _dense(positions, (paged.n_tokens,), i32, dev, "positions"),
                 _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(lengths, paged._heads, i32, dev, "lengths"),
@@ -595,7 +613,7 @@ def ckv_gather_pages(shape, params, paged, k, v, indices, budgets, offsets, page
             raise ValueError(f"{name} must be on device {dev}")
     Nu, Hkv = paged._heads
     rows = Hkv * min(params.budget_per_head, shape.seq_len)
-    _paged_call(lib().ckv_gather_pages, "ckv_gather_pages", dev, stream, C.byref(shape), C.byref(params), paged._ref,
+    _paged_call("ckv_gather_pages", dev, stream, C.addressof(shape), C.addressof(params), C.addressof(paged),
                 k.data_ptr(), v.data_ptr(), _dense(indices, (Nu, rows), i32, dev, "indices"),
                 _dense(budgets, paged._heads, i32, dev, "budgets"), _dense(offsets, (Nu, Hkv + 1), i32, dev, "offsets"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _same(k_pages, paged._pages, "k_pages"),
@@ -607,7 +625,7 @@ def ckv_paged_attend(paged, q, k_pages, v_pages, page_table, lengths, token_star
     """Attention of the packed tokens q [T, H, d] over the cache (lengths count the tokens' own rows when causal)."""
     dev, i32 = paged._device, torch.int32
     qs = paged._q
-    _paged_call(lib().ckv_paged_attend, "ckv_paged_attend", dev, stream, paged._ref, _same(q, qs, "q"),
+    _paged_call("ckv_paged_attend", dev, stream, C.addressof(paged), _same(q, qs, "q"),
                 _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _dense(lengths, paged._heads, i32, dev, "lengths"),
                 _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(out, qs[0], paged._dtype, dev, "out"),
@@ -622,7 +640,7 @@ def ckv_tree_masks(parents, token_starts, masks, ws, positions=None, first_posit
     dev, i32, (T, words), Nu = masks.get_device(), torch.int32, masks.shape, token_starts.numel() - 1
     if ws is None or ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise ValueError("ws must be a dense uint8 tensor on the device of the masks")
-    _paged_call(lib().ckv_tree_masks, "ckv_tree_masks", dev, stream, Nu, T, words, _dense(parents, (T,), i32, dev, "parents"),
+    _paged_call("ckv_tree_masks", dev, stream, Nu, T, words, _dense(parents, (T,), i32, dev, "parents"),
                 _dense(token_starts, (Nu + 1,), i32, dev, "token_starts"),
                 None if first_positions is None else _dense(first_positions, (Nu,), i32, dev, "first_positions"),
                 _dense(masks, (T, words), i32, dev, "masks"),
@@ -637,7 +655,7 @@ def ckv_tree_attend(paged, q, k_pages, v_pages, page_table, lengths, token_start
     if masks is None or masks.dim() != 2:
         raise ValueError("masks must be [T, words]")
     words = masks.shape[1]
-    _paged_call(lib().ckv_tree_attend, "ckv_tree_attend", dev, stream, paged._ref, _same(q, qs, "q"),
+    _paged_call("ckv_tree_attend", dev, stream, C.addressof(paged), _same(q, qs, "q"),
                 _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _dense(lengths, paged._heads, i32, dev, "lengths"),
                 _dense(token_starts, paged._starts, i32, dev, "token_starts"), _dense(masks, (paged.n_tokens, words), i32, dev, "masks"),
@@ -670,7 +688,7 @@ def ckv_keep_rows(paged, rows, begins, counts, lengths, page_table, k_pages, v_p
     place; begins, counts and tails are per (unit, KV head) or per sequence (Nu / layers).  new_lengths receives what is left."""
     dev, i32 = paged._device, torch.int32
     n_lists = -1 if begins is None else begins.numel()
-    _paged_call(lib().ckv_keep_rows, "ckv_keep_rows", dev, stream, paged._ref, int(layers), _list_of(rows, None, dev, "rows"),
+    _paged_call("ckv_keep_rows", dev, stream, C.addressof(paged), int(layers), _list_of(rows, None, dev, "rows"),
                 rows.numel(), _list_of(begins, n_lists, dev, "begins"), _list_of(counts, n_lists, dev, "counts"), n_lists,
                 None if tails is None else _list_of(tails, n_lists, dev, "tails"),
                 None if refs is None else _list_of(refs, paged.n_pages, dev, "refs"),
@@ -684,7 +702,7 @@ def ckv_pages_reserve(paged, new_rows, lengths, held, page_table, refs, k_pages,
     written are replaced by copies.  room [2] receives the free pages left and how many there were too few."""
     dev, i32 = paged._device, torch.int32
     new_ptr = _list_of(new_rows, None, dev, "new_rows")
-    _paged_call(lib().ckv_pages_reserve, "ckv_pages_reserve", dev, stream, paged._ref, int(layers), new_ptr, new_rows.numel(),
+    _paged_call("ckv_pages_reserve", dev, stream, C.addressof(paged), int(layers), new_ptr, new_rows.numel(),
                 _dense(lengths, paged._heads, i32, dev, "lengths"), _dense(held, paged._heads, i32, dev, "held"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _list_of(refs, paged.n_pages, dev, "refs"),
                 _same(k_pages, paged._pages, "k_pages"), _same(v_pages, paged._pages, "v_pages"),
@@ -694,7 +712,7 @@ def ckv_pages_reserve(paged, new_rows, lengths, held, page_table, refs, k_pages,
 def ckv_pages_trim(paged, lengths, held, page_table, refs, ws, stream=None):
     """Gives back the pages behind each head's lengths (None: all of them)."""
     dev, i32 = paged._device, torch.int32
-    _paged_call(lib().ckv_pages_trim, "ckv_pages_trim", dev, stream, paged._ref,
+    _paged_call("ckv_pages_trim", dev, stream, C.addressof(paged),
                 None if lengths is None else _dense(lengths, paged._heads, i32, dev, "lengths"),
                 _dense(held, paged._heads, i32, dev, "held"), _dense(page_table, paged._table, i32, dev, "page_table"),
                 _list_of(refs, paged.n_pages, dev, "refs"), _ws_of(paged, ws), ws.numel())
@@ -708,7 +726,7 @@ def ckv_pages_fork(paged, parents, lengths, held, page_table, refs, new_lengths,
     parents_ptr = _list_of(parents, None, dev, "parents")
     n_new, (Nu, Hkv) = parents.numel(), paged._heads or (0, 0)
     units = int(layers) * n_new
-    _paged_call(lib().ckv_pages_fork, "ckv_pages_fork", dev, stream, paged._ref, int(layers), n_new, parents_ptr,
+    _paged_call("ckv_pages_fork", dev, stream, C.addressof(paged), int(layers), n_new, parents_ptr,
                 _dense(lengths, paged._heads, i32, dev, "lengths"), _dense(held, paged._heads, i32, dev, "held"),
                 _dense(page_table, paged._table, i32, dev, "page_table"), _list_of(refs, paged.n_pages, dev, "refs"), int(bool(keep_old)),
                 _dense(new_lengths, (units, Hkv), i32, dev, "new_lengths"), _dense(new_held, (units, Hkv), i32, dev, "new_held"),
