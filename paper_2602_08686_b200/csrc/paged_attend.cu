@@ -369,7 +369,7 @@ PagedWs paged_ws(const ckv_paged& pg) {
   PagedWs w{};
   size_t o = 0;
   w.status = o, o += 256;
-  const size_t rows = wants_tc(pg) ? kTcRows : (pg.dtype == CKV_BF16 ? kMmaRows : kRowsM);
+  const size_t rows = wants_tc(pg) ? kTcRows : (pg.dtype == CKV_BF16 ? kMmaRows : kTileRows);
   w.split = o, o = up256(o + kWorkers * sizeof(int4));
   w.ml = o, o = up256(o + kWorkers * 2 * rows * sizeof(float2));
   w.o = o, o = up256(o + kWorkers * 2 * rows * kHeadDim * sizeof(float));
@@ -377,20 +377,25 @@ PagedWs paged_ws(const ckv_paged& pg) {
   return w;
 }
 
-// tree null: the tokens see what pg.causal says.
-static cudaError_t launch_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
-                                 const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
-                                 int tree_words, void* out, float* lse, char* ws, cudaStream_t st) {
+WorkArgs work_args(const ckv_paged& pg, const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
+                   int tree_words, char* ws) {
   const PagedWs w = paged_ws(pg);
-  const bool bf16 = pg.dtype == CKV_BF16, tc = wants_tc(pg);
-  const int64_t most = pg.max_new > 0 && pg.max_new < pg.n_tokens ? pg.max_new : pg.n_tokens;   // tokens of a unit
-  const float scale = pg.scale != 0.f ? pg.scale : 0.08838834764831845f;
   WorkArgs a{};
   a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = tree ? 0 : pg.causal;
   a.tree = tree, a.tree_words = tree_words;
   a.P = pg.page_size, a.log_p = log2_of(pg.page_size), a.n_pages = pg.n_pages, a.max_pages = pg.max_pages;
   a.starts = starts, a.lengths = lengths, a.table = table, a.status = reinterpret_cast<int*>(ws + w.status);
   a.split = reinterpret_cast<int4*>(ws + w.split), a.ml = reinterpret_cast<float2*>(ws + w.ml), a.o = reinterpret_cast<float*>(ws + w.o);
+  return a;
+}
+
+cudaError_t launch_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
+                          const int32_t* lengths, const int32_t* starts, const uint32_t* tree, int tree_words, void* out, float* lse,
+                          char* ws, cudaStream_t st) {
+  const bool bf16 = pg.dtype == CKV_BF16, tc = wants_tc(pg);
+  const int64_t most = most_tokens(pg);
+  const float scale = attend_scale(pg);
+  WorkArgs a = work_args(pg, table, lengths, starts, tree, tree_words, ws);
   if (tc) {
     a.slot_rows = kTcRows;
     return launch_attend_tc(pg, a, most, scale, q, k_pages, v_pages, out, lse, st);
@@ -423,11 +428,6 @@ cudaError_t launch_paged_attend(const ckv_paged& pg, const void* q, const void* 
                                 const int32_t* table, const int32_t* lengths, const int32_t* starts, void* out, float* lse,
                                 char* ws, cudaStream_t st) {
   return launch_attend(pg, q, k_pages, v_pages, table, lengths, starts, nullptr, 0, out, lse, ws, st);
-}
-cudaError_t launch_tree_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages,
-                               const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
-                               int tree_words, void* out, float* lse, char* ws, cudaStream_t st) {
-  return launch_attend(pg, q, k_pages, v_pages, table, lengths, starts, tree, tree_words, out, lse, ws, st);
 }
 
 }  // namespace ckv

@@ -148,6 +148,16 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
     }
     __syncthreads();
     for (int j = begin; j < end; j += stride) {
+      uint32_t sees[MT][2];                    // kTree: which of the group's keys the thread's rows see; asked for ahead of the products
+      if (kTree && j + kGroup > least) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const int r = mt * 16 + hh * 8 + p;
+            sees[mt][hh] = r < rows ? tree_bits(tree_words_of(a, it, (it.block * a.M + r) / a.G), a.tree_words, j - (it.len - it.n)) : 0xffffffffu;
+          }
+      }
       float s[MT][2][4];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
@@ -168,16 +178,6 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
       load_k(j + stride, page);
       uint32_t pr[MT][4];
       const bool mask = j + kGroup > least || now_page < 0;
-      uint32_t sees[MT][2];                    // kTree: which of the group's keys the thread's rows see
-      if (kTree && mask) {
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const int r = mt * 16 + hh * 8 + p;
-            sees[mt][hh] = r < rows ? tree_bits(tree_words_of(a, it, (it.block * a.M + r) / a.G), a.tree_words, j - (it.len - it.n)) : 0xffffffffu;
-          }
-      }
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_mma_kernel(WorkArgs a, ckv_
           for (int e = 0; e < 4; ++e) {
             s[mt][t][e] *= x_scale;
             if (mask && (now_page < 0 || j + t * 8 + 2 * c + (e & 1) >= limit[mt][e >> 1])) s[mt][t][e] = -INFINITY;
-            if (kTree && mask && !(sees[mt][e >> 1] >> (t * 8 + 2 * c + (e & 1)) & 1u)) s[mt][t][e] = -INFINITY;
+            if (kTree && j + kGroup > least && !(sees[mt][e >> 1] >> (t * 8 + 2 * c + (e & 1)) & 1u)) s[mt][t][e] = -INFINITY;
           }
         bool raise = false;
         float top[2];
@@ -382,7 +382,12 @@ template <bool kTree>
 cudaError_t launch_few(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                        const void* v_pages, void* out, float* lse, cudaStream_t st) {
   WorkArgs a = base;
-  const bool few = most * a.G <= 16;
+  bool few = most * a.G <= 16;
+  if (kTree && !few) {
+    set_blocks(a, most, 16, 0, kMmaTile, 2);
+    const int n_cta = cluster_size(pg, kShortFew, a.blocks);
+    few = n_cta > 0 && (int64_t)a.Nu * a.Hkv * a.blocks * n_cta <= kWorkers;
+  }
   set_blocks(a, most, few ? 16 : 32, 0, kMmaTile, 2);
   const float x_scale = scale * kLog2e;
   if (const int n_cta = cluster_size(pg, few ? kShortFew : kShortMore, a.blocks)) {

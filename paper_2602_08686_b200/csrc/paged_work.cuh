@@ -444,6 +444,16 @@ constexpr ShortRule kShortFew{kMmaCtaKeys, 100, 800}, kShortMore{kMmaCtaKeys, 50
 int cluster_size(const ckv_paged& pg, const ShortRule& rule, int64_t blocks);
 cudaError_t launch_attend_mma(const ckv_paged& pg, const WorkArgs& base, int64_t most, float scale, const void* q, const void* k_pages,
                               const void* v_pages, void* out, float* lse, cudaStream_t st);
+constexpr int kTileRows = 64;        // most query rows of a block of the fp32 kernel for drafted trees
+inline int64_t most_tokens(const ckv_paged& pg) { return pg.max_new > 0 && pg.max_new < pg.n_tokens ? pg.max_new : pg.n_tokens; }   // of a unit
+inline float attend_scale(const ckv_paged& pg) { return pg.scale != 0.f ? pg.scale : 0.08838834764831845f; }
+// Everything but the block and tile sizes and slot_rows.
+WorkArgs work_args(const ckv_paged& pg, const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
+                   int tree_words, char* ws);
+// tree null: the tokens see what pg.causal says.
+cudaError_t launch_attend(const ckv_paged& pg, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
+                          const int32_t* lengths, const int32_t* starts, const uint32_t* tree, int tree_words, void* out, float* lse,
+                          char* ws, cudaStream_t st);
 // rows: the most query rows a block has.
 template <bool BF16>
 cudaError_t launch_join(const WorkArgs& a, int workers, int rows, void* out, float* lse, cudaStream_t st);

@@ -6,6 +6,7 @@ exponential of it by a factor 1 + dx + 2^-22, sums of non-negative terms over `d
 r = dx + 2^-20 + depth * 2^-24 the lse is off by at most r + 2^-23 |lse|, the output by 2 r max|v| + 2^-24 |out|; in bf16 each
 probability is rounded for its product (2^-8 max|v| at the worst) and the output once more (2^-8 |out|).
 """
+import copy
 import math
 import random
 
@@ -125,6 +126,21 @@ def r_of(q, k, length, scale=1 / math.sqrt(D)):
     return 132 * EPS * norm(q) * norm(k) * scale + 2.0 ** -20 + (length / 8 + 256) * EPS
 
 
+def widened(c, H):
+    """The same cache under a table so wide that fp32 calls of more than 16 query rows a head go to the tensor cores."""
+    Nu, Hkv, width = c.table.shape
+    wide = torch.full((Nu, Hkv, max(width, 80000 // (c.P * Nu * Hkv) + 1)), 0x7ffffff0, dtype=torch.int32, device="cuda")
+    wide[:, :, :width] = c.table
+    other = copy.copy(c)
+    other.table = wide
+    return other
+
+
+def caches(c, H, counts):
+    """c, and widened where that picks another kernel."""
+    return [c, widened(c, H)] if c.k_pages.dtype == torch.float32 and max(counts) * H // c.table.shape[1] > 16 else [c]
+
+
 def check_attend(c, q, starts, sees, out, lse, scale=None):
     want, want_lse = TR.attend(q, starts, c.rows, sees, scale)
     live = torch.zeros(q.shape[0], dtype=torch.bool, device="cuda")
@@ -210,14 +226,16 @@ def test_attend(B, dtype, kind, H, Hkv, page, counts, lens):
     for u, s in enumerate(padded):
         bits = (s.reshape(-1, words, 32).astype(np.uint64) << np.arange(32, dtype=np.uint64)).sum(-1).astype(np.uint32)
         masks[st[u]:st[u + 1]] = torch.from_numpy(bits.view(np.int32))
-    for max_new in (0, max(counts)):
-        out, lse = run_attend(B, c, q, st, masks.cuda(), max_new=max_new)
-        check_attend(c, q, st, sees, out, lse)
+    for cache in caches(c, H, counts):
+        for max_new in (0, max(counts)):
+            out, lse = run_attend(B, cache, q, st, masks.cuda(), max_new=max_new)
+            check_attend(c, q, st, sees, out, lse)
 
 
 @pytest.mark.parametrize("dtype,Nu,Hkv,H,n,rows", [
     (torch.bfloat16, 3, 2, 8, 4, 9000), (torch.bfloat16, 2, 2, 8, 63, 9000), (torch.bfloat16, 40, 4, 16, 20, 700),
-    (torch.bfloat16, 1, 1, 7, 300, 20000), (torch.float32, 2, 2, 8, 5, 9000), (torch.float32, 40, 4, 8, 3, 300)])
+    (torch.bfloat16, 1, 1, 7, 300, 20000), (torch.float32, 2, 2, 8, 5, 9000), (torch.float32, 40, 4, 8, 3, 300), (torch.float32, 1, 2, 14, 70, 5000),
+    (torch.float32, 30, 2, 8, 33, 400), (torch.float32, 1, 1, 8, 32, 16000)])
 def test_attend_long_and_many(B, dtype, Nu, Hkv, H, n, rows):
     """Caches whose work is split over the SMs, and more heads than there are SMs."""
     rng = random.Random(n)
@@ -250,7 +268,7 @@ def test_a_chain_is_a_causal_chunk(B, dtype, n):
 
 
 @pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
-@pytest.mark.parametrize("dtype,n", [(torch.bfloat16, 3), (torch.bfloat16, 8), (torch.bfloat16, 70), (torch.bfloat16, 200), (torch.float32, 9)])
+@pytest.mark.parametrize("dtype,n", [(torch.bfloat16, 3), (torch.bfloat16, 8), (torch.bfloat16, 70), (torch.bfloat16, 200), (torch.float32, 9), (torch.float32, 40)])
 def test_values_that_are_not_finite(B, dtype, n, bad):
     """A value element of a drafted token's row that is not finite reaches the tokens that see the row, in that element, and no
     others; the row's key, where it is not finite either, the tokens that see it and no others."""
@@ -270,8 +288,8 @@ def test_values_that_are_not_finite(B, dtype, n, bad):
             c.v_pages[int(c.table[0, g, j // 32]), j % 32, 5 * g + 3] = bad
         c.rows[0][g] = (k, v)
     touched = torch.from_numpy(sees[0][:, hit].any(1)).cuda()
-    for max_new in (0, n):
-        out, lse = run_attend(B, c, q, [0, n], masks, max_new=max_new)
+    for max_new, cache in [(m, x) for m in (0, n) for x in caches(c, H, [n])]:
+        out, lse = run_attend(B, cache, q, [0, n], masks, max_new=max_new)
         for g in range(Hkv):
             mine = out[:, 4 * g:4 * g + 4]
             assert not torch.isfinite(mine[touched][:, :, 5 * g + 3]).any()
@@ -294,13 +312,45 @@ def test_values_that_are_not_finite(B, dtype, n, bad):
         for x in hit:
             j = c.lens[0][g] - n + x
             c.v_pages[int(c.table[0, g, j // 32]), j % 32] = clean[g][1][j].cuda()
-    out, lse = run_attend(B, c, q, [0, n], masks, max_new=n)
-    ill = torch.from_numpy(sees[0][:, t]).cuda()
-    assert torch.isnan(lse[ill]).all() and torch.isnan(out[ill]).all()
-    assert torch.isfinite(lse[~ill]).all() and torch.isfinite(out[~ill]).all()
+    for cache in caches(c, H, [n]):
+        out, lse = run_attend(B, cache, q, [0, n], masks, max_new=n)
+        ill = torch.from_numpy(sees[0][:, t]).cuda()
+        assert torch.isnan(lse[ill]).all() and torch.isnan(out[ill]).all()
+        assert torch.isfinite(lse[~ill]).all() and torch.isfinite(out[~ill]).all()
 
 
-@pytest.mark.parametrize("dtype,n,pages", [(torch.float32, 6, 3), (torch.bfloat16, 6, 3), (torch.bfloat16, 40, 4), (torch.bfloat16, 40, 2)])
+@pytest.mark.parametrize("dtype,n", [(torch.float32, 3), (torch.float32, 20), (torch.bfloat16, 3), (torch.bfloat16, 20), (torch.bfloat16, 70)])
+def test_infinite_keys_and_values_of_the_prefix(B, dtype, n):
+    """Rows that every token sees.  A key with an infinity gives the logit its product with the query has: minus infinity is a row of no
+    weight, plus infinity makes the token NaN.  A value with an infinity makes that element infinite."""
+    H, Hkv, base = 8, 2, 150
+    c = R.Cache([[n + base, n + base + 60]], 32, dtype=dtype, device="cuda", seed=n)
+    q = torch.randn(n, H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).to(dtype)
+    q[:, :, 5] = q[:, :, 5].abs() + 0.5
+    q[-1, :, 5] *= -1                                                       # one token that meets the infinity with the other sign
+    sees = some_sees([n], "tree", random.Random(n))
+    masks = TR.pack(sees, 3, n, [0, n]).cuda()
+    place = lambda j, g: (int(c.table[0, g, j // 32]), j % 32)
+    for g in range(Hkv):
+        k, v = (x.clone() for x in c.rows[0][g])
+        k[17, 5], v[33, 9] = -math.inf, math.inf
+        c.k_pages[place(17, g)][5], c.v_pages[place(33, g)][9] = -math.inf, math.inf
+        c.rows[0][g] = (k, v)
+    for cache in caches(c, H, [n]):
+        out, lse = run_attend(B, cache, q, [0, n], masks, max_new=n)
+        assert torch.isnan(lse[-1]).all() and torch.isnan(out[-1]).all()
+        assert torch.isfinite(lse[:-1]).all() and not torch.isfinite(out[:-1, :, 9]).any()
+        rest = [d for d in range(D) if d != 9]
+        clean = [[(torch.cat((k[:17], k[18:])), torch.cat((v[:17], v[18:])).nan_to_num(0, 0, 0)) for k, v in c.rows[0]]]
+        want, want_lse = TR.attend(q, [0, n], clean, sees)
+        vmax = max(float(v.double().abs().max()) for _, v in clean[0])
+        r = r_of(q, torch.cat([k for k, _ in clean[0]]), n + 300)
+        tol = (2.0 ** -8 * (vmax + want.abs()) if dtype == torch.bfloat16 else EPS * want.abs()) + 2 * r * vmax
+        assert ((out.double() - want).abs() <= tol)[:-1][:, :, rest].all()
+        assert ((lse.double() - want_lse).abs() <= r + 2 * EPS * want_lse.abs())[:-1].all()
+
+
+@pytest.mark.parametrize("dtype,n,pages", [(torch.float32, 6, 3), (torch.float32, 40, 700), (torch.bfloat16, 6, 3), (torch.bfloat16, 40, 4), (torch.bfloat16, 40, 2)])
 def test_rows_past_the_table_and_bad_pages(B, dtype, n, pages):
     """Rows the table has no page for, and rows of a page outside the pool, are left out (drafted ones among them), and said."""
     P, H = 16, 4
@@ -345,8 +395,9 @@ def test_words_that_do_not_reach_all_tokens(B):
         q = torch.randn(n, 4, D, device="cuda").to(dtype)
         sees = [np.ones((n, n), dtype=bool)]
         sees[0][:, 32:] = False
-        out, lse = run_attend(B, c, q, [0, n], torch.full((n, 1), -1, dtype=torch.int32, device="cuda"), max_new=n)
-        check_attend(c, q, [0, n], sees, out, lse)
+        for cache in caches(c, 4, [n]):
+            out, lse = run_attend(B, cache, q, [0, n], torch.full((n, 1), -1, dtype=torch.int32, device="cuda"), max_new=n)
+            check_attend(c, q, [0, n], sees, out, lse)
 
 
 @pytest.mark.parametrize("scale", [0.5, -0.09, 2.0 ** -20])
@@ -355,8 +406,44 @@ def test_scales(B, scale):
         c = R.Cache([[n + 700, n + 10]], 64, dtype=dtype, device="cuda", seed=n)
         q = torch.randn(n, 8, D, device="cuda").to(dtype)
         sees = some_sees([n], "tree", random.Random(n))
-        out, lse = run_attend(B, c, q, [0, n], TR.pack(sees, 3, n, [0, n]).cuda(), scale=scale, max_new=n)
-        check_attend(c, q, [0, n], sees, out, lse, scale=scale)
+        for cache in caches(c, 8, [n]):
+            out, lse = run_attend(B, cache, q, [0, n], TR.pack(sees, 3, n, [0, n]).cuda(), scale=scale, max_new=n)
+            check_attend(c, q, [0, n], sees, out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("size", [1.0, 30.0, 1000.0])
+@pytest.mark.parametrize("dtype,n", [(torch.float32, 3), (torch.float32, 24), (torch.bfloat16, 70)])
+def test_large_logits(B, dtype, n, size):
+    """Logits that rise along the cache, to thousands: the running maximum moves at every tile."""
+    L = n + 900
+    c = R.Cache([[L, L - 33]], 32, dtype=dtype, device="cuda", seed=n)
+    q = torch.randn(n, 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).to(dtype)
+    for g in range(2):
+        k, v = c.rows[0][g]
+        rise = torch.linspace(0, size / 10, k.shape[0])[:, None] * q[0, 4 * g].float().cpu() / D ** 0.5
+        k = (k.float() * min(size, 3.0) + rise).to(dtype)
+        c.rows[0][g] = (k, v)
+        for j in range(0, k.shape[0], 32):
+            c.k_pages[int(c.table[0, g, j // 32]), :min(32, k.shape[0] - j)] = k[j:j + 32].cuda()
+    sees = some_sees([n], "tree", random.Random(n))
+    for cache in caches(c, 8, [n]):
+        out, lse = run_attend(B, cache, q, [0, n], TR.pack(sees, 3, n, [0, n]).cuda(), max_new=n)
+        check_attend(c, q, [0, n], sees, out, lse)
+
+
+def test_fp32_is_as_exact_as_multiplications_in_fp32(B):
+    """The three-product form against the plain kernel's: 2-norms of the errors against 64 bits."""
+    n, H = 24, 8
+    c = R.Cache([[n + 4000, n + 3500]], 64, dtype=torch.float32, device="cuda", seed=1)
+    q = torch.randn(n, H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    sees = some_sees([n], "tree", random.Random(n))
+    masks = TR.pack(sees, 1, n, [0, n]).cuda()
+    want, want_lse = TR.attend(q, [0, n], c.rows, sees)
+    out, lse = run_attend(B, widened(c, H), q, [0, n], masks, max_new=n)
+    # roundings of a product's two halves (2^-22 each) and of the unit's sums (a unit in the last place each, few in a row): a few 2^-23,
+    # and not the 2^-12 of a product of two tf32 numbers
+    assert (out.double() - want).norm() <= 8 * 2.0 ** -23 * want.norm()
+    assert (lse.double() - want_lse).norm() <= 4 * 2.0 ** -23 * want_lse.norm()
 
 
 def test_same_bits_again_on_two_streams_and_in_a_graph(B):
