@@ -444,7 +444,7 @@ ckv_status ckv_tree_attend(const ckv_paged* paged, const void* q, const void* k_
  * n_lists is Nu * Hkv (a list per head: what a retention pass over the cache chose) or Nu / layers (a list per sequence, shared by its
  * layers and heads: the accepted tokens of a drafted tree, tails = its tokens).  rows [n_rows] int32; begins, counts, tails [n_lists].
  * refs_or_null [n_pages]: how many heads hold each page; rows are not moved into a page that several hold (ckv_pages_reserve makes it the
- * head's own).  A head with such a page, a list that does not ascend or leaves its span or `rows`, or a page number outside the
+ * head's own; without refs it is for the caller to know that no page that is written is shared).  A head with such a page, a list that does not ascend or leaves its span or `rows`, or a page number outside the
  * pool is left as it is, new_lengths = lengths, and reported (CKV_ERR_PAGE).  Units come layer by layer here and below: unit = layer
  * * sequences + sequence.  Of `paged` the page fields, units, heads and dtype are read.  ws: 256 bytes.
  */

@@ -412,8 +412,8 @@ __global__ void __launch_bounds__(kThreads, kWarp ? 2 : 4) reserve_apply_kernel(
 
 // ------------------------------------------------------------------------------------------------ pages given back
 // 2^log_t threads a pair, four pages each at a time.
-__global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pairs, int log_t, const int32_t* __restrict__ lengths, int32_t* __restrict__ held,
-                                                              const int32_t* __restrict__ table, int32_t* __restrict__ refs, int* __restrict__ status) {
+__global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pairs, int log_t, const int32_t* lengths, int32_t* held, const int32_t* table,
+                                                              int32_t* refs, int* status) {
   pdl_wait();
   pdl_launch_dependents();
   const int pair = (int)(blockIdx.x * (kThreads >> log_t) + (threadIdx.x >> log_t)), t = threadIdx.x & ((1 << log_t) - 1);
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pai
     for (int i = 0; i < 4; ++i) {
       if (s0 + (i << log_t) >= end) continue;
       if ((unsigned)page[i] >= (unsigned)pool.n_pages) bad = true;
-      else if (atomicSub(&refs[page[i]], 1) < 1) bad = true;
+      else if (atomicSub(&refs[page[i]], 1) < 1) atomicAdd(&refs[page[i]], 1), bad = true;   // nobody held it
     }
   }
   __syncthreads();     // all of the pair's threads have read `held`
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(ForkArgs a) {
     for (int s = lane; more && s < held; s += 32) {
       const int page = a.table[(int64_t)pair * a.pool.max_pages + s];
       if ((unsigned)page >= (unsigned)a.pool.n_pages) bad = true;
-      else if (atomicAdd(&a.refs[page], more) < 1) bad = true;    // a page that is held has been counted
+      else if (atomicAdd(&a.refs[page], more) < 1) atomicSub(&a.refs[page], more), bad = true;    // a page that is held has been counted
     }
   }
   if (bad) report_status(a.status, kStatusPage);

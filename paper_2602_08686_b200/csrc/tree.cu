@@ -16,8 +16,8 @@ constexpr int kThreads = 512;
 // memory a token has `quads` times four words.
 __global__ void __launch_bounds__(kThreads) tree_masks_kernel(int T, int words, int quads, int log_w, int most,
                                                               const int32_t* __restrict__ parents, const int32_t* __restrict__ starts,
-                                                              const int32_t* __restrict__ first_positions, uint32_t* __restrict__ masks,
-                                                              int32_t* __restrict__ positions, int* __restrict__ status) {
+                                                              const int32_t* first_positions, uint32_t* __restrict__ masks, int32_t* positions,
+                                                              int* status) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   uint4* const mask = reinterpret_cast<uint4*>(smem_raw);                // [most][quads]
   int2* const link = reinterpret_cast<int2*>(mask + most * quads);       // [2][most]: (next ancestor or -1, depth so far)

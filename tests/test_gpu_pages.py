@@ -207,6 +207,9 @@ def test_reserve_says_what_is_wrong(B):
         c.refs[c.table[u, 0, 0].long()] = 0
         B.ckv_pages_trim(c.pg, None, c.held, c.table, c.refs, c.ws)
         c.fine(B, B.ERR_PAGE)
+        c.ref.refs[c.ref.table[u, 0, 0]] = 1
+        c.ref.trim()
+        c.same()                                                            # counts of others, and none below zero
 
 
 @pytest.mark.parametrize("keep_old", [False, True])
