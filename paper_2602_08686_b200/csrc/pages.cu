@@ -22,6 +22,11 @@ struct Pool {           // rows of the two pools, in bytes
 // may be cut into slices of their 16-byte pieces, a group each, where there are few pairs.
 // Entries that stay where they are (list[i] == i, a prefix of the list) are not touched.
 // Every group of a pair looks its list and pages over first and comes to the same answer: a pair is moved whole or left alone.
+// Bound: long lists HBM, as far as one CTA of an SM can keep it busy between two meetings; short ones five dependent reads.  64 heads'
+// lists of 2048 to 4096 of 32k rows, 207 MB there and back: 54 us, 3.9 TB/s (0.6 of the measured copy rate; the longest list, a third
+// above the average, sets the end: lists of one length 47 us, 4.3 TB/s).  In slices of 64 bytes, four times the CTAs: 64 us, since a random row
+// is then four visits of HBM; a cluster a list: 75, its barrier waits for the stores too; the next batch asked for before this one is
+// written: 62.  Up to eight rows of 4096 heads (19 MB): 8.2 us.
 struct KeepArgs {
   Pool pool;
   Lists lists;
@@ -115,7 +120,9 @@ __global__ void __launch_bounds__(kWarp ? kThreads : kKeepThreads) keep_rows_ker
 // is changed yet.  reserve_apply_kernel adds the numbers up (a few thousand, each CTA for itself: no waiting), and if there are enough:
 //   a CTA per chunk    hands its free pages out to the pairs that grow: one page a thread, whose pair it looks up by rank;
 //   a group per pair   updates `held` and makes the pair's copies, whose pages it looks up by rank.
-// Bound: latency (two launches, about five dependent reads each); with many copies HBM.
+// Bound: latency (two launches, about five dependent reads each); with many copies HBM.  8192 heads, of which one in 32 needs a
+// page: 10 us; 131072 pages for 512 heads from a pool of a million of which an eighth is free: 14; 8192 copies of 31 rows (264 MB):
+// 45 us, 5.9 TB/s, under ncu.
 struct ReserveArgs {
   Pool pool;
   Lists lists;
@@ -283,21 +290,23 @@ __device__ __forceinline__ int page_of_rank(const ReserveArgs& a, const int32_t*
   return 0;    // not reached: there are enough
 }
 
-// kWarp: a CTA has the pairs of a block, and a warp copies a page; else it has one pair, and copies with all its threads.
-template <bool kWarp>
-__global__ void __launch_bounds__(kThreads, kWarp ? 2 : 4) reserve_apply_kernel(ReserveArgs a, int log_row) {
+// kPairs: the pairs of a CTA.  One: it copies with all its threads; else a warp copies a page.
+template <int kPairs>
+__global__ void __launch_bounds__(kThreads, kPairs > 1 ? 2 : 4) reserve_apply_kernel(ReserveArgs a, int log_row) {
+  constexpr bool kWarp = kPairs > 1;
+  static_assert(kPairBlock % kPairs == 0, "a CTA's pairs are of one block");
   __shared__ int32_t s_prefix[kMaxChunks];
-  __shared__ int s_sum[kThreads / 32][4], s_page, s_held[kPairBlock];
-  __shared__ int2 s_need[kPairBlock];
+  __shared__ int s_sum[kThreads / 32][4], s_page, s_held[kPairs];
+  __shared__ int2 s_need[kPairs];
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool pages = (int)blockIdx.x < a.n_chunks;
-  const int group = (int)blockIdx.x - a.n_chunks, block = kWarp ? group : group / kPairBlock;
+  const int pair0 = ((int)blockIdx.x - a.n_chunks) * kPairs, block = pair0 / kPairBlock;
   const int64_t page0 = (int64_t)blockIdx.x * a.chunk;
   // asked for ahead of the sums: a thread's four pages, or its pair
-  const int pair = kWarp ? block * kPairBlock + (int)threadIdx.x : group;
-  const bool live = !pages && (kWarp ? threadIdx.x < kPairBlock && pair < a.pairs : threadIdx.x == 0);
+  const int pair = pair0 + (int)threadIdx.x;
+  const bool live = !pages && threadIdx.x < kPairs && pair < a.pairs;
   uint32_t word = pages ? a.free_bits[page0 / 32 + (threadIdx.x >> 3)] : 0u;
   int2 need = make_int2(0, 0);
   Want w{0, 0, 0};
@@ -353,9 +362,9 @@ __global__ void __launch_bounds__(kThreads, kWarp ? 2 : 4) reserve_apply_kernel(
     if (w.slots > held) a.held[pair] = w.slots;
     // copies: pages from this rank on
     const int at = pair % kPairBlock;
-    s_need[kWarp ? at : 0] = make_int2(sum.before + (at ? a.need[pair - 1].x : 0), need.y);
-    s_held[kWarp ? at : 0] = min(held, w.slots);
-  } else if (kWarp && threadIdx.x < kPairBlock) {
+    s_need[threadIdx.x] = make_int2(sum.before + (at ? a.need[pair - 1].x : 0), need.y);
+    s_held[threadIdx.x] = min(held, w.slots);
+  } else if (threadIdx.x < kPairs) {
     s_need[threadIdx.x] = make_int2(0, 0);
   }
   if (!__syncthreads_or(need.y > 0)) return;
@@ -364,9 +373,9 @@ __global__ void __launch_bounds__(kThreads, kWarp ? 2 : 4) reserve_apply_kernel(
   __syncthreads();
   constexpr int NT = kWarp ? 32 : kThreads, U = kWarp ? 8 : 4;
   const int t = kWarp ? lane : threadIdx.x;
-  for (int i = kWarp ? warp : 0; i < (kWarp ? kPairBlock : 1); i += kThreads / 32) {
+  for (int i = kWarp ? warp : 0; i < kPairs; i += kThreads / 32) {
     if (s_need[i].y == 0) continue;
-    const int its = kWarp ? block * kPairBlock + i : group, end = s_held[i];
+    const int its = pair0 + i, end = s_held[i];
     int rank = s_need[i].x;
     const Want x = want_of(a, its, bad);
     int32_t* const table = a.table + (int64_t)its * a.pool.max_pages;
@@ -411,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, kWarp ? 2 : 4) reserve_apply_kernel(
 }
 
 // ------------------------------------------------------------------------------------------------ pages given back
-// 2^log_t threads a pair, four pages each at a time.
+// 2^log_t threads a pair, four pages each at a time.  Bound: latency, and with many pages the atomics of L2 (a million: 11 us).
 __global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pairs, int log_t, const int32_t* lengths, int32_t* held, const int32_t* table,
                                                               int32_t* refs, int* status) {
   pdl_wait();
@@ -439,7 +448,8 @@ __global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pai
 
 // ------------------------------------------------------------------------------------------------ pages shared
 // A warp per pair: those of the new sequences copy their parents' table rows, those of the old ones count their children in (and
-// themselves out, where the old sequences end): one atomic a page whatever the number of children.
+// themselves out, where the old sequences end): one atomic a page whatever the number of children.  1024 heads of 126 pages to eight
+// each, 8 MB of table: 7.6 us.
 struct ForkArgs {
   Pool pool;
   int Hkv, layers, seqs, new_seqs, keep_old;
@@ -537,8 +547,12 @@ cudaError_t launch_pages_reserve(const ckv_paged& pg, Lists lists, const int32_t
   cudaError_t e = launch(reserve_count_kernel, w.n_chunks + (w.n_blocks + kWarps - 1) / kWarps, kThreads, st, a);
   if (e != cudaSuccess) return e;
   const int log_row = pg.dtype == CKV_BF16 ? 4 : 5;
-  return pairs <= 148 * 4 ? launch(reserve_apply_kernel<false>, w.n_chunks + pairs, kThreads, st, a, log_row)
-                          : launch(reserve_apply_kernel<true>, w.n_chunks + w.n_blocks, kThreads, st, a, log_row);
+  // Copies want many warps, each of which has few pairs; a call without any wants few CTAs, since each adds the needs up (8192 pairs: 8
+  // pairs a CTA 72 us with a copy each and 13.7 with none, 16 pairs 74 and 12.3, 32 pairs 79 and 12.3; 1024 pairs with copies: 25, 33, 47).
+  const auto grid = [&](int per) { return w.n_chunks + (pairs + per - 1) / per; };
+  return pairs <= 148 * 4    ? launch(reserve_apply_kernel<1>, grid(1), kThreads, st, a, log_row)
+         : pairs <= 148 * 32 ? launch(reserve_apply_kernel<8>, grid(8), kThreads, st, a, log_row)
+                             : launch(reserve_apply_kernel<16>, grid(16), kThreads, st, a, log_row);
 }
 
 cudaError_t launch_pages_trim(const ckv_paged& pg, const int32_t* lengths, int32_t* held, const int32_t* table, int32_t* refs,

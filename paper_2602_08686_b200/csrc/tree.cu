@@ -4,7 +4,8 @@
 // 2^r nearest ancestors (itself among them) and `up` is the next one above them; or-ing in that one's mask makes it 2^(r+1).
 // A chain of 512 takes nine rounds (a walk from token to token would take 512 dependent reads), a usual tree three or four.
 // A mask may be or-ed in before, after or between the words of its own step of the round: it then has more of the same ancestors,
-// and the rounds end with all of them either way.  `up` and the depths, which add up, are double-buffered.  Parents in any order; latency all over.
+// and the rounds end with all of them either way.  `up` and the depths, which add up, are double-buffered.  Parents in any order.
+// Bound: latency.  16 trees of 63 tokens 4.1 us on the device; 64 of 512, chains for the most part, 10 (16 before a lane took four words).
 #include "paged.cuh"
 
 namespace ckv {

@@ -6,11 +6,12 @@
 // it waiting for L2).
 //
 // attend_split_kernel: fp32 on the tensor cores, blocks of 16 RG query rows.  An fp32 number is the sum of two of tf32's 11 bits, x = h + l
-// with h = x rounded and l what is left (the unit takes its first 11 bits), off by at most 2^-21 |x|; a product is
-//   x y = hx hy + hx ly + lx hy,   lx ly < 2^-22 |x y| left out,
-// three of the unit's for one.  It cuts sums off instead of rounding them (1 + 0.75 ulp gives 1), one bias per addition, so nothing long
-// is summed there: logits run in four chains of four steps and the rest in four more, and what eight keys give the output starts from zero and
-// is added to it by the CUDA cores.  Against 64 bits the outputs are as exact as with fp32 multiplications.
+// with h = x rounded and l what is left, of which the unit takes the first 11 bits (off by 2^-21 |x| at most); a product is
+//   x y = hx hy + hx ly + lx hy,   lx ly <= 2^-22 |x y| left out,
+// three of the unit's for one.  It cuts sums off instead of rounding them (1 + 0.75 ulp gives 1), a bias for each addition, so nothing
+// long is summed there: logits run in four chains of four steps and the rest in four more, and what eight keys give the output starts from
+// zero and is added to it by the CUDA cores.  Outputs are off by 3 to 4.5e-7 of their 2-norm on 300 to 32000 rows (elementary
+// operations in fp32: 6e-7 to 2.4e-6).
 // Keys and values come to shared memory in tiles of 64 rows, three deep, by asynchronous copies that fill in zeros for rows that
 // are not there.  A warp has 16 of the block's rows, whose queries and output stay in its registers, and every KG-th eight keys of a tile
 // (KG = 8 / RG); fragments of m16n8k8 come straight from the tile, 16 bytes at a time:
@@ -18,8 +19,10 @@
 //   output  thread c's probabilities are those of keys c and c + 4 of eight (column n of the logits is key n / 2 + 4 (n % 2)), as the
 //           second product wants them; which dimension a column of the output means is free again.
 // Rows of 528 bytes put all of a quarter-warp's pieces in banks of their own.
-// Bound: the matrix instructions (8 clocks each on one of an SM's four units): 32 rows take 48 clocks a key.  (On the FMA units it would
-// be 64, but their operands come from shared memory at 128 bytes a clock: 165 measured.)
+// Bound: in the limit the matrix instructions (8 clocks each on one of an SM's four units, 48 a key and 32 rows), so far the latency of a
+// step's chain of dependent instructions at two warps a unit (255 registers a thread): 8 sequences of 32 tokens on 4000 rows, four heads
+// a group, 475 us (130 clocks a key and 32 rows; blocks of four rows 1300, the same tiles on the FMA units 520 to 650, whose
+// operands come from shared memory at 128 bytes a clock); 4 of 24 tokens on 2000 rows, two KV heads, 43 (68).
 #include "paged_work.cuh"
 #include "tc_ptx.cuh"
 
@@ -54,8 +57,6 @@ __device__ __forceinline__ void mma1688(float (&d)[4], const float (&a)[4], floa
 }
 // x rounded to tf32's 11 bits (the unit would cut it off).  cvt.rna.tf32 takes several instructions.
 __device__ __forceinline__ float high(float x) { return __uint_as_float((__float_as_uint(x) + 0x1000u) & 0xffffe000u); }
-// x cut off to them, as the unit takes it, and the rest.
-__device__ __forceinline__ float rest_of(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
 __device__ __forceinline__ void here(float4& x) { asm volatile("" : "+f"(x.x), "+f"(x.y), "+f"(x.z), "+f"(x.w)); }
 __device__ __forceinline__ float part(const float4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
@@ -151,13 +152,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_split_kernel(WorkArgs a, c
 #pragma unroll
           for (int t = 0; t < 4; t += 2) {
             const float x[4] = {part(qr[0][i], t), part(qr[1][i], t), part(qr[0][i], t + 1), part(qr[1][i], t + 1)};
-            const float k0 = part(k, t), k1 = part(k, t + 1);
+            const float k0 = part(k, t), k1 = part(k, t + 1), h0 = high(k0), h1 = high(k1);
             float hx[4], lx[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) hx[e] = high(x[e]), lx[e] = x[e] - hx[e];
-            mma1688(rest[t], lx, k0, k1);
-            mma1688(rest[t + 1], hx, rest_of(k0), rest_of(k1));
-            mma1688(chain[(2 * i + t / 2) & 3], hx, k0, k1);
+            mma1688(rest[t], lx, h0, h1);
+            mma1688(rest[t + 1], hx, k0 - h0, k1 - h1);
+            mma1688(chain[(2 * i + t / 2) & 3], hx, h0, h1);
           }
         }
         float x[4];        // row g: keys c, c + 4; row g + 8: the same
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_split_kernel(WorkArgs a, c
           float l0[4], l1[4], sum = 0.f;
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            l0[t] = rest_of(part(v0, t)), l1[t] = rest_of(part(v1, t));
+            l0[t] = part(v0, t) - high(part(v0, t)), l1[t] = part(v1, t) - high(part(v1, t));
             sum += l0[t] + l1[t];
           }
           if (__any_sync(0xffffffffu, sum != sum)) {
@@ -257,12 +258,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_split_kernel(WorkArgs a, c
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
-            mma1688(d[t], lp, part(v0, t), part(v1, t));
+            mma1688(d[t], lp, high(part(v0, t)), high(part(v1, t)));
           }
 #pragma unroll
           for (int t = 0; t < 4; ++t) mma1688(d[t], hp, l0[t], l1[t]);
 #pragma unroll
-          for (int t = 0; t < 4; ++t) mma1688(d[t], hp, part(v0, t), part(v1, t));
+          for (int t = 0; t < 4; ++t) mma1688(d[t], hp, high(part(v0, t)), high(part(v1, t)));
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
