@@ -22,29 +22,47 @@ bool is_on(const at::Tensor& t, PyObject* dtype, PyObject* device) {
   return THPDtype_Check(dtype) && reinterpret_cast<THPDtype*>(dtype)->scalar_type == t.scalar_type() && t.is_cuda() &&
          PyLong_Check(device) && PyLong_AsLongLong(device) == t.get_device();
 }
-PyObject* address(const at::Tensor& t) { return PyLong_FromUnsignedLongLong(reinterpret_cast<uintptr_t>(t.data_ptr())); }
+// A tensor without memory of its own (a wrapper that other code sees as a CUDA tensor) has no address, or throws: no answer.
+PyObject* address(const at::Tensor& t) {
+  const void* const p = t.data_ptr();
+  if (!p && t.numel() > 0) Py_RETURN_NONE;
+  return PyLong_FromUnsignedLongLong(reinterpret_cast<uintptr_t>(p));
+}
+template <class F>
+PyObject* or_none(F&& f) {
+  try {
+    return f();
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+}
 
 // dense(tensor, shape, dtype, device): the address of a contiguous tensor of that shape, type and CUDA device, or None.
 PyObject* dense(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 4 || !THPVariable_Check(args[0])) Py_RETURN_NONE;
-  const at::Tensor& t = THPVariable_Unpack(args[0]);
-  if (!is_on(t, args[2], args[3]) || !t.is_contiguous() || !same_shape(t, args[1])) Py_RETURN_NONE;
-  return address(t);
+  return or_none([&]() -> PyObject* {
+    const at::Tensor& t = THPVariable_Unpack(args[0]);
+    if (!is_on(t, args[2], args[3]) || !t.is_contiguous() || !same_shape(t, args[1])) Py_RETURN_NONE;
+    return address(t);
+  });
 }
 
 // same(tensor, (shape, stride, dtype, device)): the address of a tensor of that layout, or None (also where only strides of extents of
 // one differ).
 PyObject* same(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 2 || !THPVariable_Check(args[0]) || !PyTuple_Check(args[1]) || PyTuple_GET_SIZE(args[1]) != 4) Py_RETURN_NONE;
-  const at::Tensor& t = THPVariable_Unpack(args[0]);
-  PyObject *const shape = PyTuple_GET_ITEM(args[1], 0), *const stride = PyTuple_GET_ITEM(args[1], 1);
-  if (!is_on(t, PyTuple_GET_ITEM(args[1], 2), PyTuple_GET_ITEM(args[1], 3)) || !same_shape(t, shape)) Py_RETURN_NONE;
-  for (int64_t i = 0; i < t.dim(); ++i)
-    if (PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i)) != t.stride(i)) {
-      PyErr_Clear();
-      Py_RETURN_NONE;
-    }
-  return address(t);
+  return or_none([&]() -> PyObject* {
+    const at::Tensor& t = THPVariable_Unpack(args[0]);
+    PyObject *const shape = PyTuple_GET_ITEM(args[1], 0), *const stride = PyTuple_GET_ITEM(args[1], 1);
+    if (!is_on(t, PyTuple_GET_ITEM(args[1], 2), PyTuple_GET_ITEM(args[1], 3)) || !same_shape(t, shape)) Py_RETURN_NONE;
+    if (!PyTuple_Check(stride) || PyTuple_GET_SIZE(stride) != t.dim()) Py_RETURN_NONE;
+    for (int64_t i = 0; i < t.dim(); ++i)
+      if (PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i)) != t.stride(i)) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+      }
+    return address(t);
+  });
 }
 
 // call(address of a function, arguments ...): its int result.  Arguments are integers and addresses (None: null), each of which takes a

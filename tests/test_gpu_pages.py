@@ -1,5 +1,6 @@
 """GPU tests of the calls that manage the pages of a cache, against statements of them one entry at a time (tests/tree_reference.py);
 rows are compared bit by bit.  Then the calls together, as a decoder makes them."""
+import os
 import random
 
 import numpy as np
@@ -494,3 +495,46 @@ def test_two_streams_with_states_of_their_own(B):
             c.ref.reserve([3, 40, 0, 17], 8)
             c.ref.trim(c.ref.lengths)
         c.fine(B), c.same()
+
+
+def test_the_readme_s_step_that_drafts_trees(B):
+    """The lines under "A step that drafts trees", twice; the second time the sequences are those that the first forked."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as f:
+        lines = f.read().split("A step that drafts trees")[1].split("\n\n")[1].split("\n")
+    assert len(lines) == 7 and all(x.startswith("    ckv.ckv_") for x in lines)
+    P, H, Hkv, S, n, width = 16, 8, 2, 2, 6, 8
+    z = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    kp, vp = (torch.randn(64, P, D, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    qkv = torch.randn(S * n, H + 2 * Hkv, D, generator=gen, device="cuda").bfloat16()
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    q_rot, out, lse = torch.zeros(S * n, H, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(S * n, H, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(S * n, H, device="cuda")
+    parents = [-1, 0, 0, 1, 2, -1]
+    names = dict(ckv=B, k_pages=kp, v_pages=vp, q=q, k=k, v=v, q_rot=q_rot, out=out, lse=lse, refs=z(64), held=z(S, Hkv), page_table=z(S, Hkv, width), lengths=z(S, Hkv),
+                 longer=z(S, Hkv), room=z(2), parents=i32(parents * S), token_starts=i32([0, n, 2 * n]), masks=z(S * n, 1), positions=z(S * n), next_position=i32([0, 0]),
+                 new=i32([n, n]), path=i32([0, 1, 3, 5]), begins=i32([0, 3]), counts=i32([3, 1]), lengths2=z(S, Hkv), held2=z(S, Hkv), page_table2=z(S, Hkv, width),
+                 parent_of_each=i32([0, 0]), rotary=B.make_rotary(10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)))
+    for turn in range(2):
+        pg = names["pg"] = B.make_paged(kp, names["page_table"], q=q, k_new=k, max_new=n)
+        names["pg_rot"] = B.make_paged(kp, names["page_table"], q=q_rot, max_new=n)
+        names["ws"] = torch.empty(max(B.ckv_paged_workspace_bytes(pg), B.ckv_pages_workspace_bytes(pg)), dtype=torch.uint8, device="cuda")
+        before = names["lengths"].clone()
+        exec("\n".join(x[4:] for x in lines), names)
+        assert B.ckv_device_status(names["ws"]) == B.OK and names["room"][1] == 0
+        assert torch.equal(names["lengths"], before + names["counts"][:, None])
+        assert torch.equal(names["lengths2"], names["lengths"][:1].expand(S, Hkv))       # both go on from the first
+        assert names["positions"].tolist() == [int(p) + d for p in names["next_position"] for d in (0, 1, 1, 2, 2, 0)]
+        # the rows kept are the path's, turned by their positions
+        L = int(before[0, 0])
+        angle = names["positions"][:n].double()[:, None, None] * names["rotary"]._keep[0]
+        a, b = k[:n, :, :64].double(), k[:n, :, 64:].double()
+        want = torch.cat((a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()), -1)
+        for i, t in enumerate((0, 1, 3)):
+            row = kp[names["page_table"][0, :, (L + i) // P].long(), (L + i) % P]
+            # rounded to bf16 once, of an fp32 angle and products (40 * 2^-24 of a pair's sizes)
+            assert ((row.double() - want[t]).abs() <= 2.0 ** -8 * want[t].abs() + 40 * EPS * 2 * want[t].abs().max()).all()
+        assert int(names["refs"].sum()) == int(names["held2"].sum())
+        for x, y in (("lengths", "lengths2"), ("held", "held2"), ("page_table", "page_table2")):
+            names[x], names[y] = names[y], names[x]
+        names["next_position"] = names["lengths"][:, 0].contiguous()
