@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(kWarp ? kThreads : kKeepThreads) keep_rows_ker
 //   a CTA per chunk    hands its free pages out to the pairs that grow: one page a thread, whose pair it looks up by rank;
 //   a group per pair   updates `held` and makes the pair's copies, whose pages it looks up by rank.
 // Bound: latency (two launches, about five dependent reads each); with many copies HBM.  8192 heads, of which one in 32 needs a
-// page: 10 us; 131072 pages for 512 heads from a pool of a million of which an eighth is free: 14; 8192 copies of 31 rows (264 MB):
-// 45 us, 5.9 TB/s, under ncu.
+// page: 13 us in all; 131072 pages for 512 heads from a pool of a million of which an eighth is free: 4.4 and 13 under ncu; 8192 copies of
+// 31 rows (264 MB there and back): 50 us, 5.3 TB/s.
 struct ReserveArgs {
   Pool pool;
   Lists lists;

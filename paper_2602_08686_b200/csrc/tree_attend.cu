@@ -21,8 +21,10 @@
 // Rows of 528 bytes put all of a quarter-warp's pieces in banks of their own.
 // Bound: in the limit the matrix instructions (8 clocks each on one of an SM's four units, 48 a key and 32 rows), so far the latency of a
 // step's chain of dependent instructions at two warps a unit (255 registers a thread): 8 sequences of 32 tokens on 4000 rows, four heads
-// a group, 475 us (130 clocks a key and 32 rows; blocks of four rows 1300, the same tiles on the FMA units 520 to 650, whose
-// operands come from shared memory at 128 bytes a clock); 4 of 24 tokens on 2000 rows, two KV heads, 43 (68).
+// a group, 480 to 490 us (130 clocks a key and 32 rows; blocks of four rows 1300, the same tiles on the FMA units 520 to 650, whose
+// operands come from shared memory at 128 bytes a clock); 4 of 24 tokens on 2000 rows, two KV heads, 43 (68).  Not kept: 16 keys a step
+// with two chains (445, errors half as large again), 12 warps with split queries in shared memory (426, and 31 instead of 25 us for 4 of
+// 8 tokens on 2000 rows).
 #include "paged_work.cuh"
 #include "tc_ptx.cuh"
 
