@@ -25,6 +25,8 @@
 // operands come from shared memory at 128 bytes a clock); 4 of 24 tokens on 2000 rows, two KV heads, 43 (68).  Not kept: 16 keys a step
 // with two chains (445, errors half as large again), 12 warps with split queries in shared memory (426, and 31 instead of 25 us for 4 of
 // 8 tokens on 2000 rows).
+#include <cfloat>
+
 #include "paged_work.cuh"
 #include "tc_ptx.cuh"
 
@@ -211,8 +213,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_split_kernel(WorkArgs a, c
           l[h] += p[e];
           hp[e] = high(p[e]), lp[e] = p[e] - hp[e];
         }
-        // output.  0 * NaN is not 0, and an infinity splits into one and a NaN: values that are not finite are left out of the products
-        // and added, element by element, to the rows that see them.
+        // output.  0 * NaN is not 0, and an infinity splits into one and a NaN, the largest finite numbers (whose first part is rounded up)
+        // into two infinities: values whose parts are not finite are left out of the products and added, element by element, to the
+        // rows that see them.
         const int piece = ((g >> 1) + 4 * (g & 1)) * 4;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {              // 32 dimensions at a time
@@ -223,13 +226,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_split_kernel(WorkArgs a, c
             l0[t] = part(v0, t) - high(part(v0, t)), l1[t] = part(v1, t) - high(part(v1, t));
             sum += l0[t] + l1[t];
           }
-          if (__any_sync(0xffffffffu, sum != sum)) {
-            const float big = 3.4028234e38f;
+          if (__any_sync(0xffffffffu, !(fabsf(sum) <= FLT_MAX))) {
             uint32_t mine = 0;                     // bit (t, key): element t of the thread's four
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              if (!(fabsf(part(v0, t)) <= big)) mine |= 1u << (2 * t), l0[t] = 0.f, (t == 0 ? v0.x : t == 1 ? v0.y : t == 2 ? v0.z : v0.w) = 0.f;
-              if (!(fabsf(part(v1, t)) <= big)) mine |= 2u << (2 * t), l1[t] = 0.f, (t == 0 ? v1.x : t == 1 ? v1.y : t == 2 ? v1.z : v1.w) = 0.f;
+              if (!(fabsf(l0[t]) <= FLT_MAX)) mine |= 1u << (2 * t), l0[t] = 0.f, (t == 0 ? v0.x : t == 1 ? v0.y : t == 2 ? v0.z : v0.w) = 0.f;
+              if (!(fabsf(l1[t]) <= FLT_MAX)) mine |= 2u << (2 * t), l1[t] = 0.f, (t == 0 ? v1.x : t == 1 ? v1.y : t == 2 ? v1.z : v1.w) = 0.f;
             }
 #pragma unroll 1
             for (uint32_t lanes = __ballot_sync(0xffffffffu, mine != 0u); lanes; lanes &= lanes - 1) {

@@ -319,6 +319,59 @@ def test_values_that_are_not_finite(B, dtype, n, bad):
         assert torch.isfinite(lse[~ill]).all() and torch.isfinite(out[~ill]).all()
 
 
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype,n", [(torch.float32, 3), (torch.float32, 20), (torch.float32, 40), (torch.bfloat16, 3), (torch.bfloat16, 20), (torch.bfloat16, 70)])
+def test_largest_finite_numbers(B, dtype, n, sign):
+    """Rows of the type's largest number, keys and values: tokens that do not see them have what they would have without; in tokens that
+    see a value of that size (their sums may pass the type's range before they are divided) it stays of its sign."""
+    H, Hkv, base = 8, 2, 90
+    c = R.Cache([[n + base, n + 200]], 32, dtype=dtype, device="cuda", seed=n)
+    sees = some_sees([n], "tree", random.Random(n))
+    q = torch.randn(n, H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).to(dtype)
+    masks = TR.pack(sees, (n + 31) // 32, n, [0, n]).cuda()
+    want, want_lse = TR.attend(q, [0, n], c.rows, sees)
+    vmax = max(float(v.double().abs().max()) for _, v in c.rows[0])
+    r = r_of(q, torch.cat([k for k, _ in c.rows[0]]), n + 200)
+    tol = (2.0 ** -8 * (vmax + want.abs()) if dtype == torch.bfloat16 else EPS * want.abs()) + 2 * r * vmax
+    hit = sorted({n // 2, n - 1}) if n > 3 else [2]                        # so that some tokens see none
+    clear = ~torch.from_numpy(sees[0][:, hit].any(1)).cuda()
+    assert clear.any() and (~clear).any()
+    for pool in (c.v_pages, c.k_pages):
+        for g in range(Hkv):
+            for t in hit:
+                j = c.lens[0][g] - n + t
+                pool[int(c.table[0, g, j // 32]), j % 32] = sign * torch.finfo(dtype).max
+        for cache in caches(c, H, [n]):
+            out, lse = run_attend(B, cache, q, [0, n], masks, max_new=n)
+            assert ((out.double() - want).abs() <= tol)[clear].all()
+            assert ((lse.double() - want_lse).abs() <= r + 2 * EPS * want_lse.abs())[clear].all()
+            if pool is c.v_pages:
+                assert (out[~clear] * sign > vmax).all()
+
+
+@pytest.mark.parametrize("bits", [0x7fffffff, -1, 0x7f800001, -0x7fffff])      # quiet and signalling, of both signs
+def test_every_nan(B, bits):
+    """A drafted token's key, or value, of NaNs with this pattern: NaN in the tokens that see it and nothing of it in the others."""
+    n, H, Hkv = 20, 8, 2
+    sees = some_sees([n], "tree", random.Random(n))
+    masks = TR.pack(sees, 1, n, [0, n]).cuda()
+    q = torch.randn(n, H, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))
+    ill = torch.from_numpy(sees[0][:, n // 2]).cuda()
+    assert ill.any() and (~ill).any()
+    for name in ("k_pages", "v_pages"):
+        c = R.Cache([[n + 90, n + 200]], 32, dtype=torch.float32, device="cuda", seed=n)
+        want, _ = TR.attend(q, [0, n], c.rows, sees)
+        vmax = max(float(v.double().abs().max()) for _, v in c.rows[0])
+        tol = EPS * want.abs() + 2 * vmax * r_of(q, torch.cat([k for k, _ in c.rows[0]]), n + 200)
+        for g in range(Hkv):
+            j = c.lens[0][g] - n + n // 2
+            getattr(c, name).view(torch.int32)[int(c.table[0, g, j // 32]), j % 32] = bits
+        for cache in caches(c, H, [n]):
+            out, lse = run_attend(B, cache, q, [0, n], masks, max_new=n)
+            assert torch.isnan(out[ill]).all() and ((out.double() - want).abs() <= tol)[~ill].all()
+            assert torch.isnan(lse[ill]).all() if name == "k_pages" else torch.isfinite(lse).all()
+
+
 @pytest.mark.parametrize("dtype,n", [(torch.float32, 3), (torch.float32, 20), (torch.bfloat16, 3), (torch.bfloat16, 20), (torch.bfloat16, 70)])
 def test_infinite_keys_and_values_of_the_prefix(B, dtype, n):
     """Rows that every token sees.  A key with an infinity gives the logit its product with the query has: minus infinity is a row of no
