@@ -402,6 +402,11 @@ __device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o
   tmem_wait_st();
 }
 
+// Minus infinity where `hidden` is not zero; in PTX, so that the steps that hide nothing do not run it too, as selects.
+__device__ __forceinline__ void hide_if(uint32_t& logit, uint32_t hidden) {
+  asm volatile("{ .reg .pred p; setp.ne.u32 p, %1, 0; @p mov.b32 %0, 0xff800000; }" : "+r"(logit) : "r"(hidden));
+}
+
 template <bool kTree>
 __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int stream, int quarter,
                                              int lane) {
@@ -433,11 +438,6 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       const int j = pair ? g >> 1 : g, h = pair ? g & 1 : stream;
       const int key0 = (t0 + j) * kTile + h * kStep;
       const uint32_t buf = n_steps & 1, s_buf = s_addr + buf * kStep;
-      uint32_t hidden[2] = {0u, 0u};                          // kTree: the step's keys that are no ancestors; read ahead of the logits
-      if (kTree && live && key0 + kStep > least) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) hidden[i] = ~tree_bits(words, a.w.tree_words, key0 + 32 * i - (it.len - it.n));
-      }
       if (!wait_warp(bar_s + buf * 8, (n_steps >> 1) & 1, w, 6)) return;
       tc_fence_after();
       uint32_t s[kStep];
@@ -445,8 +445,20 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       const uint32_t bad = *(volatile uint32_t*)&sm.bad[(n_all + j) % kInfo];
       if (key0 + kStep > least || bad) {
 #pragma unroll
-        for (int i = 0; i < kStep; ++i)
-          if (key0 + i >= limit || (bad >> ((h * kStep + i) >> a.w.log_p) & 1) || (kTree && (hidden[i >> 5] >> (i & 31) & 1u))) s[i] = 0xff800000u;
+        for (int i = 0; i < kStep; ++i) {
+          if (kTree && !bad) break;
+          if ((!kTree && key0 + i >= limit) || (bad >> ((h * kStep + i) >> a.w.log_p) & 1)) s[i] = 0xff800000u;
+        }
+        // A tree's rows see keys without any order: tests key by key would part the warp 64 times (5 us a step, 0.6 this way).  The words
+        // are read here and not ahead of the logits, which costs the steps that need none 2 %.
+#pragma unroll
+        for (int x = 0; kTree && x < 2; ++x) {
+          const int sees = limit - key0 - 32 * x;
+          const uint32_t hide = (live ? ~tree_bits(words, a.w.tree_words, key0 + 32 * x - (it.len - it.n)) : 0u) |
+                                (sees <= 0 ? 0xffffffffu : sees < 32 ? 0xffffffffu << sees : 0u);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) hide_if(s[32 * x + i], hide & 1u << i);
+        }
       }
       // Rows that have seen nothing yet take their reference here; what O holds for them is zero.
       if (open) {
