@@ -115,12 +115,25 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const W
 //
 // One warp looks the items up for all (lengths, token counts, divisions: 2000 to 6000 clocks each where every warp did it between
 // two items).
+//
+// Where units have several blocks, a share's first item, if it begins inside it, is worked on last.  Shares of `s` tiles cut items of
+// `t` end to end: worker k begins at tile (k s) % t, and in that order the workers would be all over the cache.  This way all begin at tile
+// 0 of their items, and what is put off is at tile t - s + (tiles done) for all of them, so that what one reads from memory the others find
+// in L2: four chunks of 256 tokens on 32k rows, eight heads a group, 471 to 483 us (519 to 549 in order), as with rows that fit L2 (472).
 __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter& w, int lane) {
   Walk k;
   k.start(a.w, sm.plan);
   // this wait takes as long as an item does; the others are for one step's work
   const Waiter patient{w.abort_flag, w.status, 64 * w.limit_ns};
+  Walk off;                  // the item put off
+  off.live = false;
   for (uint32_t i = 0;; ++i) {
+    if (a.w.rounds && k.live && k.it.t0 > 0) {
+      off = k;
+      k.next(a.w, sm.plan);
+    }
+    const bool last = !k.live && off.live;
+    if (last) k = off;
     if (!wait_warp(smem_u32(&sm.job_empty[i % kJobs]), ((i / kJobs) & 1) ^ 1, patient, 10)) return;
     if (lane == 0) {
       Job& job = sm.jobs[i % kJobs];
@@ -136,7 +149,8 @@ __device__ __forceinline__ void job_role(const TcArgs& a, Smem& sm, const Waiter
       bar_arrive(smem_u32(&sm.job_full[i % kJobs]));
     }
     if (!k.live) return;
-    k.next(a.w, sm.plan);
+    if (last) k.live = off.live = false;
+    else k.next(a.w, sm.plan);
   }
 }
 // The i-th item, for a warp that arrives on its `job_empty` when it is done with it; null: a wait has given up.
@@ -402,11 +416,6 @@ __device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o
   tmem_wait_st();
 }
 
-// Minus infinity where `hidden` is not zero; in PTX, so that the steps that hide nothing do not run it too, as selects.
-__device__ __forceinline__ void hide_if(uint32_t& logit, uint32_t hidden) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %1, 0; @p mov.b32 %0, 0xff800000; }" : "+r"(logit) : "r"(hidden));
-}
-
 template <bool kTree>
 __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int stream, int quarter,
                                              int lane) {
@@ -428,7 +437,6 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     const bool live = r < a.TQ * a.w.G && token < it.n;
     auto limit_of = [&](int tk) { return rows_seen(a.w, it.n, it.len, tk + 1); };
     const int limit = live ? limit_of(token) : 0, least = kTree ? job->see : limit_of(tok0);
-    const uint32_t* const words = kTree && live ? tree_words_of(a.w, it, token) : nullptr;   // what the row's token sees of the tree
     // rows of no token hold what shared memory held, or another unit's queries: above everything, they ask for no step again
     float m = live ? -INFINITY : INFINITY, l = 0.f;
     bool open = true;                                         // some row of the warp has no reference yet
@@ -449,15 +457,19 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
           if (kTree && !bad) break;
           if ((!kTree && key0 + i >= limit) || (bad >> ((h * kStep + i) >> a.w.log_p) & 1)) s[i] = 0xff800000u;
         }
-        // A tree's rows see keys without any order: tests key by key would part the warp 64 times (5 us a step, 0.6 this way).  The words
-        // are read here and not ahead of the logits, which costs the steps that need none 2 %.
+        // A tree's rows see keys without any order: tests key by key would part the warp 64 times (5 us a step, 0.6 this way).  What this
+        // takes is looked up anew each time, from a place the compiler knows nothing of: carried along it would cost the steps
+        // that need none of it.
+        const Job* at = job;
+        asm volatile("" : "+l"(at));
 #pragma unroll
         for (int x = 0; kTree && x < 2; ++x) {
           const int sees = limit - key0 - 32 * x;
-          const uint32_t hide = (live ? ~tree_bits(words, a.w.tree_words, key0 + 32 * x - (it.len - it.n)) : 0u) |
-                                (sees <= 0 ? 0xffffffffu : sees < 32 ? 0xffffffffu << sees : 0u);
+          uint32_t hide = sees <= 0 ? 0xffffffffu : sees < 32 ? 0xffffffffu << sees : 0u;
+          if (sees > 0) hide |= ~tree_bits(tree_words_of(a.w, at->it, token), a.w.tree_words, key0 + 32 * x - (at->it.len - at->it.n));
 #pragma unroll
-          for (int i = 0; i < 32; ++i) hide_if(s[32 * x + i], hide & 1u << i);
+          for (int i = 0; i < 32; ++i)
+            if (hide >> i & 1u) s[32 * x + i] = 0xff800000u;
         }
       }
       // Rows that have seen nothing yet take their reference here; what O holds for them is zero.
@@ -504,7 +516,7 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
       for (int x = pair ? 0 : 2 * stream; x < (pair ? 4 : 2 * stream + 2); ++x) {   // the stream's keys
         uint32_t odd = sm.odd[(n_all + j) % kInfo][x];
         const int key0 = (t0 + j) * kTile + x * 32;
-        const uint32_t see = kTree && live ? tree_bits(words, a.w.tree_words, key0 - (it.len - it.n)) : 0xffffffffu;
+        const uint32_t see = kTree && live ? tree_bits(tree_words_of(a.w, it, token), a.w.tree_words, key0 - (it.len - it.n)) : 0xffffffffu;
         for (; odd; odd &= odd - 1) {
           const int i = __ffs(odd) - 1;
           add_row(a, it, o_addr, key0 + i, key0 + i < limit && (see >> i & 1u), token, r_head, m);
