@@ -249,6 +249,20 @@ def test_attend_long_and_many(B, dtype, Nu, Hkv, H, n, rows):
     check_attend(c, q, st, sees, out, lse)
 
 
+@pytest.mark.parametrize("Nu,Hkv,H,n,rows", [(6, 4, 16, 200, 1500), (2, 1, 8, 250, 6000), (12, 4, 28, 140, 900), (1, 2, 2, 600, 3000), (40, 2, 8, 130, 500)])
+def test_shares_of_units_with_several_blocks(B, Nu, Hkv, H, n, rows):
+    """Shares that begin inside an item, hold whole ones and end in another: fewer items than SMs, about as many, more."""
+    rng = random.Random(n)
+    lens = [[rows + n - rng.randint(0, 200) for _ in range(Hkv)] for _ in range(Nu)]
+    counts = [n if u == 0 else n - rng.randint(0, n // 2) for u in range(Nu)]
+    c = R.Cache(lens, 16, dtype=torch.bfloat16, device="cuda", seed=n)
+    st = starts_of(counts)
+    q = torch.randn(st[-1], H, D, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda").bfloat16()
+    sees = some_sees(counts, "tree", rng)
+    out, lse = run_attend(B, c, q, st, TR.pack(sees, (n + 31) // 32, st[-1], st).cuda(), max_new=n)
+    check_attend(c, q, st, sees, out, lse)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n", [4, 12, 90])
 def test_a_chain_is_a_causal_chunk(B, dtype, n):
