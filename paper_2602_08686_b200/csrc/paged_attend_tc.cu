@@ -38,7 +38,8 @@ constexpr int kTile = 128, kStep = 64;         // keys of a tile, and of a step
 constexpr uint32_t kHalf = 128 * 128;          // 128 rows x 64 bf16
 constexpr uint32_t kTileBytes = 2 * kHalf;
 constexpr int kTcGranule = kBothTiles;         // least cost a CTA takes on (two tiles: 31 us instead of 27 for 40 tokens on 2048 rows)
-constexpr int kInfo = 8;                       // ring of per-tile notes from the loader
+constexpr int kInfo = 8;                       // ring of per-tile notes
+constexpr int kNoted = kInfo - 3;              // tiles of an item whose notes its end still finds: the other stream is up to three tiles on
 constexpr int kJobs = 4;                       // ring of items
 // A step's sum above it is done again with a new reference.  Sums and outputs of up to 2^24 rows (2^18 steps) then stay below 2^34 and
 // 2^34 max|v|, in range for values up to 2^94 (the largest fp32 is 2^128).
@@ -416,6 +417,24 @@ __device__ __noinline__ void add_row(const TcArgs& a, const Item& it, uint32_t o
   tmem_wait_st();
 }
 
+// Which of 32 value rows from `key0` on clean_values has left out, from the rows as they lie in memory (a warp, a row each).
+__device__ __noinline__ uint32_t odd_rows(const TcArgs& a, const Item& it, int key0, int see, int lane) {
+  const int key = key0 + lane;
+  uint32_t hit = 0;
+  if (key >= see && key < it.visible) {
+    const int page = a.w.table[((int64_t)it.u * a.w.Hkv + it.g) * a.w.max_pages + (key >> a.w.log_p)];
+    if ((unsigned)page < (unsigned)a.w.n_pages) {
+      const uint4* const v = reinterpret_cast<const uint4*>(a.v + page * a.page_stride + (key & (a.w.P - 1)) * a.page_row);
+      const uint32_t e = 0x7f807f80u;
+      for (int i = 0; i < 16; ++i) {
+        const uint4 x = v[i];
+        hit |= __vcmpeq2(x.x & e, e) | __vcmpeq2(x.y & e, e) | __vcmpeq2(x.z & e, e) | __vcmpeq2(x.w & e, e);
+      }
+    }
+  }
+  return __ballot_sync(0xffffffffu, hit != 0u);
+}
+
 template <bool kTree>
 __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t tmem, const Waiter& w, int stream, int quarter,
                                              int lane) {
@@ -511,11 +530,12 @@ __device__ __forceinline__ void softmax_role(const TcArgs& a, Smem& sm, uint32_t
     float* part = a.w.o + slot * kHeadDim;
     if (!wait_warp(smem_u32(&sm.item_done[stream]), n_items & 1, w, 7)) return;
     tc_fence_after();
-    // value rows that were left out because they are not finite, for the tokens that see them
+    // value rows that were left out because they are not finite, for the tokens that see them.  A block of a chunk has them in its last two
+    // or three tiles; a tree, whose rows may all be hidden from some token, in more than the notes' ring has room for.
     for (int j = n - 1; job->odd && j >= 0 && late_row(a, *job, j) < kTile; --j) {
       for (int x = pair ? 0 : 2 * stream; x < (pair ? 4 : 2 * stream + 2); ++x) {   // the stream's keys
-        uint32_t odd = sm.odd[(n_all + j) % kInfo][x];
         const int key0 = (t0 + j) * kTile + x * 32;
+        uint32_t odd = !kTree || j >= n - kNoted ? sm.odd[(n_all + j) % kInfo][x] : odd_rows(a, it, key0, job->see, lane);
         const uint32_t see = kTree && live ? tree_bits(tree_words_of(a.w, it, token), a.w.tree_words, key0 - (it.len - it.n)) : 0xffffffffu;
         for (; odd; odd &= odd - 1) {
           const int i = __ffs(odd) - 1;
