@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kWarp ? kThreads : kKeepThreads) keep_rows_ker
 #pragma unroll 4
   for (int i = t; i < n; i += NT) {
     const int x = rows[i];
-    if (x <= (i ? rows[i - 1] : -1) || x >= span) {
+    if (x < i || x >= span || (i && x <= rows[i - 1])) {     // x < i: a list that ascends from zero on never is; such an x may lie before the table
       ok = false;
     } else if (x != i) {       // from and to pages of the pool, and to none that others hold
       first = min(first, i);
