@@ -457,8 +457,10 @@ ckv_status ckv_keep_rows(const ckv_paged* paged, int32_t layers, const int32_t* 
  * Whose the pages are.  The caller keeps, next to the page table and the lengths, refs [n_pages] int32 (how many heads hold each page;
  * 0: it is free; all zero to begin with) and held [Nu,Hkv] int32 (pages each head holds: table entries 0 .. held-1).  These
  * calls and no others change the two; ckv_append and ckv_gather_pages write rows of pages that have been reserved.  Counts, held and
- * table entries follow from the inputs alone.  A page number outside the pool, a count that would fall below zero, a held
- * outside 0..max_pages or a negative length is reported (CKV_ERR_PAGE) and nothing is done for that entry.
+ * table entries follow from the inputs alone.  A page number outside the pool or a count that would fall below zero is reported
+ * (CKV_ERR_PAGE) and nothing is done for that entry; a held outside 0..max_pages or a negative length is reported and nothing is done for
+ * that head (a new sequence that continues one is empty).  (Where fewer holders of a page have been counted than it has, what a fork that ends the
+ * old batch leaves in its count depends on their order.)
  */
 
 /* Bytes of work space ckv_pages_reserve needs (0 on invalid arguments); the other calls of this section use 256 of them. */

@@ -63,7 +63,8 @@ __global__ void __launch_bounds__(kWarp ? kThreads : kKeepThreads) keep_rows_ker
 #pragma unroll 4
   for (int i = t; i < n; i += NT) {
     const int x = rows[i];
-    if (x < i || x >= span || (i && x <= rows[i - 1])) {     // x < i: a list that ascends from zero on never is; such an x may lie before the table
+    const int before = i ? rows[i - 1] : -1;
+    if (x < i || x <= before || x >= span) {   // x < i: a list that ascends from zero on never is; such an x may lie before the table
       ok = false;
     } else if (x != i) {       // from and to pages of the pool, and to none that others hold
       first = min(first, i);
@@ -136,14 +137,15 @@ struct ReserveArgs {
   int2* need;
 };
 
-// What a pair wants: its first slot to be written and the number of slots it wants to hold (0: nothing).
+// What a pair wants: its first slot to be written and the number of slots it wants to hold (0: nothing, as a pair whose state is none gets).
 struct Want {
   int first, slots, rows;    // rows in the first slot's page
 };
-__device__ __forceinline__ Want want_of(const ReserveArgs& a, int pair, bool& bad) {
+__device__ __forceinline__ Want want_of(const ReserveArgs& a, int pair, int held, bool& bad) {
   const int len = a.lengths[pair], more = a.new_rows[a.lists.of(pair)];
-  bad |= len < 0 || more < 0;
-  if (len < 0 || more <= 0) return {0, 0, 0};
+  const bool none = len < 0 || held < 0 || held > a.pool.max_pages;
+  bad |= none || more < 0;
+  if (none || more <= 0) return {0, 0, 0};
   const int64_t slots = ((int64_t)len + more + a.pool.P - 1) >> a.pool.log_p;
   bad |= slots > a.pool.max_pages;
   return {len >> a.pool.log_p, (int)min(slots, (int64_t)a.pool.max_pages), len & (a.pool.P - 1)};
@@ -184,16 +186,14 @@ __global__ void __launch_bounds__(kThreads) reserve_count_kernel(ReserveArgs a) 
   int need = 0, copies = 0;
   bool bad = false;
   if (pair < a.pairs) {
-    const Want w = want_of(a, pair, bad);
-    int held = a.held[pair];
-    bad |= held < 0 || held > a.pool.max_pages;
-    held = min(max(held, 0), a.pool.max_pages);
+    const int held = a.held[pair];
+    const Want w = want_of(a, pair, held, bad);
     for (int s = w.first; s < min(held, w.slots); ++s) {
       const int page = a.table[(int64_t)pair * a.pool.max_pages + s];
       if ((unsigned)page >= (unsigned)a.pool.n_pages) bad = true;
       else copies += a.refs[page] > 1;
     }
-    need = copies + max(w.slots - held, 0);
+    need = copies + (w.slots ? max(w.slots - held, 0) : 0);
   }
   if (bad) report_status(a.status, kStatusPage);
   int sum = need;
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, kPairs > 1 ? 2 : 4) reserve_apply_ke
   Want w{0, 0, 0};
   int held = 0;
   bool bad = false;
-  if (live) need = a.need[pair], w = want_of(a, pair, bad), held = a.held[pair];
+  if (live) need = a.need[pair], held = a.held[pair], w = want_of(a, pair, held, bad);
   const Sums sum = add_up(a, pages, pages ? (int)blockIdx.x : block, s_sum);
   const bool enough = sum.need <= sum.free;
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.room) {
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, kPairs > 1 ? 2 : 4) reserve_apply_ke
         const int2 n = a.need[to];
         const int before = to % kPairBlock ? a.need[to - 1].x : 0, which = r - before;
         if (which < n.y) continue;                       // a copy
-        const Want x = want_of(a, to, bad);
+        const Want x = want_of(a, to, 0, bad);           // (one that needs a page holds a number of them that can be)
         const int page = (int)(page0 + (w0 + (threadIdx.x >> 3)) * 32 + 4 * (threadIdx.x & 7) + __ffs(bits) - 1);
         a.table[(int64_t)to * a.pool.max_pages + x.slots - (n.x - before) + which] = page;
         a.refs[page] = 1;
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, kPairs > 1 ? 2 : 4) reserve_apply_ke
     return;
   }
   if (live) {
-    if (w.slots > held) a.held[pair] = w.slots;
+    if (w.slots && w.slots > held) a.held[pair] = w.slots;
     // copies: pages from this rank on
     const int at = pair % kPairBlock;
     s_need[threadIdx.x] = make_int2(sum.before + (at ? a.need[pair - 1].x : 0), need.y);
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, kPairs > 1 ? 2 : 4) reserve_apply_ke
     if (s_need[i].y == 0) continue;
     const int its = pair0 + i, end = s_held[i];
     int rank = s_need[i].x;
-    const Want x = want_of(a, its, bad);
+    const Want x = want_of(a, its, 0, bad);
     int32_t* const table = a.table + (int64_t)its * a.pool.max_pages;
     for (int s = x.first; s < end; ++s) {
       const int old = table[s];
@@ -428,8 +428,9 @@ __global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pai
   const int pair = (int)(blockIdx.x * (kThreads >> log_t) + (threadIdx.x >> log_t)), t = threadIdx.x & ((1 << log_t) - 1);
   const bool live = pair < pairs;
   const int len = live && lengths ? lengths[pair] : 0, have = live ? held[pair] : 0;
-  bool bad = len < 0 || have < 0 || have > pool.max_pages;
-  const int end = min(have, pool.max_pages), keep = len < 0 ? have : (int)(((int64_t)len + pool.P - 1) >> pool.log_p);
+  const bool none = len < 0 || have < 0 || have > pool.max_pages;      // the pair is left as it is
+  bool bad = none;
+  const int end = none ? 0 : have, keep = none ? 0 : (int)(((int64_t)len + pool.P - 1) >> pool.log_p);
   for (int s0 = keep + t; s0 < end; s0 += 4 << log_t) {
     int page[4];
 #pragma unroll
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(kThreads) pages_trim_kernel(Pool pool, int pai
     }
   }
   __syncthreads();     // all of the pair's threads have read `held`
-  if (live && t == 0 && keep < have) held[pair] = keep;
+  if (live && t == 0 && keep < end) held[pair] = keep;
   if (bad) report_status(status, kStatusPage);
 }
 
@@ -471,8 +472,8 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(ForkArgs a) {
     if (p >= 0 && p < a.seqs) {
       const int64_t from = ((int64_t)layer * a.seqs + p) * a.Hkv + g;
       len = a.lengths[from], held = a.held[from];
-      bad = held < 0 || held > a.pool.max_pages;
-      held = min(max(held, 0), a.pool.max_pages);
+      bad = len < 0 || held < 0 || held > a.pool.max_pages;
+      if (bad) len = held = 0;       // nothing to go on from
       const int32_t* const src = a.table + from * a.pool.max_pages;
       int32_t* const dst = a.new_table + (int64_t)pair * a.pool.max_pages;
 #pragma unroll 4
@@ -485,11 +486,16 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(ForkArgs a) {
     const int pair = (int)(w - fresh), unit = pair / a.Hkv, seq = unit % a.seqs;
     int more = a.keep_old ? 0 : -1;
     for (int i = 0; i < a.new_seqs; i += 32) more += __popc(__ballot_sync(0xffffffffu, i + lane < a.new_seqs && a.parents[i + lane] == seq));
-    const int held = min(a.held[pair], a.pool.max_pages);
+    const int len = a.lengths[pair], have = a.held[pair];
+    bad = len < 0 || have < 0 || have > a.pool.max_pages;
+    const int held = bad ? 0 : have;
     for (int s = lane; more && s < held; s += 32) {
       const int page = a.table[(int64_t)pair * a.pool.max_pages + s];
+      // A page that is held has been counted.  Children of one that is not are counted all the same: an addition that is undone could pass for a
+      // holder's in between.
       if ((unsigned)page >= (unsigned)a.pool.n_pages) bad = true;
-      else if (atomicAdd(&a.refs[page], more) < 1) atomicSub(&a.refs[page], more), bad = true;    // a page that is held has been counted
+      else if (atomicAdd(&a.refs[page], more) >= 1) continue;
+      else if (bad = true; more < 0) atomicSub(&a.refs[page], more);
     }
   }
   if (bad) report_status(a.status, kStatusPage);
