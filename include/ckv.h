@@ -471,8 +471,10 @@ size_t ckv_pages_workspace_bytes(const ckv_paged* paged);
  * share the pages they will write (slots lengths / page_size on), those are replaced by pages of their own, with copies of the
  * rows below lengths.  new_rows [n_lists] int32, n_lists Nu * Hkv (for example a retention pass's budgets) or Nu / layers; a head of no
  * new rows is left as it is.  Pages are the free ones of lowest number, handed out head by head, slot by slot.  All or nothing: where
- * too few pages are free nothing is changed.  room_or_null [2] int32: the free pages there are afterwards, and how many there were too
- * few (0: done).  Slots past the table are not reserved, and are reported (CKV_ERR_PAGE).
+ * too few pages are free nothing is changed.  room_or_null [2] int32: the free pages that were not handed out, and how many there were
+ * too few (0: done).  Every head that writes a shared page gets a copy, the last of its holders too: where all of them write in one call
+ * the page is free afterwards, and is in the room of the next call (one without new rows tells how many pages are free).
+ * Slots past the table are not reserved, and are reported (CKV_ERR_PAGE).
  */
 ckv_status ckv_pages_reserve(const ckv_paged* paged, int32_t layers, const int32_t* new_rows, int32_t n_lists, const int32_t* lengths,
                              int32_t* held, int32_t* page_table, int32_t* refs, void* k_pages, void* v_pages, int32_t* room_or_null,
