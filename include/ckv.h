@@ -474,6 +474,8 @@ size_t ckv_pages_workspace_bytes(const ckv_paged* paged);
  * too few pages are free nothing is changed.  room_or_null [2] int32: the free pages that were not handed out, and how many there were
  * too few (0: done).  Every head that writes a shared page gets a copy, the last of its holders too: where all of them write in one call
  * the page is free afterwards, and is in the room of the next call (one without new rows tells how many pages are free).
+ * Where room[1] is not 0, tokens must not be appended: ckv_append does not look at refs or held, and writes wherever the table entries point
+ * (pages that are still shared, entries past held that are of pages long given back).
  * Slots past the table are not reserved, and are reported (CKV_ERR_PAGE).
  */
 ckv_status ckv_pages_reserve(const ckv_paged* paged, int32_t layers, const int32_t* new_rows, int32_t n_lists, const int32_t* lengths,

@@ -700,7 +700,7 @@ def ckv_keep_rows(paged, rows, begins, counts, lengths, page_table, k_pages, v_p
 def ckv_pages_reserve(paged, new_rows, lengths, held, page_table, refs, k_pages, v_pages, ws, room=None, layers=1, stream=None):
     """Pages for the next new_rows rows (per (unit, KV head) or per sequence) of every head, all or nothing; shared pages that will be
     written are replaced by copies.  room [2] receives the free pages that were not handed out (pages that lost their last holder in this
-    call are free too, and in the room of the next) and how many there were too few."""
+    call are free too, and in the room of the next) and how many there were too few: not zero, tokens must not be appended."""
     dev, i32 = paged._device, torch.int32
     new_ptr = _list_of(new_rows, None, dev, "new_rows")
     _paged_call("ckv_pages_reserve", dev, stream, C.addressof(paged), int(layers), new_ptr, new_rows.numel(),
