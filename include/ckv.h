@@ -369,7 +369,8 @@ typedef struct {
 ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const void* q, const void* k,
                       const int32_t* positions, const int32_t* token_starts, void* q_out, void* k_out, void* stream);
 
-/* Bytes of work space ckv_paged_attend needs (0 on invalid arguments).  ckv_append and ckv_gather_pages use the first 256 of
+/* Bytes of work space that ckv_paged_attend and ckv_tree_attend need (0 on invalid arguments; in fp32 ckv_paged_attend alone does with 618496,
+ * without the room of a tree's blocks).  ckv_append and ckv_gather_pages use the first 256 of
  * them, the status section, so that one work space serves the calls of a step. */
 size_t ckv_paged_workspace_bytes(const ckv_paged* paged);
 

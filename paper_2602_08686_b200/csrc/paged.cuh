@@ -18,7 +18,8 @@ struct PagedWs {
   size_t o;        // float [workers][2][rows][128]         its unnormalised output
   size_t total;
 };
-PagedWs paged_ws(const ckv_paged& pg);
+PagedWs paged_ws(const ckv_paged& pg);   // of ckv_paged_attend
+PagedWs tree_ws(const ckv_paged& pg);    // of ckv_tree_attend: no less
 
 // Records a code in the status word of a work space that no call may have cleared yet; the first code stays until it is
 // read.  (Two reporters may both find a fresh work space: they then store the same kind of code.)

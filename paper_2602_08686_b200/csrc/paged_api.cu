@@ -6,11 +6,6 @@ using namespace ckv;
 #pragma GCC visibility push(default)
 extern "C" {
 
-size_t ckv_paged_workspace_bytes(const ckv_paged* paged) {
-  if (check_tokens(paged) != CKV_OK || check_pages(paged) != CKV_OK) return 0;
-  return paged_ws(*paged).total;
-}
-
 ckv_status ckv_rotate(const ckv_paged* paged, const ckv_rotary* rotary, const void* q, const void* k,
                       const int32_t* positions, const int32_t* token_starts, void* q_out, void* k_out, void* stream) {
   CKV_TRY(check_tokens(paged));

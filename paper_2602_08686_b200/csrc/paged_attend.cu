@@ -365,21 +365,23 @@ int cluster_size(const ckv_paged& pg, const ShortRule& rule, int64_t blocks) {
 }
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-PagedWs paged_ws(const ckv_paged& pg) {
+static PagedWs ws_of(const ckv_paged& pg, int f32_rows) {
   PagedWs w{};
   size_t o = 0;
   w.status = o, o += 256;
-  const size_t rows = wants_tc(pg) ? kTcRows : (pg.dtype == CKV_BF16 ? kMmaRows : kTileRows);
+  const size_t rows = wants_tc(pg) ? kTcRows : (pg.dtype == CKV_BF16 ? kMmaRows : f32_rows);
   w.split = o, o = up256(o + kWorkers * sizeof(int4));
   w.ml = o, o = up256(o + kWorkers * 2 * rows * sizeof(float2));
   w.o = o, o = up256(o + kWorkers * 2 * rows * kHeadDim * sizeof(float));
   w.total = o;
   return w;
 }
+PagedWs paged_ws(const ckv_paged& pg) { return ws_of(pg, kRowsM); }
+PagedWs tree_ws(const ckv_paged& pg) { return ws_of(pg, kTileRows); }
 
 WorkArgs work_args(const ckv_paged& pg, const int32_t* table, const int32_t* lengths, const int32_t* starts, const uint32_t* tree,
                    int tree_words, char* ws) {
-  const PagedWs w = paged_ws(pg);
+  const PagedWs w = tree ? tree_ws(pg) : paged_ws(pg);
   WorkArgs a{};
   a.Nu = pg.n_units, a.H = pg.n_q_heads, a.Hkv = pg.n_kv_heads, a.G = a.H / a.Hkv, a.T = pg.n_tokens, a.causal = tree ? 0 : pg.causal;
   a.tree = tree, a.tree_words = tree_words;

@@ -34,6 +34,11 @@ Range refs_of(const ckv_paged& pg, const void* refs) { return ints_of(refs, pg.n
 #pragma GCC visibility push(default)
 extern "C" {
 
+size_t ckv_paged_workspace_bytes(const ckv_paged* paged) {     // enough for either attention
+  if (check_tokens(paged) != CKV_OK || check_pages(paged) != CKV_OK) return 0;
+  return tree_ws(*paged).total;
+}
+
 ckv_status ckv_tree_masks(int32_t n_units, int32_t n_tokens, int32_t words, const int32_t* parents, const int32_t* token_starts,
                           const int32_t* first_positions_or_null, uint32_t* masks, int32_t* positions_or_null, void* ws, size_t ws_bytes,
                           void* stream) {
@@ -59,13 +64,13 @@ ckv_status ckv_tree_attend(const ckv_paged* paged, const void* q, const void* k_
   CKV_TRY(check_pages(paged));
   if (words < 1) return CKV_ERR_INVALID_ARG;
   if (words > (1 << 15)) return CKV_ERR_UNSUPPORTED;
-  CKV_TRY(check_paged_ws(paged_ws(*paged).total, ws, ws_bytes));
+  CKV_TRY(check_paged_ws(tree_ws(*paged).total, ws, ws_bytes));
   if (paged->n_tokens == 0) return CKV_OK;
   if (!good({q, k_pages, v_pages}, 16) || !good({out}, 32) || !good({page_table, lengths, token_starts, masks}, 4)) return CKV_ERR_INVALID_ARG;
   if (lse_or_null && !aligned(lse_or_null, 4)) return CKV_ERR_INVALID_ARG;
   if (!token_strides(*paged, paged->q_stride_tok, paged->q_stride_head, paged->n_q_heads)) return CKV_ERR_INVALID_ARG;
   const int64_t T = paged->n_tokens, H = paged->n_q_heads, e = esize(*paged);
-  if (!all_apart({range_of(out, T, H, H * kHeadDim, kHeadDim, e), ints_of(lse_or_null, T * H), bytes_of(ws, paged_ws(*paged).total)},
+  if (!all_apart({range_of(out, T, H, H * kHeadDim, kHeadDim, e), ints_of(lse_or_null, T * H), bytes_of(ws, tree_ws(*paged).total)},
                  {range_of(q, T, H, paged->q_stride_tok, paged->q_stride_head, e), pool_of(*paged, k_pages), pool_of(*paged, v_pages),
                   table_of(*paged, page_table), heads_of(*paged, lengths), starts_of(*paged, token_starts), ints_of(masks, T * words)}))
     return CKV_ERR_INVALID_ARG;
