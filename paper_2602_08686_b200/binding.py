@@ -74,19 +74,22 @@ class ckv_rotary(C.Structure):
 
 
 _lib = None
-_m = None       # csrc/marshal.cpp: argument checks of the paged calls
+_m = None       # csrc/marshal.cpp: argument checks of the paged calls, and the calls themselves
+_m_error = None # why it is not there
 _entry = {}     # addresses of the paged calls
 
 
 def lib() -> C.CDLL:
     """Loads libckv.so; raises if it has not been built (``python -m paper_2602_08686_b200.build``)."""
-    global _lib, _m
+    global _lib, _m, _m_error
     if _lib is None:
-        for path in (LIB_PATH, os.path.join(_HERE, "_marshal.so")):
-            if not os.path.exists(path):
-                raise RuntimeError(f"{path} is missing: build it with `python -m paper_2602_08686_b200.build` "
-                                   "(there is no CPU fallback)")
-        from . import _marshal as _m
+        if not os.path.exists(LIB_PATH):
+            raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2602_08686_b200.build` "
+                               "(there is no CPU fallback)")
+        try:
+            from . import _marshal as _m
+        except ImportError as e:      # the paged calls alone need it
+            _m_error = e
         L = C.CDLL(LIB_PATH)
         vp, sz, i32p, fp = C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p
         shp, prm = C.POINTER(ckv_shape), C.POINTER(ckv_params)
@@ -460,6 +463,9 @@ def _paged_call(what: str, device: int, stream, *args) -> None:
     if device < 0:
         raise ValueError("the paged calls take CUDA tensors")
     lib()
+    if _m is None:
+        raise RuntimeError(f"{what} needs {os.path.join(_HERE, '_marshal.so')}, which is missing or was built for another Python or torch: build it with "
+                           "`python -m paper_2602_08686_b200.build`") from _m_error
     if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return _paged_call(what, device, stream, *args)

@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libckv.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")        # the binding's argument checks (a Python extension)
+MARSHAL_FOR = os.path.join(HERE, "_build", "marshal_for")   # the Python and torch that it was built for
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -52,18 +53,36 @@ def build_lib(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def built_for() -> str:
+    from importlib.metadata import version
+    return f"{sys.version}\ntorch {version('torch')}\n"
+
+
+def marshal_stale() -> bool:
+    """Older than its source, or built for another Python or torch (or nobody knows for which)."""
+    if not (os.path.exists(MARSHAL) and os.path.exists(MARSHAL_FOR)):
+        return True
+    with open(MARSHAL_FOR) as f:
+        return f.read() != built_for() or os.path.getmtime(MARSHAL) < os.path.getmtime(os.path.join(CSRC, "marshal.cpp"))
+
+
 def build_marshal(force: bool = False) -> str:
     src = os.path.join(CSRC, "marshal.cpp")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= os.path.getmtime(src):
+    if not force and not marshal_stale():
         return MARSHAL
     import sysconfig
 
     import torch
     root = os.path.dirname(torch.__file__)
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+    out = MARSHAL[:-3] + f".{os.getpid()}.so"          # another process may be loading the one there is
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", *[a for i in inc for a in ("-isystem", i)],
-                           src, "-o", MARSHAL, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+                           src, "-o", out, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    os.replace(out, MARSHAL)
+    os.makedirs(os.path.dirname(MARSHAL_FOR), exist_ok=True)
+    with open(MARSHAL_FOR, "w") as f:
+        f.write(built_for())
     return MARSHAL
 
 
